@@ -4,8 +4,9 @@
  * The entry points are the dense fp32 operator programs evaluated in
  * arXiv 2006.06762 ("Ansor"): GMM, C2D and DEP of the single-operator
  * benchmark (Sec. 7.1, shapes in Appendix C) and the ConvLayer and TBS
- * subgraphs (Sec. 7.2).  All arithmetic is fp32 in, fp32 accumulate, fp32 out
- * (Sec. 7: float32 is used for all evaluations).  Large products multiply each
+ * subgraphs (Sec. 7.2), and the operators of a transformer block around them.
+ * All arithmetic of the former is fp32 in, fp32 accumulate, fp32 out
+ * (Sec. 7: float32 is used for all evaluations); the latter have an element type.  Large products multiply each
  * float as the exact sum of three bf16 numbers: of the nine products of the
  * pieces only the smallest, below 2^-34 of the product, is left out.  A result of
  * one term is then at most 1.06 x 2^-24 of it off (an fp32 product 1.00), one of n
@@ -76,8 +77,21 @@ typedef enum { ANR_LAYOUT_NCHW = 0 } anr_layout;
 
 typedef enum {
     ANR_OP_GEMM = 0, ANR_OP_CONV2D = 1, ANR_OP_CONV_BN_RELU = 2, ANR_OP_DWCONV = 3,
-    ANR_OP_TBG = 4, ANR_OP_TBS = 5, ANR_OP_NRM = 6
+    ANR_OP_TBG = 4, ANR_OP_TBS = 5, ANR_OP_NRM = 6,
+    ANR_OP_GROUP_NORM = 7, ANR_OP_GROUP_NORM_BACKWARD = 8, ANR_OP_ROTARY = 9,
+    ANR_OP_GATED_FF = 10, ANR_OP_GATED_FF_BACKWARD = 11
 } anr_op;
+
+/* Types of the elements of group norm, rotary positions and the gated feed-forward
+ * block.  The operators above take float32 only. */
+typedef enum { ANR_F32 = 0, ANR_F16 = 1, ANR_BF16 = 2 } anr_dtype;
+
+/* Activations: z; max(z, 0) (a NaN stays one); z sigmoid(z); z Phi(z) with the normal
+ * distribution's Phi, by the error function; and z sigmoid(2 sqrt(2/pi) (z + 0.044715 z^3)),
+ * which is the usual form with tanh. */
+typedef enum {
+    ANR_ACT_NONE = 0, ANR_ACT_RELU = 1, ANR_ACT_SILU = 2, ANR_ACT_GELU = 3, ANR_ACT_GELU_TANH = 4
+} anr_act;
 
 /*
  * GMM.  C[b] = A[b] (M x K) . B[b] (K x N), b = 0 .. batch-1; all row-major.
@@ -274,6 +288,117 @@ typedef struct {
  * order is fixed, so results do not vary from run to run. */
 anr_status anr_nrm(const anr_nrm_desc *desc, const float *x, float *out,
                    void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Operators of a transformer block on images, video and tokens, around the scores of
+ * anr_tbg / anr_tbs and the products of anr_gemm.  Elements are of `dtype`; sums,
+ * statistics and angles are held in 32 bits or more, and a result is rounded to
+ * `dtype` once unless its comment says otherwise.  Pointers are aligned to their
+ * element; 16-byte alignment of pointers, extents and strides selects the faster
+ * kernels.  An extent of zero tokens, images or pixels is no error: outputs without
+ * elements stay as they are, sums over nothing are written as zeros.  Results do not
+ * vary from run to run.
+ *
+ * Group norm, channels last.  Element (n,h,w,c) of x is x[n*sn + h*sh + w*sw + c]
+ * with strides (sn, sh, sw) in elements, all three zero: packed [N,H,W,C].
+ * x_stride is x's; y_stride that of y, or of dy in the backward call; dx_stride that
+ * of dx.  Every stride >= 1 for an extent above 1 and no view overlaps itself.
+ * Channels are cut into `groups` equal runs; C / groups <= 8192.  param_dtype is the
+ * type of gamma, beta, dgamma and dbeta: float32 or `dtype`.
+ */
+typedef struct {
+    int32_t N, H, W, C;
+    int32_t groups;
+    int32_t act;         /* anr_act   */
+    int32_t dtype;       /* anr_dtype */
+    int32_t param_dtype; /* anr_dtype */
+    int64_t x_stride[3];
+    int64_t y_stride[3];
+    int64_t dx_stride[3];
+} anr_group_norm_desc;
+
+/* y = act((x - mean) rstd gamma + beta) with the mean and rstd = 1/sqrt(var + eps)
+ * (var: the mean square difference) of each group of each image over its pixels and
+ * channels.  gamma, beta: C each, NULL for ones and zeros.  mean, rstd: [N, groups]
+ * float32 outputs for a backward call, or NULL.  eps is finite and not negative. */
+anr_status anr_group_norm(const anr_group_norm_desc *desc, const void *x, const void *gamma, const void *beta,
+                          float eps, void *y, float *mean, float *rstd, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Gradients of anr_group_norm, whose x, gamma, beta, mean and rstd it takes: with
+ * xhat = (x - mean) rstd and dz = dy act'(xhat gamma + beta), dgamma = sum dz xhat and
+ * dbeta = sum dz over images and pixels, and dx = rstd (dz gamma - a - xhat b) with the
+ * group's means a of dz gamma and b of dz gamma xhat.  dx, dgamma, dbeta: NULL for what is
+ * not wanted, not all three. */
+anr_status anr_group_norm_backward(const anr_group_norm_desc *desc, const void *dy, const void *x, const void *gamma,
+                                   const void *beta, const float *mean, const float *rstd, void *dx, void *dgamma,
+                                   void *dbeta, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Rotary positions with up to four axes (time, height, width, ...).  q [B,S,H,D] and k
+ * [B,S,Hk,D] as in anr_tbg, strides in elements for (b, s, h), all three zero: packed;
+ * the d-stride is 1.  Pairs of dimensions turn by an angle: pair i by
+ * positions[axis(i), b, s] * inv_freq[i] (inv_freq: device floats, one for each pair),
+ * where the first section[0] pairs belong to axis 0, the next section[1] to axis 1 and so
+ * on; n = sum of the sections <= D/2.  Dimensions of pair i:
+ *   ANR_ROTARY_HALVES           i and n + i
+ *   ANR_ROTARY_ADJACENT         2 i and 2 i + 1
+ *   ANR_ROTARY_SECTION_HALVES   each axis has a block of 2 section[a] dimensions: p and p + section[a]
+ * Dimensions from 2 n on are copied.  positions are of pos_type with strides in elements
+ * for (axis, b, s), zero where an axis, sequence or token shares them.  The angle is
+ * formed in 64 bits.  inverse turns the other way: what a backward pass does with the
+ * gradients.
+ */
+typedef enum { ANR_ROTARY_HALVES = 0, ANR_ROTARY_ADJACENT = 1, ANR_ROTARY_SECTION_HALVES = 2 } anr_rotary_pairing;
+typedef enum { ANR_POS_I32 = 0, ANR_POS_I64 = 1, ANR_POS_F32 = 2 } anr_pos_type;
+typedef struct {
+    int32_t B, S, H, Hk, D;
+    int32_t axes;        /* 1 .. 4 */
+    int32_t section[4];  /* pairs of each axis; those from `axes` on are ignored */
+    int32_t pairing;     /* anr_rotary_pairing */
+    int32_t inverse;     /* 0 or 1 */
+    int32_t dtype;       /* anr_dtype */
+    int32_t pos_type;    /* anr_pos_type */
+    int32_t reserved;    /* 0 */
+    int64_t q_stride[3], k_stride[3];
+    int64_t q_out_stride[3], k_out_stride[3];
+    int64_t pos_stride[3];
+} anr_rotary_desc;
+
+/* q_out and k_out: turned q and k; each may be its input itself, with the same strides.  k
+ * and k_out may be NULL where Hk is 0.  D <= 2048. */
+anr_status anr_rotary(const anr_rotary_desc *desc, const void *q, const void *k, const void *positions,
+                      const float *inv_freq, void *q_out, void *k_out, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Gated feed-forward block of T tokens of C channels with F hidden ones, weights as
+ * [outputs, inputs]: w_gate and w_up [F,C], w_down [C,F].  Row-major, leading dimensions
+ * in elements, 0 for packed: x and dx (ldx, lddx), y and dy (ldy: y in the forward, dy in
+ * the backward call), gate and up, both [T,F] (ldpre), both w_gate and w_up (ldw), w_down
+ * (ld_down), and the weights' gradients alike (lddw, ld_ddown).  act is any anr_act
+ * (ANR_ACT_NONE: a bilinear block).  C and F <= 2^20, leading dimensions and T < 2^22.
+ */
+typedef struct {
+    int64_t T, C, F;
+    int32_t act;         /* anr_act   */
+    int32_t dtype;       /* anr_dtype */
+    int64_t ldx, ldy, ldpre, lddx;
+    int64_t ldw, ld_down;
+    int64_t lddw, ld_ddown;
+} anr_gated_ff_desc;
+
+/* g = x w_gate^T, u = x w_up^T, h = act(g) u, y = h w_down^T.  g and u go to `gate` and `up`
+ * where those are given (both or neither), which a backward call takes.  h is held in `dtype`
+ * between the products, made from g and u before they are rounded. */
+anr_status anr_gated_ff(const anr_gated_ff_desc *desc, const void *x, const void *w_gate, const void *w_up,
+                        const void *w_down, void *y, void *gate, void *up, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Gradients of anr_gated_ff from its x, weights, gate and up: dh = dy w_down,
+ * dg = dh u act'(g), du = dh act(g), dx = dg w_gate + du w_up, dw_gate = dg^T x,
+ * dw_up = du^T x, dw_down = dy^T h.  dg, du and h are held in `dtype` between the products.
+ * dx, dw_gate, dw_up, dw_down: NULL for what is not wanted, not all four. */
+anr_status anr_gated_ff_backward(const anr_gated_ff_desc *desc, const void *dy, const void *x, const void *w_gate,
+                                 const void *w_up, const void *w_down, const void *gate, const void *up, void *dx,
+                                 void *dw_gate, void *dw_up, void *dw_down, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Bytes of device workspace `op` (an anr_op) needs for `desc` (the matching
  * descriptor type): a function of the descriptor only, enough for any pointer

@@ -2,7 +2,8 @@
 extension module ``_native`` (csrc/binding_native.cpp).
 
 Function names and arguments mirror ``include/anr.h``.  Every tensor argument
-is a torch CUDA tensor (float32); torch is used for device memory and for the
+is a torch CUDA tensor (float32; group norm, rotary positions and the gated
+feed-forward block also float16 and bfloat16); torch is used for device memory and for the
 current HIP stream, nothing else.  There is no CPU path: if the library has not
 been built, importing this module raises.
 """
@@ -30,11 +31,16 @@ from paper_2006_06762_amd import _native  # noqa: E402
 ANR_OK, ANR_ERR_NULL, ANR_ERR_INVALID_ARG, ANR_ERR_UNSUPPORTED, ANR_ERR_WORKSPACE, ANR_ERR_LAUNCH = range(6)
 ANR_LAYOUT_NCHW = 0
 ANR_OP_GEMM, ANR_OP_CONV2D, ANR_OP_CONV_BN_RELU, ANR_OP_DWCONV, ANR_OP_TBG, ANR_OP_TBS, ANR_OP_NRM = range(7)
+ANR_OP_GROUP_NORM, ANR_OP_GROUP_NORM_BACKWARD, ANR_OP_ROTARY, ANR_OP_GATED_FF, ANR_OP_GATED_FF_BACKWARD = range(7, 12)
+ANR_F32, ANR_F16, ANR_BF16 = range(3)
+ANR_ACT_NONE, ANR_ACT_RELU, ANR_ACT_SILU, ANR_ACT_GELU, ANR_ACT_GELU_TANH = range(5)
+ANR_ROTARY_HALVES, ANR_ROTARY_ADJACENT, ANR_ROTARY_SECTION_HALVES = range(3)
+ANR_POS_I32, ANR_POS_I64, ANR_POS_F32 = range(3)
 
 EXPORTS = ("anr_gemm", "anr_conv2d", "anr_conv2d_noalloc", "anr_conv2d_packed_size", "anr_conv2d_pack_weights",
            "anr_conv2d_packed", "anr_conv_bn_relu_packed", "anr_conv_bn_relu", "anr_dwconv", "anr_tbg", "anr_tbs", "anr_nrm",
            "anr_workspace_size", "anr_conv2d_fast_workspace_size", "anr_conv2d_route", "anr_status_string", "anr_version", "anr_last_hip_error",
-           "anr_last_hip_error_string")
+           "anr_last_hip_error_string", "anr_group_norm", "anr_group_norm_backward", "anr_rotary", "anr_gated_ff", "anr_gated_ff_backward")
 
 
 class GemmDesc(ctypes.Structure):
@@ -77,6 +83,26 @@ class TbgDesc(ctypes.Structure):
                 ("o_stride", ctypes.c_int64 * 4)]
 
 
+class GroupNormDesc(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("H", ctypes.c_int32), ("W", ctypes.c_int32), ("C", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3), ("dx_stride", ctypes.c_int64 * 3)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("S", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("axes", ctypes.c_int32), ("section", ctypes.c_int32 * 4), ("pairing", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("pos_type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3), ("q_out_stride", ctypes.c_int64 * 3),
+                ("k_out_stride", ctypes.c_int64 * 3), ("pos_stride", ctypes.c_int64 * 3)]
+
+
+class GatedFfDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("C", ctypes.c_int64), ("F", ctypes.c_int64), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64), ("ldpre", ctypes.c_int64), ("lddx", ctypes.c_int64),
+                ("ldw", ctypes.c_int64), ("ld_down", ctypes.c_int64), ("lddw", ctypes.c_int64), ("ld_ddown", ctypes.c_int64)]
+
+
 _vp = ctypes.c_void_p
 _lib.anr_gemm.argtypes = [ctypes.POINTER(GemmDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_conv2d.argtypes = [ctypes.POINTER(ConvDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
@@ -92,12 +118,18 @@ _lib.anr_dwconv.argtypes = [ctypes.POINTER(ConvDesc), _vp, _vp, _vp, _vp, ctypes
 _lib.anr_tbg.argtypes = [ctypes.POINTER(TbgDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_tbs.argtypes = [ctypes.POINTER(TbgDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_nrm.argtypes = [ctypes.POINTER(NrmDesc), _vp, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.anr_group_norm.argtypes = [ctypes.POINTER(GroupNormDesc), _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.anr_group_norm_backward.argtypes = [ctypes.POINTER(GroupNormDesc)] + [_vp] * 10 + [ctypes.c_size_t, _vp]
+_lib.anr_rotary.argtypes = [ctypes.POINTER(RotaryDesc)] + [_vp] * 7 + [ctypes.c_size_t, _vp]
+_lib.anr_gated_ff.argtypes = [ctypes.POINTER(GatedFfDesc)] + [_vp] * 8 + [ctypes.c_size_t, _vp]
+_lib.anr_gated_ff_backward.argtypes = [ctypes.POINTER(GatedFfDesc)] + [_vp] * 12 + [ctypes.c_size_t, _vp]
 _lib.anr_workspace_size.argtypes = [ctypes.c_int, _vp, ctypes.POINTER(ctypes.c_size_t)]
 _lib.anr_conv2d_fast_workspace_size.argtypes = [ctypes.POINTER(ConvDesc), ctypes.POINTER(ctypes.c_size_t)]
 _lib.anr_conv2d_route.argtypes = [ctypes.POINTER(ConvDesc), ctypes.POINTER(ConvRoute)]
 for _name in ("anr_gemm", "anr_conv2d", "anr_conv2d_noalloc", "anr_conv2d_packed_size", "anr_conv2d_pack_weights",
               "anr_conv2d_packed", "anr_conv_bn_relu_packed", "anr_conv_bn_relu", "anr_dwconv", "anr_tbg", "anr_tbs",
-              "anr_workspace_size", "anr_conv2d_fast_workspace_size"):
+              "anr_workspace_size", "anr_conv2d_fast_workspace_size", "anr_group_norm", "anr_group_norm_backward", "anr_rotary",
+              "anr_gated_ff", "anr_gated_ff_backward"):
     getattr(_lib, _name).restype = ctypes.c_int
 _lib.anr_status_string.argtypes = [ctypes.c_int]
 _lib.anr_status_string.restype = ctypes.c_char_p
@@ -153,12 +185,21 @@ _fast.anr_tbg.argtypes = _vp4 + [_vp, _sz, _vp]
 _fast.anr_tbs.argtypes = _vp4 + [_vp, _sz, _vp]
 _fast.anr_nrm.argtypes = [_vp] * 3 + [_vp, _sz, _vp]
 
+_fast.anr_group_norm.argtypes = [_vp] * 4 + [_fl] + [_vp] * 4 + [_sz, _vp]
+_fast.anr_group_norm_backward.argtypes = [_vp] * 11 + [_sz, _vp]
+_fast.anr_rotary.argtypes = [_vp] * 8 + [_sz, _vp]
+_fast.anr_gated_ff.argtypes = [_vp] * 9 + [_sz, _vp]
+_fast.anr_gated_ff_backward.argtypes = [_vp] * 13 + [_sz, _vp]
+
 _pack_gemm = struct.Struct("@10q").pack
 _pack_conv = struct.Struct("@14i8q2i").pack
 _pack_tbg = struct.Struct("@4i12q").pack
 _pack_nrm = struct.Struct("@5q").pack
-assert [struct.calcsize(f) for f in ("@10q", "@14i8q2i", "@4i12q", "@5q")] == \
-    [ctypes.sizeof(t) for t in (GemmDesc, ConvDesc, TbgDesc, NrmDesc)]
+_pack_group_norm = struct.Struct("@8i9q").pack
+_pack_rotary = struct.Struct("@15i15q").pack
+_pack_gated_ff = struct.Struct("@3q2i8q").pack
+assert [struct.calcsize(f) for f in ("@10q", "@14i8q2i", "@4i12q", "@5q", "@8i9q", "@15i15q", "@3q2i8q")] == \
+    [ctypes.sizeof(t) for t in (GemmDesc, ConvDesc, TbgDesc, NrmDesc, GroupNormDesc, RotaryDesc, GatedFfDesc)]
 _NO_STRIDES = (0, 0, 0, 0)
 _f32 = torch.float32
 
@@ -446,6 +487,207 @@ def _nrm(x, out, ws=None):
     _with_workspace(_fast.anr_nrm, "anr_nrm", ANR_OP_NRM, d, (_ptr(x), _ptr(out)), ws, NrmDesc)
     return out
 
+
+# ---- operators of a transformer block
+_DTYPES = {torch.float32: ANR_F32, torch.float16: ANR_F16, torch.bfloat16: ANR_BF16}
+_POSITIONS = {torch.int32: ANR_POS_I32, torch.int64: ANR_POS_I64, torch.float32: ANR_POS_F32}
+
+
+def _dtype(t):
+    if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES:
+        raise TypeError("expected a float32, float16 or bfloat16 CUDA tensor")
+    return _DTYPES[t.dtype]
+
+
+def _like(name, t, shape, dtype):
+    """The address of a tensor on the current device with that shape and type; of None, None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype:
+        raise TypeError("%s: expected a %s CUDA tensor" % (name, str(dtype).replace("torch.", "")))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: expected the shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError("%s: is on another device than the current one" % name)
+    return t.data_ptr()
+
+
+def _vector(name, t, shape, dtype):
+    """_like of a packed tensor."""
+    if t is not None and isinstance(t, torch.Tensor) and not t.is_contiguous():
+        raise ValueError("%s: must be packed" % name)
+    return _like(name, t, shape, dtype)
+
+
+def _channels_last(name, t):
+    """Strides (n, h, w) of a tensor [N,C,S] or [N,C,H,W] whose channels are neighbours."""
+    shape, s = t.shape, t.stride()
+    if len(shape) not in (3, 4):
+        raise ValueError("%s: expected [N,C,S] or [N,C,H,W]" % name)
+    if s[1] != 1 and shape[1] != 1:
+        raise ValueError("%s: channels must be neighbours in memory (channels last)" % name)
+    out = (s[0], 0 if len(shape) == 3 else s[2], s[-1])
+    extents = (shape[0], 1 if len(shape) == 3 else shape[2], shape[-1])
+    if any(st == 0 and n > 1 for st, n in zip(out, extents)):
+        raise ValueError("%s: must not be expanded" % name)
+    return tuple(st if n > 1 else 0 for st, n in zip(out, extents))
+
+
+def _group_norm_call(x, views, groups, act, param):
+    """The descriptor of a call on x and `views`, (name, tensor) like x with None for an absent one."""
+    dtype = _dtype(x)
+    strides = [_channels_last("x", x)]
+    for name, t in views:
+        if t is not None:
+            _like(name, t, x.shape, x.dtype)
+        strides.append(_channels_last(name, t) if t is not None else strides[0])
+    N, C = x.shape[:2]
+    H, W = (1, x.shape[2]) if x.dim() == 3 else x.shape[2:]
+    while len(strides) < 3:
+        strides.append((0, 0, 0))
+    try:
+        return _pack_group_norm(N, H, W, C, groups, act, dtype, _DTYPES[param], *(v for s in strides for v in s))
+    except struct.error:
+        raise AnrError(ANR_ERR_UNSUPPORTED, "group norm")
+
+
+def _param_dtype(x, *vectors):
+    """The type of the parameters of a norm: that of those given."""
+    given = {v.dtype for v in vectors if isinstance(v, torch.Tensor)}
+    if len(given) > 1 or not given <= {torch.float32, x.dtype}:
+        raise TypeError("gamma and beta (and their gradients) must be of one type: float32 or x's")
+    return given.pop() if given else torch.float32
+
+
+def _group_norm(x, groups, y, gamma=None, beta=None, eps=1e-5, act=ANR_ACT_NONE, mean=None, rstd=None, ws=None):
+    """y = act((x - mean) * rstd * gamma + beta) over `groups` runs of channels; x, y [N,C,S] or [N,C,H,W] channels last."""
+    param = _param_dtype(x, gamma, beta)
+    d = _group_norm_call(x, (("y", y),), groups, act, param)
+    C, stats = (x.shape[1],), (x.shape[0], groups)
+    args = (_like("x", x, x.shape, x.dtype), _vector("gamma", gamma, C, param), _vector("beta", beta, C, param), eps, _like("y", y, x.shape, x.dtype),
+            _vector("mean", mean, stats, _f32), _vector("rstd", rstd, stats, _f32))
+    _with_workspace(_fast.anr_group_norm, "anr_group_norm", ANR_OP_GROUP_NORM, d, args, ws, GroupNormDesc)
+    return y
+
+
+def _group_norm_backward(dy, x, groups, gamma, beta, mean, rstd, dx=None, dgamma=None, dbeta=None, act=ANR_ACT_NONE, ws=None):
+    """Gradients of group_norm, into those of dx, dgamma and dbeta that are given, from its arguments and the mean and rstd that it wrote."""
+    param = _param_dtype(x, gamma, beta, dgamma, dbeta)
+    d = _group_norm_call(x, (("dy", dy), ("dx", dx)), groups, act, param)
+    C, stats = (x.shape[1],), (x.shape[0], groups)
+    args = (_like("dy", dy, x.shape, x.dtype), _like("x", x, x.shape, x.dtype), _vector("gamma", gamma, C, param), _vector("beta", beta, C, param),
+            _vector("mean", mean, stats, _f32), _vector("rstd", rstd, stats, _f32), _like("dx", dx, x.shape, x.dtype), _vector("dgamma", dgamma, C, param),
+            _vector("dbeta", dbeta, C, param))
+    _with_workspace(_fast.anr_group_norm_backward, "anr_group_norm_backward", ANR_OP_GROUP_NORM_BACKWARD, d, args, ws, GroupNormDesc)
+    return dx, dgamma, dbeta
+
+
+def _token_strides(name, t):
+    """Strides (b, s, h) of a tensor [B,S,H,D]; none for one that is packed."""
+    if t.dim() != 4:
+        raise ValueError("%s: expected [B,S,H,D]" % name)
+    if t.is_contiguous():
+        return (0, 0, 0)
+    s = t.stride()
+    if s[3] != 1 and t.shape[3] != 1:
+        raise ValueError("%s: innermost dimension must be contiguous" % name)
+    s = tuple(st if n > 1 else 0 for st, n in zip(s[:3], t.shape))
+    if s == (0, 0, 0) and t.numel() != t.shape[3]:
+        raise ValueError("%s: must not be expanded over all its tokens and heads" % name)
+    return s
+
+
+def _rotary(q, k, positions, inv_freq, q_out, k_out, sections=None, pairing=ANR_ROTARY_HALVES, inverse=False):
+    """q_out and k_out: q [B,S,H,D] and k [B,S,Hk,D] turned by positions[axis] * inv_freq; each may be its input itself, k and k_out None.
+    positions [axes,B,S] or [axes,S]; inv_freq one float for each pair of dimensions; sections: pairs of each axis (one axis: all)."""
+    dtype = _dtype(q)
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out belong together")
+    if not isinstance(positions, torch.Tensor) or positions.dtype not in _POSITIONS:
+        raise TypeError("positions: expected an int32, int64 or float32 CUDA tensor")
+    if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+        raise ValueError("inv_freq: expected one float for each pair")
+    strides = [_token_strides("q", q)]
+    B, S, H, D = q.shape
+    Hk = 0
+    if k is not None:
+        strides.append(_token_strides("k", k))
+        Hk = k.shape[2]
+    else:
+        strides.append((0, 0, 0))
+    addresses = [_like("q", q, (B, S, H, D), q.dtype), _like("k", k, (B, S, Hk, D), q.dtype)]
+    outs = [_like("q_out", q_out, (B, S, H, D), q.dtype), _like("k_out", k_out, (B, S, Hk, D), q.dtype)]
+    strides += [_token_strides("q_out", q_out), _token_strides("k_out", k_out) if k is not None else (0, 0, 0)]
+    n = inv_freq.shape[0]
+    sections = (n,) if sections is None else tuple(sections)
+    axes = len(sections)
+    if not 1 <= axes <= 4 or sum(sections) != n:
+        raise ValueError("sections: one to four numbers of pairs, %d together" % n)
+    if positions.dim() == 2:
+        positions = positions[:, None].expand(-1, B, -1)
+    at = _like("positions", positions, (axes, B, S), positions.dtype)
+    try:
+        d = _pack_rotary(B, S, H, Hk, D, axes, *sections, *(0,) * (4 - axes), pairing, bool(inverse), dtype, _POSITIONS[positions.dtype], 0, *strides[0],
+                         *strides[1], *strides[2], *strides[3], *positions.stride())
+    except struct.error:
+        raise AnrError(ANR_ERR_UNSUPPORTED, "anr_rotary")
+    _check(_fast.anr_rotary(d, *addresses, at, _vector("inv_freq", inv_freq, (n,), _f32), *outs, None, 0, _stream()), "anr_rotary")
+    return q_out, k_out
+
+
+def _rows(name, t, shape, dtype):
+    """(address, leading dimension) of a matrix with neighbouring columns; of None, None and 0."""
+    at = _like(name, t, shape, dtype)
+    if t is None:
+        return at, 0
+    s = t.stride()
+    if (s[1] != 1 and t.shape[1] != 1) or (s[0] < t.shape[1] and t.shape[0] > 1):
+        raise ValueError("%s: innermost dimension must be contiguous, rows must not overlap" % name)
+    return at, s[0] if t.shape[0] > 1 else 0
+
+
+def _shared(names, a, b):
+    """The leading dimension of two matrices of as many rows, either of which may be absent."""
+    if a[0] is not None and b[0] is not None and a[1] != b[1]:
+        raise ValueError("%s: must have the same strides" % names)
+    return a[1] or b[1]
+
+
+def _matrix(name, t):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError("%s: expected a matrix" % name)
+    return t.shape
+
+
+def _gated_ff(x, w_gate, w_up, w_down, y, act=ANR_ACT_SILU, gate=None, up=None, ws=None):
+    """y = (act(x.w_gate^T) * (x.w_up^T)).w_down^T; x, y [T,C], w_gate and w_up [F,C], w_down [C,F].  gate and up [T,F]: the two
+    products, where a backward pass is to follow."""
+    dtype, (T, C), F = _dtype(x), _matrix("x", x), _matrix("w_gate", w_gate)[0]
+    if (gate is None) != (up is None):
+        raise ValueError("gate and up belong together")
+    t = x.dtype
+    xs, wg, wu, wd, ys = (_rows(n, v, s, t) for n, v, s in (("x", x, (T, C)), ("w_gate", w_gate, (F, C)), ("w_up", w_up, (F, C)), ("w_down", w_down, (C, F)),
+                                                            ("y", y, (T, C))))
+    g, u = _rows("gate", gate, (T, F), t), _rows("up", up, (T, F), t)
+    d = _pack_gated_ff(T, C, F, act, dtype, xs[1], ys[1], _shared("gate and up", g, u), 0, _shared("w_gate and w_up", wg, wu), wd[1], 0, 0)
+    _with_workspace(_fast.anr_gated_ff, "anr_gated_ff", ANR_OP_GATED_FF, d, (xs[0], wg[0], wu[0], wd[0], ys[0], g[0], u[0]), ws, GatedFfDesc)
+    return y
+
+
+def _gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, dx=None, dw_gate=None, dw_up=None, dw_down=None, act=ANR_ACT_SILU, ws=None):
+    """Gradients of gated_ff, into those of dx, dw_gate, dw_up and dw_down that are given, from its arguments and the gate and up that it wrote."""
+    dtype, (T, C), F = _dtype(x), _matrix("x", x), _matrix("w_gate", w_gate)[0]
+    t = x.dtype
+    ins = [_rows(n, v, s, t) for n, v, s in (("dy", dy, (T, C)), ("x", x, (T, C)), ("w_gate", w_gate, (F, C)), ("w_up", w_up, (F, C)), ("w_down", w_down, (C, F)),
+                                             ("gate", gate, (T, F)), ("up", up, (T, F)))]
+    outs = [_rows(n, v, s, t) for n, v, s in (("dx", dx, (T, C)), ("dw_gate", dw_gate, (F, C)), ("dw_up", dw_up, (F, C)), ("dw_down", dw_down, (C, F)))]
+    d = _pack_gated_ff(T, C, F, act, dtype, ins[1][1], ins[0][1], _shared("gate and up", ins[5], ins[6]), outs[0][1], _shared("w_gate and w_up", ins[2], ins[3]),
+                       ins[4][1], _shared("dw_gate and dw_up", outs[1], outs[2]), outs[3][1])
+    _with_workspace(_fast.anr_gated_ff_backward, "anr_gated_ff_backward", ANR_OP_GATED_FF_BACKWARD, d, tuple(v[0] for v in ins + outs), ws, GatedFfDesc)
+    return dx, dw_gate, dw_up, dw_down
+
+
+group_norm, group_norm_backward, rotary, gated_ff, gated_ff_backward = _group_norm, _group_norm_backward, _rotary, _gated_ff, _gated_ff_backward
 
 # The operators as programs call them: the functions above without Python's part in the usual case.
 _OPERATORS = ("gemm", "conv2d", "conv_bn_relu", "conv2d_packed", "conv_bn_relu_packed", "dwconv", "tbg", "tbs", "nrm")

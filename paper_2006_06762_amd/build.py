@@ -16,7 +16,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libanr.so")
 NATIVE = os.path.join(HERE, "_native.so")       # the binding's extension module (csrc/binding_native.cpp)
 
-SOURCES = ["api.cpp", "gemm.hip", "tbg.hip", "conv_direct.hip", "conv_igemm.hip", "conv_gather.hip", "conv_pieces.hip", "conv_pointwise.hip", "conv_stem.hip", "dwconv.hip", "nrm.hip", "static_scratch.hip"]
+SOURCES = ["api.cpp", "gemm.hip", "tbg.hip", "conv_direct.hip", "conv_igemm.hip", "conv_gather.hip", "conv_pieces.hip", "conv_pointwise.hip", "conv_stem.hip", "dwconv.hip", "nrm.hip", "static_scratch.hip",
+           "api_blocks.cpp", "group_norm.hip", "rotary.hip", "gated_ff.hip", "mm16_f16.hip", "mm16_bf16.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
@@ -38,6 +39,8 @@ FILE_FLAGS = {
     "conv_pieces.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "conv_stem.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "mm16_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "mm16_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

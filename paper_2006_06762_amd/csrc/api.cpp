@@ -6,11 +6,12 @@
 #include <cmath>
 
 #include "anr_kernels.h"
+#include "blocks_internal.h"
 #include "conv_internal.h"
 
 namespace {
 
-constexpr int kVersion = 300;   // 0.3.0
+constexpr int kVersion = 400;   // 0.4.0
 
 // HIP status of the most recent failed launch made by this thread (diagnostics only).
 thread_local int g_last_hip_error = 0;
@@ -21,6 +22,14 @@ anr_status launch_status(hipError_t e)
     g_last_hip_error = (int)e;
     return ANR_ERR_LAUNCH;
 }
+
+}  // namespace
+
+namespace anr {
+anr_status launch_result(hipError_t e) { return launch_status(e); }
+}  // namespace anr
+
+namespace {
 
 bool all_zero(const int64_t s[4]) { return s[0] == 0 && s[1] == 0 && s[2] == 0 && s[3] == 0; }
 
@@ -400,7 +409,7 @@ anr_status anr_workspace_size(int op, const void* desc, size_t* bytes)
         case ANR_OP_TBG: st = check_tbg(static_cast<const anr_tbg_desc*>(desc), false, &tg); break;
         case ANR_OP_TBS: st = check_tbg(static_cast<const anr_tbg_desc*>(desc), true, &tg); break;
         case ANR_OP_NRM: st = check_nrm(static_cast<const anr_nrm_desc*>(desc), &na); break;
-        default: return ANR_ERR_INVALID_ARG;
+        default: return anr::blocks_workspace_size(op, desc, bytes);
     }
     if (st != ANR_OK) return st;
     *bytes = 0;

@@ -1,0 +1,138 @@
+// Elements of the operators that have an element type (anr_dtype), and the activations: values are float32 from
+// where they are loaded to where they are stored, with one rounding there.
+#pragma once
+#include <type_traits>
+
+#include "anr.h"
+#include "anr_device.h"
+
+namespace anr {
+
+typedef _Float16 half_t;
+typedef __bf16 bf16_t;
+
+template <typename T>
+__device__ __forceinline__ float to_float(T v) { return (float)v; }
+template <typename T>
+__device__ __forceinline__ T from_float(float v) { return (T)v; }          // to nearest, ties to even
+
+// V elements that are loaded and stored together; aligned as the pointer is known to be.
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Pack {
+    T v[V];
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void load_floats(const T* p, float (&out)[V])
+{
+    const Pack<T, V> a = *reinterpret_cast<const Pack<T, V>*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = to_float(a.v[i]);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> pack_floats(const float (&in)[V])
+{
+    Pack<T, V> a;
+#pragma unroll
+    for (int i = 0; i < V; ++i) a.v[i] = from_float<T>(in[i]);
+    return a;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_floats(T* p, const float (&in)[V])
+{
+    *reinterpret_cast<Pack<T, V>*>(p) = pack_floats<T, V>(in);
+}
+
+// An element of a vector whose type is known at run time only (norm parameters: a few per thread).
+__device__ __forceinline__ float load_any(const void* p, int64_t i, int dtype)
+{
+    return dtype == ANR_F32 ? static_cast<const float*>(p)[i] : dtype == ANR_F16 ? (float)static_cast<const half_t*>(p)[i] : (float)static_cast<const bf16_t*>(p)[i];
+}
+__device__ __forceinline__ void store_any(void* p, int64_t i, int dtype, float v)
+{
+    if (dtype == ANR_F32) static_cast<float*>(p)[i] = v;
+    else if (dtype == ANR_F16) static_cast<half_t*>(p)[i] = (half_t)v;
+    else static_cast<bf16_t*>(p)[i] = (bf16_t)v;
+}
+
+// Sigmoid.  QUICK: by the hardware's exponential and reciprocal, whose relative error of about 2^-21 for |z| < 16 (it grows
+// with |z|, the argument being rounded) is far below a rounding to 16 bits; else by the library's, for float32.
+template <bool QUICK>
+__device__ __forceinline__ float sigmoid(float z)
+{
+    if (QUICK) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
+    return 1.f / (1.f + expf(-z));
+}
+
+constexpr float kTwoRootTwoOverPi = 1.59576912160573071f;      // 2 sqrt(2 / pi)
+constexpr float kRootHalf = 0.70710678118654752f;
+constexpr float kOneOverRootTwoPi = 0.39894228040143268f;
+
+// act(z).
+template <int ACT, bool QUICK>
+__device__ __forceinline__ float activation(float z)
+{
+    if (ACT == ANR_ACT_RELU) return z < 0.f ? 0.f : z;                     // (a NaN stays one)
+    if (ACT == ANR_ACT_SILU) return z * sigmoid<QUICK>(z);
+    if (ACT == ANR_ACT_GELU) return 0.5f * z * (1.f + erff(z * kRootHalf));
+    if (ACT == ANR_ACT_GELU_TANH) return z * sigmoid<QUICK>(kTwoRootTwoOverPi * fmaf(0.044715f * z * z, z, z));
+    return z;
+}
+
+// act(z) and act'(z).  A factor of zero takes what it multiplies with it, also where that has overflowed.
+template <int ACT, bool QUICK>
+__device__ __forceinline__ float activation_and_slope(float z, float& slope)
+{
+    slope = 1.f;
+    if (ACT == ANR_ACT_RELU) {
+        slope = z > 0.f ? 1.f : z <= 0.f ? 0.f : z;                        // (a NaN stays one)
+        return z < 0.f ? 0.f : z;
+    }
+    if (ACT == ANR_ACT_SILU) {
+        const float s = sigmoid<QUICK>(z), rest = 1.f - s;
+        slope = rest == 0.f || s == 0.f ? s : s * fmaf(z, rest, 1.f);
+        return z * s;
+    }
+    if (ACT == ANR_ACT_GELU) {
+        const float phi = 0.5f * (1.f + erff(z * kRootHalf));
+        const float density = kOneOverRootTwoPi * (QUICK ? __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z) : expf(-0.5f * z * z));
+        slope = density == 0.f ? phi : fmaf(z, density, phi);
+        return z * phi;
+    }
+    if (ACT == ANR_ACT_GELU_TANH) {
+        const float s = sigmoid<QUICK>(kTwoRootTwoOverPi * fmaf(0.044715f * z * z, z, z)), both = s * (1.f - s);
+        slope = both == 0.f ? s : fmaf(both * z, kTwoRootTwoOverPi * fmaf(3.f * 0.044715f * z, z, 1.f), s);
+        return z * s;
+    }
+    return z;
+}
+
+// f(std::integral_constant<int, ACT>) for the activation of a descriptor.
+template <typename F>
+inline auto with_activation(int act, F f)
+{
+    switch (act) {
+        case ANR_ACT_RELU: return f(std::integral_constant<int, ANR_ACT_RELU>{});
+        case ANR_ACT_SILU: return f(std::integral_constant<int, ANR_ACT_SILU>{});
+        case ANR_ACT_GELU: return f(std::integral_constant<int, ANR_ACT_GELU>{});
+        case ANR_ACT_GELU_TANH: return f(std::integral_constant<int, ANR_ACT_GELU_TANH>{});
+        default: return f(std::integral_constant<int, ANR_ACT_NONE>{});
+    }
+}
+
+// f(T{}) for the element type of a descriptor.
+template <typename F>
+inline auto with_type(int dtype, F f)
+{
+    switch (dtype) {
+        case ANR_F16: return f(half_t{});
+        case ANR_BF16: return f(bf16_t{});
+        default: return f(float{});
+    }
+}
+
+constexpr int element_bytes(int dtype) { return dtype == ANR_F32 ? 4 : 2; }
+
+}  // namespace anr

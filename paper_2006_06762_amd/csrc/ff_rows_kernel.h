@@ -1,0 +1,141 @@
+// Products of a few rows X [T,K], T <= 16 TB, with a large matrix W [N,K] (rows of k), as single tokens need them:
+// D[t][n] = sum_k X[t][k] W[n][k], and for the gated block the same with two matrices and act(g) u of their sums.
+//
+// Bound: reading W once.  A work-group takes 16 rows of W (of both matrices), its waves share the k in chunks of 128 bytes
+// a row and join their sums in LDS; W goes from memory straight into the operands of the matrix instructions, sixteen tokens wide
+// (which cost nothing here), without LDS: nothing of it is used twice.  A lane's part of a chunk are 32 bytes of a row, so
+// the order of k differs from memory's, in both operands alike.
+#pragma once
+#include "anr_kernels.h"
+#include "element_types.h"
+#include "mm16_kernel.h"
+
+namespace anr {
+namespace ffrows {
+
+using mm16::f16x8;
+using mm16::b16x8;
+using mm16::kExtent;
+using mm16::kNowhere;
+using mm16::u32x4;
+
+struct Args {
+    const void* x;
+    const void* w[2];               // rows: the one matrix; gated: gate's and up's
+    void* d;
+    void *gate, *up;                // gated: where the sums go, or null
+    int64_t ldx, ldw[2], ldd, ld_pre;
+    int T, N, K;
+    int act;
+};
+
+// Sixteen bytes of each operand.
+__device__ __forceinline__ f32x4 multiply(u32x4 w, u32x4 x, f32x4 c, half_t)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(u32x4 w, u32x4 x, f32x4 c, bf16_t)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, w), __builtin_bit_cast(b16x8, x), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(u32x4 w, u32x4 x, f32x4 c, float)
+{
+    const f32x4 a = __builtin_bit_cast(f32x4, w), b = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = mfma16(a[i], b[i], c);
+    return c;
+}
+
+// Elements k .. k + 16 / sizeof(T) - 1 of the row at byte `row` of a matrix; those past K are zeros.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ u32x4 load_unit(__amdgpu_buffer_rsrc_t rsrc, uint32_t row, int k, int K)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (ALIGNED) return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(k < K ? row + k * (int)sizeof(T) : kNowhere), 0, 0));
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const int at = (int)(k + j < K ? row + (k + j) * (int)sizeof(T) : kNowhere);
+        if (sizeof(T) == 4) v[j * (int)sizeof(T) / 4] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0);
+        else v[j / 2] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0) << (16 * (j & 1));
+    }
+    return v;
+}
+
+template <typename T, int TB, bool GATED, bool ALIGNED>
+__global__ __launch_bounds__(1024) void rows_kernel(const Args a)
+{
+    constexpr int E = 16 / sizeof(T), CHUNK = 128 / sizeof(T), MATS = GATED ? 2 : 1;
+    constexpr int U = TB == 1 ? 3 : TB == 2 ? 2 : 1;                   // chunks of a wave whose loads are on their way together
+    extern __shared__ __attribute__((aligned(16))) float sums[];       // [wave][TB][MATS][4][64]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int n0 = blockIdx.x * 16, r = lane & 15, g = lane >> 4;
+    __amdgpu_buffer_rsrc_t wr[MATS];
+    uint32_t wrow[MATS], xrow[TB];
+#pragma unroll
+    for (int m = 0; m < MATS; ++m) {
+        wr[m] = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(static_cast<const T*>(a.w[m]) + n0 * a.ldw[m]), 0, kExtent, 0x00020000);
+        wrow[m] = (uint32_t)(min(r, a.N - 1 - n0) * a.ldw[m] * sizeof(T));
+    }
+    const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(a.x), 0, kExtent, 0x00020000);
+#pragma unroll
+    for (int t = 0; t < TB; ++t) xrow[t] = (uint32_t)(min(t * 16 + r, a.T - 1) * a.ldx * sizeof(T));
+    f32x4 acc[MATS][TB];
+#pragma unroll
+    for (int m = 0; m < MATS; ++m)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) acc[m][t] = zero4();
+    const int chunks = (a.K + CHUNK - 1) / CHUNK;
+    for (int c = wave; c < chunks; c += waves * U) {
+        u32x4 w[U][MATS][2], x[U][TB][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int k = (c + u * waves) * CHUNK + (2 * g + i) * E;
+#pragma unroll
+                for (int m = 0; m < MATS; ++m) w[u][m][i] = load_unit<T, ALIGNED>(wr[m], wrow[m], k, a.K);
+#pragma unroll
+                for (int t = 0; t < TB; ++t) x[u][t][i] = load_unit<T, ALIGNED>(xr, xrow[t], k, a.K);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int m = 0; m < MATS; ++m)
+#pragma unroll
+                    for (int t = 0; t < TB; ++t) acc[m][t] = multiply(w[u][m][i], x[u][t][i], acc[m][t], T{});
+    }
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int m = 0; m < MATS; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[(((wave * TB + t) * MATS + m) * 4 + e) * 64 + lane] = acc[m][t][e];
+    __syncthreads();
+    // register e of lane l: row 4 (l / 16) + e of W, token l % 16
+    for (int i = tid; i < TB * 256; i += (int)blockDim.x) {
+        const int t = i >> 8, e = (i >> 6) & 3, l = i & 63, token = t * 16 + (l & 15), n = n0 + 4 * (l >> 4) + e;
+        float v[MATS];
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) {
+            v[m] = 0.f;
+            for (int w = 0; w < waves; ++w) v[m] += sums[(((w * TB + t) * MATS + m) * 4 + e) * 64 + l];
+        }
+        if (token >= a.T || n >= a.N) continue;
+        float out = v[0];
+        if (GATED) {
+            if (a.gate) {
+                static_cast<T*>(a.gate)[token * a.ld_pre + n] = from_float<T>(v[0]);
+                static_cast<T*>(a.up)[token * a.ld_pre + n] = from_float<T>(v[MATS - 1]);
+            }
+            mm16::device_activation(a.act, [&](auto act) { out = activation<decltype(act)::value, sizeof(T) == 2>(v[0]) * v[MATS - 1]; });
+        }
+        static_cast<T*>(a.d)[token * a.ldd + n] = from_float<T>(out);
+    }
+}
+
+}  // namespace ffrows
+}  // namespace anr

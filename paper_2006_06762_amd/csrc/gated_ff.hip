@@ -1,0 +1,427 @@
+// Gated feed-forward block: which kernels a call runs, and the kernels between its products.
+//
+//   few tokens     ff_rows_kernel.h: two launches, each reads its weights once
+//   16-bit types   mm16_kernel.h: gate, up, activation and product in one launch, then the down projection; backward
+//                  three (dh with dg, du and h where they are formed; dx; the weights' gradients together)
+//   float32        the library's GEMM (gemm.hip) and the kernels here
+#include <algorithm>
+
+#include "blocks_internal.h"
+#include "element_types.h"
+#include "ff_rows_kernel.h"
+#include "mm16_launch.h"
+
+namespace anr {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kFewTokens = 64;                  // at most four blocks of sixteen (ff_rows_kernel.h)
+
+size_t whole_lines(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+// ---- float32: the kernels between the products
+
+// h = act(gate) up, all [T,F]; h packed.
+template <int ACT>
+__global__ __launch_bounds__(kThreads) void product_of_gate_kernel(const float* gate, const float* up, int64_t ld, float* h, int64_t T, int64_t F)
+{
+    for (int64_t t = blockIdx.y; t < T; t += gridDim.y)
+        for (int64_t f = (int64_t)blockIdx.x * kThreads + threadIdx.x; f < F; f += (int64_t)gridDim.x * kThreads)
+            h[t * F + f] = activation<ACT, false>(gate[t * ld + f]) * up[t * ld + f];
+}
+
+// From dh, gate and up [T,F]: dgu [T, 2F] (dg and du side by side), the same turned [2F, T], and h [T,F].
+template <int ACT>
+__global__ __launch_bounds__(kThreads) void hidden_gradients_kernel(const float* dh, const float* gate, const float* up, int64_t ld, float* dgu, float* turned, float* h,
+                                                                    int64_t T, int64_t F)
+{
+    __shared__ float tile[2][32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t f0 = (int64_t)blockIdx.x * 32;
+    for (int64_t t0 = (int64_t)blockIdx.y * 32; t0 < T; t0 += (int64_t)gridDim.y * 32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t t = t0 + y + 8 * i, f = f0 + x;
+            if (t >= T || f >= F) continue;
+            const float g = gate[t * ld + f], u = up[t * ld + f], d = dh[t * F + f];
+            float slope;
+            const float a = activation_and_slope<ACT, false>(g, slope);
+            const float dg = d * u * slope, du = d * a;
+            dgu[t * 2 * F + f] = dg;
+            dgu[t * 2 * F + F + f] = du;
+            h[t * F + f] = a * u;
+            tile[0][y + 8 * i][x] = dg;
+            tile[1][y + 8 * i][x] = du;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t f = f0 + y + 8 * i, t = t0 + x;
+            if (f >= F || t >= T) continue;
+            turned[f * T + t] = tile[0][x][y + 8 * i];
+            turned[(F + f) * T + t] = tile[1][x][y + 8 * i];
+        }
+        __syncthreads();
+    }
+}
+
+// out [C,R] = in [R,C] turned.
+__global__ __launch_bounds__(kThreads) void turn_kernel(const float* in, int64_t ld, float* out, int64_t R, int64_t C)
+{
+    __shared__ float tile[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t c0 = (int64_t)blockIdx.x * 32;
+    for (int64_t r0 = (int64_t)blockIdx.y * 32; r0 < R; r0 += (int64_t)gridDim.y * 32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r0 + y + 8 * i < R && c0 + x < C) tile[y + 8 * i][x] = in[(r0 + y + 8 * i) * ld + c0 + x];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c0 + y + 8 * i < C && r0 + x < R) out[(c0 + y + 8 * i) * R + r0 + x] = tile[x][y + 8 * i];
+        __syncthreads();
+    }
+}
+
+// out [R,C] packed = in [R,C].
+__global__ __launch_bounds__(kThreads) void pack_kernel(const float* in, int64_t ld, float* out, int64_t R, int64_t C)
+{
+    for (int64_t r = blockIdx.y; r < R; r += gridDim.y)
+        for (int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x; c < C; c += (int64_t)gridDim.x * kThreads) out[r * C + c] = in[r * ld + c];
+}
+
+// D [M,N] in T = the sum of the `splits` packed matrices at `parts`.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void join_kernel(const float* parts, int splits, T* d, int64_t ldd, int64_t M, int64_t N)
+{
+    for (int64_t m = blockIdx.y; m < M; m += gridDim.y)
+        for (int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x; n < N; n += (int64_t)gridDim.x * kThreads) {
+            float sum = 0.f;
+            for (int s = 0; s < splits; ++s) sum += parts[((int64_t)s * M + m) * N + n];
+            d[m * ldd + n] = from_float<T>(sum);
+        }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void zero_kernel(T* d, int64_t ldd, int64_t M, int64_t N)
+{
+    for (int64_t m = blockIdx.y; m < M; m += gridDim.y)
+        for (int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x; n < N; n += (int64_t)gridDim.x * kThreads) d[m * ldd + n] = T(0.f);
+}
+
+dim3 grid_of(int64_t columns, int64_t per, int64_t rows, int64_t rows_per)
+{
+    return dim3((unsigned)((columns + per - 1) / per), (unsigned)std::max<int64_t>(1, std::min<int64_t>((rows + rows_per - 1) / rows_per, 65535)));
+}
+
+// C [M,N] = A [M,K] B, B as [N,K] (nk) or [K,N].
+hipError_t gemm(const float* A, int64_t lda, const float* B, int64_t ldb, bool nk, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, hipStream_t stream)
+{
+    GemmArgs g{};
+    g.A = A;
+    g.B = B;
+    g.C = C;
+    g.M = (int)M;
+    g.N = (int)N;
+    g.K = (int)K;
+    g.lda = lda;
+    g.ldb = ldb;
+    g.ldc = ldc;
+    g.batch = g.batch_inner = 1;
+    g.b_is_nk = nk;
+    return launch_gemm(g, stream);
+}
+
+// ---- few tokens
+
+template <typename T, int TB, bool GATED, bool ALIGNED>
+hipError_t launch_rows_as(const ffrows::Args& a, hipStream_t stream)
+{
+    static LdsLimit limit;
+    // waves of a work-group: eight for each CU over all work-groups, as far as there are chunks for them
+    const int groups = (a.N + 15) / 16, chunks = (int)(((int64_t)a.K * sizeof(T) + 127) / 128);
+    int waves = 2;
+    while (waves < (TB == 4 ? 8 : 16) && groups * waves < 2048 && 2 * waves <= chunks) waves *= 2;
+    const size_t lds = (size_t)waves * TB * (GATED ? 2 : 1) * 256 * sizeof(float);
+    auto* const kernel = ffrows::rows_kernel<T, TB, GATED, ALIGNED>;
+    const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit) : hipSuccess;
+    return e != hipSuccess ? e : launch_kernel(kernel, dim3(groups), dim3(64 * waves), lds, stream, a);
+}
+
+template <typename T, bool GATED>
+hipError_t launch_rows(const ffrows::Args& a, bool aligned, hipStream_t stream)
+{
+    auto with = [&](auto tb) {
+        constexpr int TB = decltype(tb)::value;
+        return aligned ? launch_rows_as<T, TB, GATED, true>(a, stream) : launch_rows_as<T, TB, GATED, false>(a, stream);
+    };
+    if (a.T <= 16) return with(std::integral_constant<int, 1>{});
+    if (a.T <= 32) return with(std::integral_constant<int, 2>{});
+    return with(std::integral_constant<int, 4>{});
+}
+
+// 16-byte units: pointer, leading dimension and extent.
+bool whole_units(const void* p, int64_t ld, int64_t extent, int es) { return is_aligned16(p) && ld * es % 16 == 0 && extent * es % 16 == 0; }
+
+hipError_t forward_few(const GatedFfArgs& g, hipStream_t stream)
+{
+    const anr_gated_ff_desc& d = g.d;
+    const int es = element_bytes(d.dtype);
+    return with_type(d.dtype, [&](auto t) {
+        using T = decltype(t);
+        ffrows::Args a{};
+        a.x = g.x;
+        a.w[0] = g.w_gate;
+        a.w[1] = g.w_up;
+        a.d = g.ws;
+        a.gate = g.gate;
+        a.up = g.up;
+        a.ldx = d.ldx;
+        a.ldw[0] = a.ldw[1] = d.ldw;
+        a.ldd = d.F;
+        a.ld_pre = d.ldpre;
+        a.T = (int)d.T;
+        a.N = (int)d.F;
+        a.K = (int)d.C;
+        a.act = d.act;
+        hipError_t e = launch_rows<T, true>(a, whole_units(g.x, d.ldx, d.C, es) && whole_units(g.w_gate, d.ldw, d.C, es) && whole_units(g.w_up, d.ldw, d.C, es), stream);
+        if (e != hipSuccess) return e;
+        ffrows::Args b{};
+        b.x = g.ws;
+        b.w[0] = g.w_down;
+        b.d = g.y;
+        b.ldx = d.F;
+        b.ldw[0] = d.ld_down;
+        b.ldd = d.ldy;
+        b.T = (int)d.T;
+        b.N = (int)d.C;
+        b.K = (int)d.F;
+        return launch_rows<T, false>(b, whole_units(g.ws, d.F, d.F, es) && whole_units(g.w_down, d.ld_down, d.F, es), stream);
+    });
+}
+
+// ---- 16-bit products
+
+mm16::Problem problem(const void* x, int64_t ldx, const void* w, int64_t ldw, void* d, int64_t ldd, int64_t M, int64_t N, int64_t K)
+{
+    mm16::Problem p{};
+    p.x[0] = p.x[1] = x;
+    p.w[0] = p.w[1] = w;
+    p.d = d;
+    p.ldx = ldx;
+    p.ldw = ldw;
+    p.ldd = ldd;
+    p.M = (int)M;
+    p.N = (int)N;
+    p.K = (int)K;
+    p.segments = 1;
+    return p;
+}
+
+int64_t tiles_of(int64_t M, int64_t N, int tile_m, int tile_n) { return ((M + tile_m - 1) / tile_m) * ((N + tile_n - 1) / tile_n); }
+
+// Work-groups that share a tile's k, for products with fewer tiles than CUs: as many as fill them, with four chunks each or more.
+int splits_of(int64_t M, int64_t N, int64_t chunks)
+{
+    const int64_t tiles = tiles_of(M, N, 128, 128);
+    if (tiles >= 256) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(512 + tiles - 1) / tiles, chunks / 4, 16}));
+}
+
+hipError_t launch(mm16::Form form, int dtype, bool aligned, mm16::Args& a, hipStream_t stream)
+{
+    const int n_share = form == mm16::FORM_GATED ? 2 : 1;
+    int64_t tiles256 = 0;
+    for (int i = 0; i < a.problems; ++i) tiles256 += tiles_of(a.p[i].M, a.p[i].N, 256, 256 / n_share);
+    const int tile = a.splits == 1 && tiles256 >= 200 ? 256 : 128;
+    a.first_tile[0] = 0;
+    for (int i = 0; i < a.problems; ++i) {
+        a.p[i].tiles_m = (a.p[i].M + tile - 1) / tile;
+        a.p[i].tiles_n = (a.p[i].N + tile / n_share - 1) / (tile / n_share);
+        a.first_tile[i + 1] = a.first_tile[i] + a.p[i].tiles_m * a.p[i].tiles_n;
+    }
+    a.band = 8;
+    return dtype == ANR_F16 ? mm16::launch_products_f16(form, tile, aligned, a, stream) : mm16::launch_products_bf16(form, tile, aligned, a, stream);
+}
+
+// A product whose k may be shared: through `parts` where it is.
+hipError_t launch_shared(mm16::Form form, int dtype, bool aligned, const mm16::Problem& p, int splits, float* parts, hipStream_t stream)
+{
+    mm16::Args a{};
+    a.p[0] = p;
+    a.problems = 1;
+    a.splits = splits;
+    if (splits > 1) a.p[0].d = parts;
+    hipError_t e = launch(form, dtype, aligned, a, stream);
+    if (e != hipSuccess || splits == 1) return e;
+    return with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        return launch_kernel(join_kernel<T>, grid_of(p.N, kThreads, p.M, 1), dim3(kThreads), 0, stream, parts, splits, static_cast<T*>(p.d), p.ldd, (int64_t)p.M, (int64_t)p.N);
+    });
+}
+
+int64_t chunks_of(int64_t K) { return (K + mm16::BK - 1) / mm16::BK; }
+
+hipError_t forward_16(const GatedFfArgs& g, hipStream_t stream)
+{
+    const anr_gated_ff_desc& d = g.d;
+    char* const ws = static_cast<char*>(g.ws);
+    mm16::Args a{};
+    a.p[0] = problem(g.x, d.ldx, g.w_gate, d.ldw, ws, d.F, d.T, d.F, d.C);
+    a.p[0].w[1] = g.w_up;
+    a.problems = a.splits = 1;
+    a.act = d.act;
+    a.gate = g.gate;
+    a.up = g.up;
+    a.ld_pre = d.ldpre;
+    const bool aligned = whole_units(g.x, d.ldx, d.C, 2) && whole_units(g.w_gate, d.ldw, d.C, 2) && whole_units(g.w_up, d.ldw, d.C, 2);
+    hipError_t e = launch(mm16::FORM_GATED, d.dtype, aligned, a, stream);
+    if (e != hipSuccess) return e;
+    const mm16::Problem down = problem(ws, d.F, g.w_down, d.ld_down, g.y, d.ldy, d.T, d.C, d.F);
+    return launch_shared(mm16::FORM_ROWS, d.dtype, whole_units(ws, d.F, d.F, 2) && whole_units(g.w_down, d.ld_down, d.F, 2), down, splits_of(d.T, d.C, chunks_of(d.F)),
+                         reinterpret_cast<float*>(ws + whole_lines((size_t)d.T * d.F * 2)), stream);
+}
+
+hipError_t backward_16(const GatedFfArgs& g, hipStream_t stream)
+{
+    const anr_gated_ff_desc& d = g.d;
+    const int64_t T = d.T, C = d.C, F = d.F;
+    char* const dg = static_cast<char*>(g.ws);
+    char* const du = dg + 2 * F;                        // side by side: rows of 2 F
+    char* const h = dg + whole_lines((size_t)T * F * 4);
+    float* const parts = reinterpret_cast<float*>(h + whole_lines((size_t)T * F * 2));
+    mm16::Args a{};
+    a.p[0] = problem(g.dy, d.ldy, g.w_down, d.ld_down, dg, 2 * F, T, F, C);
+    a.problems = a.splits = 1;
+    a.act = d.act;
+    a.gate = g.gate;
+    a.up = g.up;
+    a.ld_pre = d.ldpre;
+    a.du = du;
+    a.h = h;
+    a.ld_h = F;
+    hipError_t e = launch(mm16::FORM_HIDDEN_GRADS, d.dtype, whole_units(g.dy, d.ldy, C, 2) && whole_units(g.w_down, d.ld_down, F, 2), a, stream);
+    if (e == hipSuccess && g.dx) {
+        mm16::Problem p = problem(dg, 2 * F, g.w_gate, d.ldw, g.dx, d.lddx, T, C, F);
+        p.x[1] = du;
+        p.w[1] = g.w_up;
+        p.segments = 2;
+        const bool aligned = F % 8 == 0 && whole_units(g.w_gate, d.ldw, C, 2) && whole_units(g.w_up, d.ldw, C, 2);
+        e = launch_shared(mm16::FORM_INPUT_GRAD, d.dtype, aligned, p, splits_of(T, C, 2 * chunks_of(F)), parts, stream);
+    }
+    if (e != hipSuccess || !(g.dw_gate || g.dw_up || g.dw_down)) return e;
+    mm16::Args b{};
+    b.splits = 1;
+    bool aligned = F % 8 == 0 && C % 8 == 0;
+    if (g.dw_gate) b.p[b.problems++] = problem(dg, 2 * F, g.x, d.ldx, g.dw_gate, d.lddw, F, C, T);
+    if (g.dw_up) b.p[b.problems++] = problem(du, 2 * F, g.x, d.ldx, g.dw_up, d.lddw, F, C, T);
+    if (g.dw_gate || g.dw_up) aligned = aligned && whole_units(g.x, d.ldx, C, 2);
+    if (g.dw_down) {
+        b.p[b.problems++] = problem(g.dy, d.ldy, h, F, g.dw_down, d.ld_ddown, C, F, T);
+        aligned = aligned && whole_units(g.dy, d.ldy, C, 2);
+    }
+    return launch(mm16::FORM_WEIGHT_GRADS, d.dtype, aligned, b, stream);
+}
+
+// ---- float32 products
+
+hipError_t forward_32(const GatedFfArgs& g, hipStream_t stream)
+{
+    const anr_gated_ff_desc& d = g.d;
+    float* const h = static_cast<float*>(g.ws);
+    float* gate = static_cast<float*>(g.gate);
+    float* up = static_cast<float*>(g.up);
+    int64_t ld = d.ldpre;
+    if (!gate) {
+        gate = h + whole_lines((size_t)d.T * d.F * 4) / 4;
+        up = gate + whole_lines((size_t)d.T * d.F * 4) / 4;
+        ld = d.F;
+    }
+    const float* const x = static_cast<const float*>(g.x);
+    hipError_t e = gemm(x, d.ldx, static_cast<const float*>(g.w_gate), d.ldw, true, gate, ld, d.T, d.F, d.C, stream);
+    if (e == hipSuccess) e = gemm(x, d.ldx, static_cast<const float*>(g.w_up), d.ldw, true, up, ld, d.T, d.F, d.C, stream);
+    if (e == hipSuccess)
+        e = with_activation(d.act, [&](auto act) {
+            return launch_kernel(product_of_gate_kernel<decltype(act)::value>, grid_of(d.F, kThreads, d.T, 1), dim3(kThreads), 0, stream, gate, up, ld, h, d.T, d.F);
+        });
+    if (e != hipSuccess) return e;
+    return gemm(h, d.F, static_cast<const float*>(g.w_down), d.ld_down, true, static_cast<float*>(g.y), d.ldy, d.T, d.C, d.F, stream);
+}
+
+hipError_t backward_32(const GatedFfArgs& g, hipStream_t stream)
+{
+    const anr_gated_ff_desc& d = g.d;
+    const int64_t T = d.T, C = d.C, F = d.F;
+    const size_t tf = whole_lines((size_t)T * F * 4) / 4;
+    float* const dh = static_cast<float*>(g.ws);
+    float* const h = dh + tf;
+    float* const dgu = h + tf;                          // [T, 2F]
+    float* const turned = dgu + 2 * tf;                 // [2F, T]
+    float* const weights = turned + 2 * tf;             // [2F, C], gate's and up's
+    float* const dy_turned = weights + whole_lines((size_t)F * C * 8) / 4;
+    const float *const dy = static_cast<const float*>(g.dy), *const x = static_cast<const float*>(g.x);
+    hipError_t e = gemm(dy, d.ldy, static_cast<const float*>(g.w_down), d.ld_down, false, dh, F, T, F, C, stream);
+    if (e == hipSuccess)
+        e = with_activation(d.act, [&](auto act) {
+            return launch_kernel(hidden_gradients_kernel<decltype(act)::value>, grid_of(F, 32, T, 32), dim3(kThreads), 0, stream, static_cast<const float*>(dh),
+                                 static_cast<const float*>(g.gate), static_cast<const float*>(g.up), d.ldpre, dgu, turned, h, T, F);
+        });
+    if (e == hipSuccess && g.dx) {
+        e = launch_kernel(pack_kernel, grid_of(C, kThreads, F, 1), dim3(kThreads), 0, stream, static_cast<const float*>(g.w_gate), d.ldw, weights, F, C);
+        if (e == hipSuccess) e = launch_kernel(pack_kernel, grid_of(C, kThreads, F, 1), dim3(kThreads), 0, stream, static_cast<const float*>(g.w_up), d.ldw, weights + F * C, F, C);
+        if (e == hipSuccess) e = gemm(dgu, 2 * F, weights, C, false, static_cast<float*>(g.dx), d.lddx, T, C, 2 * F, stream);
+    }
+    if (e == hipSuccess && g.dw_gate) e = gemm(turned, T, x, d.ldx, false, static_cast<float*>(g.dw_gate), d.lddw, F, C, T, stream);
+    if (e == hipSuccess && g.dw_up) e = gemm(turned + F * T, T, x, d.ldx, false, static_cast<float*>(g.dw_up), d.lddw, F, C, T, stream);
+    if (e == hipSuccess && g.dw_down) {
+        e = launch_kernel(turn_kernel, grid_of(C, 32, T, 32), dim3(kThreads), 0, stream, dy, d.ldy, dy_turned, T, C);
+        if (e == hipSuccess) e = gemm(dy_turned, T, h, F, false, static_cast<float*>(g.dw_down), d.ld_ddown, C, F, T, stream);
+    }
+    return e;
+}
+
+}  // namespace
+
+size_t gated_ff_workspace_bytes(const GatedFfArgs& g, bool backward)
+{
+    const anr_gated_ff_desc& d = g.d;
+    const size_t T = (size_t)d.T, C = (size_t)d.C, F = (size_t)d.F;
+    if (T == 0) return 0;
+    if (d.dtype == ANR_F32) {
+        const size_t tf = whole_lines(T * F * 4);
+        if (backward) return 6 * tf + whole_lines(F * C * 8) + whole_lines(T * C * 4);
+        return T <= kFewTokens ? tf : 3 * tf;
+    }
+    const size_t tf = whole_lines(T * F * 2);
+    const int splits = splits_of(d.T, d.C, (backward ? 2 : 1) * chunks_of(d.F));
+    const size_t parts = splits > 1 ? (size_t)splits * T * C * 4 : 0;
+    if (backward) return whole_lines(T * F * 4) + tf + parts;
+    return T <= kFewTokens ? tf : tf + parts;
+}
+
+hipError_t launch_gated_ff(const GatedFfArgs& g, hipStream_t stream)
+{
+    if (g.d.T == 0) return hipSuccess;
+    if (g.d.T <= kFewTokens) return forward_few(g, stream);
+    return g.d.dtype == ANR_F32 ? forward_32(g, stream) : forward_16(g, stream);
+}
+
+hipError_t launch_gated_ff_backward(const GatedFfArgs& g, hipStream_t stream)
+{
+    const anr_gated_ff_desc& d = g.d;
+    if (d.T > 0) return d.dtype == ANR_F32 ? backward_32(g, stream) : backward_16(g, stream);
+    hipError_t e = hipSuccess;
+    auto zero = [&](void* p, int64_t ld, int64_t M, int64_t N) {
+        if (e == hipSuccess && p)
+            e = with_type(d.dtype, [&](auto t) {
+                using T = decltype(t);
+                return launch_kernel(zero_kernel<T>, grid_of(N, kThreads, M, 1), dim3(kThreads), 0, stream, static_cast<T*>(p), ld, M, N);
+            });
+    };
+    zero(g.dw_gate, d.lddw, d.F, d.C);
+    zero(g.dw_up, d.lddw, d.F, d.C);
+    zero(g.dw_down, d.ld_ddown, d.C, d.F);
+    return e;
+}
+
+}  // namespace anr

@@ -1,0 +1,375 @@
+// Group norm with an activation, channels last, forward and backward.
+//
+// A group is Cg neighbouring channels of all pixels of an image: short runs of memory, C apart.  A work-group takes a
+// chunk of whole groups (at least 128 bytes of a pixel's channels, so that lines are used whole) of a slab of pixels; its
+// threads are columns of V channels by rows of pixels, and a thread keeps the sums of its V channels over its pixels.
+//
+// The statistics of a thread are mean and sum of squared differences M2, from blocks of four pixels that are joined by
+//     d = mean_b - mean_a,  mean = mean_a + d n_b / n,  M2 = M2_a + M2_b + d^2 n_a n_b / n,
+// Values are taken relative to one of their own, the group's first in the image, so that a mean far from zero costs no bits
+// (M2 by joins feels the rounding of the means that it joins: without this, values at 4096 spreads gave an rstd 4e-6 off).  Many of them are joined in two passes, mean = sum n_i mean_i / n and
+// M2 = sum M2_i + n_i (mean_i - mean)^2: threads of a work-group through LDS, slabs through the workspace, where the
+// work-groups of the second kernel join them again each for itself (fewer launches than a kernel that does).
+#pragma once
+#include "anr_kernels.h"
+#include "element_types.h"
+
+namespace anr {
+namespace gnorm {
+
+constexpr int kThreads = 256;
+
+// Offsets of pixels; flat: one stride from pixel to pixel.
+struct Pixels {
+    int64_t sn, sh, sw;
+    __device__ __forceinline__ int64_t at(int p, int W, const FastDiv& by_w, bool flat) const
+    {
+        if (flat) return (int64_t)p * sw;
+        const int h = by_w.div(p);
+        return (int64_t)h * sh + (int64_t)(p - h * W) * sw;
+    }
+};
+
+struct Args {
+    const void *x, *dy;
+    void* y;
+    const void *gamma, *beta;
+    void *dgamma, *dbeta;
+    float *mean, *rstd;
+    float* ws;                      // partial sums of the slabs
+    float* sums;                    // backward: sums of a channel over an image's slabs, [N][2][C]
+    float* group_sums;              // backward: [N][groups][2]
+    Pixels px, pdy, py;
+    FastDiv by_w;
+    float eps;
+    int N, HW, W, C, groups, cg, flat, param_dtype;
+    int chunk;                      // channels of a chunk: whole groups
+    int slabs, slab_pixels;
+};
+
+// What a work-group works on.
+struct Place {
+    int slab, n, c0, channels, p0, p1;
+    int columns, tx, ty, rows;      // of V channels; rows of threads
+    __device__ __forceinline__ Place(const Args& a, int V)
+    {
+        slab = blockIdx.x;
+        n = blockIdx.z;
+        c0 = blockIdx.y * a.chunk;
+        channels = min(a.chunk, a.C - c0);
+        p0 = slab * a.slab_pixels;
+        p1 = min(a.HW, p0 + a.slab_pixels);
+        columns = channels / V;
+        const int wide = min(columns, kThreads);
+        rows = kThreads / wide;
+        ty = threadIdx.x / wide;
+        tx = ty < rows ? threadIdx.x - ty * wide : columns;          // (threads that are left over have no column)
+    }
+};
+
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// First kernel of the forward pass: mean and M2 of each group of the chunk over the slab.
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void stats_kernel(const Args a)
+{
+    extern __shared__ __attribute__((aligned(16))) float lds[];      // [rows][channels] of (mean, M2)
+    const Place s(a, V);
+    const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
+    const int first = s.p0 + s.ty;
+    const int mine = s.tx < s.columns && first < s.p1 ? (s.p1 - first + s.rows - 1) / s.rows : 0;
+    for (int col = s.tx; col < s.columns; col += kThreads) {
+        float mean[V], m2[V], origin[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            mean[i] = m2[i] = 0.f;
+            origin[i] = to_float(x[(col * V + i) / a.cg * a.cg]);
+        }
+        const T* const xc = x + col * V;
+        int k = 0;
+        for (; k + 4 <= mine; k += 4) {
+            float v[4][V];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                load_floats<T, V>(xc + a.px.at(first + (k + u) * s.rows, a.W, a.by_w, a.flat), v[u]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[u][i] -= origin[i];
+            }
+            const float n = (float)k, share = 4.f / (n + 4.f), weight = n * share;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float m = 0.25f * ((v[0][i] + v[1][i]) + (v[2][i] + v[3][i]));
+                float q = 0.f;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) q = fmaf(v[u][i] - m, v[u][i] - m, q);
+                const float d = m - mean[i];
+                m2[i] += fmaf(d * d, weight, q);
+                mean[i] = fmaf(d, share, mean[i]);
+            }
+        }
+        for (; k < mine; ++k) {
+            float v[V];
+            load_floats<T, V>(xc + a.px.at(first + k * s.rows, a.W, a.by_w, a.flat), v);
+            const float share = 1.f / (float)(k + 1);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[i] -= origin[i];
+                const float d = v[i] - mean[i];
+                mean[i] = fmaf(d, share, mean[i]);
+                m2[i] = fmaf(d, v[i] - mean[i], m2[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float* const at = lds + 2 * (s.ty * s.channels + col * V + i);
+            at[0] = mean[i];
+            at[1] = m2[i];
+        }
+    }
+    __syncthreads();
+    const int groups = s.channels / a.cg, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int pixels = s.p1 - s.p0;
+    for (int g = wave; g < groups; g += kThreads / 64) {
+        float sum = 0.f;
+        for (int e = lane; e < s.rows * a.cg; e += 64) {
+            const int row = e / a.cg, c = g * a.cg + e - row * a.cg;
+            const int count = pixels > row ? (pixels - row + s.rows - 1) / s.rows : 0;
+            sum = fmaf((float)count, lds[2 * (row * s.channels + c)], sum);
+        }
+        const float mean = wave_sum(sum) / ((float)pixels * (float)a.cg);
+        float q = 0.f;
+        for (int e = lane; e < s.rows * a.cg; e += 64) {
+            const int row = e / a.cg, c = g * a.cg + e - row * a.cg;
+            const int count = pixels > row ? (pixels - row + s.rows - 1) / s.rows : 0;
+            const float d = lds[2 * (row * s.channels + c)] - mean;
+            q += fmaf((float)count * d, d, lds[2 * (row * s.channels + c) + 1]);
+        }
+        q = wave_sum(q);
+        if (lane == 0) {
+            float* const at = a.ws + 2 * (((int64_t)s.n * a.slabs + s.slab) * a.groups + s.c0 / a.cg + g);
+            at[0] = mean;
+            at[1] = q;
+        }
+    }
+}
+
+// Parameter i of gamma or beta.
+__device__ __forceinline__ float parameter(const void* p, int i, int dtype, float absent) { return p ? load_any(p, i, dtype) : absent; }
+
+// Second kernel of the forward pass.
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
+{
+    constexpr bool QUICK = sizeof(T) == 2;
+    extern __shared__ __attribute__((aligned(16))) float lds[];      // [groups of the chunk] of (mean, rstd)
+    const Place s(a, V);
+    const int groups = s.channels / a.cg, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g0 = s.c0 / a.cg;
+    for (int g = wave; g < groups; g += kThreads / 64) {
+        const float* const at = a.ws + 2 * ((int64_t)s.n * a.slabs * a.groups + g0 + g);
+        float sum = 0.f;
+        for (int i = lane; i < a.slabs; i += 64) sum = fmaf((float)(min(a.HW, (i + 1) * a.slab_pixels) - i * a.slab_pixels), at[2 * (int64_t)i * a.groups], sum);
+        const float mean = wave_sum(sum) / (float)a.HW;              // (relative to the group's first value)
+        float q = 0.f;
+        for (int i = lane; i < a.slabs; i += 64) {
+            const float pixels = (float)(min(a.HW, (i + 1) * a.slab_pixels) - i * a.slab_pixels), d = at[2 * (int64_t)i * a.groups] - mean;
+            q += fmaf(pixels * (float)a.cg * d, d, at[2 * (int64_t)i * a.groups + 1]);
+        }
+        const float rstd = 1.f / sqrtf(wave_sum(q) / ((float)a.HW * (float)a.cg) + a.eps);
+        if (lane == 0) {
+            const float whole = mean + to_float(static_cast<const T*>(a.x)[s.n * a.px.sn + s.c0 + g * a.cg]);
+            lds[2 * g] = whole;
+            lds[2 * g + 1] = rstd;
+            if (s.slab == 0 && a.mean) a.mean[(int64_t)s.n * a.groups + g0 + g] = whole;
+            if (s.slab == 0 && a.rstd) a.rstd[(int64_t)s.n * a.groups + g0 + g] = rstd;
+        }
+    }
+    __syncthreads();
+    const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
+    T* const y = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
+    for (int col = s.tx; col < s.columns; col += kThreads) {
+        float mean[V], scale[V], shift[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = col * V + i, g = c / a.cg;
+            mean[i] = lds[2 * g];
+            scale[i] = lds[2 * g + 1] * parameter(a.gamma, s.c0 + c, a.param_dtype, 1.f);
+            shift[i] = parameter(a.beta, s.c0 + c, a.param_dtype, 0.f);
+        }
+#pragma unroll 4
+        for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
+            float v[V];
+            load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = activation<ACT, QUICK>(fmaf(v[i] - mean[i], scale[i], shift[i]));
+            store_floats<T, V>(y + a.py.at(p, a.W, a.by_w, a.flat) + col * V, v);
+        }
+    }
+}
+
+// What a thread keeps of its channels in the backward pass.
+template <int V>
+struct Channels {
+    float mean[V], rstd[V], gamma[V], beta[V];
+    __device__ __forceinline__ void load(const Args& a, int n, int c0)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = c0 + i, g = c / a.cg;
+            mean[i] = a.mean[(int64_t)n * a.groups + g];
+            rstd[i] = a.rstd[(int64_t)n * a.groups + g];
+            gamma[i] = parameter(a.gamma, c, a.param_dtype, 1.f);
+            beta[i] = parameter(a.beta, c, a.param_dtype, 0.f);
+        }
+    }
+    // xhat and dz of one element
+    template <int ACT, bool QUICK>
+    __device__ __forceinline__ void element(int i, float x, float dy, float& hat, float& dz) const
+    {
+        hat = (x - mean[i]) * rstd[i];
+        float slope = 1.f;
+        if (ACT != ANR_ACT_NONE) activation_and_slope<ACT, QUICK>(fmaf(hat, gamma[i], beta[i]), slope);
+        dz = dy * slope;
+    }
+};
+
+// First kernel of the backward pass: sums of dz and dz xhat of each channel over the slab.
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(kThreads) void backward_sums_kernel(const Args a)
+{
+    constexpr bool QUICK = sizeof(T) == 2;
+    extern __shared__ __attribute__((aligned(16))) float lds[];      // [rows][2][channels]
+    const Place s(a, V);
+    const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
+    const T* const dy = static_cast<const T*>(a.dy) + s.n * a.pdy.sn + s.c0;
+    for (int col = s.tx; col < s.columns; col += kThreads) {
+        Channels<V> ch;
+        ch.load(a, s.n, s.c0 + col * V);
+        float sum[V], with_hat[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] = with_hat[i] = 0.f;
+#pragma unroll 4
+        for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
+            float v[V], d[V];
+            load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
+            load_floats<T, V>(dy + a.pdy.at(p, a.W, a.by_w, a.flat) + col * V, d);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float hat, dz;
+                ch.template element<ACT, QUICK>(i, v[i], d[i], hat, dz);
+                sum[i] += dz;
+                with_hat[i] = fmaf(dz, hat, with_hat[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            lds[(2 * s.ty) * s.channels + col * V + i] = sum[i];
+            lds[(2 * s.ty + 1) * s.channels + col * V + i] = with_hat[i];
+        }
+    }
+    __syncthreads();
+    float* const out = a.ws + ((int64_t)s.n * a.slabs + s.slab) * 2 * a.C + s.c0;
+    for (int e = threadIdx.x; e < 2 * s.channels; e += kThreads) {
+        const int which = e >= s.channels, c = e - which * s.channels;
+        float sum = 0.f;
+        for (int r = 0; r < s.rows; ++r) sum += lds[(2 * r + which) * s.channels + c];
+        out[(int64_t)which * a.C + c] = sum;
+    }
+}
+
+// Second kernel: sums over an image's slabs, and those of its groups with gamma.
+__global__ __launch_bounds__(kThreads) void backward_groups_kernel(const Args a)
+{
+    extern __shared__ __attribute__((aligned(16))) float lds[];      // [2][channels]
+    const int n = blockIdx.z, c0 = blockIdx.y * a.chunk, channels = min(a.chunk, a.C - c0);
+    const float* const in = a.ws + (int64_t)n * a.slabs * 2 * a.C + c0;
+    for (int e = threadIdx.x; e < 2 * channels; e += kThreads) {
+        const int which = e >= channels, c = e - which * channels;
+        float sum = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < a.slabs; ++i) sum += in[((int64_t)i * 2 + which) * a.C + c];
+        a.sums[((int64_t)n * 2 + which) * a.C + c0 + c] = sum;
+        lds[e] = sum * parameter(a.gamma, c0 + c, a.param_dtype, 1.f);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * (channels / a.cg); e += kThreads) {
+        const int which = e & 1, g = e >> 1;
+        float sum = 0.f;
+        for (int c = 0; c < a.cg; ++c) sum += lds[which * channels + g * a.cg + c];
+        a.group_sums[((int64_t)n * a.groups + c0 / a.cg + g) * 2 + which] = sum / ((float)a.HW * (float)a.cg);
+    }
+}
+
+// dgamma and dbeta of the chunk: sums over the images.
+__device__ __forceinline__ void parameter_gradients(const Args& a)
+{
+    const int c0 = blockIdx.y * a.chunk, channels = min(a.chunk, a.C - c0);
+    for (int e = threadIdx.x; e < 2 * channels; e += kThreads) {
+        const int which = e >= channels, c = c0 + e - which * channels;
+        void* const out = which ? a.dgamma : a.dbeta;
+        if (!out) continue;
+        float sum = 0.f;
+#pragma unroll 8
+        for (int n = 0; n < a.N; ++n) sum += a.sums[((int64_t)n * 2 + which) * a.C + c];
+        store_any(out, c, a.param_dtype, sum);
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void backward_parameters_kernel(const Args a) { parameter_gradients(a); }
+
+// Third kernel: dx, and in the first slab of the first image the parameters' gradients.
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
+{
+    constexpr bool QUICK = sizeof(T) == 2;
+    const Place s(a, V);
+    const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
+    const T* const dy = static_cast<const T*>(a.dy) + s.n * a.pdy.sn + s.c0;
+    T* const dx = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
+    for (int col = s.tx; col < s.columns; col += kThreads) {
+        Channels<V> ch;
+        ch.load(a, s.n, s.c0 + col * V);
+        float mean_dz[V], mean_with_hat[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int g = (s.c0 + col * V + i) / a.cg;
+            mean_dz[i] = a.group_sums[((int64_t)s.n * a.groups + g) * 2];
+            mean_with_hat[i] = a.group_sums[((int64_t)s.n * a.groups + g) * 2 + 1];
+        }
+#pragma unroll 2
+        for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
+            float v[V], d[V];
+            load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
+            load_floats<T, V>(dy + a.pdy.at(p, a.W, a.by_w, a.flat) + col * V, d);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float hat, dz;
+                ch.template element<ACT, QUICK>(i, v[i], d[i], hat, dz);
+                v[i] = ch.rstd[i] * (fmaf(dz, ch.gamma[i], -mean_dz[i]) - hat * mean_with_hat[i]);
+            }
+            store_floats<T, V>(dx + a.py.at(p, a.W, a.by_w, a.flat) + col * V, v);
+        }
+    }
+    if (s.n == 0 && s.slab == 0) parameter_gradients(a);
+}
+
+// Nothing to norm: means of zero, spreads of zero, gradients of zero.
+__global__ __launch_bounds__(kThreads) void empty_kernel(const Args a, bool backward)
+{
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (!backward && i < (int64_t)a.N * a.groups) {
+        if (a.mean) a.mean[i] = 0.f;
+        if (a.rstd) a.rstd[i] = 1.f / sqrtf(a.eps);
+    }
+    if (backward && i < a.C) {
+        if (a.dgamma) store_any(a.dgamma, i, a.param_dtype, 0.f);
+        if (a.dbeta) store_any(a.dbeta, i, a.param_dtype, 0.f);
+    }
+}
+
+}  // namespace gnorm
+}  // namespace anr

@@ -1,0 +1,10 @@
+// mm16_kernel.h for bf16.
+#include "mm16_launch.h"
+
+namespace anr {
+namespace mm16 {
+
+hipError_t launch_products_bf16(Form form, int tile, bool aligned, const Args& a, hipStream_t stream) { return launch_products<bf16_t>(form, tile, aligned, a, stream); }
+
+}  // namespace mm16
+}  // namespace anr

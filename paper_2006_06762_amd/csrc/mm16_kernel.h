@@ -1,0 +1,400 @@
+// Matrix products of 16-bit types on the matrix pipes, D[m][n] = sum_k X[m][k] W[n][k], for the products of the gated
+// feed-forward block: sums in float32, one rounding where they are stored.
+//
+// Each operand lies in memory with k contiguous (K_ROWS: rows of k) or with its own index contiguous (K_COLUMNS: rows
+// are k).  A work-group takes a tile of BM x BN, its waves WM x WN parts of it in blocks of 32 x 32
+// (v_mfma_f32_32x32x16), and walks k in chunks of 64: global -> registers -> LDS -> operands, with two LDS buffers, so that
+// one is multiplied while the other is filled and the loads of the chunk after that are on their way.
+//
+// LDS.  K_ROWS: 128 bytes of k per row, 16-byte units exchanged by row (unit ^ row % 8), so that eight rows' same unit, which an
+// operand read takes together, lie in different banks.  K_COLUMNS: rows of k as they come, 64 bytes apart from the next
+// one beyond their length; ds_read_b64_tr_b16 turns 4 k x 16 columns as it reads, each lane gets four k of its column,
+// and the four rows of such a read are in different banks.
+//
+// W is the instruction's first operand: register r of a lane is then n = 8 (r / 4) + 4 (lane / 32) + r % 4 of the block and
+// m = lane % 32: four neighbouring columns of a row of D.
+#pragma once
+#include "anr_kernels.h"
+#include "element_types.h"
+
+namespace anr {
+namespace mm16 {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef half_t f16x8 __attribute__((ext_vector_type(8)));
+typedef bf16_t b16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int BK = 64;                          // k of a chunk
+constexpr uint32_t kNowhere = 0x80000000u;      // byte offset past every descriptor's extent: loads zeros
+constexpr int kExtent = 0x7fffffff;
+
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c, half_t)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c, bf16_t)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
+}
+
+enum Kind { K_ROWS, K_COLUMNS };
+enum Epilogue {
+    STORE,          // D in the element type
+    PARTIAL,        // D in float32, [split][M][N] packed
+    GATED,          // W's rows alternate by 32 between two matrices: act(D of the first) * D of the second
+    GATED_BACKWARD  // D is dh: gradients of gate and up, and h
+};
+
+// One product.  Two pointers of an operand: K_ROWS of GATED: gate's and up's weights; else the sum runs over
+// `segments` pairs of operands of K each.
+struct Problem {
+    const void* x[2];
+    const void* w[2];
+    void* d;
+    int64_t ldx, ldw, ldd;
+    int M, N, K;
+    int segments;
+    int tiles_m, tiles_n;
+};
+
+struct Args {
+    Problem p[3];
+    int problems;
+    int first_tile[4];              // of each problem, and of the one behind the last
+    int band;                       // tiles are walked in bands of so many rows of tiles
+    int splits;                     // work-groups that share a tile's k (PARTIAL)
+    int act;
+    // GATED: where gate and up go (or null); GATED_BACKWARD: gate and up, and where dg, du and h go (leading dimensions
+    // ld_pre and problem 0's ldd)
+    void *gate, *up;
+    int64_t ld_pre;
+    void *du, *h;
+    int64_t ld_h;
+};
+
+// An operand of R rows (its own index) in LDS.
+template <Kind KIND, int R>
+struct Image {
+    static constexpr int ROW = KIND == K_ROWS ? BK * 2 : R * 2 + 64;
+    static constexpr int BYTES = (KIND == K_ROWS ? R : BK) * ROW;
+};
+
+template <int BM, int BN, Kind XK, Kind WK>
+constexpr size_t lds_bytes() { return 2 * (size_t)(Image<XK, BM>::BYTES + Image<WK, BN>::BYTES); }
+
+// Global -> registers -> LDS of one operand's chunk by NT threads.
+template <typename T, Kind KIND, int R, int NT, bool ALIGNED, bool PAIRED>
+struct Stager {
+    static constexpr int UNITS = R * BK / 8 / NT;                     // 16-byte units of a thread
+    static constexpr int ROW_UNITS = KIND == K_ROWS ? BK / 8 : R / 8; // units of a row of memory
+    static_assert(R * BK / 8 % NT == 0 && NT % ROW_UNITS == 0, "whole units for every thread");
+    const char* base[2];            // of the tile: element (first row, k = 0)
+    int64_t ld;                     // elements
+    int own, K;                     // rows (own index) from the tile's first on; k
+    int first;                      // this thread's row of memory in the first unit, and its unit in the row
+    int unit;
+    uint32_t offset[UNITS];         // bytes from the chunk's base, or nowhere
+    int which;                      // PAIRED: the matrix of unit 0 (units of a thread alternate by NT / 8 rows)
+    u32x4 data[UNITS];
+
+    // `rows`: extent of the operand's own index; `row0`: the tile's first
+    __device__ __forceinline__ void init(const void* p0, const void* p1, int64_t ld_, int row0, int rows, int k, int tid)
+    {
+        ld = ld_;
+        own = rows - row0;
+        K = k;
+        first = tid / ROW_UNITS;
+        unit = tid % ROW_UNITS;
+        const int64_t start = KIND == K_ROWS ? (int64_t)row0 * ld : row0;
+        base[0] = static_cast<const char*>(p0) + 2 * start;
+        base[1] = static_cast<const char*>(p1) + 2 * start;
+        if (KIND == K_ROWS) {
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) {
+                int r = first + i * (NT / ROW_UNITS);
+                if (PAIRED) r = (r >> 6) * 32 + (r & 31);
+                offset[i] = (uint32_t)(min(r, own - 1) * ld * 2) + unit * 16;
+            }
+            which = PAIRED ? __builtin_amdgcn_readfirstlane((first >> 5) & 1) : 0;
+        } else {
+            const int column = ALIGNED ? min(unit * 8, own - 8) : unit * 8;
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) offset[i] = (uint32_t)((first + i * (NT / ROW_UNITS)) * ld * 2) + column * 2;
+            which = 0;
+        }
+    }
+    __device__ __forceinline__ int matrix_of(int i) const { return PAIRED ? (which + i * (NT / ROW_UNITS) / 32) & 1 : 0; }
+
+    // chunk of k from k0 on, of segment `seg`
+    __device__ __forceinline__ void load(int k0, int seg)
+    {
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const char* const b = ((PAIRED ? matrix_of(i) : seg) ? base[1] : base[0]) + 2 * (KIND == K_ROWS ? (int64_t)k0 : k0 * ld);
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(b), 0, kExtent, 0x00020000);
+            const int k = KIND == K_ROWS ? k0 + unit * 8 : k0 + first + i * (NT / ROW_UNITS);
+            if (ALIGNED) {
+                data[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(k < K ? offset[i] : kNowhere), 0, 0));
+            } else {
+                uint16_t e[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool in = KIND == K_ROWS ? k + j < K : k < K && unit * 8 + j < own;
+                    e[j] = __builtin_amdgcn_raw_buffer_load_b16(rsrc, (int)(in ? offset[i] + 2 * j : kNowhere), 0, 0);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) data[i][j] = e[2 * j] | (uint32_t)e[2 * j + 1] << 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char* lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int r = first + i * (NT / ROW_UNITS);
+            const int at = KIND == K_ROWS ? r * Image<KIND, R>::ROW + ((unit ^ (r & 7)) * 16) : r * Image<KIND, R>::ROW + unit * 16;
+            *reinterpret_cast<u32x4*>(lds + at) = data[i];
+        }
+    }
+};
+
+// Eight k from 16 step + 8 (lane / 32) on of row `row0 + lane % 32`.
+template <Kind KIND, int R>
+__device__ __forceinline__ u32x4 operand(const char* lds, int row0, int step, int lane)
+{
+    if (KIND == K_ROWS) {
+        const int r = row0 + (lane & 31), u = 2 * step + (lane >> 5);
+        return *reinterpret_cast<const u32x4*>(lds + r * Image<KIND, R>::ROW + ((u ^ (r & 7)) * 16));
+    }
+    typedef __attribute__((address_space(3))) s16x4 lds_t;
+    const int j = lane & 15;
+    const char* const at = lds + (step * 16 + (lane >> 5) * 8 + (j >> 2)) * Image<KIND, R>::ROW + (row0 + ((lane >> 4) & 1) * 16 + (j & 3) * 4) * 2;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(uintptr_t)at));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(uintptr_t)(at + 4 * Image<KIND, R>::ROW)));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+
+// Four neighbouring elements of a row from column n on, of which `in` exist.
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float (&v)[4], int in, bool aligned)
+{
+    if (aligned && in >= 4) {
+        store_floats<T, 4>(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < in) p[i] = from_float<T>(v[i]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, float (&v)[4], int in, bool aligned)
+{
+    if (aligned && in >= 4) {
+        load_floats<T, 4>(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < in ? to_float(p[i]) : 0.f;
+    }
+}
+
+// f(std::integral_constant<int, ACT>) on the device.
+template <typename F>
+__device__ __forceinline__ void device_activation(int act, F f)
+{
+    switch (act) {
+        case ANR_ACT_RELU: f(std::integral_constant<int, ANR_ACT_RELU>{}); break;
+        case ANR_ACT_SILU: f(std::integral_constant<int, ANR_ACT_SILU>{}); break;
+        case ANR_ACT_GELU: f(std::integral_constant<int, ANR_ACT_GELU>{}); break;
+        case ANR_ACT_GELU_TANH: f(std::integral_constant<int, ANR_ACT_GELU_TANH>{}); break;
+        default: f(std::integral_constant<int, ANR_ACT_NONE>{}); break;
+    }
+}
+
+template <typename T, int BM, int BN, int WM, int WN, Kind XK, Kind WK, Epilogue EPI, bool ALIGNED>
+__global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void product_kernel(const Args args)
+{
+    constexpr int NT = 64 * WM * WN, MB = BM / (32 * WM), NB = BN / (32 * WN);
+    constexpr int XBYTES = Image<XK, BM>::BYTES, BUF = XBYTES + Image<WK, BN>::BYTES;
+    constexpr bool PAIRED = EPI == GATED;
+    constexpr int TILE_N = PAIRED ? BN / 2 : BN;                      // columns of D in a tile
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    // Work-group ids are dealt round-robin over the 8 XCDs, each with its own L2: every XCD gets a contiguous run of tiles,
+    // walked in bands of `band` rows of tiles, column by column
+    int id = blockIdx.x;
+    {
+        const int all = (int)gridDim.x, per = all >> 3, rest = all & 7, xcd = id & 7, slot = id >> 3;
+        id = xcd * per + (xcd < rest ? xcd : rest) + slot;
+    }
+    const int split = EPI == PARTIAL ? id % args.splits : 0;
+    if (EPI == PARTIAL) id /= args.splits;
+    const int which = (args.problems > 1 && id >= args.first_tile[1]) + (args.problems > 2 && id >= args.first_tile[2]);
+    const Problem& p = args.p[which];
+    id -= args.first_tile[which];
+    const int band = id / (args.band * p.tiles_n), rows = min(args.band, p.tiles_m - band * args.band), in_band = id - band * args.band * p.tiles_n;
+    const int m0 = (band * args.band + in_band % rows) * BM, n0 = (in_band / rows) * TILE_N;
+    const int M = p.M, N = p.N, K = p.K;
+
+    Stager<T, XK, BM, NT, ALIGNED, false> sx;
+    Stager<T, WK, BN, NT, ALIGNED, PAIRED> sw;
+    sx.init(p.x[0], p.x[1], p.ldx, m0, M, K, tid);
+    sw.init(p.w[0], p.w[1], p.ldw, n0, N, K, tid);
+
+    const int chunks = (K + BK - 1) / BK, all = chunks * (PAIRED ? 1 : p.segments);
+    int c0 = 0, c1 = all;
+    if (EPI == PARTIAL) {
+        c0 = (int)((int64_t)all * split / args.splits);
+        c1 = (int)((int64_t)all * (split + 1) / args.splits);
+    }
+    auto load = [&](int c) {
+        const int seg = !PAIRED && c >= chunks;
+        const int k0 = (c - (seg ? chunks : 0)) * BK;
+        sx.load(k0, seg);
+        sw.load(k0, seg);
+    };
+    auto store = [&](int buf) {
+        sx.store(lds + buf * BUF);
+        sw.store(lds + buf * BUF + XBYTES);
+    };
+
+    f32x16 acc[NB][MB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[n][m][r] = 0.f;
+
+    if (c0 < c1) {
+        load(c0);
+        store(0);
+        if (c0 + 1 < c1) load(c0 + 1);
+        __syncthreads();
+#pragma unroll 1
+        for (int c = c0; c < c1; ++c) {
+            const char* const x = lds + ((c - c0) & 1) * BUF;
+            const char* const w = x + XBYTES;
+#pragma unroll
+            for (int s = 0; s < BK / 16; ++s) {
+                u32x4 xv[MB], wv[NB];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) wv[n] = operand<WK, BN>(w, (wn * NB + n) * 32, s, lane);
+#pragma unroll
+                for (int m = 0; m < MB; ++m) xv[m] = operand<XK, BM>(x, (wm * MB + m) * 32, s, lane);
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int m = 0; m < MB; ++m) acc[n][m] = mfma(wv[n], xv[m], acc[n][m], T{});
+            }
+            if (c + 1 < c1) store((c + 1 - c0) & 1);
+            if (c + 2 < c1) load(c + 2);
+            __syncthreads();
+        }
+    }
+
+    const int half = lane >> 5;
+    if constexpr (EPI == STORE) {
+        T* const d = static_cast<T*>(p.d);
+        const bool aligned = ((reinterpret_cast<uintptr_t>(d) | (uintptr_t)(2 * p.ldd)) & 7) == 0;
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+            const int row = m0 + (wm * MB + m) * 32 + (lane & 31);
+            if (row >= M) continue;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = n0 + (wn * NB + n) * 32 + 8 * q + 4 * half;
+                    const float v[4] = {acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+                    store4(d + (int64_t)row * p.ldd + col, v, N - col, aligned);
+                }
+        }
+    } else if constexpr (EPI == PARTIAL) {
+        float* const d = static_cast<float*>(p.d) + (int64_t)split * M * N;
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+            const int row = m0 + (wm * MB + m) * 32 + (lane & 31);
+            if (row >= M) continue;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = n0 + (wn * NB + n) * 32 + 8 * q + 4 * half;
+                    const float v[4] = {acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+                    store4(d + (int64_t)row * N + col, v, N - col, N % 4 == 0);
+                }
+        }
+    } else if constexpr (EPI == GATED) {
+        static_assert(NB % 2 == 0, "blocks of gate and up side by side");
+        T* const d = static_cast<T*>(p.d);
+        T *const gate = static_cast<T*>(args.gate), *const up = static_cast<T*>(args.up);
+        const bool aligned = ((reinterpret_cast<uintptr_t>(d) | (uintptr_t)(2 * p.ldd)) & 7) == 0;
+        const bool aligned_pre = ((reinterpret_cast<uintptr_t>(gate) | reinterpret_cast<uintptr_t>(up) | (uintptr_t)(2 * args.ld_pre)) & 7) == 0;
+        device_activation(args.act, [&](auto act) {
+#pragma unroll
+            for (int m = 0; m < MB; ++m) {
+                const int row = m0 + (wm * MB + m) * 32 + (lane & 31);
+                if (row >= M) continue;
+#pragma unroll
+                for (int n = 0; n < NB; n += 2)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int col = n0 + (wn * NB + n) / 2 * 32 + 8 * q + 4 * half;
+                        float g[4], u[4], h[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            g[e] = acc[n][m][4 * q + e];
+                            u[e] = acc[n + 1][m][4 * q + e];
+                            h[e] = activation<decltype(act)::value, true>(g[e]) * u[e];
+                        }
+                        if (gate) {
+                            store4(gate + (int64_t)row * args.ld_pre + col, g, N - col, aligned_pre);
+                            store4(up + (int64_t)row * args.ld_pre + col, u, N - col, aligned_pre);
+                        }
+                        store4(d + (int64_t)row * p.ldd + col, h, N - col, aligned);
+                    }
+            }
+        });
+    } else {
+        T* const d = static_cast<T*>(p.d);
+        T *const du = static_cast<T*>(args.du), *const h = static_cast<T*>(args.h);
+        const T *const gate = static_cast<const T*>(args.gate), *const up = static_cast<const T*>(args.up);
+        const bool aligned = N % 4 == 0;                              // (workspace: rows of 2 F and of F elements)
+        const bool aligned_pre = ((reinterpret_cast<uintptr_t>(gate) | reinterpret_cast<uintptr_t>(up) | (uintptr_t)(2 * args.ld_pre)) & 7) == 0;
+        device_activation(args.act, [&](auto act) {
+#pragma unroll
+            for (int m = 0; m < MB; ++m) {
+                const int row = m0 + (wm * MB + m) * 32 + (lane & 31);
+                if (row >= M) continue;
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int col = n0 + (wn * NB + n) * 32 + 8 * q + 4 * half;
+                        float g[4], u[4], dg[4], dup[4], hh[4];
+                        load4(gate + (int64_t)row * args.ld_pre + col, g, N - col, aligned_pre);
+                        load4(up + (int64_t)row * args.ld_pre + col, u, N - col, aligned_pre);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float dh = acc[n][m][4 * q + e];
+                            float slope;
+                            const float a = activation_and_slope<decltype(act)::value, true>(g[e], slope);
+                            dg[e] = dh * u[e] * slope;
+                            dup[e] = dh * a;
+                            hh[e] = a * u[e];
+                        }
+                        store4(d + (int64_t)row * p.ldd + col, dg, N - col, aligned);
+                        store4(du + (int64_t)row * p.ldd + col, dup, N - col, aligned);
+                        store4(h + (int64_t)row * args.ld_h + col, hh, N - col, aligned);
+                    }
+            }
+        });
+    }
+}
+
+}  // namespace mm16
+}  // namespace anr

@@ -1,0 +1,673 @@
+"""Group norm, rotary positions and the gated feed-forward block against their definitions in 64 bits (oracle/blocks.py).
+
+Bounds are those of the arithmetic: u = 2^-24 is half a unit of float32's last place relative to a value, HALF[t] that of the type
+of the result, which is rounded once (or once more where the header says that a value between two products is held in that
+type).  A sum of n products is off by at most (n + 8) u of the sum of their magnitudes.  Activations and their
+slopes are evaluated to 64 u of 1 + |z|: the quick exponential's argument is rounded, 1.5 |z| u, and what follows are a few
+roundings (|z| stays below 20 here)."""
+import numpy as np
+import pytest
+
+from oracle import blocks as O
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF = {t: torch.finfo(t).eps / 2 for t in TYPES.values()}
+TINY = {t: torch.finfo(t).smallest_normal * torch.finfo(t).eps / 2 for t in TYPES.values()}      # half the spacing of denormals
+ACTS = ("none", "relu", "silu", "gelu", "gelu_tanh")
+
+
+@pytest.fixture(scope="module")
+def anr():
+    from paper_2006_06762_amd import binding
+    return binding
+
+
+def rng(seed):
+    return np.random.Generator(np.random.PCG64(seed))
+
+
+def dev(a, t):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(t).cuda()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def within(name, got, want, bound, t):
+    got = host(got)
+    assert got.shape == want.shape
+    over = np.abs(got - want) - (bound + HALF[t] * (np.abs(want) + bound) + TINY[t])
+    at = np.unravel_index(np.argmax(over), over.shape) if over.size else ()
+    assert not over.size or np.max(over) <= 0, "%s: %s got %r, want %r, bound %r" % (name, at, got[at], want[at], np.broadcast_to(bound, want.shape)[at])
+
+
+def nans(*shape, dtype):
+    return torch.full(shape, float("nan"), dtype=dtype, device="cuda")
+
+
+# ------------------------------------------------------------------ group norm
+def images(a, t, spare=0, crop=0):
+    """[N,C,H,W] channels last on the GPU; spare: channels of a wider tensor around it, crop: pixels around it."""
+    N, C, H, W = a.shape
+    wide = torch.zeros((N, H + crop, W + crop, C + spare), dtype=t, device="cuda")
+    view = wide[:, crop // 2:crop // 2 + H, :W, spare // 2:spare // 2 + C]
+    view.copy_(torch.from_numpy(np.ascontiguousarray(a.transpose(0, 2, 3, 1))).to(t))
+    return view.permute(0, 3, 1, 2)
+
+
+def norm_case(anr, seed, N, C, H, W, groups, act, t, shift=1.0, spare=0, crop=0, param=None, eps=1e-5):
+    r = rng(seed)
+    x = images(r.normal(size=(N, C, H, W)) * r.uniform(0.5, 2, size=(1, C, 1, 1)) + shift * r.normal(size=(1, C, 1, 1)), t, spare, crop)
+    pt = param or t
+    g, b = dev(r.normal(size=C) * 0.3 + 1, pt), dev(r.normal(size=C) * 0.3, pt)
+    g64, b64 = host(g), host(b)
+    per = (1, C, 1, 1)
+    x64 = host(x)
+
+    y = images(np.full((N, C, H, W), np.nan), t, spare, crop)
+    mean, rstd = nans(N, groups, dtype=torch.float32), nans(N, groups, dtype=torch.float32)
+    assert anr.group_norm(x, groups, y, g, b, eps, getattr(anr, "ANR_ACT_" + act.upper()), mean, rstd) is y
+    want, m64, r64, z = O.group_norm(x64, groups, g64, b64, eps, act)
+    v = x64.reshape(N, groups, -1)
+    # the mean of n values: blocks of four and joins of at most 64 parts one after another, each rounded: 64 u of the largest magnitude
+    largest = np.abs(v).max(2)
+    within("mean", mean, m64, 64 * U * largest, torch.float32)
+    # M2 is off by 64 u of itself and by what the mean's error makes of it; the square root halves it
+    within("rstd", rstd, r64, r64 * 64 * U * (1 + (largest * r64) ** 2 * 64 * U), torch.float32)
+    spread = lambda s: np.broadcast_to(s[:, :, None], (N, groups, C // groups * H * W)).reshape(x64.shape)  # noqa: E731
+    dz = np.abs(g64.reshape(per)) * 64 * U * (2 * np.abs(z - b64.reshape(per)) / np.maximum(np.abs(g64.reshape(per)), 1e-30) + spread(largest * r64)) + 4 * U * np.abs(z)
+    within("y", y, want, 1.13 * dz + 64 * U * (1 + np.abs(z)) * (act not in ("none", "relu")), t)
+
+    # gradients, from the mean and rstd that the forward pass wrote
+    dy = images(r.normal(size=(N, C, H, W)), t, spare, crop)
+    dx, dg, db = images(np.full((N, C, H, W), np.nan), t, spare, crop), nans(C, dtype=pt), nans(C, dtype=pt)
+    anr.group_norm_backward(dy, x, groups, g, b, mean, rstd, dx, dg, db, getattr(anr, "ANR_ACT_" + act.upper()))
+    dy64, m, s = host(dy), host(mean), host(rstd)
+    wx, wg, wb, dz64, hat, mean_d, mean_dh = O.group_norm_backward(dy64, x64, groups, g64, b64, m, s, act)
+    # xhat: a difference and a product, the difference exact to u of its terms; the slope's own slope is at most 1.2
+    ehat = 4 * U * (np.abs(hat) + spread((largest + np.abs(m)) * s))
+    eslope = (64 * U * (1 + np.abs(z)) + 1.2 * (np.abs(g64.reshape(per)) * ehat + 2 * U * np.abs(z))) * (act != "none")
+    edz = np.abs(dy64) * eslope + 2 * U * np.abs(dz64)
+    if act == "relu":                   # (its slope jumps at zero)
+        edz = edz * (np.abs(z) > 1e-4) + np.abs(dy64) * (np.abs(z) <= 1e-4)
+    total = lambda v: v.sum((0, 2, 3))  # noqa: E731
+    within("dbeta", db, wb, total(edz) + 128 * U * total(np.abs(dz64)), pt)
+    within("dgamma", dg, wg, total(edz * np.abs(hat) + np.abs(dz64) * ehat) + 128 * U * total(np.abs(dz64 * hat)), pt)
+    means = lambda v: spread(v.reshape(N, groups, -1).mean(2))  # noqa: E731
+    ag = np.abs(g64.reshape(per))
+    err = edz * ag + means(edz * ag) + np.abs(hat) * means(edz * ag * np.abs(hat) + np.abs(dz64) * ag * ehat) + ehat * mean_dh
+    size = np.abs(dz64) * ag + mean_d + np.abs(hat) * mean_dh
+    within("dx", dx, wx, spread(s) * (err + 128 * U * size), t)
+    return x, y, dx
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("act", ACTS)
+def test_group_norm_types_and_activations(anr, t, act):
+    norm_case(anr, 1, 2, 64, 9, 7, 8, act, TYPES[t])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("shape", [(1, 8, 1, 1, 1), (3, 32, 1, 1, 32), (1, 3, 5, 4, 1), (2, 30, 3, 11, 3), (1, 64, 40, 33, 64), (1, 40, 37, 19, 4), (2, 24, 1, 130, 3),
+                                   (1, 2560, 5, 3, 32), (1, 3000, 2, 3, 2), (1, 8190, 2, 1, 1), (2, 320, 21, 20, 32), (5, 16, 64, 3, 2), (1, 128, 70, 90, 32),
+                                   (1, 7, 33, 65, 7), (2, 1, 9, 9, 1)])
+def test_group_norm_shapes(anr, t, shape):
+    N, C, H, W, groups = shape
+    # (one value in a group: its rstd is 1/sqrt(eps), and what is left of the norm is what was rounded)
+    norm_case(anr, 2, N, C, H, W, groups, "silu", TYPES[t], eps=1e-5 if C // groups * H * W > 1 else 1.0)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("spare,crop", [(0, 3), (8, 0), (16, 2), (3, 1), (1, 0)])
+def test_group_norm_views(anr, t, spare, crop):
+    x, y, dx = norm_case(anr, 3, 2, 48, 12, 10, 6, "gelu", TYPES[t], spare=spare, crop=crop)
+    for v in (y, dx):                   # nothing around the view is written
+        whole = torch.as_strided(v, (v.untyped_storage().nbytes() // v.element_size(),), (1,), 0).clone()
+        assert not torch.isnan(whole).any()
+        inside = v.double().sum()
+        assert torch.allclose(whole.double().sum(), inside, rtol=1e-9, atol=1e-6)
+
+
+def test_group_norm_values_far_from_zero(anr):
+    """A mean of a thousand spreads costs no bits of the spread."""
+    norm_case(anr, 4, 1, 32, 40, 40, 4, "none", torch.float32, shift=0.0)
+    r = rng(5)
+    x64 = (r.normal(size=(1, 32, 60, 60)) + 4096).astype(np.float32).astype(np.float64)
+    x = images(x64, torch.float32)
+    y, rstd = torch.empty_like(x), nans(1, 4, dtype=torch.float32)
+    anr.group_norm(x, 4, y, rstd=rstd)
+    want, _, r64, _ = O.group_norm(x64, 4, np.ones(32), np.zeros(32), 1e-5, "none")
+    # the mean is rounded to 4096 * 2^-24, 2.4e-4 of a spread of 1; joined in parts that are as far off; M2 feels its square
+    within("y", y, want, 8 * 4096 * U, torch.float32)
+    within("rstd", rstd, r64, 64 * U, torch.float32)
+
+
+def test_group_norm_parameters_of_another_type(anr):
+    norm_case(anr, 6, 2, 64, 6, 6, 4, "silu", torch.bfloat16, param=torch.float32)
+    norm_case(anr, 6, 2, 63, 6, 6, 3, "silu", torch.float16, param=torch.float32)
+
+
+def test_group_norm_without_what_is_not_wanted(anr):
+    r = rng(8)
+    x = images(r.normal(size=(2, 32, 7, 5)), torch.float32)
+    one, zero = torch.ones(32, device="cuda"), torch.zeros(32, device="cuda")
+    y, z, mean, rstd = torch.empty_like(x), torch.empty_like(x), nans(2, 4, dtype=torch.float32), nans(2, 4, dtype=torch.float32)
+    anr.group_norm(x, 4, y)
+    anr.group_norm(x, 4, z, one, zero, mean=mean)
+    assert torch.equal(y, z)
+    anr.group_norm(x, 4, z, rstd=rstd)
+    dy = torch.randn_like(x)
+    every = [torch.empty_like(x), nans(32, dtype=torch.float32), nans(32, dtype=torch.float32)]
+    anr.group_norm_backward(dy, x, 4, one, zero, mean, rstd, *every)
+    for i in range(3):
+        for keep in ((i,), tuple(j for j in range(3) if j != i)):
+            part = [torch.full_like(v, float("nan")) if j in keep else None for j, v in enumerate(every)]
+            anr.group_norm_backward(dy, x, 4, None, None, mean, rstd, *part)
+            assert all(torch.equal(part[j], every[j]) for j in keep)
+    # three dimensions
+    y3 = torch.empty_like(x.flatten(2).contiguous().transpose(1, 2).contiguous().transpose(1, 2))
+    x3 = y3.clone().copy_(x.flatten(2))
+    anr.group_norm(x3, 4, y3)
+    assert torch.equal(y3, y.flatten(2))
+
+
+def test_group_norm_of_one_value_everywhere(anr):
+    x = images(np.full((2, 16, 5, 5), 3.0), torch.bfloat16)
+    y, mean, rstd = torch.empty_like(x), nans(2, 2, dtype=torch.float32), nans(2, 2, dtype=torch.float32)
+    anr.group_norm(x, 2, y, eps=1e-6, mean=mean, rstd=rstd)
+    assert (y == 0).all() and (mean == 3).all() and torch.allclose(rstd, torch.tensor(1e3, device="cuda"))
+
+
+def test_group_norm_an_image_of_infinities_leaves_the_others(anr):
+    r = rng(9)
+    a = r.normal(size=(3, 32, 6, 6))
+    x = images(a, torch.float16)
+    y, clean = torch.empty_like(x), torch.empty_like(x)
+    anr.group_norm(x, 4, clean, act=anr.ANR_ACT_SILU)
+    x[1, 3, 2, 2] = float("inf")
+    x[1, 9, 0, 0] = float("nan")
+    anr.group_norm(x, 4, y, act=anr.ANR_ACT_SILU)
+    assert torch.isnan(y[1, :16]).all() and torch.equal(y[1, 16:], clean[1, 16:]) and torch.equal(y[[0, 2]], clean[[0, 2]])
+
+
+def test_group_norm_of_nothing(anr):
+    e = torch.empty(0, 5, 5, 16, device="cuda").permute(0, 3, 1, 2)
+    dg, db = nans(16, dtype=torch.float32), nans(16, dtype=torch.float32)
+    anr.group_norm(e, 4, e.clone(), mean=torch.empty(0, 4, device="cuda"))
+    anr.group_norm_backward(e, e, 4, None, None, torch.empty(0, 4, device="cuda"), torch.empty(0, 4, device="cuda"), None, dg, db)
+    assert (dg == 0).all() and (db == 0).all()
+    e = torch.empty(2, 0, 5, 16, device="cuda").permute(0, 3, 1, 2)
+    mean, rstd = nans(2, 4, dtype=torch.float32), nans(2, 4, dtype=torch.float32)
+    anr.group_norm(e, 4, e.clone(), eps=0.25, mean=mean, rstd=rstd)
+    assert (mean == 0).all() and (rstd == 2).all()
+
+
+def test_group_norm_slope_is_that_of_the_forward_pass(anr):
+    """dx along a direction against the difference of two forward passes."""
+    r = rng(10)
+    x, v, dy = (images(r.normal(size=(2, 32, 6, 5)), torch.float32) for _ in range(3))
+    g, b = dev(r.normal(size=32) + 1, torch.float32), dev(r.normal(size=32), torch.float32)
+    y, mean, rstd, dx = torch.empty_like(x), nans(2, 4, dtype=torch.float32), nans(2, 4, dtype=torch.float32), torch.empty_like(x)
+    anr.group_norm(x, 4, y, g, b, 1e-5, anr.ANR_ACT_GELU, mean, rstd)
+    anr.group_norm_backward(dy, x, 4, g, b, mean, rstd, dx, act=anr.ANR_ACT_GELU)
+    step = 2.0 ** -7
+    up, down = (anr.group_norm((x + s * v).contiguous(memory_format=torch.channels_last), 4, torch.empty_like(x), g, b, 1e-5, anr.ANR_ACT_GELU) for s in (step, -step))
+    got = float((dx.double() * v.double()).sum())
+    want = float(((up.double() - down.double()) * dy.double()).sum() / (2 * step))
+    size = float((dx.double() * v.double()).abs().sum())
+    # roundings of 1920 outputs of about 2^-23 over the step, as a random sum; the third derivative's part, step^2
+    assert abs(got - want) <= size * (step ** 2 + 1920 ** 0.5 * 2.0 ** -22 / step)
+
+
+def test_group_norm_refuses(anr):
+    x = images(np.zeros((2, 16, 4, 4)), torch.float32)
+    g = torch.zeros(16, device="cuda")
+    for args, kwargs in [((x.contiguous(), 4, x), {}), ((x, 4, x.contiguous()), {}), ((x, 4, x[:, :8]), {}), ((x[0], 4, x[0]), {"gamma": g[:8]}), ((x, 4, x), {"gamma": g[::2]}),
+                         ((x, 4, x), {"mean": torch.zeros(2, 5, device="cuda")}), ((x[:1].expand(2, -1, -1, -1), 4, x), {})]:
+        with pytest.raises(ValueError):
+            anr.group_norm(*args, **kwargs)
+    for args, kwargs in [((x, 4, x.half()), {}), ((x, 4, x), {"gamma": g.half()}), ((x, 4, x), {"gamma": g, "beta": g.half()}), ((x, 4, x), {"mean": torch.zeros(2, 4, device="cuda").half()})]:
+        with pytest.raises(TypeError):
+            anr.group_norm(*args, **kwargs)
+    for kwargs in ({"groups": 5}, {"groups": 0}, {"act": 9}, {"eps": -1.0}):
+        with pytest.raises(anr.AnrError):
+            anr.group_norm(**{"x": x, "groups": 4, "y": x.clone(), **kwargs})
+    with pytest.raises(ValueError):
+        anr.group_norm(images(np.zeros((2, 64, 40, 40)), torch.float32), 4, images(np.zeros((2, 64, 40, 40)), torch.float32), ws=torch.empty(4, dtype=torch.uint8, device="cuda"))
+
+
+# ------------------------------------------------------------------ rotary positions
+def rotary_case(anr, seed, B, S, H, Hk, D, sections, pairing, t, inverse=False, far=100, pos_type=torch.int64, layout="plain", in_place=False, shared=False):
+    r = rng(seed)
+    n = sum(sections)
+
+    def tokens(heads):
+        a = r.normal(size=(B, S, heads, D))
+        if layout == "heads":           # [B,H,S,D] as attention keeps them
+            out = torch.empty(B, heads, S, D, dtype=t, device="cuda").transpose(1, 2)
+        elif layout == "slice":         # a part of a fused projection's rows
+            out = torch.empty(B, S, 3 * heads * D + 8, dtype=t, device="cuda")[..., 8:8 + heads * D].unflatten(-1, (heads, D)) if heads else torch.empty(B, S, 0, D, dtype=t, device="cuda")
+        elif layout == "odd":
+            out = torch.empty(B, S, heads, D + 1, dtype=t, device="cuda")[..., 1:]
+        else:
+            out = torch.empty(B, S, heads, D, dtype=t, device="cuda")
+        return out.copy_(torch.from_numpy(a).to(t))
+
+    q, k = tokens(H), tokens(Hk) if Hk else None
+    pos = r.integers(0, far + 1, size=(len(sections), 1 if shared else B, S)) if pos_type != torch.float32 else r.uniform(0, far, size=(len(sections), 1 if shared else B, S))
+    positions = torch.from_numpy(pos).to(pos_type).cuda()
+    p64 = np.broadcast_to(host(positions), (len(sections), B, S))
+    if shared:
+        positions = positions[:, 0]
+    freq = torch.from_numpy(10000.0 ** -(np.arange(n) / max(1, n))).float().cuda()
+    q64, k64 = host(q), host(k) if Hk else None
+    qo, ko = (q, k) if in_place else (torch.full_like(q, float("nan")), torch.full_like(k, float("nan")) if Hk else None)
+    anr.rotary(q, k, positions, freq, qo, ko, sections, getattr(anr, "ANR_ROTARY_" + pairing.upper()), inverse)
+    first, second = O.rotary_pairs(sections, pairing)
+    for got, x in ((qo, q64), (ko, k64)):
+        if got is None:
+            continue
+        want = O.rotary(x, p64, host(freq), sections, pairing, inverse)
+        # sine and cosine to 2 u, two products and a sum: 4 u of the magnitudes; the angle's 64 bits are off by far less
+        size = np.zeros_like(x)
+        if n:
+            size[..., first] = size[..., second] = np.abs(x[..., first]) + np.abs(x[..., second])
+        within("tokens", got, want, 4 * U * size, t)
+        assert np.array_equal(host(got)[..., 2 * n:], x[..., 2 * n:])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("pairing", ["halves", "adjacent", "section_halves"])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotary_types_and_pairings(anr, t, pairing, inverse):
+    rotary_case(anr, 20, 2, 7, 4, 2, 64, (8, 16, 8), pairing, TYPES[t], inverse)
+    rotary_case(anr, 21, 2, 7, 3, 1, 70, (5, 3, 0, 9), pairing, TYPES[t], inverse)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("case", [(1, 1, 1, 0, 2, (1,)), (1, 1, 32, 8, 128, (16, 24, 24)), (64, 1, 8, 8, 80, (40,)), (1, 513, 1, 1, 96, (16, 16)), (3, 5, 2, 2, 256, (0, 128)),
+                                  (2, 3, 5, 0, 64, (0,)), (1, 9, 2, 1, 2048, (1024,)), (2, 2, 1, 3, 33, (16,)), (1, 2, 7, 7, 72, (4, 0, 8, 8)), (1, 300, 17, 1, 8, (2, 2))])
+def test_rotary_shapes(anr, t, case):
+    for pairing in ("halves", "adjacent", "section_halves"):
+        rotary_case(anr, 22, *case, pairing, TYPES[t])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("layout", ["heads", "slice", "odd"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rotary_views(anr, t, layout, in_place):
+    for pairing in ("halves", "adjacent"):
+        rotary_case(anr, 23, 2, 6, 4, 2, 64, (16, 16), pairing, TYPES[t], layout=layout, in_place=in_place)
+
+
+@pytest.mark.parametrize("pos_type", [torch.int32, torch.int64, torch.float32])
+@pytest.mark.parametrize("far", [0, 5000, 10 ** 8])
+def test_rotary_far_positions(anr, pos_type, far):
+    rotary_case(anr, 24, 2, 5, 2, 2, 64, (16, 16), "halves", torch.float32, far=far, pos_type=pos_type)
+    rotary_case(anr, 25, 2, 5, 2, 2, 64, (16, 16), "section_halves", torch.bfloat16, far=far, pos_type=pos_type, shared=True, inverse=True)
+
+
+def test_rotary_positions_that_are_expanded_or_negative(anr):
+    q = torch.randn(3, 4, 2, 16, device="cuda")
+    freq = torch.rand(8, device="cuda")
+    pos = torch.tensor([[-3, 0, 1, 700]], device="cuda")
+    want = O.rotary(host(q), np.broadcast_to(host(pos)[:, None], (1, 3, 4)), host(freq), (8,), "halves", False)
+    for p in (pos, pos[:, None].expand(1, 3, 4), pos[:, None].repeat(1, 3, 1)):
+        out, _ = anr.rotary(q, None, p, freq, torch.empty_like(q), None)
+        within("q", out, want, 8 * U * 5, torch.float32)
+    one = torch.tensor([[[5]]], device="cuda").expand(1, 3, 4)
+    out, _ = anr.rotary(q, None, one, freq, torch.empty_like(q), None)
+    within("q", out, O.rotary(host(q), np.full((1, 3, 4), 5), host(freq), (8,), "halves", False), 8 * U * 5, torch.float32)
+
+
+def test_rotary_values_that_are_not_finite_stay_in_their_pairs(anr):
+    q = torch.randn(2, 3, 2, 24, device="cuda")
+    freq, pos = torch.rand(8, device="cuda"), torch.arange(3, device="cuda")[None]
+    clean, _ = anr.rotary(q, None, pos, freq, torch.empty_like(q), None)
+    q[1, 2, 0, 3], q[0, 0, 1, 20] = float("inf"), float("nan")
+    out, _ = anr.rotary(q, None, pos, freq, torch.empty_like(q), None)
+    touched = torch.zeros_like(q, dtype=torch.bool)
+    touched[1, 2, 0, 3] = touched[1, 2, 0, 11] = touched[0, 0, 1, 20] = True
+    assert torch.equal(out[~touched], clean[~touched]) and not torch.isfinite(out[touched]).any()
+
+
+def test_rotary_offsets_beyond_32_bits(anr):
+    B, S, H, D = 1, 70001, 256, 128                      # 2.3e9 elements, 4.6 GB
+    q = torch.zeros(B, S, H, D, dtype=torch.bfloat16, device="cuda")
+    q[:, -3:] = torch.randn(1, 3, H, D, device="cuda")
+    tail = q[:, -3:].clone()
+    freq, pos = torch.rand(64, device="cuda"), torch.arange(S, device="cuda")[None]
+    anr.rotary(q, None, pos, freq, q, None, None, anr.ANR_ROTARY_ADJACENT)
+    want = O.rotary(host(tail), host(pos)[:, None, -3:], host(freq), (64,), "adjacent", False)
+    within("q", q[:, -3:], want, 8 * U * 5, torch.bfloat16)
+    assert not q[:, :-3].any()
+    del q
+    torch.cuda.empty_cache()
+
+
+def test_rotary_refuses(anr):
+    q, freq, pos = torch.zeros(2, 3, 2, 16, device="cuda"), torch.zeros(8, device="cuda"), torch.zeros(1, 3, dtype=torch.int64, device="cuda")
+    for args in [(q[0], None, pos, freq, q[0], None), (q, None, pos, freq[:, None], q, None), (q, None, pos, freq, q, None, (4, 3)), (q, None, pos, freq, q, None, (4, 4)),
+                 (q, None, pos, freq, q, None, ()), (q, None, pos[:, :2], freq, q, None), (q, q[:1], pos, freq, q, q[:1]), (q.transpose(2, 3), None, pos, freq, q, None),
+                 (q[:, :, :, :1].expand(-1, -1, -1, 16), None, pos, freq, q, None), (q[:1, :1, :1].expand(2, 3, 2, 16), None, pos, freq, q, None),
+                 (q, q, pos, freq, q, None), (q, None, pos, freq[::2], q, None)]:
+        with pytest.raises(ValueError):
+            anr.rotary(*args)
+    for args in [(q, None, pos.short(), freq, q, None), (q, None, pos, freq.half(), q, None), (q, None, pos, freq, q.half(), None), (q.double(), None, pos, freq, q, None),
+                 (q, None, pos.cpu(), freq, q, None)]:
+        with pytest.raises(TypeError):
+            anr.rotary(*args)
+    for args in [(q, None, pos, torch.zeros(9, device="cuda"), torch.empty_like(q), None), (q, None, pos, freq, torch.empty_like(q), None, None, 3),
+                 (q, None, pos, freq, torch.zeros(1, 3, 2, 16, device="cuda").expand(2, -1, -1, -1), None),
+                 (q, None, torch.zeros(2, 3, dtype=torch.int64, device="cuda"), freq, torch.empty_like(q), None, (9, -1))]:
+        with pytest.raises(anr.AnrError):
+            anr.rotary(*args)
+
+
+# ------------------------------------------------------------------ gated feed-forward block
+def matrix(r, rows, cols, t, scale=1.0, spare=0):
+    wide = torch.zeros(rows, cols + spare, dtype=t, device="cuda")
+    out = wide[:, :cols]
+    return out.copy_(torch.from_numpy(r.normal(size=(rows, cols)) * scale).to(t))
+
+
+def empty_matrix(rows, cols, t, spare=0):
+    return torch.full((rows, cols + spare), float("nan"), dtype=t, device="cuda")[:, :cols]
+
+
+def hidden_bounds(act, gate, up, eg, eu, t):
+    """(h, bound of its error before it is rounded) from gate and up that are off by eg and eu."""
+    a, slope = O.act(act, gate)
+    ea = 1.2 * eg + 64 * U * (1 + np.abs(gate))
+    return a * up, np.abs(up) * ea + (np.abs(a) + ea) * eu + 2 * U * np.abs(a * up)
+
+
+def ff_case(anr, seed, T, C, F, act, t, save=True, spare=0, fused=False, backward=True):
+    r = rng(seed)
+    x = matrix(r, T, C, t, spare=spare)
+    if fused:                            # gate's and up's weights in one tensor
+        both = matrix(r, 2 * F, C, t, C ** -0.5, spare)
+        wg, wu = both[:F], both[F:]
+    else:
+        wg, wu = matrix(r, F, C, t, C ** -0.5, spare), matrix(r, F, C, t, C ** -0.5, spare)
+    wd = matrix(r, C, F, t, F ** -0.5, spare)
+    y = empty_matrix(T, C, t, spare)
+    gate, up = (empty_matrix(T, F, t, spare), empty_matrix(T, F, t, spare)) if save else (None, None)
+    code = getattr(anr, "ANR_ACT_" + act.upper())
+    assert anr.gated_ff(x, wg, wu, wd, y, code, gate, up) is y
+    x64, g64, u64, d64 = (host(v) for v in (x, wg, wu, wd))
+    want, wgate, wup = O.gated_ff(x64, g64, u64, d64, act)
+    eg, eu = (C + 8) * U * (np.abs(x64) @ np.abs(g64).T), (C + 8) * U * (np.abs(x64) @ np.abs(u64).T)
+    h, eh = hidden_bounds(act, wgate, wup, eg, eu, t)
+    eh = eh + HALF[t] * (np.abs(h) + eh) + TINY[t]
+    within("y", y, want, eh @ np.abs(d64).T + (F + 8) * U * ((np.abs(h) + eh) @ np.abs(d64).T), t)
+    if save:
+        within("gate", gate, wgate, eg, t)
+        within("up", up, wup, eu, t)
+    if not backward:
+        return
+    if not save:
+        gate, up = dev(wgate, t), dev(wup, t)
+    dy = matrix(r, T, C, t, spare=spare)
+    dx, dwg, dwu, dwd = empty_matrix(T, C, t, spare), empty_matrix(F, C, t, spare), empty_matrix(F, C, t, spare), empty_matrix(C, F, t, spare)
+    anr.gated_ff_backward(dy, x, wg, wu, wd, gate, up, dx, dwg, dwu, dwd, code)
+    y64, gt, ut = host(dy), host(gate), host(up)
+    wants = O.gated_ff_backward(y64, x64, g64, u64, d64, gt, ut, act)
+    a, slope = O.act(act, gt)
+    dh, edh = y64 @ d64, (C + 8) * U * (np.abs(y64) @ np.abs(d64))
+    es = 64 * U * (1 + np.abs(gt)) * (act not in ("none", "relu"))
+    held = lambda v, e: e + HALF[t] * (np.abs(v) + e) + TINY[t]  # noqa: E731
+    dg, du, hh = dh * ut * slope, dh * a, a * ut
+    edg = held(dg, np.abs(ut) * (edh * (np.abs(slope) + es) + np.abs(dh) * es) + 3 * U * np.abs(dg))
+    edu = held(du, edh * np.abs(a) + (np.abs(dh) + edh) * es + 2 * U * np.abs(du))
+    ehh = held(hh, np.abs(ut) * es + 2 * U * np.abs(hh))
+    A = np.abs
+    sums = lambda p, ep, q, n: ep @ A(q) + (n + 8) * U * ((A(p) + ep) @ A(q))  # noqa: E731
+    within("dx", dx, wants[0], sums(dg, edg, g64, 2 * F) + sums(du, edu, u64, 2 * F), t)
+    within("dw_gate", dwg, wants[1], sums(dg.T, edg.T, x64, T), t)
+    within("dw_up", dwu, wants[2], sums(du.T, edu.T, x64, T), t)
+    within("dw_down", dwd, wants[3], (ehh.T @ A(y64) + (T + 8) * U * ((A(hh) + ehh).T @ A(y64))).T, t)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T", [5, 130])
+def test_gated_ff_types_and_activations(anr, t, act, T):
+    ff_case(anr, 30, T, 64, 96, act, TYPES[t])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 32, 33, 48, 64, 65, 127, 128, 129, 257])
+def test_gated_ff_tokens(anr, t, T):
+    ff_case(anr, 31, T, 72, 200, "silu", TYPES[t])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("C,F", [(1, 1), (8, 8), (7, 9), (3, 130), (131, 5), (64, 257), (250, 64), (136, 520), (515, 77), (264, 264)])
+def test_gated_ff_widths(anr, t, C, F):
+    for T in (1, 40, 70, 300):
+        ff_case(anr, 32, T, C, F, "gelu", TYPES[t])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("spare", [0, 8, 1])
+def test_gated_ff_views(anr, t, spare):
+    for T in (3, 100):
+        ff_case(anr, 33, T, 64, 128, "gelu_tanh", TYPES[t], spare=spare, fused=True)
+        ff_case(anr, 34, T, 64, 128, "silu", TYPES[t], save=False, spare=spare, fused=True)
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_gated_ff_larger(anr, t):
+    """Sizes of every tile and of work shared over k."""
+    for T, C, F in ((40, 256, 1024), (200, 512, 1536), (700, 640, 1100), (1300, 256, 2048), (2100, 1024, 520)):
+        ff_case(anr, 35, T, C, F, "silu", TYPES[t])
+
+
+def test_gated_ff_rows_around_a_view_stay_as_they_are(anr):
+    for t in TYPES.values():
+        for T in (5, 100):
+            r = rng(36)
+            x, wg, wu, wd = (matrix(r, *s, t) for s in ((T, 40), (56, 40), (56, 40), (40, 56)))
+            whole = torch.full((T + 4, 48), 7.0, dtype=t, device="cuda")
+            anr.gated_ff(x, wg, wu, wd, whole[2:2 + T, 4:44])
+            inside = torch.zeros_like(whole, dtype=torch.bool)
+            inside[2:2 + T, 4:44] = True
+            assert (whole[~inside] == 7).all() and not (whole[inside] == 7).all()
+
+
+def test_gated_ff_without_what_is_not_wanted(anr):
+    for t in TYPES.values():
+        for T in (20, 150):
+            r = rng(37)
+            x, dy, wg, wu, wd = (matrix(r, *s, t) for s in ((T, 64), (T, 64), (96, 64), (96, 64), (64, 96)))
+            y, gate, up = empty_matrix(T, 64, t), empty_matrix(T, 96, t), empty_matrix(T, 96, t)
+            anr.gated_ff(x, wg, wu, wd, y, gate=gate, up=up)
+            assert torch.equal(anr.gated_ff(x, wg, wu, wd, torch.empty_like(y)), y)
+            every = [empty_matrix(T, 64, t), empty_matrix(96, 64, t), empty_matrix(96, 64, t), empty_matrix(64, 96, t)]
+            anr.gated_ff_backward(dy, x, wg, wu, wd, gate, up, *every)
+            for i in range(4):
+                for keep in ((i,), tuple(j for j in range(4) if j != i)):
+                    part = [torch.full_like(v, float("nan")) if j in keep else None for j, v in enumerate(every)]
+                    anr.gated_ff_backward(dy, x, wg, wu, wd, gate, up, *part)
+                    assert all(torch.equal(part[j], every[j]) for j in keep)
+
+
+def test_gated_ff_of_no_tokens(anr):
+    for t in TYPES.values():
+        r = rng(38)
+        wg, wu, wd = (matrix(r, *s, t) for s in ((24, 16), (24, 16), (16, 24)))
+        e, f = torch.empty(0, 16, dtype=t, device="cuda"), torch.empty(0, 24, dtype=t, device="cuda")
+        anr.gated_ff(e, wg, wu, wd, e.clone(), gate=f, up=f.clone())
+        dwg, dwu, dwd = empty_matrix(24, 16, t, 3), empty_matrix(24, 16, t, 3), empty_matrix(16, 24, t)
+        anr.gated_ff_backward(e, e, wg, wu, wd, f, f, e.clone(), dwg, dwu, dwd)
+        assert not dwg.any() and not dwu.any() and not dwd.any()
+
+
+def test_gated_ff_a_token_that_is_not_finite_leaves_the_others(anr):
+    for t in TYPES.values():
+        for T, C, F in ((6, 64, 96), (130, 72, 160), (130, 77, 45)):
+            r = rng(39)
+            x, wg, wu, wd = (matrix(r, *s, t) for s in ((T, C), (F, C), (F, C), (C, F)))
+            y = anr.gated_ff(x, wg, wu, wd, empty_matrix(T, C, t))
+            x[3, 1], x[5, C - 1] = float("inf"), float("nan")
+            z = anr.gated_ff(x, wg, wu, wd, empty_matrix(T, C, t))
+            rest = [i for i in range(T) if i not in (3, 5)]
+            # (float32 tiles that meet such a value are computed again in another order)
+            assert torch.equal(y[rest], z[rest]) if t is not torch.float32 else torch.allclose(y[rest], z[rest], rtol=1e-4, atol=1e-3)
+            assert not torch.isfinite(z[3]).any() and torch.isnan(z[5]).all()
+
+
+def test_gated_ff_slope_is_that_of_the_forward_pass(anr):
+    r = rng(40)
+    T, C, F = 30, 24, 40
+    args = [matrix(r, *s, torch.float32, w) for s, w in (((T, C), 1), ((F, C), 0.3), ((F, C), 0.3), ((C, F), 0.3))]
+    dy = matrix(r, T, C, torch.float32)
+    gate, up = empty_matrix(T, F, torch.float32), empty_matrix(T, F, torch.float32)
+    anr.gated_ff(*args, empty_matrix(T, C, torch.float32), anr.ANR_ACT_GELU_TANH, gate, up)
+    grads = [torch.empty_like(a) for a in args]
+    anr.gated_ff_backward(dy, *args, gate, up, *grads, anr.ANR_ACT_GELU_TANH)
+    step = 2.0 ** -7
+    for i in range(4):
+        v = torch.randn_like(args[i])
+        ends = [anr.gated_ff(*args[:i], args[i] + s * v, *args[i + 1:], empty_matrix(T, C, torch.float32), anr.ANR_ACT_GELU_TANH).double() for s in (step, -step)]
+        got, want = float((grads[i].double() * v.double()).sum()), float(((ends[0] - ends[1]) * dy.double()).sum() / (2 * step))
+        size = float((grads[i].double() * v.double()).abs().sum())
+        # roundings of 720 outputs of about 2^-22 over the step, as a random sum; the third derivative's part, step^2
+        assert abs(got - want) <= size * (step ** 2 + 720 ** 0.5 * 2.0 ** -21 / step), i
+
+
+def test_gated_ff_refuses(anr):
+    m = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
+    x, w, d = m(4, 16), m(24, 16), m(16, 24)
+    for args, kwargs in [((x, w, w, d.t(), x), {}), ((x, w, w[:8], d, x), {}), ((x, w, w, d, x[:2]), {}), ((x.t(), w, w, d, x), {}), ((x, w, w, d, x), {"gate": m(4, 24)}),
+                         ((x, w, m(24, 20)[:, :16], d, x), {}), ((x[:1].expand(4, 16), w, w, d, x), {}), ((x, w, w, d, m(16, 4).t()), {})]:
+        with pytest.raises(ValueError):
+            anr.gated_ff(*args, **kwargs)
+    for args in [(x, w, w, d, x.half()), (x.half(), w, w, d, x), (x.double(), w, w, d, x)]:
+        with pytest.raises(TypeError):
+            anr.gated_ff(*args)
+    with pytest.raises(anr.AnrError):
+        anr.gated_ff(x, w, w, d, x.clone(), 9)
+    with pytest.raises(ValueError):
+        anr.gated_ff(x, w, w, d, x.clone(), ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(anr.AnrError):
+        anr.gated_ff_backward(x, x, w, w, d, m(4, 24), m(4, 24))
+
+
+# ------------------------------------------------------------------ together
+class Block:
+    """An image's block as a program would run it: norm, queries and keys, rotary positions, scores, feed-forward, and back."""
+
+    def __init__(self, anr, t, N=2, C=64, edge=6, heads=4, F=96, seed=50):
+        r = rng(seed)
+        self.anr, self.t, self.shape = anr, t, (N, C, edge, heads, F)
+        S = edge * edge
+        self.x = images(r.normal(size=(N, C, edge, edge)), t)
+        self.gamma, self.beta = dev(r.normal(size=C) * 0.2 + 1, t), dev(r.normal(size=C) * 0.2, t)
+        self.w = [matrix(r, *s, t, 0.15) for s in ((F, C), (F, C), (C, F))]
+        self.dy = matrix(r, N * S, C, t)
+        self.positions = torch.stack([torch.arange(S) // edge, torch.arange(S) % edge]).cuda()
+        self.freq = torch.from_numpy(100.0 ** -(np.arange(C // heads // 2) / 8)).float().cuda()
+        e = lambda *s, dtype=t: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+        self.y, self.mean, self.rstd = torch.empty_like(self.x), e(N, 8, dtype=torch.float32), e(N, 8, dtype=torch.float32)
+        self.q, self.k = e(N, S, heads, C // heads), e(N, S, heads, C // heads)
+        self.scores = e(N, heads, S, S, dtype=torch.float32)
+        self.out, self.gate, self.up = e(N * S, C), e(N * S, F), e(N * S, F)
+        self.grads = [e(N * S, C), *(torch.zeros_like(w) for w in self.w)]
+        self.dx, self.dgamma, self.dbeta = torch.empty_like(self.x), e(C), e(C)
+
+    def run(self):
+        anr, (N, C, edge, heads, F) = self.anr, self.shape
+        S = edge * edge
+        anr.group_norm(self.x, 8, self.y, self.gamma, self.beta, 1e-5, anr.ANR_ACT_SILU, self.mean, self.rstd)
+        tokens = self.y.permute(0, 2, 3, 1).reshape(N * S, C)
+        q = tokens.view(N, S, heads, C // heads)
+        sections = (C // heads // 4, C // heads // 4)
+        anr.rotary(q, q, self.positions, self.freq, self.q, self.k, sections)
+        if self.t is torch.float32:
+            anr.tbs(self.q, self.k, self.scores)
+        anr.gated_ff(tokens, *self.w, self.out, anr.ANR_ACT_GELU, self.gate, self.up)
+        anr.gated_ff_backward(self.dy, tokens, *self.w, self.gate, self.up, *self.grads, anr.ANR_ACT_GELU)
+        dtokens = self.grads[0].view(N, edge, edge, C).permute(0, 3, 1, 2)
+        anr.group_norm_backward(dtokens, self.x, 8, self.gamma, self.beta, self.mean, self.rstd, self.dx, self.dgamma, self.dbeta, anr.ANR_ACT_SILU)
+
+    def results(self):
+        return [self.y, self.q, self.k, self.scores, self.out, *self.grads, self.dx, self.dgamma, self.dbeta]
+
+
+def test_a_block_in_float32_is_its_definition(anr):
+    b = Block(anr, torch.float32)
+    b.run()
+    N, C, edge, heads, F = b.shape
+    S = edge * edge
+    x, g, bt, (wg, wu, wd), dy = host(b.x), host(b.gamma), host(b.beta), [host(w) for w in b.w], host(b.dy)
+    y, mean, rstd, _ = O.group_norm(x, 8, g, bt, 1e-5, "silu")
+    tokens = y.transpose(0, 2, 3, 1).reshape(N * S, C)
+    pos = np.broadcast_to(host(b.positions)[:, None], (2, N, S))
+    q = O.rotary(tokens.reshape(N, S, heads, -1), pos, host(b.freq), (4, 4), "halves", False)
+    scores = np.matmul(q.transpose(0, 2, 1, 3), q.transpose(0, 2, 3, 1))
+    scores = np.exp(scores - scores.max(-1, keepdims=True))
+    scores /= scores.sum(-1, keepdims=True)
+    out, gate, up = O.gated_ff(tokens, wg, wu, wd, "gelu")
+    grads = O.gated_ff_backward(dy, tokens, wg, wu, wd, gate, up, "gelu")
+    dx, dg, db = O.group_norm_backward(grads[0].reshape(N, edge, edge, C).transpose(0, 3, 1, 2), x, 8, g, bt, mean, rstd, "silu")[:3]
+    for got, want in zip(b.results(), [y, q, q, scores, out, *grads, dx, dg, db]):
+        # (each step's own bounds are tested above: here a wrong layout or order would be off by as much as the values)
+        assert np.linalg.norm(host(got) - want) <= 1e-5 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_a_captured_block_replays(anr, t):
+    """Two graphs of one block, replayed in turn with eager work between."""
+    b, c = Block(anr, TYPES[t]), Block(anr, TYPES[t], seed=51)
+    for v in (b, c):
+        v.run()
+    want = [[r.clone() for r in v.results()] for v in (b, c)]
+    graphs = []
+    for v in (b, c):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            v.run()
+        graphs.append(graph)
+    for _ in range(3):
+        for v, graph, w in zip((b, c), graphs, want):
+            for r in v.results():
+                r.fill_(float("nan"))
+            v.scores.zero_()
+            graph.replay()
+            other = Block(anr, TYPES[t], seed=52)
+            other.run()
+            torch.cuda.synchronize()
+            assert all(torch.equal(r, s) for r, s in zip(v.results(), w))
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_blocks_on_streams_of_their_own(anr, t):
+    blocks = [Block(anr, TYPES[t], seed=60 + i, F=96 + 8 * i) for i in range(4)]
+    for b in blocks:
+        b.run()
+    want = [[r.clone() for r in b.results()] for b in blocks]
+    streams = [torch.cuda.Stream() for _ in blocks]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for b, s in zip(blocks, streams):
+            with torch.cuda.stream(s):
+                b.run()
+    torch.cuda.synchronize()
+    assert all(torch.equal(r, s) for b, w in zip(blocks, want) for r, s in zip(b.results(), w))
+
+
+def test_results_are_the_same_from_run_to_run_and_with_a_workspace_of_ones_own(anr):
+    for t in TYPES.values():
+        r = rng(70)
+        x, wg, wu, wd = (matrix(r, *s, t) for s in ((150, 256), (512, 256), (512, 256), (256, 512)))
+        y = anr.gated_ff(x, wg, wu, wd, empty_matrix(150, 256, t))
+        d = anr.GatedFfDesc(150, 256, 512, anr.ANR_ACT_SILU, {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}[t])
+        ws = torch.full((anr.workspace_size(anr.ANR_OP_GATED_FF, d),), 0x7f, dtype=torch.uint8, device="cuda")
+        assert torch.equal(anr.gated_ff(x, wg, wu, wd, empty_matrix(150, 256, t), ws=ws), y)
