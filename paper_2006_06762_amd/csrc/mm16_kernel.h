@@ -90,7 +90,8 @@ struct Stager {
     static constexpr int UNITS = R * BK / 8 / NT;                     // 16-byte units of a thread
     static constexpr int ROW_UNITS = KIND == K_ROWS ? BK / 8 : R / 8; // units of a row of memory
     static_assert(R * BK / 8 % NT == 0 && NT % ROW_UNITS == 0, "whole units for every thread");
-    const char* base[2];            // of the tile: element (first row, k = 0)
+    const char* base;               // of the tile: element (first row, k = 0)
+    int64_t other;                  // bytes from there to the second matrix
     int64_t ld;                     // elements
     int own, K;                     // rows (own index) from the tile's first on; k
     int first;                      // this thread's row of memory in the first unit, and its unit in the row
@@ -108,8 +109,8 @@ struct Stager {
         first = tid / ROW_UNITS;
         unit = tid % ROW_UNITS;
         const int64_t start = KIND == K_ROWS ? (int64_t)row0 * ld : row0;
-        base[0] = static_cast<const char*>(p0) + 2 * start;
-        base[1] = static_cast<const char*>(p1) + 2 * start;
+        base = static_cast<const char*>(p0) + 2 * start;
+        other = static_cast<const char*>(p1) - static_cast<const char*>(p0);
         if (KIND == K_ROWS) {
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
@@ -132,7 +133,7 @@ struct Stager {
     {
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
-            const char* const b = ((PAIRED ? matrix_of(i) : seg) ? base[1] : base[0]) + 2 * (KIND == K_ROWS ? (int64_t)k0 : k0 * ld);
+            const char* const b = base + ((PAIRED ? matrix_of(i) : seg) ? other : 0) + 2 * (KIND == K_ROWS ? (int64_t)k0 : k0 * ld);
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(b), 0, kExtent, 0x00020000);
             const int k = KIND == K_ROWS ? k0 + unit * 8 : k0 + first + i * (NT / ROW_UNITS);
             if (ALIGNED) {
@@ -176,26 +177,26 @@ __device__ __forceinline__ u32x4 operand(const char* lds, int row0, int step, in
     return u32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
-// Four neighbouring elements of a row from column n on, of which `in` exist.
+// Eight neighbouring elements of a row, of which `in` exist.
 template <typename T>
-__device__ __forceinline__ void store4(T* p, const float (&v)[4], int in, bool aligned)
+__device__ __forceinline__ void store8(T* p, const float (&v)[8], int in, bool aligned)
 {
-    if (aligned && in >= 4) {
-        store_floats<T, 4>(p, v);
+    if (aligned && in >= 8) {
+        store_floats<T, 8>(p, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
             if (i < in) p[i] = from_float<T>(v[i]);
     }
 }
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, float (&v)[4], int in, bool aligned)
+__device__ __forceinline__ void load8(const T* p, float (&v)[8], int in, bool aligned)
 {
-    if (aligned && in >= 4) {
-        load_floats<T, 4>(p, v);
+    if (aligned && in >= 8) {
+        load_floats<T, 8>(p, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < in ? to_float(p[i]) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = i < in ? to_float(p[i]) : 0.f;
     }
 }
 
@@ -296,102 +297,104 @@ __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void product_kern
         }
     }
 
-    const int half = lane >> 5;
+    // The sums leave through LDS, 32 rows of a wave at a time, so that eight lanes read and write 128 bytes of a row
+    // (GATED: four lanes 64 bytes).  From the registers it would be 8 bytes a row: dh with its three results and two operands
+    // took 1.27 ms at 8192 x 11264 x 4096, of which 0.56 behind the products.
+    constexpr int ROW = NB * 128 + 16;                                // bytes; the 16 put eight rows' same column in different banks
+    static_assert((size_t)(NT / 64) * 32 * ROW <= lds_bytes<BM, BN, XK, WK>(), "fits the chunks' room");
+    char* const own = lds + wave * 32 * ROW;
+    constexpr int LANES = (PAIRED ? NB / 2 : NB) * 4;                 // of a row
+    const int part = lane % LANES;
+    auto emit = [&](auto f) {
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<f32x4*>(own + (lane & 31) * ROW + (n * 32 + 8 * q + 4 * (lane >> 5)) * 4) =
+                        f32x4{acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < 32 * LANES / 64; ++i) {
+                const int r = i * (64 / LANES) + lane / LANES, row = m0 + (wm * MB + m) * 32 + r;
+                if (row < M) f(row, own + r * ROW);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    auto eight = [&](const char* at, float (&v)[8]) {
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(at), hi = *reinterpret_cast<const f32x4*>(at + 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = lo[i];
+            v[4 + i] = hi[i];
+        }
+    };
+    auto whole = [](const void* q, int64_t ld) { return ((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(2 * ld)) & 15) == 0; };
     if constexpr (EPI == STORE) {
         T* const d = static_cast<T*>(p.d);
-        const bool aligned = ((reinterpret_cast<uintptr_t>(d) | (uintptr_t)(2 * p.ldd)) & 7) == 0;
-#pragma unroll
-        for (int m = 0; m < MB; ++m) {
-            const int row = m0 + (wm * MB + m) * 32 + (lane & 31);
-            if (row >= M) continue;
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int col = n0 + (wn * NB + n) * 32 + 8 * q + 4 * half;
-                    const float v[4] = {acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
-                    store4(d + (int64_t)row * p.ldd + col, v, N - col, aligned);
-                }
-        }
+        const bool aligned = whole(d, p.ldd);
+        const int col = n0 + wn * NB * 32 + part * 8;
+        emit([&](int row, const char* at) {
+            float v[8];
+            eight(at + part * 32, v);
+            store8(d + (int64_t)row * p.ldd + col, v, N - col, aligned);
+        });
     } else if constexpr (EPI == PARTIAL) {
         float* const d = static_cast<float*>(p.d) + (int64_t)split * M * N;
-#pragma unroll
-        for (int m = 0; m < MB; ++m) {
-            const int row = m0 + (wm * MB + m) * 32 + (lane & 31);
-            if (row >= M) continue;
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int col = n0 + (wn * NB + n) * 32 + 8 * q + 4 * half;
-                    const float v[4] = {acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
-                    store4(d + (int64_t)row * N + col, v, N - col, N % 4 == 0);
-                }
-        }
+        const int col = n0 + wn * NB * 32 + part * 8;
+        emit([&](int row, const char* at) {
+            float v[8];
+            eight(at + part * 32, v);
+            store8(d + (int64_t)row * N + col, v, N - col, N % 8 == 0);
+        });
     } else if constexpr (EPI == GATED) {
-        static_assert(NB % 2 == 0, "blocks of gate and up side by side");
+        static_assert(NB == 2, "a block of gate and one of up");
         T* const d = static_cast<T*>(p.d);
         T *const gate = static_cast<T*>(args.gate), *const up = static_cast<T*>(args.up);
-        const bool aligned = ((reinterpret_cast<uintptr_t>(d) | (uintptr_t)(2 * p.ldd)) & 7) == 0;
-        const bool aligned_pre = ((reinterpret_cast<uintptr_t>(gate) | reinterpret_cast<uintptr_t>(up) | (uintptr_t)(2 * args.ld_pre)) & 7) == 0;
+        const bool aligned = whole(d, p.ldd), aligned_pre = whole(gate, args.ld_pre) && whole(up, args.ld_pre);
+        const int col = n0 + wn * 32 + part * 8;
         device_activation(args.act, [&](auto act) {
+            emit([&](int row, const char* at) {
+                float g[8], u[8], h[8];
+                eight(at + part * 32, g);
+                eight(at + 128 + part * 32, u);
 #pragma unroll
-            for (int m = 0; m < MB; ++m) {
-                const int row = m0 + (wm * MB + m) * 32 + (lane & 31);
-                if (row >= M) continue;
-#pragma unroll
-                for (int n = 0; n < NB; n += 2)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int col = n0 + (wn * NB + n) / 2 * 32 + 8 * q + 4 * half;
-                        float g[4], u[4], h[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            g[e] = acc[n][m][4 * q + e];
-                            u[e] = acc[n + 1][m][4 * q + e];
-                            h[e] = activation<decltype(act)::value, true>(g[e]) * u[e];
-                        }
-                        if (gate) {
-                            store4(gate + (int64_t)row * args.ld_pre + col, g, N - col, aligned_pre);
-                            store4(up + (int64_t)row * args.ld_pre + col, u, N - col, aligned_pre);
-                        }
-                        store4(d + (int64_t)row * p.ldd + col, h, N - col, aligned);
-                    }
-            }
+                for (int e = 0; e < 8; ++e) h[e] = activation<decltype(act)::value, true>(g[e]) * u[e];
+                if (gate) {
+                    store8(gate + (int64_t)row * args.ld_pre + col, g, N - col, aligned_pre);
+                    store8(up + (int64_t)row * args.ld_pre + col, u, N - col, aligned_pre);
+                }
+                store8(d + (int64_t)row * p.ldd + col, h, N - col, aligned);
+            });
         });
     } else {
         T* const d = static_cast<T*>(p.d);
         T *const du = static_cast<T*>(args.du), *const h = static_cast<T*>(args.h);
         const T *const gate = static_cast<const T*>(args.gate), *const up = static_cast<const T*>(args.up);
-        const bool aligned = N % 4 == 0;                              // (workspace: rows of 2 F and of F elements)
-        const bool aligned_pre = ((reinterpret_cast<uintptr_t>(gate) | reinterpret_cast<uintptr_t>(up) | (uintptr_t)(2 * args.ld_pre)) & 7) == 0;
+        const bool aligned = whole(d, p.ldd) && whole(du, p.ldd) && whole(h, args.ld_h), aligned_pre = whole(gate, args.ld_pre) && whole(up, args.ld_pre);
+        const int col = n0 + wn * NB * 32 + part * 8;
         device_activation(args.act, [&](auto act) {
+            emit([&](int row, const char* at) {
+                float g[8], u[8], dh[8], hh[8];
+                load8(gate + (int64_t)row * args.ld_pre + col, g, N - col, aligned_pre);
+                load8(up + (int64_t)row * args.ld_pre + col, u, N - col, aligned_pre);
+                eight(at + part * 32, dh);
 #pragma unroll
-            for (int m = 0; m < MB; ++m) {
-                const int row = m0 + (wm * MB + m) * 32 + (lane & 31);
-                if (row >= M) continue;
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int col = n0 + (wn * NB + n) * 32 + 8 * q + 4 * half;
-                        float g[4], u[4], dg[4], dup[4], hh[4];
-                        load4(gate + (int64_t)row * args.ld_pre + col, g, N - col, aligned_pre);
-                        load4(up + (int64_t)row * args.ld_pre + col, u, N - col, aligned_pre);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float dh = acc[n][m][4 * q + e];
-                            float slope;
-                            const float a = activation_and_slope<decltype(act)::value, true>(g[e], slope);
-                            dg[e] = dh * u[e] * slope;
-                            dup[e] = dh * a;
-                            hh[e] = a * u[e];
-                        }
-                        store4(d + (int64_t)row * p.ldd + col, dg, N - col, aligned);
-                        store4(du + (int64_t)row * p.ldd + col, dup, N - col, aligned);
-                        store4(h + (int64_t)row * args.ld_h + col, hh, N - col, aligned);
-                    }
-            }
+                for (int e = 0; e < 8; ++e) {
+                    float slope;
+                    const float a = activation_and_slope<decltype(act)::value, true>(g[e], slope);
+                    hh[e] = a * u[e];
+                    g[e] = dh[e] * u[e] * slope;
+                    u[e] = dh[e] * a;
+                }
+                store8(d + (int64_t)row * p.ldd + col, g, N - col, aligned);
+                store8(du + (int64_t)row * p.ldd + col, u, N - col, aligned);
+                store8(h + (int64_t)row * args.ld_h + col, hh, N - col, aligned);
+            });
         });
     }
 }
