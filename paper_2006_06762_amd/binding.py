@@ -687,16 +687,15 @@ def _gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, dx=None, dw_gate=N
     return dx, dw_gate, dw_up, dw_down
 
 
-group_norm, group_norm_backward, rotary, gated_ff, gated_ff_backward = _group_norm, _group_norm_backward, _rotary, _gated_ff, _gated_ff_backward
-
 # The operators as programs call them: the functions above without Python's part in the usual case.
-_OPERATORS = ("gemm", "conv2d", "conv_bn_relu", "conv2d_packed", "conv_bn_relu_packed", "dwconv", "tbg", "tbs", "nrm")
+_OPERATORS = ("gemm", "conv2d", "conv_bn_relu", "conv2d_packed", "conv_bn_relu_packed", "dwconv", "tbg", "tbs", "nrm", "group_norm",
+              "group_norm_backward", "rotary", "gated_ff", "gated_ff_backward")
 for _name in _OPERATORS:
     globals()["_" + _name].__name__ = globals()["_" + _name].__qualname__ = _name      # (what their errors say)
 _native.setup(tuple(globals()["_" + n] for n in _OPERATORS),
               tuple(ctypes.cast(getattr(_fast, "anr_" + n), _vp).value for n in _OPERATORS),
               ctypes.cast(_fast.anr_conv2d_fast_workspace_size, _vp).value, ctypes.cast(_fast.anr_workspace_size, _vp).value)
 from paper_2006_06762_amd._native import (gemm, conv2d, conv_bn_relu, conv2d_packed, conv_bn_relu_packed, dwconv, tbg, tbs,  # noqa: E402
-                                          nrm)
+                                          nrm, group_norm, group_norm_backward, rotary, gated_ff, gated_ff_backward)
 for _name in _OPERATORS:
     globals()[_name].__module__ = __name__          # (where a pickle of one finds it again, in a process that has not imported torch)

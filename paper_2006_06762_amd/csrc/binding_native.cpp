@@ -1,4 +1,4 @@
-// The operators of binding.py for the calls that programs make over and over: plain float32 GPU tensors, a descriptor within
+// The operators of binding.py for the calls that programs make over and over: plain GPU tensors, a descriptor within
 // its fields' ranges.  Anything else (and every error) goes to the Python function of the same
 // name, so what is accepted, refused and raised is decided there.
 //
@@ -23,19 +23,25 @@
 namespace {
 
 // ---- what binding.py hands over (setup): its functions, the library's entry points
-enum Op { GEMM, CONV2D, CONV_BN_RELU, CONV2D_PACKED, CONV_BN_RELU_PACKED, DWCONV, TBG, TBS, NRM, OPS };
+enum Op { GEMM, CONV2D, CONV_BN_RELU, CONV2D_PACKED, CONV_BN_RELU_PACKED, DWCONV, TBG, TBS, NRM, GROUP_NORM, GROUP_NORM_BACKWARD, ROTARY, GATED_FF, GATED_FF_BACKWARD, OPS };
 PyObject* g_python[OPS];
 using Call3 = anr_status (*)(const void*, const void*, const void*, void*, void*, size_t, void*);
 using CallBn = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, float, void*, void*, size_t, void*);
 using CallNrm = anr_status (*)(const void*, const void*, void*, void*, size_t, void*);
+using CallNorm = anr_status (*)(const void*, const void*, const void*, const void*, float, void*, void*, void*, void*, size_t, void*);
+using CallNormBackward = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, size_t, void*);
+using CallRotary = anr_status (*)(const void*, const void*, const void*, const void*, const void*, void*, void*, void*, size_t, void*);
+using CallFf = anr_status (*)(const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, size_t, void*);
+using CallFfBackward = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, void*,
+                                      size_t, void*);
 using CallFastSize = anr_status (*)(const void*, size_t*);
 using CallSize = anr_status (*)(int, const void*, size_t*);
 void* g_entry[OPS];
 CallFastSize g_fast_size;
 CallSize g_size;
 
-// A tensor that is memory on a GPU and nothing else: no subclass, no wrapper of a transform, float32.
-const at::Tensor* plain(PyObject* o, at::ScalarType type = at::kFloat)
+// A tensor that is memory on a GPU and nothing else: no subclass, no wrapper of a transform.
+const at::Tensor* plain_memory(PyObject* o)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
@@ -43,7 +49,12 @@ const at::Tensor* plain(PyObject* o, at::ScalarType type = at::kFloat)
     const c10::TensorImpl* impl = t.unsafeGetTensorImpl();
     constexpr c10::DispatchKeySet usual({c10::DispatchKey::CUDA, c10::DispatchKey::AutogradCUDA, c10::DispatchKey::AutocastCUDA, c10::DispatchKey::ADInplaceOrView});
     if ((impl->key_set().raw_repr() & ~usual.raw_repr()) != 0 || impl->has_symbolic_sizes_strides() || !impl->has_storage()) return nullptr;
-    return t.is_cuda() && t.scalar_type() == type ? &t : nullptr;
+    return t.is_cuda() ? &t : nullptr;
+}
+const at::Tensor* plain(PyObject* o, at::ScalarType type = at::kFloat)
+{
+    const at::Tensor* const t = plain_memory(o);
+    return t && t->scalar_type() == type ? t : nullptr;
 }
 
 void* data(const at::Tensor* t) { return t->mutable_data_ptr(); }
@@ -327,6 +338,247 @@ bool run_nrm(PyObject* const* a)
     return ws.here && accepted<CallNrm>(NRM, &d, data(x), data(out), ws.ptr, ws.bytes, s.stream);
 }
 
+// ---- operators with an element type
+
+int type_code(at::ScalarType t) { return t == at::kFloat ? ANR_F32 : t == at::kHalf ? ANR_F16 : t == at::kBFloat16 ? ANR_BF16 : -1; }
+bool absent(PyObject* o) { return !o || o == Py_None; }
+
+// Tensors of a call, all of them plain ones on the current device; `fine` tells whether each was as it has to be.
+struct Tensors {
+    const Stream s;
+    bool fine = true;
+
+    // a tensor with these sizes
+    const at::Tensor* get(PyObject* o, at::ScalarType type, c10::IntArrayRef sizes)
+    {
+        const at::Tensor* const t = fine ? plain(o, type) : nullptr;
+        fine = t && t->device().index() == s.device && t->sizes() == sizes;
+        return fine ? t : nullptr;
+    }
+    const at::Tensor* optional(PyObject* o, at::ScalarType type, c10::IntArrayRef sizes) { return absent(o) ? nullptr : get(o, type, sizes); }
+    const at::Tensor* packed(PyObject* o, at::ScalarType type, c10::IntArrayRef sizes)
+    {
+        const at::Tensor* const t = optional(o, type, sizes);
+        if (t && !t->is_contiguous()) fine = false;
+        return t;
+    }
+    // a matrix, and its leading dimension (0: one row at most)
+    const at::Tensor* matrix(PyObject* o, at::ScalarType type, int64_t rows, int64_t cols, int64_t* ld)
+    {
+        const at::Tensor* const t = optional(o, type, {rows, cols});
+        if (!t) return nullptr;
+        if ((t->stride(1) != 1 && cols != 1) || (t->stride(0) < cols && rows > 1)) fine = false;
+        const int64_t step = rows > 1 ? t->stride(0) : 0;
+        if (ld) *ld = step;
+        return t;
+    }
+    // one of two matrices that share a leading dimension
+    const at::Tensor* matrix_like(PyObject* o, at::ScalarType type, int64_t rows, int64_t cols, const at::Tensor* other, int64_t* ld)
+    {
+        int64_t mine = 0;
+        const at::Tensor* const t = matrix(o, type, rows, cols, &mine);
+        if (!t) return nullptr;
+        if (other && mine != *ld) fine = false;
+        *ld = mine;
+        return t;
+    }
+};
+void* data_or_null(const at::Tensor* t) { return t ? data(t) : nullptr; }
+
+// Strides (n, h, w) of a tensor [N,C,S] or [N,C,H,W] whose channels are neighbours.
+bool channels_last(const at::Tensor* t, int64_t* out)
+{
+    const int64_t n = t->dim();
+    if (t->stride(1) != 1 && t->size(1) != 1) return false;
+    const int64_t extent[3] = {t->size(0), n == 3 ? 1 : t->size(2), t->size(n - 1)}, stride[3] = {t->stride(0), n == 3 ? 0 : t->stride(2), t->stride(n - 1)};
+    for (int i = 0; i < 3; ++i) {
+        if (extent[i] > 1 && stride[i] == 0) return false;
+        out[i] = extent[i] > 1 ? stride[i] : 0;
+    }
+    return true;
+}
+
+// What a norm's calls have in common: x and a tensor like it, the parameters' type, the descriptor but for the strides.
+struct Norm {
+    Tensors t;
+    const at::Tensor* x = nullptr;
+    at::ScalarType type, param = at::kFloat;
+    int64_t C = 0;
+    int32_t groups = 0;
+    anr_group_norm_desc d{};
+
+    bool init(PyObject* x_, PyObject* groups_, PyObject* act, std::initializer_list<PyObject*> parameters)
+    {
+        x = plain_memory(x_);
+        if (!x || x->device().index() != t.s.device || (x->dim() != 3 && x->dim() != 4)) return false;
+        type = x->scalar_type();
+        d.dtype = type_code(type);
+        if (d.dtype < 0 || !int32(groups_, &groups) || (act && !int32(act, &d.act))) return false;
+        bool given = false;
+        for (PyObject* const o : parameters) {
+            if (absent(o)) continue;
+            const at::Tensor* const v = plain_memory(o);
+            if (!v || (given && v->scalar_type() != param)) return false;
+            param = v->scalar_type();
+            given = true;
+        }
+        if (param != at::kFloat && param != type) return false;
+        C = x->size(1);
+        d.groups = groups;
+        d.param_dtype = type_code(param);
+        const int64_t n = x->dim();
+        d.H = 1;
+        return fits(x->size(0), &d.N) && fits(C, &d.C) && (n == 3 || fits(x->size(2), &d.H)) && fits(x->size(n - 1), &d.W) && channels_last(x, d.x_stride);
+    }
+    const at::Tensor* vector(PyObject* o) { return t.packed(o, param, {C}); }
+    const at::Tensor* statistic(PyObject* o) { return t.packed(o, at::kFloat, {x->size(0), groups}); }
+};
+
+bool run_group_norm(PyObject* const* a)
+{
+    Norm n;
+    if ((a[9] && a[9] != Py_None) || (a[5] && !PyFloat_CheckExact(a[5])) || !n.init(a[0], a[1], a[6], {a[3], a[4]})) return false;
+    const at::Tensor* const y = n.t.get(a[2], n.type, n.x->sizes());
+    const at::Tensor *gamma = n.vector(a[3]), *beta = n.vector(a[4]), *mean = n.statistic(a[7]), *rstd = n.statistic(a[8]);
+    if (!n.t.fine || !channels_last(y, n.d.y_stride)) return false;
+    size_t need = 0;
+    if (g_size(ANR_OP_GROUP_NORM, &n.d, &need) != ANR_OK) return false;
+    const Workspace ws(need, n.t.s);
+    return ws.here && accepted<CallNorm>(GROUP_NORM, &n.d, data(n.x), data_or_null(gamma), data_or_null(beta), a[5] ? (float)PyFloat_AS_DOUBLE(a[5]) : 1e-5f, data(y),
+                                         data_or_null(mean), data_or_null(rstd), ws.ptr, ws.bytes, n.t.s.stream);
+}
+
+bool run_group_norm_backward(PyObject* const* a)
+{
+    Norm n;
+    if ((a[11] && a[11] != Py_None) || !n.init(a[1], a[2], a[10], {a[3], a[4], a[8], a[9]})) return false;
+    const at::Tensor *dy = n.t.get(a[0], n.type, n.x->sizes()), *dx = n.t.optional(a[7], n.type, n.x->sizes());
+    const at::Tensor *gamma = n.vector(a[3]), *beta = n.vector(a[4]), *mean = n.statistic(a[5]), *rstd = n.statistic(a[6]), *dgamma = n.vector(a[8]), *dbeta = n.vector(a[9]);
+    if (!n.t.fine || !channels_last(dy, n.d.y_stride) || !channels_last(dx ? dx : n.x, n.d.dx_stride)) return false;
+    size_t need = 0;
+    if (g_size(ANR_OP_GROUP_NORM_BACKWARD, &n.d, &need) != ANR_OK) return false;
+    const Workspace ws(need, n.t.s);
+    return ws.here && accepted<CallNormBackward>(GROUP_NORM_BACKWARD, &n.d, data(dy), data(n.x), data_or_null(gamma), data_or_null(beta), data_or_null(mean), data_or_null(rstd),
+                                                 data_or_null(dx), data_or_null(dgamma), data_or_null(dbeta), ws.ptr, ws.bytes, n.t.s.stream);
+}
+
+// Strides (b, s, h) of a tensor [B,S,H,D], zeros for a packed one.
+bool token_strides(const at::Tensor* t, int64_t* out)
+{
+    for (int i = 0; i < 3; ++i) out[i] = 0;
+    if (t->is_contiguous()) return true;
+    if (t->stride(3) != 1 && t->size(3) != 1) return false;
+    bool all = true;
+    for (int i = 0; i < 3; ++i) {
+        out[i] = t->size(i) > 1 ? t->stride(i) : 0;
+        all = all && out[i] == 0;
+    }
+    return !all || t->numel() == t->size(3);
+}
+
+bool run_rotary(PyObject* const* a)
+{
+    Tensors t;
+    const at::Tensor *q = plain_memory(a[0]), *positions = plain_memory(a[2]), *freq = plain(a[3]);
+    const bool with_k = a[1] != Py_None;
+    const at::Tensor* const k = with_k ? plain_memory(a[1]) : nullptr;
+    if (!q || !positions || !freq || (with_k && !k) || with_k != (a[5] != Py_None) || q->dim() != 4 || (k && k->dim() != 4) || freq->dim() != 1) return false;
+    anr_rotary_desc d{};
+    d.dtype = type_code(q->scalar_type());
+    d.pos_type = positions->scalar_type() == at::kLong ? ANR_POS_I64 : positions->scalar_type() == at::kInt ? ANR_POS_I32 : positions->scalar_type() == at::kFloat ? ANR_POS_F32 : -1;
+    if (d.dtype < 0 || d.pos_type < 0) return false;
+    const at::ScalarType type = q->scalar_type();
+    const int64_t B = q->size(0), S = q->size(1), H = q->size(2), D = q->size(3), Hk = k ? k->size(2) : 0;
+    t.get(a[0], type, q->sizes());
+    if (k) t.get(a[1], type, {B, S, Hk, D});
+    const at::Tensor* const q_out = t.get(a[4], type, q->sizes());
+    const at::Tensor* const k_out = k ? t.get(a[5], type, k->sizes()) : nullptr;
+    if (!t.fine || !freq->is_contiguous() || freq->device().index() != t.s.device) return false;
+    d.axes = 1;
+    int64_t pairs = 0;
+    if (absent(a[6])) {
+        if (!fits(freq->size(0), &d.section[0])) return false;
+        pairs = freq->size(0);
+    } else {
+        if (!PyTuple_CheckExact(a[6]) || PyTuple_GET_SIZE(a[6]) < 1 || PyTuple_GET_SIZE(a[6]) > 4) return false;
+        d.axes = (int32_t)PyTuple_GET_SIZE(a[6]);
+        for (int i = 0; i < d.axes; ++i) {
+            if (!int32(PyTuple_GET_ITEM(a[6], i), &d.section[i])) return false;
+            pairs += d.section[i];
+        }
+    }
+    if (pairs != freq->size(0) || (a[7] && !int32(a[7], &d.pairing)) || (a[8] && !PyBool_Check(a[8]))) return false;
+    d.inverse = a[8] == Py_True;
+    const bool each = positions->dim() == 3;                // [axes,B,S], or [axes,S] for all sequences
+    if ((!each && positions->dim() != 2) || positions->device().index() != t.s.device || positions->size(0) != d.axes || (each && positions->size(1) != B) ||
+        positions->size(positions->dim() - 1) != S)
+        return false;
+    d.pos_stride[0] = positions->stride(0);
+    d.pos_stride[1] = each ? positions->stride(1) : 0;
+    d.pos_stride[2] = positions->stride(positions->dim() - 1);
+    if (!fits(B, &d.B) || !fits(S, &d.S) || !fits(H, &d.H) || !fits(Hk, &d.Hk) || !fits(D, &d.D)) return false;
+    if (!token_strides(q, d.q_stride) || !token_strides(q_out, d.q_out_stride) || (k && (!token_strides(k, d.k_stride) || !token_strides(k_out, d.k_out_stride)))) return false;
+    return accepted<CallRotary>(ROTARY, &d, data(q), data_or_null(k), data(positions), data(freq), data(q_out), data_or_null(k_out), nullptr, 0, t.s.stream);
+}
+
+bool run_gated_ff(PyObject* const* a)
+{
+    Tensors t;
+    const at::Tensor *x = plain_memory(a[0]), *first = plain_memory(a[1]);
+    anr_gated_ff_desc d{};
+    if (!x || !first || x->dim() != 2 || first->dim() != 2 || (a[8] && a[8] != Py_None) || absent(a[6]) != absent(a[7])) return false;
+    const at::ScalarType type = x->scalar_type();
+    d.dtype = type_code(type);
+    d.act = ANR_ACT_SILU;
+    if (d.dtype < 0 || (a[5] && !int32(a[5], &d.act))) return false;
+    d.T = x->size(0);
+    d.C = x->size(1);
+    d.F = first->size(0);
+    t.matrix(a[0], type, d.T, d.C, &d.ldx);
+    const at::Tensor* const wg = t.matrix(a[1], type, d.F, d.C, &d.ldw);
+    const at::Tensor* const wu = t.matrix_like(a[2], type, d.F, d.C, wg, &d.ldw);
+    const at::Tensor *wd = t.matrix(a[3], type, d.C, d.F, &d.ld_down), *y = t.matrix(a[4], type, d.T, d.C, &d.ldy);
+    const at::Tensor* const gate = t.matrix(a[6], type, d.T, d.F, &d.ldpre);
+    const at::Tensor* const up = t.matrix_like(a[7], type, d.T, d.F, gate, &d.ldpre);
+    if (!t.fine || !wu || !wd || !y) return false;
+    size_t need = 0;
+    if (g_size(ANR_OP_GATED_FF, &d, &need) != ANR_OK) return false;
+    const Workspace ws(need, t.s);
+    return ws.here &&
+           accepted<CallFf>(GATED_FF, &d, data(x), data(wg), data(wu), data(wd), data(y), data_or_null(gate), data_or_null(up), ws.ptr, ws.bytes, t.s.stream);
+}
+
+bool run_gated_ff_backward(PyObject* const* a)
+{
+    Tensors t;
+    const at::Tensor *x = plain_memory(a[1]), *first = plain_memory(a[2]);
+    anr_gated_ff_desc d{};
+    if (!x || !first || x->dim() != 2 || first->dim() != 2 || (a[12] && a[12] != Py_None)) return false;
+    const at::ScalarType type = x->scalar_type();
+    d.dtype = type_code(type);
+    d.act = ANR_ACT_SILU;
+    if (d.dtype < 0 || (a[11] && !int32(a[11], &d.act))) return false;
+    d.T = x->size(0);
+    d.C = x->size(1);
+    d.F = first->size(0);
+    const at::Tensor* const dy = t.matrix(a[0], type, d.T, d.C, &d.ldy);
+    t.matrix(a[1], type, d.T, d.C, &d.ldx);
+    const at::Tensor* const wg = t.matrix(a[2], type, d.F, d.C, &d.ldw);
+    const at::Tensor* const wu = t.matrix_like(a[3], type, d.F, d.C, wg, &d.ldw);
+    const at::Tensor *wd = t.matrix(a[4], type, d.C, d.F, &d.ld_down), *gate = t.matrix(a[5], type, d.T, d.F, &d.ldpre);
+    const at::Tensor* const up = t.matrix_like(a[6], type, d.T, d.F, gate, &d.ldpre);
+    const at::Tensor* const dx = t.matrix(a[7], type, d.T, d.C, &d.lddx);
+    const at::Tensor* const dwg = t.matrix(a[8], type, d.F, d.C, &d.lddw);
+    const at::Tensor* const dwu = t.matrix_like(a[9], type, d.F, d.C, dwg, &d.lddw);
+    const at::Tensor* const dwd = t.matrix(a[10], type, d.C, d.F, &d.ld_ddown);
+    if (!t.fine || !dy || !wu || !wd || !gate || !up) return false;
+    size_t need = 0;
+    if (g_size(ANR_OP_GATED_FF_BACKWARD, &d, &need) != ANR_OK) return false;
+    const Workspace ws(need, t.s);
+    return ws.here && accepted<CallFfBackward>(GATED_FF_BACKWARD, &d, data(dy), data(x), data(wg), data(wu), data(wd), data(gate), data(up), data_or_null(dx), data_or_null(dwg),
+                                               data_or_null(dwu), data_or_null(dwd), ws.ptr, ws.bytes, t.s.stream);
+}
+
 // Parameters of each operator, the required ones first, and which of them it returns.
 const char* const kGemm[] = {"A", "B", "C"};
 const char* const kConv[] = {"x", "w", "y", "stride", "pad", "ws", "dil", "groups", "route"};
@@ -335,9 +587,23 @@ const char* const kPacked[] = {"desc", "x", "pack", "y", "ws"};
 const char* const kDw[] = {"x", "w", "y", "stride", "pad", "dil"};
 const char* const kScores[] = {"q", "k", "out"};
 const char* const kNrm[] = {"x", "out", "ws"};
+const char* const kNorm[] = {"x", "groups", "y", "gamma", "beta", "eps", "act", "mean", "rstd", "ws"};
+const char* const kNormBackward[] = {"dy", "x", "groups", "gamma", "beta", "mean", "rstd", "dx", "dgamma", "dbeta", "act", "ws"};
+const char* const kRotary[] = {"q", "k", "positions", "inv_freq", "q_out", "k_out", "sections", "pairing", "inverse"};
+const char* const kFf[] = {"x", "w_gate", "w_up", "w_down", "y", "act", "gate", "up", "ws"};
+const char* const kFfBackward[] = {"dy", "x", "w_gate", "w_up", "w_down", "gate", "up", "dx", "dw_gate", "dw_up", "dw_down", "act", "ws"};
+
+// The parameters `result` to `last`: one of them itself, more as a tuple.
+PyObject* returned(PyObject* const* a, int result, int last)
+{
+    if (result == last) return Py_NewRef(a[result]);
+    PyObject* const tuple = PyTuple_New(last - result + 1);
+    for (int i = result; tuple && i <= last; ++i) PyTuple_SET_ITEM(tuple, i - result, Py_NewRef(a[i] ? a[i] : Py_None));
+    return tuple;
+}
 
 template <int OP, int N, typename Run>
-PyObject* call(const char* const (&names)[N], int required, int result, Run run, PyObject* const* args, Py_ssize_t n, PyObject* kwnames)
+PyObject* call(const char* const (&names)[N], int required, int result, int last, Run run, PyObject* const* args, Py_ssize_t n, PyObject* kwnames)
 {
     PyObject* a[N];
     if (!g_python[OP]) {
@@ -345,10 +611,7 @@ PyObject* call(const char* const (&names)[N], int required, int result, Run run,
         return nullptr;
     }
     try {
-        if (!at::impl::torch_function_mode_enabled() && arguments(names, required, args, n, kwnames, a) && run(a)) {
-            Py_INCREF(a[result]);
-            return a[result];
-        }
+        if (!at::impl::torch_function_mode_enabled() && arguments(names, required, args, n, kwnames, a) && run(a)) return returned(a, result, last);
     } catch (...) {
         // (memory that cannot be had: Python raises it)
     }
@@ -356,10 +619,11 @@ PyObject* call(const char* const (&names)[N], int required, int result, Run run,
     return PyObject_Vectorcall(g_python[OP], args, (size_t)n, kwnames);
 }
 
-#define ANR_OPERATOR(fn, op, names, required, result, ...)                                        \
+#define ANR_OPERATOR(fn, op, names, required, result, ...) ANR_OPERATOR_OF(fn, op, names, required, result, result, __VA_ARGS__)
+#define ANR_OPERATOR_OF(fn, op, names, required, result, last, ...)                                        \
     PyObject* fn(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kwnames)               \
     {                                                                                             \
-        return call<op>(names, required, result, [](PyObject* const* a) { return __VA_ARGS__; }, args, n, kwnames); \
+        return call<op>(names, required, result, last, [](PyObject* const* a) { return __VA_ARGS__; }, args, n, kwnames); \
     }
 ANR_OPERATOR(py_gemm, GEMM, kGemm, 3, 2, run_gemm(a))
 ANR_OPERATOR(py_conv2d, CONV2D, kConv, 3, 2, run_conv2d(a))
@@ -370,7 +634,13 @@ ANR_OPERATOR(py_dwconv, DWCONV, kDw, 3, 2, run_dwconv(a))
 ANR_OPERATOR(py_tbg, TBG, kScores, 3, 2, run_scores(TBG, a))
 ANR_OPERATOR(py_tbs, TBS, kScores, 3, 2, run_scores(TBS, a))
 ANR_OPERATOR(py_nrm, NRM, kNrm, 2, 1, run_nrm(a))
+ANR_OPERATOR(py_group_norm, GROUP_NORM, kNorm, 3, 2, run_group_norm(a))
+ANR_OPERATOR_OF(py_group_norm_backward, GROUP_NORM_BACKWARD, kNormBackward, 7, 7, 9, run_group_norm_backward(a))
+ANR_OPERATOR_OF(py_rotary, ROTARY, kRotary, 6, 4, 5, run_rotary(a))
+ANR_OPERATOR(py_gated_ff, GATED_FF, kFf, 5, 4, run_gated_ff(a))
+ANR_OPERATOR_OF(py_gated_ff_backward, GATED_FF_BACKWARD, kFfBackward, 7, 7, 10, run_gated_ff_backward(a))
 #undef ANR_OPERATOR
+#undef ANR_OPERATOR_OF
 
 // setup(functions, entries, fast_size, size): tuples in the order of the operators, entry points as integers.
 PyObject* py_setup(PyObject*, PyObject* args)
@@ -421,6 +691,24 @@ PyMethodDef g_methods[] = {
     {"tbs", as_cfunction(py_tbs), METH_FASTCALL | METH_KEYWORDS, "tbs(q, k, out)\n--\n\ntbg followed by a softmax over the last axis."},
     {"nrm", as_cfunction(py_nrm), METH_FASTCALL | METH_KEYWORDS,
      "nrm(x, out, ws=None)\n--\n\nout[b] = sqrt(sum of squares of x[b]).  x [N,M] or [b,N,M] with unit column stride, out [1] / [b]."},
+    {"group_norm", as_cfunction(py_group_norm), METH_FASTCALL | METH_KEYWORDS,
+     "group_norm(x, groups, y, gamma=None, beta=None, eps=1e-05, act=0, mean=None, rstd=None, ws=None)\n--\n\n"
+     "y = act((x - mean) * rstd * gamma + beta) over `groups` runs of channels; x, y [N,C,S] or [N,C,H,W] channels last.\n"
+     "mean, rstd: float32 [N,groups], written where given, for a backward pass."},
+    {"group_norm_backward", as_cfunction(py_group_norm_backward), METH_FASTCALL | METH_KEYWORDS,
+     "group_norm_backward(dy, x, groups, gamma, beta, mean, rstd, dx=None, dgamma=None, dbeta=None, act=0, ws=None)\n--\n\n"
+     "Gradients of group_norm, into those of dx, dgamma and dbeta that are given, from its arguments and the mean and rstd that it wrote."},
+    {"rotary", as_cfunction(py_rotary), METH_FASTCALL | METH_KEYWORDS,
+     "rotary(q, k, positions, inv_freq, q_out, k_out, sections=None, pairing=0, inverse=False)\n--\n\n"
+     "q_out and k_out: q [B,S,H,D] and k [B,S,Hk,D] turned by positions[axis] * inv_freq; each may be its input itself, k and k_out None.\n"
+     "positions [axes,B,S] or [axes,S]; inv_freq one float for each pair of dimensions; sections: pairs of each axis (one axis: all)."},
+    {"gated_ff", as_cfunction(py_gated_ff), METH_FASTCALL | METH_KEYWORDS,
+     "gated_ff(x, w_gate, w_up, w_down, y, act=2, gate=None, up=None, ws=None)\n--\n\n"
+     "y = (act(x.w_gate^T) * (x.w_up^T)).w_down^T; x, y [T,C], w_gate and w_up [F,C], w_down [C,F].  gate and up [T,F]: the two\n"
+     "products, where a backward pass is to follow."},
+    {"gated_ff_backward", as_cfunction(py_gated_ff_backward), METH_FASTCALL | METH_KEYWORDS,
+     "gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, dx=None, dw_gate=None, dw_up=None, dw_down=None, act=2, ws=None)\n--\n\n"
+     "Gradients of gated_ff, into those of dx, dw_gate, dw_up and dw_down that are given, from its arguments and the gate and up that it wrote."},
     {"setup", py_setup, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -16,9 +16,15 @@ struct Plan {
     Args args;
     bool vector;                    // 16-byte loads
     int chunks;
+    int table;                      // floats of a table of the kernels that read twice
     size_t bytes;                   // of workspace
     size_t lds;                     // of the kernels that sum
+    int resident;                   // threads of the resident kernel, or 0
+    int held;                       // its vectors a thread: 4, 8 or 16
+    size_t resident_lds;
 };
+
+constexpr int kResidentThreads = 1024;
 
 int common_multiple(int a, int b)
 {
@@ -33,6 +39,20 @@ int common_multiple(int a, int b)
 
 // Strides that keep 16-byte units whole.
 bool whole_units(const void* p, const int64_t* s, int V) { return is_aligned16(p) && s[0] % V == 0 && s[1] % V == 0 && s[2] % V == 0; }
+
+// Where the resident kernels run: a chunk of an image fits the registers of a work-group (vectors of four channels a thread).
+// Timed with groups of 8 and 10 channels of 256 and 320, batch 1 to 32, SiLU, against the kernels that read twice (us, resident / not):
+// forward, 16 bits, 14^2 7.9 / 14, 28^2 (12 to 16 vectors) 14 / 15; float32 20^2 10 / 15, 28^2 (7) 14.5 / 15.5, but 40^2 (13) 19 / 13
+// with 8 work-groups, 23 / 21 with 128, 28 / 32 with 256. Backward, float32 28^2 19 / 19 to 28 / 30; 16 bits 20^2 (7) 15 / 22, 28^2 (13)
+// 22 / 19. So: eight vectors, and sixteen in the forward pass of 16-bit types or with work-groups for most CUs.
+bool resident_pays(const GroupNormArgs& g, const Args& a, bool backward, int64_t work_groups)
+{
+    const int columns = a.chunk / kHeldChannels;
+    if (columns > 256) return false;
+    const int rows = kResidentThreads / columns;
+    const int most = !backward && (g.dtype != ANR_F32 || work_groups >= 192) ? 16 : 8;
+    return (a.HW + rows - 1) / rows <= most;
+}
 
 Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
 {
@@ -62,6 +82,7 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
     a.flat = flat(g.xs) && (!backward || flat(g.dys)) && flat(g.ys);
     a.W = g.W;
     a.by_w = make_fastdiv(g.W);
+    a.by_cg = make_fastdiv(a.cg);
 
     const int es = element_bytes(g.dtype), V = vector ? 16 / es : 1;
     p.vector = vector;
@@ -70,14 +91,30 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
     a.chunk = std::min(g.C, least * std::max(1, (128 / es + least - 1) / least));
     p.chunks = (g.C + a.chunk - 1) / a.chunk;
     const int columns = a.chunk / V, rows = kThreads / std::min(columns, kThreads);
-    // Slabs: about four work-groups per CU, four pixels for each thread or more, and at most 128 that are joined.
+    p.table = table_floats(std::min(a.chunk, kThreads * V));
+    // Slabs: about four work-groups per CU as far as each thread has eight pixels, one per CU as far as it has two, and at most 128
+    // that are joined.
     const int64_t others = (int64_t)p.chunks * g.N;
-    int64_t slabs = (1024 + others - 1) / others;
-    slabs = std::max<int64_t>(1, std::min({slabs, (int64_t)a.HW / (4 * rows), (int64_t)128}));
+    int64_t slabs = std::min((1024 + others - 1) / others, (int64_t)a.HW / (8 * rows));
+    slabs = std::max(slabs, std::min((256 + others - 1) / others, (int64_t)a.HW / (2 * rows)));
+    slabs = std::max<int64_t>(1, std::min<int64_t>(slabs, 128));
     a.slab_pixels = (int)((a.HW + slabs - 1) / slabs);
     a.slabs = (a.HW + a.slab_pixels - 1) / a.slab_pixels;
-    p.lds = sizeof(float) * 2 * (size_t)std::max(rows, 1) * a.chunk;
-    const size_t partial = sizeof(float) * 2 * (size_t)g.N * a.slabs * (backward ? (size_t)g.C : (size_t)g.groups);
+    p.lds = sizeof(float) * (2 * (size_t)rows * a.chunk + (backward ? 4 : 1) * (size_t)p.table);
+    if (vector && resident_pays(g, a, backward, others)) {
+        const int held_columns = a.chunk / kHeldChannels;
+        const int64_t vectors = (int64_t)a.HW * held_columns;
+        p.resident = (int)std::min<int64_t>(kResidentThreads, (vectors + 63) / 64 * 64);
+        p.resident = std::max(p.resident, (held_columns + 63) / 64 * 64);
+        const int resident_rows = p.resident / held_columns, each = (a.HW + resident_rows - 1) / resident_rows;
+        p.held = each <= 4 ? 4 : each <= 8 ? 8 : 16;
+        const size_t groups = a.chunk / a.cg;
+        p.resident_lds = sizeof(float) * (backward ? 6 * (size_t)table_floats(a.chunk) + table_floats(2 * groups) + 2 * (size_t)resident_rows * a.chunk
+                                                   : 3 * (size_t)table_floats(a.chunk) + table_floats(groups) + (size_t)resident_rows * a.chunk);
+        a.slabs = 1;
+        a.slab_pixels = a.HW;
+    }
+    const size_t partial = p.resident ? 0 : sizeof(float) * 2 * (size_t)g.N * a.slabs * (backward ? (size_t)g.C : (size_t)g.groups);
     const size_t sums = backward ? sizeof(float) * 2 * (size_t)g.N * g.C : 0;
     p.bytes = partial + sums + (backward ? sizeof(float) * 2 * (size_t)g.N * g.groups : 0);
     a.ws = static_cast<float*>(g.ws);
@@ -144,12 +181,31 @@ hipError_t launch_group_norm(const GroupNormArgs& g, hipStream_t stream)
         using T = decltype(t);
         return with_width<T>(p, [&](auto v) {
             constexpr int V = decltype(v)::value;
+            if constexpr (V > 1) {
+                if (p.resident)
+                    return with_activation(g.act, [&](auto act) {
+                        constexpr int ACT = decltype(act)::value;
+                        auto launch = [&](auto kernel, LdsLimit& limit) {
+                            const hipError_t e = p.resident_lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), p.resident_lds, limit) : hipSuccess;
+                            return e != hipSuccess ? e : launch_kernel(kernel, grid, dim3(p.resident), p.resident_lds, stream, p.args);
+                        };
+                        static LdsLimit limits[3];
+                        if (p.held == 4) return launch(resident_kernel<T, ACT, 4>, limits[0]);
+                        return p.held == 8 ? launch(resident_kernel<T, ACT, 8>, limits[1]) : launch(resident_kernel<T, ACT, 16>, limits[2]);
+                    });
+            }
             static LdsLimit limit;
             hipError_t e = p.lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(stats_kernel<T, V>), p.lds, limit) : hipSuccess;
             if (e == hipSuccess) e = launch_kernel(stats_kernel<T, V>, grid, dim3(kThreads), p.lds, stream, p.args);
             if (e != hipSuccess) return e;
+            const size_t apply_lds = sizeof(float) * (3 * (size_t)p.table + 2 * (size_t)(p.args.chunk / p.args.cg));
             return with_activation(g.act, [&](auto act) {
-                return launch_kernel(apply_kernel<T, V, decltype(act)::value>, grid, dim3(kThreads), sizeof(float) * 2 * (p.args.chunk / p.args.cg), stream, p.args);
+                static LdsLimit limit_apply;
+                if (apply_lds > 65536) {
+                    const hipError_t f = raise_lds_limit(reinterpret_cast<const void*>(apply_kernel<T, V, decltype(act)::value>), apply_lds, limit_apply);
+                    if (f != hipSuccess) return f;
+                }
+                return launch_kernel(apply_kernel<T, V, decltype(act)::value>, grid, dim3(kThreads), apply_lds, stream, p.args);
             });
         });
     });
@@ -166,15 +222,28 @@ hipError_t launch_group_norm_backward(const GroupNormArgs& g, hipStream_t stream
             constexpr int V = decltype(v)::value;
             return with_activation(g.act, [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
-                static LdsLimit limit, limit_groups;
-                const size_t lds = sizeof(float) * 2 * p.args.chunk;
+                static LdsLimit limit, limit_groups, limit_apply;
+                const size_t lds = sizeof(float) * 2 * p.args.chunk, apply_lds = sizeof(float) * 6 * (size_t)p.table;
+                if constexpr (V > 1) {
+                    if (p.resident) {
+                        auto launch = [&](auto kernel, LdsLimit& held) {
+                            const hipError_t f = p.resident_lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), p.resident_lds, held) : hipSuccess;
+                            return f != hipSuccess ? f : launch_kernel(kernel, grid, dim3(p.resident), p.resident_lds, stream, p.args);
+                        };
+                        static LdsLimit limits[2];
+                        const hipError_t f = p.held == 4 ? launch(backward_resident_kernel<T, ACT, 4>, limits[0]) : launch(backward_resident_kernel<T, ACT, 8>, limits[1]);
+                        if (f != hipSuccess || (!g.dgamma && !g.dbeta)) return f;
+                        return launch_kernel(backward_parameters_kernel, dim3(1, p.chunks, 1), dim3(kThreads), 0, stream, p.args);
+                    }
+                }
                 hipError_t e = p.lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(backward_sums_kernel<T, V, ACT>), p.lds, limit) : hipSuccess;
                 if (e == hipSuccess && lds > 65536) e = raise_lds_limit(reinterpret_cast<const void*>(backward_groups_kernel), lds, limit_groups);
                 if (e == hipSuccess) e = launch_kernel(backward_sums_kernel<T, V, ACT>, grid, dim3(kThreads), p.lds, stream, p.args);
                 if (e == hipSuccess) e = launch_kernel(backward_groups_kernel, dim3(1, p.chunks, g.N), dim3(kThreads), lds, stream, p.args);
                 if (e != hipSuccess) return e;
                 if (!g.y) return launch_kernel(backward_parameters_kernel, dim3(1, p.chunks, 1), dim3(kThreads), 0, stream, p.args);
-                return launch_kernel(backward_apply_kernel<T, V, ACT>, grid, dim3(kThreads), 0, stream, p.args);
+                if (apply_lds > 65536) e = raise_lds_limit(reinterpret_cast<const void*>(backward_apply_kernel<T, V, ACT>), apply_lds, limit_apply);
+                return e != hipSuccess ? e : launch_kernel(backward_apply_kernel<T, V, ACT>, grid, dim3(kThreads), apply_lds, stream, p.args);
             });
         });
     });

@@ -10,6 +10,8 @@
 // (M2 by joins feels the rounding of the means that it joins: without this, values at 4096 spreads gave an rstd 4e-6 off).  Many of them are joined in two passes, mean = sum n_i mean_i / n and
 // M2 = sum M2_i + n_i (mean_i - mean)^2: threads of a work-group through LDS, slabs through the workspace, where the
 // work-groups of the second kernel join them again each for itself (fewer launches than a kernel that does).
+//
+// Where a work-group can hold a chunk of an image in its registers (resident kernels), it is read once, in one launch.
 #pragma once
 #include "anr_kernels.h"
 #include "element_types.h"
@@ -40,7 +42,7 @@ struct Args {
     float* sums;                    // backward: sums of a channel over an image's slabs, [N][2][C]
     float* group_sums;              // backward: [N][groups][2]
     Pixels px, pdy, py;
-    FastDiv by_w;
+    FastDiv by_w, by_cg;
     float eps;
     int N, HW, W, C, groups, cg, flat, param_dtype;
     int chunk;                      // channels of a chunk: whole groups
@@ -51,7 +53,7 @@ struct Args {
 struct Place {
     int slab, n, c0, channels, p0, p1;
     int columns, tx, ty, rows;      // of V channels; rows of threads
-    __device__ __forceinline__ Place(const Args& a, int V)
+    __device__ __forceinline__ Place(const Args& a, int V, int threads = kThreads)
     {
         slab = blockIdx.x;
         n = blockIdx.z;
@@ -60,8 +62,8 @@ struct Place {
         p0 = slab * a.slab_pixels;
         p1 = min(a.HW, p0 + a.slab_pixels);
         columns = channels / V;
-        const int wide = min(columns, kThreads);
-        rows = kThreads / wide;
+        const int wide = min(columns, threads);
+        rows = threads / wide;
         ty = threadIdx.x / wide;
         tx = ty < rows ? threadIdx.x - ty * wide : columns;          // (threads that are left over have no column)
     }
@@ -74,22 +76,56 @@ __device__ __forceinline__ float wave_sum(float v)
     return v;
 }
 
+// Parameter i of gamma or beta.
+__device__ __forceinline__ float parameter(const void* p, int i, int dtype, float absent) { return p ? load_any(p, i, dtype) : absent; }
+
+// The first value of each channel's group, for n of the chunk's channels from `first` on.
+template <typename T>
+__device__ __forceinline__ void origins(const Args& a, const T* x, int first, int n, float* out, int threads)
+{
+    for (int c = threadIdx.x; c < n; c += threads) out[c] = to_float(x[a.by_cg.div(first + c) * a.cg]);
+}
+
+// V values of a table of channels.
+template <int V>
+__device__ __forceinline__ void from_table(const float* table, int c, float (&out)[V])
+{
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(table + c + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) out[i + j] = v[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[i] = table[c + i];
+    }
+}
+
+// Floats of a table in LDS: whole 16-byte units.
+__device__ __host__ __forceinline__ constexpr int table_floats(int channels) { return (channels + 3) & ~3; }
+
 // First kernel of the forward pass: mean and M2 of each group of the chunk over the slab.
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void stats_kernel(const Args a)
 {
-    extern __shared__ __attribute__((aligned(16))) float lds[];      // [rows][channels] of (mean, M2)
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the table, then [rows][channels] of (mean, M2)
     const Place s(a, V);
+    float* const lds = shared + table_floats(min(s.channels, kThreads * V));
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     const int first = s.p0 + s.ty;
     const int mine = s.tx < s.columns && first < s.p1 ? (s.p1 - first + s.rows - 1) / s.rows : 0;
-    for (int col = s.tx; col < s.columns; col += kThreads) {
+    for (int base = 0; base < s.columns; base += kThreads) {         // (one round but for groups of thousands of channels)
+        const int here = min(s.channels - base * V, kThreads * V), col = base + s.tx;
+        __syncthreads();
+        origins(a, x, base * V, here, shared, kThreads);
+        __syncthreads();
+        if (col >= s.columns) continue;
         float mean[V], m2[V], origin[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            mean[i] = m2[i] = 0.f;
-            origin[i] = to_float(x[(col * V + i) / a.cg * a.cg]);
-        }
+        for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.f;
+        from_table<V>(shared, s.tx * V, origin);
         const T* const xc = x + col * V;
         int k = 0;
         for (; k + 4 <= mine; k += 4) {
@@ -137,14 +173,14 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(const Args a)
     for (int g = wave; g < groups; g += kThreads / 64) {
         float sum = 0.f;
         for (int e = lane; e < s.rows * a.cg; e += 64) {
-            const int row = e / a.cg, c = g * a.cg + e - row * a.cg;
+            const int row = a.by_cg.div(e), c = g * a.cg + e - row * a.cg;
             const int count = pixels > row ? (pixels - row + s.rows - 1) / s.rows : 0;
             sum = fmaf((float)count, lds[2 * (row * s.channels + c)], sum);
         }
         const float mean = wave_sum(sum) / ((float)pixels * (float)a.cg);
         float q = 0.f;
         for (int e = lane; e < s.rows * a.cg; e += 64) {
-            const int row = e / a.cg, c = g * a.cg + e - row * a.cg;
+            const int row = a.by_cg.div(e), c = g * a.cg + e - row * a.cg;
             const int count = pixels > row ? (pixels - row + s.rows - 1) / s.rows : 0;
             const float d = lds[2 * (row * s.channels + c)] - mean;
             q += fmaf((float)count * d, d, lds[2 * (row * s.channels + c) + 1]);
@@ -158,16 +194,15 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(const Args a)
     }
 }
 
-// Parameter i of gamma or beta.
-__device__ __forceinline__ float parameter(const void* p, int i, int dtype, float absent) { return p ? load_any(p, i, dtype) : absent; }
-
 // Second kernel of the forward pass.
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
-    extern __shared__ __attribute__((aligned(16))) float lds[];      // [groups of the chunk] of (mean, rstd)
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // tables of mean, scale and shift, then [groups] of (mean, rstd)
     const Place s(a, V);
+    const int table = table_floats(min(s.channels, kThreads * V));
+    float* const lds = shared + 3 * table;
     const int groups = s.channels / a.cg, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g0 = s.c0 / a.cg;
     for (int g = wave; g < groups; g += kThreads / 64) {
         const float* const at = a.ws + 2 * ((int64_t)s.n * a.slabs * a.groups + g0 + g);
@@ -188,18 +223,23 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
             if (s.slab == 0 && a.rstd) a.rstd[(int64_t)s.n * a.groups + g0 + g] = rstd;
         }
     }
-    __syncthreads();
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     T* const y = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
-    for (int col = s.tx; col < s.columns; col += kThreads) {
-        float mean[V], scale[V], shift[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = col * V + i, g = c / a.cg;
-            mean[i] = lds[2 * g];
-            scale[i] = lds[2 * g + 1] * parameter(a.gamma, s.c0 + c, a.param_dtype, 1.f);
-            shift[i] = parameter(a.beta, s.c0 + c, a.param_dtype, 0.f);
+    for (int base = 0; base < s.columns; base += kThreads) {
+        const int first = base * V, here = min(s.channels - first, kThreads * V), col = base + s.tx;
+        __syncthreads();
+        for (int c = threadIdx.x; c < here; c += kThreads) {
+            const int g = a.by_cg.div(first + c);
+            shared[c] = lds[2 * g];
+            shared[table + c] = lds[2 * g + 1] * parameter(a.gamma, s.c0 + first + c, a.param_dtype, 1.f);
+            shared[2 * table + c] = parameter(a.beta, s.c0 + first + c, a.param_dtype, 0.f);
         }
+        __syncthreads();
+        if (col >= s.columns) continue;
+        float mean[V], scale[V], shift[V];
+        from_table<V>(shared, s.tx * V, mean);
+        from_table<V>(shared + table, s.tx * V, scale);
+        from_table<V>(shared + 2 * table, s.tx * V, shift);
 #pragma unroll 4
         for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
             float v[V];
@@ -211,20 +251,26 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
     }
 }
 
-// What a thread keeps of its channels in the backward pass.
+// What the backward pass needs of each channel: tables of mean, rstd, gamma and beta, for n of the chunk's channels from `first` on.
+__device__ __forceinline__ void channel_tables(const Args& a, const Place& s, int first, int n, float* out, int table, int threads)
+{
+    for (int c = threadIdx.x; c < n; c += threads) {
+        const int64_t g = (int64_t)s.n * a.groups + s.c0 / a.cg + a.by_cg.div(first + c);
+        out[c] = a.mean[g];
+        out[table + c] = a.rstd[g];
+        out[2 * table + c] = parameter(a.gamma, s.c0 + first + c, a.param_dtype, 1.f);
+        out[3 * table + c] = parameter(a.beta, s.c0 + first + c, a.param_dtype, 0.f);
+    }
+}
 template <int V>
 struct Channels {
     float mean[V], rstd[V], gamma[V], beta[V];
-    __device__ __forceinline__ void load(const Args& a, int n, int c0)
+    __device__ __forceinline__ void load(const float* tables, int table, int c)
     {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = c0 + i, g = c / a.cg;
-            mean[i] = a.mean[(int64_t)n * a.groups + g];
-            rstd[i] = a.rstd[(int64_t)n * a.groups + g];
-            gamma[i] = parameter(a.gamma, c, a.param_dtype, 1.f);
-            beta[i] = parameter(a.beta, c, a.param_dtype, 0.f);
-        }
+        from_table<V>(tables, c, mean);
+        from_table<V>(tables + table, c, rstd);
+        from_table<V>(tables + 2 * table, c, gamma);
+        from_table<V>(tables + 3 * table, c, beta);
     }
     // xhat and dz of one element
     template <int ACT, bool QUICK>
@@ -242,13 +288,20 @@ template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void backward_sums_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
-    extern __shared__ __attribute__((aligned(16))) float lds[];      // [rows][2][channels]
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, then [rows][2][channels]
     const Place s(a, V);
+    const int table = table_floats(min(s.channels, kThreads * V));
+    float* const lds = shared + 4 * table;
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     const T* const dy = static_cast<const T*>(a.dy) + s.n * a.pdy.sn + s.c0;
-    for (int col = s.tx; col < s.columns; col += kThreads) {
+    for (int base = 0; base < s.columns; base += kThreads) {
+        const int col = base + s.tx;
+        __syncthreads();
+        channel_tables(a, s, base * V, min(s.channels - base * V, kThreads * V), shared, table, kThreads);
+        __syncthreads();
+        if (col >= s.columns) continue;
         Channels<V> ch;
-        ch.load(a, s.n, s.c0 + col * V);
+        ch.load(shared, table, s.tx * V);
         float sum[V], with_hat[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] = with_hat[i] = 0.f;
@@ -326,20 +379,28 @@ template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, and those of the group's two means
     const Place s(a, V);
+    const int table = table_floats(min(s.channels, kThreads * V));
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     const T* const dy = static_cast<const T*>(a.dy) + s.n * a.pdy.sn + s.c0;
     T* const dx = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
-    for (int col = s.tx; col < s.columns; col += kThreads) {
-        Channels<V> ch;
-        ch.load(a, s.n, s.c0 + col * V);
-        float mean_dz[V], mean_with_hat[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int g = (s.c0 + col * V + i) / a.cg;
-            mean_dz[i] = a.group_sums[((int64_t)s.n * a.groups + g) * 2];
-            mean_with_hat[i] = a.group_sums[((int64_t)s.n * a.groups + g) * 2 + 1];
+    for (int base = 0; base < s.columns; base += kThreads) {
+        const int first = base * V, here = min(s.channels - first, kThreads * V), col = base + s.tx;
+        __syncthreads();
+        channel_tables(a, s, first, here, shared, table, kThreads);
+        for (int c = threadIdx.x; c < here; c += kThreads) {
+            const float* const at = a.group_sums + ((int64_t)s.n * a.groups + s.c0 / a.cg + a.by_cg.div(first + c)) * 2;
+            shared[4 * table + c] = at[0];
+            shared[5 * table + c] = at[1];
         }
+        __syncthreads();
+        if (col >= s.columns) continue;
+        Channels<V> ch;
+        ch.load(shared, table, s.tx * V);
+        float mean_dz[V], mean_with_hat[V];
+        from_table<V>(shared + 4 * table, s.tx * V, mean_dz);
+        from_table<V>(shared + 5 * table, s.tx * V, mean_with_hat);
 #pragma unroll 2
         for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
             float v[V], d[V];
@@ -355,6 +416,188 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
         }
     }
     if (s.n == 0 && s.slab == 0) parameter_gradients(a);
+}
+
+// ---- resident: a work-group holds its chunk of an image, at most R vectors of four channels a thread (of eight, the
+// constants of 16-bit types' channels left no registers for the data)
+constexpr int kHeldChannels = 4;
+
+// Sums over the work-group's rows and each group's channels of a value per channel and thread; the results of group g at
+// result[g].  `part`: [rows][channels].
+template <int V>
+__device__ __forceinline__ void group_sums_of(const Args& a, const Place& s, const float (&v)[V], float* part, float* result, int threads)
+{
+    if (s.tx < s.columns) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) part[s.ty * s.channels + s.tx * V + i] = v[i];
+    }
+    __syncthreads();
+    const int groups = s.channels / a.cg, lane = threadIdx.x & 63, entries = s.rows * a.cg;
+    for (int g = threadIdx.x >> 6; g < groups; g += threads >> 6) {
+        float sum = 0.f;
+        for (int e = lane; e < entries; e += 64) {
+            const int row = a.by_cg.div(e);
+            sum += part[row * s.channels + g * a.cg + e - row * a.cg];
+        }
+        sum = wave_sum(sum);
+        if (lane == 0) result[g] = sum;
+    }
+    __syncthreads();
+}
+
+template <typename T, int ACT, int R>
+__global__ __launch_bounds__(1024) void resident_kernel(const Args a)
+{
+    constexpr bool QUICK = sizeof(T) == 2;
+    constexpr int V = kHeldChannels;
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // tables of origin, scale and shift, [groups], [rows][channels]
+    const int threads = blockDim.x;
+    const Place s(a, V, threads);
+    const int table = table_floats(s.channels), groups = s.channels / a.cg;
+    float *const result = shared + 3 * table, *const part = result + table_floats(groups);
+    const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
+    const int col = min(s.tx, s.columns - 1) * V, mine = s.tx < s.columns && s.ty < a.HW ? (a.HW - s.ty + s.rows - 1) / s.rows : 0;
+    Pack<T, V> raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) raw[r] = *reinterpret_cast<const Pack<T, V>*>(x + a.px.at(min(s.ty + r * s.rows, a.HW - 1), a.W, a.by_w, a.flat) + col);
+    origins(a, x, 0, s.channels, shared, threads);
+    for (int c = threadIdx.x; c < s.channels; c += threads) {
+        shared[table + c] = parameter(a.gamma, s.c0 + c, a.param_dtype, 1.f);
+        shared[2 * table + c] = parameter(a.beta, s.c0 + c, a.param_dtype, 0.f);
+    }
+    __syncthreads();
+    float origin[V], sum[V];
+    from_table<V>(shared, col, origin);
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] += r < mine ? to_float(raw[r].v[i]) - origin[i] : 0.f;
+    group_sums_of<V>(a, s, sum, part, result, threads);
+    const float count = 1.f / ((float)a.HW * (float)a.cg);
+    float mean[V];                                                   // relative to the origin
+    int group[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        group[i] = a.by_cg.div(col + i);
+        mean[i] = result[group[i]] * count;
+        sum[i] = 0.f;
+    }
+    const float own_mean = threadIdx.x < groups ? result[threadIdx.x] * count : 0.f;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float d = to_float(raw[r].v[i]) - origin[i] - mean[i];
+            sum[i] = r < mine ? fmaf(d, d, sum[i]) : sum[i];
+        }
+    group_sums_of<V>(a, s, sum, part, result, threads);
+    if (threadIdx.x < groups) {
+        const int64_t g = (int64_t)s.n * a.groups + s.c0 / a.cg + threadIdx.x;
+        if (a.mean) a.mean[g] = own_mean + shared[threadIdx.x * a.cg];
+        if (a.rstd) a.rstd[g] = 1.f / sqrtf(result[threadIdx.x] * count + a.eps);
+    }
+    float scale[V], shift[V];
+    from_table<V>(shared + table, col, scale);
+    from_table<V>(shared + 2 * table, col, shift);
+#pragma unroll
+    for (int i = 0; i < V; ++i) scale[i] *= 1.f / sqrtf(result[group[i]] * count + a.eps);
+    T* const y = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r >= mine) continue;
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = activation<ACT, QUICK>(fmaf(to_float(raw[r].v[i]) - origin[i] - mean[i], scale[i], shift[i]));
+        store_floats<T, V>(y + a.py.at(s.ty + r * s.rows, a.W, a.by_w, a.flat) + col, v);
+    }
+}
+
+// Backward, resident: writes the sums of each channel over the image, which the kernel of the parameters' gradients takes, and dx.
+template <typename T, int ACT, int R>
+__global__ __launch_bounds__(1024) void backward_resident_kernel(const Args a)
+{
+    constexpr bool QUICK = sizeof(T) == 2;
+    constexpr int V = kHeldChannels;
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, [2][channels], [groups] of two means, [rows][2][channels]
+    const int threads = blockDim.x;
+    const Place s(a, V, threads);
+    const int table = table_floats(s.channels), groups = s.channels / a.cg;
+    float *const total = shared + 4 * table, *const means = total + 2 * table, *const part = means + table_floats(2 * groups);
+    const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
+    const T* const dy = static_cast<const T*>(a.dy) + s.n * a.pdy.sn + s.c0;
+    const int col = min(s.tx, s.columns - 1) * V, mine = s.tx < s.columns && s.ty < a.HW ? (a.HW - s.ty + s.rows - 1) / s.rows : 0;
+    Pack<T, V> rx[R], rd[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int p = min(s.ty + r * s.rows, a.HW - 1);
+        rx[r] = *reinterpret_cast<const Pack<T, V>*>(x + a.px.at(p, a.W, a.by_w, a.flat) + col);
+        rd[r] = *reinterpret_cast<const Pack<T, V>*>(dy + a.pdy.at(p, a.W, a.by_w, a.flat) + col);
+    }
+    channel_tables(a, s, 0, s.channels, shared, table, threads);
+    __syncthreads();
+    Channels<V> ch;
+    ch.load(shared, table, col);
+    float sum[V], with_hat[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] = with_hat[i] = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r >= mine) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float hat, dz;
+            ch.template element<ACT, QUICK>(i, to_float(rx[r].v[i]), to_float(rd[r].v[i]), hat, dz);
+            sum[i] += dz;
+            with_hat[i] = fmaf(dz, hat, with_hat[i]);
+        }
+    }
+    if (s.tx < s.columns) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            part[(2 * s.ty) * s.channels + col + i] = sum[i];
+            part[(2 * s.ty + 1) * s.channels + col + i] = with_hat[i];
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * s.channels; e += threads) {
+        const int which = e >= s.channels, c = e - which * s.channels;
+        float v = 0.f;
+#pragma unroll 8
+        for (int r = 0; r < s.rows; ++r) v += part[(2 * r + which) * s.channels + c];
+        a.sums[((int64_t)s.n * 2 + which) * a.C + s.c0 + c] = v;
+        total[which * table + c] = v * shared[2 * table + c];
+    }
+    if (!a.y) return;
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * groups; e += threads) {
+        float v = 0.f;
+        for (int c = 0; c < a.cg; ++c) v += total[(e & 1) * table + (e >> 1) * a.cg + c];
+        means[e] = v / ((float)a.HW * (float)a.cg);
+    }
+    __syncthreads();
+    float mean_dz[V], mean_with_hat[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int g = a.by_cg.div(col + i);
+        mean_dz[i] = means[2 * g];
+        mean_with_hat[i] = means[2 * g + 1];
+    }
+    T* const dx = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r >= mine) continue;
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float hat, dz;
+            ch.template element<ACT, QUICK>(i, to_float(rx[r].v[i]), to_float(rd[r].v[i]), hat, dz);
+            v[i] = ch.rstd[i] * (fmaf(dz, ch.gamma[i], -mean_dz[i]) - hat * mean_with_hat[i]);
+        }
+        store_floats<T, V>(dx + a.py.at(s.ty + r * s.rows, a.W, a.by_w, a.flat) + col, v);
+    }
 }
 
 // Nothing to norm: means of zero, spreads of zero, gradients of zero.

@@ -66,8 +66,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKernelArgs
     auto source = [&](int h) { return h < a.H ? static_cast<const T*>(a.q) + in_q + h * a.qs[2] : static_cast<const T*>(a.k) + in_k + (h - a.H) * a.ks[2]; };
     auto target = [&](int h) { return h < a.H ? static_cast<T*>(a.q_out) + out_q + h * a.qos[2] : static_cast<T*>(a.k_out) + out_k + (h - a.H) * a.kos[2]; };
     if (col >= a.pair_columns) {
-        const int d = a.rest + (col - a.pair_columns) * V;
-        for (int h = group; h < a.heads; h += a.head_groups) *reinterpret_cast<Pack<T, V>*>(target(h) + d) = *reinterpret_cast<const Pack<T, V>*>(source(h) + d);
+        constexpr int W = ADJACENT && V > 1 ? 2 * V : V;
+        const int d = a.rest + (col - a.pair_columns) * W;
+        for (int h = group; h < a.heads; h += a.head_groups) *reinterpret_cast<Pack<T, W>*>(target(h) + d) = *reinterpret_cast<const Pack<T, W>*>(source(h) + d);
         return;
     }
     const int pair = col * V;
@@ -81,6 +82,27 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKernelArgs
         first = begin + pair;                       // 2 begin + (pair - begin)
         second = first + length;
     }
+    // the elements of HEADS heads are on their way while the angles are formed, and those of the next ones while these are turned
+    constexpr int HEADS = 4;
+    Pack<T, 2 * V> x[HEADS];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int j = 0; j < HEADS; ++j) {
+            const T* const from = source(min(h0 + j * a.head_groups, a.heads - 1));
+            if (ADJACENT && V > 1) {
+                x[j] = *reinterpret_cast<const Pack<T, 2 * V>*>(from + 2 * pair);
+            } else {
+                const Pack<T, V> lo = *reinterpret_cast<const Pack<T, V>*>(from + (ADJACENT ? 2 * pair : first)), hi = *reinterpret_cast<const Pack<T, V>*>(from + (ADJACENT ? 2 * pair + 1 : second));
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    x[j].v[i] = lo.v[i];
+                    x[j].v[V + i] = hi.v[i];
+                }
+            }
+        }
+    };
+    load(group);
+    __builtin_amdgcn_sched_barrier(0);
     float c[V], sn[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -91,31 +113,33 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKernelArgs
         turn_of(pos, a.inv_freq[pair + i], c[i], sn[i]);
         sn[i] = a.inverse ? -sn[i] : sn[i];
     }
-    for (int h = group; h < a.heads; h += a.head_groups) {
-        const T* const from = source(h);
-        T* const to = target(h);
-        if (ADJACENT) {
-            float x[2 * V];
-            load_floats<T, 2 * V>(from + 2 * pair, x);
+    for (int h0 = group; h0 < a.heads; h0 += HEADS * a.head_groups) {
+        if (h0 != group) load(h0);
+#pragma unroll
+        for (int j = 0; j < HEADS; ++j) {
+            const int h = h0 + j * a.head_groups;
+            if (h >= a.heads) continue;
+            T* const to = target(h);
+            float y[2 * V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float u = x[2 * i], v = x[2 * i + 1];
-                x[2 * i] = u * c[i] - v * sn[i];
-                x[2 * i + 1] = u * sn[i] + v * c[i];
+                constexpr int STEP = ADJACENT ? 2 : 1, OTHER = ADJACENT ? 1 : V;
+                const float u = to_float(x[j].v[STEP * i]), v = to_float(x[j].v[STEP * i + OTHER]);
+                y[STEP * i] = u * c[i] - v * sn[i];
+                y[STEP * i + OTHER] = u * sn[i] + v * c[i];
             }
-            store_floats<T, 2 * V>(to + 2 * pair, x);
-        } else {
-            float u[V], v[V];
-            load_floats<T, V>(from + first, u);
-            load_floats<T, V>(from + second, v);
+            if (ADJACENT && V > 1) {
+                store_floats<T, 2 * V>(to + 2 * pair, y);
+            } else {
+                float lo[V], hi[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float x = u[i], y = v[i];
-                u[i] = x * c[i] - y * sn[i];
-                v[i] = x * sn[i] + y * c[i];
+                for (int i = 0; i < V; ++i) {
+                    lo[i] = y[i];
+                    hi[i] = y[V + i];
+                }
+                store_floats<T, V>(to + (ADJACENT ? 2 * pair : first), lo);
+                store_floats<T, V>(to + (ADJACENT ? 2 * pair + 1 : second), hi);
             }
-            store_floats<T, V>(to + first, u);
-            store_floats<T, V>(to + second, v);
         }
     }
 }
@@ -178,11 +202,7 @@ hipError_t launch_rotary(const RotaryArgs& g, hipStream_t stream)
             return launch_kernel(kernel, dim3((unsigned)((b.items + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, b);
         };
         if (!whole) return adjacent ? launch(rotary_kernel<T, 1, true>, 1, 1) : launch(rotary_kernel<T, 1, false>, 1, 1);
-        if (adjacent) {
-            // (a column is one unit of pairs, and of copied dimensions half of one)
-            return launch(rotary_kernel<T, UNIT / 2, true>, UNIT / 2, UNIT / 2);
-        }
-        return launch(rotary_kernel<T, UNIT, false>, UNIT, UNIT);
+        return adjacent ? launch(rotary_kernel<T, UNIT / 2, true>, UNIT / 2, UNIT) : launch(rotary_kernel<T, UNIT, false>, UNIT, UNIT);
     });
 }
 
