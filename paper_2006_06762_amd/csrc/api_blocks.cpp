@@ -96,8 +96,8 @@ anr_status check_rotary(const anr_rotary_desc* d, anr_rotary_desc* out)
     }
     if (2 * pairs > d->D || !valid_type(d->dtype) || d->pairing < ANR_ROTARY_HALVES || d->pairing > ANR_ROTARY_SECTION_HALVES) return ANR_ERR_INVALID_ARG;
     if (d->inverse < 0 || d->inverse > 1 || d->pos_type < ANR_POS_I32 || d->pos_type > ANR_POS_F32 || d->reserved != 0) return ANR_ERR_INVALID_ARG;
-    // a thread for every column of every token, at least, in 32 bits
-    if (d->D > 2048 || (int64_t)d->H + d->Hk > 65536 || (int64_t)d->B * d->S >= (int64_t)1 << 31 || (int64_t)d->B * d->S * d->D > 0x7fffff00) return ANR_ERR_UNSUPPORTED;
+    // tokens are counted in 32 bits
+    if (d->D > 2048 || (int64_t)d->H + d->Hk > 65536 || (int64_t)d->B * d->S >= (int64_t)1 << 31) return ANR_ERR_UNSUPPORTED;
     *out = *d;
     int64_t* const strides[4] = {out->q_stride, out->k_stride, out->q_out_stride, out->k_out_stride};
     for (int t = 0; t < 4; ++t) {

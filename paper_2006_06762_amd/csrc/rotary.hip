@@ -1,9 +1,9 @@
 // Rotary positions with several axes: pairs (u, v) of a token's dimensions become (u cos - v sin, u sin + v cos), with the
 // angle positions[axis of the pair] * inv_freq[pair].
 //
-// Bound: by memory, each element is read and written once.  The angle of a pair is the same for all heads, so a thread
-// takes one column (V pairs, or V dimensions that are only copied) of one token and turns it in several heads with one
-// sine and cosine: it is computed once per column and head group.  Far positions need more than 32 bits of
+// Bound: by memory, each element is read and written once.  The angle of a pair is the same for all heads: a work-group forms
+// those of its tokens once, in LDS, and then turns the tokens' heads, whose first elements are on their way meanwhile.  (With the
+// angles formed by each thread for its own column, once for four heads, 786 MB took 260 us.)  Far positions need more than 32 bits of
 // the angle (a position of 10^6 at frequency 1 leaves 0.06 of a radian in a float), so it is formed in 64 bits as quarter
 // turns and reduced there to an eighth of a turn on either side, |t| <= pi/4, where the Taylor polynomials of degree 9 and 10
 // are off by t^11 / 11! < 2e-9 and t^12 / 12! < 2e-10 of 1: below half a unit of float's last place, 3e-8.
@@ -23,14 +23,13 @@ struct RotaryKernelArgs {
     const void* positions;
     const float* inv_freq;
     int64_t qs[3], ks[3], qos[3], kos[3], ps[3];
-    int S, H, heads;                // heads: of q and k
+    int tokens, S, H, heads;        // tokens: of all sequences; heads: of q and k
     int section_end[4];             // first pair behind each axis
     int pairs, pairing, inverse, pos_type;
-    int pair_columns, columns;      // columns of V pairs; with those of V dimensions that are copied
+    int pair_columns, columns;      // columns of V pairs; with those of V dimensions (adjacent: of 2 V) that are copied
     int rest;                       // first dimension that is copied
-    int head_groups;                // threads that share a token's column
-    uint32_t items;
-    FastDiv by_columns, by_groups, by_s;
+    int group_tokens, group_heads;  // of a work-group
+    FastDiv by_columns, by_heads, by_s, by_pairs;
 };
 
 __device__ __forceinline__ double position(const void* p, int64_t i, int type)
@@ -56,43 +55,59 @@ __device__ __forceinline__ void turn_of(double pos, float freq, float& c, float&
 template <typename T, int V, bool ADJACENT>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKernelArgs a)
 {
-    const uint32_t item = blockIdx.x * kThreads + threadIdx.x;           // (below 2^31: see the launch)
-    if (item >= a.items) return;
-    const int token_group = a.by_columns.div((int)item), col = (int)item - token_group * a.columns;
-    const int token = a.by_groups.div(token_group), group = token_group - token * a.head_groups;
-    const int b = a.by_s.div(token), s = token - b * a.S;
-    const int64_t in_q = b * a.qs[0] + s * a.qs[1], in_k = b * a.ks[0] + s * a.ks[1];
-    const int64_t out_q = b * a.qos[0] + s * a.qos[1], out_k = b * a.kos[0] + s * a.kos[1];
-    auto source = [&](int h) { return h < a.H ? static_cast<const T*>(a.q) + in_q + h * a.qs[2] : static_cast<const T*>(a.k) + in_k + (h - a.H) * a.ks[2]; };
-    auto target = [&](int h) { return h < a.H ? static_cast<T*>(a.q_out) + out_q + h * a.qos[2] : static_cast<T*>(a.k_out) + out_k + (h - a.H) * a.kos[2]; };
-    if (col >= a.pair_columns) {
-        constexpr int W = ADJACENT && V > 1 ? 2 * V : V;
-        const int d = a.rest + (col - a.pair_columns) * W;
-        for (int h = group; h < a.heads; h += a.head_groups) *reinterpret_cast<Pack<T, W>*>(target(h) + d) = *reinterpret_cast<const Pack<T, W>*>(source(h) + d);
-        return;
-    }
-    const int pair = col * V;
-    // (the pairs of a column lie in one section where sections have blocks of their own; else each has its axis)
-    int axis0 = 0;
+    extern __shared__ __attribute__((aligned(16))) float lds[];      // cosines of [tokens][pairs], then the sines
+    constexpr int W = ADJACENT && V > 1 ? 2 * V : V;                 // dimensions of a copied column
+    constexpr int AHEAD = 4;                                         // items of a thread that are on their way together
+    const int token0 = blockIdx.x * a.group_tokens, tokens = min(a.group_tokens, a.tokens - token0);
+    const int head0 = blockIdx.y * a.group_heads, heads = min(a.group_heads, a.heads - head0);
+    const int items = tokens * heads * a.columns;
+    const float *const cosines = lds, *const sines = lds + a.group_tokens * a.pairs;
+
+    // an item: a column of a head of a token, in the order of packed memory
+    struct Item {
+        int64_t from, to;           // first element of the head
+        bool in_k, copied;
+        int first, second, angle;   // dimensions, and where its angles start
+    };
+    auto item = [&](int i) {
+        Item r;
+        const int row = a.by_columns.div(i), col = i - row * a.columns;
+        const int token = heads == a.group_heads ? a.by_heads.div(row) : row / heads, h = head0 + row - token * heads;
+        const int b = a.by_s.div(token0 + token), s = token0 + token - b * a.S;
+        r.in_k = h >= a.H;
+        const int own = r.in_k ? h - a.H : h;
+        r.from = r.in_k ? b * a.ks[0] + s * a.ks[1] + own * a.ks[2] : b * a.qs[0] + s * a.qs[1] + own * a.qs[2];
+        r.to = r.in_k ? b * a.kos[0] + s * a.kos[1] + own * a.kos[2] : b * a.qos[0] + s * a.qos[1] + own * a.qos[2];
+        r.copied = col >= a.pair_columns;
+        const int pair = col * V;
+        r.angle = token * a.pairs + pair;
+        r.first = ADJACENT ? 2 * pair : pair;
+        r.second = ADJACENT ? r.first + V : a.pairs + pair;
+        if (a.pairing == ANR_ROTARY_SECTION_HALVES) {
+            int axis = 0;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) axis0 += pair >= a.section_end[i];
-    int first = pair, second = a.pairs + pair;
-    if (a.pairing == ANR_ROTARY_SECTION_HALVES) {
-        const int begin = axis0 ? a.section_end[axis0 - 1] : 0, length = a.section_end[axis0] - begin;
-        first = begin + pair;                       // 2 begin + (pair - begin)
-        second = first + length;
-    }
-    // the elements of HEADS heads are on their way while the angles are formed, and those of the next ones while these are turned
-    constexpr int HEADS = 4;
-    Pack<T, 2 * V> x[HEADS];
-    auto load = [&](int h0) {
+            for (int j = 0; j < 3; ++j) axis += pair >= a.section_end[j];
+            const int begin = axis ? a.section_end[axis - 1] : 0;
+            r.first = begin + pair;                 // 2 begin + (pair - begin)
+            r.second = r.first + a.section_end[axis] - begin;
+        }
+        if (r.copied) {
+            r.first = a.rest + (col - a.pair_columns) * W;
+            r.second = W > V ? r.first + V : r.first;
+        }
+        return r;
+    };
+    Pack<T, 2 * V> x[AHEAD];
+    Item at[AHEAD];
+    auto load = [&](int i0) {
 #pragma unroll
-        for (int j = 0; j < HEADS; ++j) {
-            const T* const from = source(min(h0 + j * a.head_groups, a.heads - 1));
+        for (int j = 0; j < AHEAD; ++j) {
+            at[j] = item(min(i0 + j * kThreads, items - 1));
+            const T* const from = static_cast<const T*>(at[j].in_k ? a.k : a.q) + at[j].from;
             if (ADJACENT && V > 1) {
-                x[j] = *reinterpret_cast<const Pack<T, 2 * V>*>(from + 2 * pair);
+                x[j] = *reinterpret_cast<const Pack<T, 2 * V>*>(from + at[j].first);
             } else {
-                const Pack<T, V> lo = *reinterpret_cast<const Pack<T, V>*>(from + (ADJACENT ? 2 * pair : first)), hi = *reinterpret_cast<const Pack<T, V>*>(from + (ADJACENT ? 2 * pair + 1 : second));
+                const Pack<T, V> lo = *reinterpret_cast<const Pack<T, V>*>(from + at[j].first), hi = *reinterpret_cast<const Pack<T, V>*>(from + at[j].second);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     x[j].v[i] = lo.v[i];
@@ -101,44 +116,49 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKernelArgs
             }
         }
     };
-    load(group);
-    __builtin_amdgcn_sched_barrier(0);
-    float c[V], sn[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
+    load(threadIdx.x);
+    for (int e = threadIdx.x; e < tokens * a.pairs; e += kThreads) {
+        const int token = a.by_pairs.div(e), pair = e - token * a.pairs;
+        const int b = a.by_s.div(token0 + token), s = token0 + token - b * a.S;
         int axis = 0;
 #pragma unroll
-        for (int j = 0; j < 3; ++j) axis += pair + i >= a.section_end[j];
-        const double pos = position(a.positions, axis * a.ps[0] + b * a.ps[1] + s * a.ps[2], a.pos_type);
-        turn_of(pos, a.inv_freq[pair + i], c[i], sn[i]);
-        sn[i] = a.inverse ? -sn[i] : sn[i];
+        for (int j = 0; j < 3; ++j) axis += pair >= a.section_end[j];
+        float c, sn;
+        turn_of(position(a.positions, axis * a.ps[0] + b * a.ps[1] + s * a.ps[2], a.pos_type), a.inv_freq[pair], c, sn);
+        lds[e] = c;
+        lds[a.group_tokens * a.pairs + e] = a.inverse ? -sn : sn;
     }
-    for (int h0 = group; h0 < a.heads; h0 += HEADS * a.head_groups) {
-        if (h0 != group) load(h0);
+    __syncthreads();
+    for (int i0 = threadIdx.x; i0 < items; i0 += AHEAD * kThreads) {
+        if (i0 >= AHEAD * kThreads) load(i0);
 #pragma unroll
-        for (int j = 0; j < HEADS; ++j) {
-            const int h = h0 + j * a.head_groups;
-            if (h >= a.heads) continue;
-            T* const to = target(h);
-            float y[2 * V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                constexpr int STEP = ADJACENT ? 2 : 1, OTHER = ADJACENT ? 1 : V;
-                const float u = to_float(x[j].v[STEP * i]), v = to_float(x[j].v[STEP * i + OTHER]);
-                y[STEP * i] = u * c[i] - v * sn[i];
-                y[STEP * i + OTHER] = u * sn[i] + v * c[i];
-            }
-            if (ADJACENT && V > 1) {
-                store_floats<T, 2 * V>(to + 2 * pair, y);
-            } else {
-                float lo[V], hi[V];
+        for (int j = 0; j < AHEAD; ++j) {
+            if (i0 + j * kThreads >= items) continue;
+            T* const to = static_cast<T*>(at[j].in_k ? a.k_out : a.q_out) + at[j].to;
+            Pack<T, 2 * V> out = x[j];
+            if (!at[j].copied) {
+                float y[2 * V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    lo[i] = y[i];
-                    hi[i] = y[V + i];
+                    constexpr int STEP = ADJACENT ? 2 : 1, OTHER = ADJACENT ? 1 : V;
+                    const float c = cosines[at[j].angle + i], sn = sines[at[j].angle + i];
+                    const float u = to_float(x[j].v[STEP * i]), v = to_float(x[j].v[STEP * i + OTHER]);
+                    y[STEP * i] = u * c - v * sn;
+                    y[STEP * i + OTHER] = u * sn + v * c;
                 }
-                store_floats<T, V>(to + (ADJACENT ? 2 * pair : first), lo);
-                store_floats<T, V>(to + (ADJACENT ? 2 * pair + 1 : second), hi);
+                out = pack_floats<T, 2 * V>(y);
+            }
+            if (ADJACENT && V > 1) {
+                *reinterpret_cast<Pack<T, 2 * V>*>(to + at[j].first) = out;
+            } else {
+                Pack<T, V> lo, hi;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    lo.v[i] = out.v[i];
+                    hi.v[i] = out.v[V + i];
+                }
+                *reinterpret_cast<Pack<T, V>*>(to + at[j].first) = lo;
+                if (!at[j].copied) *reinterpret_cast<Pack<T, V>*>(to + at[j].second) = hi;
             }
         }
     }
@@ -190,16 +210,23 @@ hipError_t launch_rotary(const RotaryArgs& g, hipStream_t stream)
         whole = whole && aligned(g.q, a.qs) && aligned(g.q_out, a.qos) && (d.Hk == 0 || (aligned(g.k, a.ks) && aligned(g.k_out, a.kos)));
         auto launch = [&](auto kernel, int pairs_per_column, int copied) {
             RotaryKernelArgs b = a;
+            b.tokens = (int)tokens;
             b.pair_columns = a.pairs / pairs_per_column;
             b.columns = b.pair_columns + (d.D - a.rest) / copied;
-            // A token's heads are shared by as many threads as fill the card, but a column's angles are worth four heads
-            const int64_t per_head = tokens * b.columns;
-            b.head_groups = (int)std::min({(int64_t)heads, std::max<int64_t>((heads + 3) / 4, (256 * 1024 + per_head - 1) / per_head), (int64_t)0x7fffff00 / per_head});
-            b.items = (uint32_t)(per_head * b.head_groups);
+            // A work-group has the angles of 512 pairs at most (1024 of one token) and eight items a thread; few tokens share their heads among
+            // work-groups as far as there are CUs for them, with an item a thread or more
+            const int64_t of_token = (int64_t)heads * b.columns;
+            b.group_tokens = (int)std::max<int64_t>(1, std::min({(int64_t)512 / std::max(1, a.pairs), 8 * kThreads / of_token, tokens}));
+            while (b.group_tokens > 1 && (tokens + b.group_tokens - 1) / b.group_tokens < 1024) b.group_tokens = (b.group_tokens + 1) / 2;
+            const int64_t blocks = (tokens + b.group_tokens - 1) / b.group_tokens, items = b.group_tokens * of_token;
+            const int64_t shares = std::max<int64_t>((items + 16 * kThreads - 1) / (16 * kThreads), std::min<int64_t>(512 / blocks, items / kThreads));
+            b.group_heads = (int)std::max<int64_t>(1, heads / std::max<int64_t>(1, shares));
             b.by_columns = make_fastdiv(b.columns);
-            b.by_groups = make_fastdiv(b.head_groups);
+            b.by_heads = make_fastdiv(b.group_heads);
             b.by_s = make_fastdiv(d.S);
-            return launch_kernel(kernel, dim3((unsigned)((b.items + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, b);
+            b.by_pairs = make_fastdiv(std::max(1, a.pairs));
+            return launch_kernel(kernel, dim3((unsigned)blocks, (unsigned)((heads + b.group_heads - 1) / b.group_heads)), dim3(kThreads),
+                                 sizeof(float) * 2 * (size_t)b.group_tokens * a.pairs, stream, b);
         };
         if (!whole) return adjacent ? launch(rotary_kernel<T, 1, true>, 1, 1) : launch(rotary_kernel<T, 1, false>, 1, 1);
         return adjacent ? launch(rotary_kernel<T, UNIT / 2, true>, UNIT / 2, UNIT) : launch(rotary_kernel<T, UNIT, false>, UNIT, UNIT);
