@@ -39,6 +39,21 @@ __device__ __forceinline__ Pack<T, V> pack_floats(const float (&in)[V])
     return a;
 }
 
+// A store that goes past L2 (see stg4_nt) where it is `streaming`: neighbouring lanes write whole lines then.
+template <typename T, int V>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& a, bool streaming)
+{
+    if constexpr (sizeof(T) * V == 16) {
+        if (streaming) {
+            asm volatile("" ::: "memory");           // (or the two stores become one, an ordinary one)
+            __builtin_nontemporal_store(__builtin_bit_cast(f32x4, a), reinterpret_cast<f32x4*>(p));
+            asm volatile("" ::: "memory");
+            return;
+        }
+    }
+    *reinterpret_cast<Pack<T, V>*>(p) = a;
+}
+
 template <typename T, int V>
 __device__ __forceinline__ void store_floats(T* p, const float (&in)[V])
 {
@@ -66,8 +81,22 @@ __device__ __forceinline__ float sigmoid(float z)
     return 1.f / (1.f + expf(-z));
 }
 
+// Phi(z), and exp(-z^2 / 2).  QUICK: by Abramowitz and Stegun's formula 7.1.26, erf to 1.5e-7, which shares the exponential; else by the
+// library's erf.
+template <bool QUICK>
+__device__ __forceinline__ float normal_below(float z, float& bell)
+{
+    if (!QUICK) {
+        bell = expf(-0.5f * z * z);
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f));
+    }
+    bell = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+    const float tail = 0.5f * bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    return z > 0.f ? 1.f - tail : tail;                                    // (a NaN's tail is one)
+}
+
 constexpr float kTwoRootTwoOverPi = 1.59576912160573071f;      // 2 sqrt(2 / pi)
-constexpr float kRootHalf = 0.70710678118654752f;
 constexpr float kOneOverRootTwoPi = 0.39894228040143268f;
 
 // act(z).
@@ -76,7 +105,10 @@ __device__ __forceinline__ float activation(float z)
 {
     if (ACT == ANR_ACT_RELU) return z < 0.f ? 0.f : z;                     // (a NaN stays one)
     if (ACT == ANR_ACT_SILU) return z * sigmoid<QUICK>(z);
-    if (ACT == ANR_ACT_GELU) return 0.5f * z * (1.f + erff(z * kRootHalf));
+    if (ACT == ANR_ACT_GELU) {
+        float bell;
+        return z * normal_below<QUICK>(z, bell);
+    }
     if (ACT == ANR_ACT_GELU_TANH) return z * sigmoid<QUICK>(kTwoRootTwoOverPi * fmaf(0.044715f * z * z, z, z));
     return z;
 }
@@ -96,8 +128,8 @@ __device__ __forceinline__ float activation_and_slope(float z, float& slope)
         return z * s;
     }
     if (ACT == ANR_ACT_GELU) {
-        const float phi = 0.5f * (1.f + erff(z * kRootHalf));
-        const float density = kOneOverRootTwoPi * (QUICK ? __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z) : expf(-0.5f * z * z));
+        float bell;
+        const float phi = normal_below<QUICK>(z, bell), density = kOneOverRootTwoPi * bell;
         slope = density == 0.f ? phi : fmaf(z, density, phi);
         return z * phi;
     }

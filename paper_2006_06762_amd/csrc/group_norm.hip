@@ -88,14 +88,29 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
     p.vector = vector;
     // Whole groups and whole units, at least a line of 128 bytes of a pixel.
     const int least = std::min(common_multiple(a.cg, V), g.C);
-    a.chunk = std::min(g.C, least * std::max(1, (128 / es + least - 1) / least));
+    auto chunk_of = [&](int bytes) { return std::min(g.C, least * std::max(1, (bytes / es + least - 1) / least)); };
+    a.chunk = chunk_of(128);
     p.chunks = (g.C + a.chunk - 1) / a.chunk;
+    // Resident kernels with work-groups for less than every CU take chunks of 64 bytes, float32 ones only where there are fewer still: 20^2 x 256
+    // float32 backward, batch 1, 14.8 -> 11.0 us, 28^2 18.6 -> 12.4, batch 16 18.8 -> 20; bf16 20^2 14.8 -> 13.0, batch 16 15.9 -> 13.7, 28^2
+    // 22 -> 17 (19 for the kernels that read twice).
+    if (vector && chunk_of(64) < a.chunk && (int64_t)p.chunks * g.N < (g.dtype == ANR_F32 ? 128 : 256) &&
+        (g.dtype != ANR_F32 || resident_pays(g, a, backward, (int64_t)p.chunks * g.N))) {
+        Args half = a;
+        half.chunk = chunk_of(64);
+        if (resident_pays(g, half, backward, (int64_t)p.chunks * g.N)) {
+            a.chunk = half.chunk;
+            p.chunks = (g.C + a.chunk - 1) / a.chunk;
+        }
+    }
+    const int line = 128 / es;
+    a.streaming = a.chunk % line == 0 && (reinterpret_cast<uintptr_t>(g.y) & 127) == 0 && g.ys[0] % line == 0 && g.ys[1] % line == 0 && g.ys[2] % line == 0;
     const int columns = a.chunk / V, rows = kThreads / std::min(columns, kThreads);
     p.table = table_floats(std::min(a.chunk, kThreads * V));
-    // Slabs: about four work-groups per CU as far as each thread has eight pixels, one per CU as far as it has two, and at most 128
-    // that are joined.
+    // Slabs: about four work-groups per CU as far as each thread has eight pixels (float32: four), one per CU as far as it has two, and at
+    // most 128 that are joined. (Eight or four, backward, 320 channels: float32 8 x 56^2 47 / 36 us, bf16 34 / 35, 4 x 95 x 63 32 / 34.)
     const int64_t others = (int64_t)p.chunks * g.N;
-    int64_t slabs = std::min((1024 + others - 1) / others, (int64_t)a.HW / (8 * rows));
+    int64_t slabs = std::min((1024 + others - 1) / others, (int64_t)a.HW / ((es == 4 ? 4 : 8) * rows));
     slabs = std::max(slabs, std::min((256 + others - 1) / others, (int64_t)a.HW / (2 * rows)));
     slabs = std::max<int64_t>(1, std::min<int64_t>(slabs, 128));
     a.slab_pixels = (int)((a.HW + slabs - 1) / slabs);

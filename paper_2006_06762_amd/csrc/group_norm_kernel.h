@@ -47,6 +47,7 @@ struct Args {
     int N, HW, W, C, groups, cg, flat, param_dtype;
     int chunk;                      // channels of a chunk: whole groups
     int slabs, slab_pixels;
+    bool streaming;                 // y's stores go past L2: a chunk's pixel is whole lines of 128 bytes
 };
 
 // What a work-group works on.
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
             load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = activation<ACT, QUICK>(fmaf(v[i] - mean[i], scale[i], shift[i]));
-            store_floats<T, V>(y + a.py.at(p, a.W, a.by_w, a.flat) + col * V, v);
+            store_pack(y + a.py.at(p, a.W, a.by_w, a.flat) + col * V, pack_floats<T, V>(v), a.streaming);
         }
     }
 }
@@ -366,7 +367,7 @@ __device__ __forceinline__ void parameter_gradients(const Args& a)
         void* const out = which ? a.dgamma : a.dbeta;
         if (!out) continue;
         float sum = 0.f;
-#pragma unroll 8
+#pragma unroll 16
         for (int n = 0; n < a.N; ++n) sum += a.sums[((int64_t)n * 2 + which) * a.C + c];
         store_any(out, c, a.param_dtype, sum);
     }
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
                 ch.template element<ACT, QUICK>(i, v[i], d[i], hat, dz);
                 v[i] = ch.rstd[i] * (fmaf(dz, ch.gamma[i], -mean_dz[i]) - hat * mean_with_hat[i]);
             }
-            store_floats<T, V>(dx + a.py.at(p, a.W, a.by_w, a.flat) + col * V, v);
+            store_pack(dx + a.py.at(p, a.W, a.by_w, a.flat) + col * V, pack_floats<T, V>(v), a.streaming);
         }
     }
     if (s.n == 0 && s.slab == 0) parameter_gradients(a);
@@ -552,6 +553,10 @@ __global__ __launch_bounds__(1024) void backward_resident_kernel(const Args a)
             ch.template element<ACT, QUICK>(i, to_float(rx[r].v[i]), to_float(rd[r].v[i]), hat, dz);
             sum[i] += dz;
             with_hat[i] = fmaf(dz, hat, with_hat[i]);
+            if (!QUICK) {                                             // (float32: what is held from here on)
+                rx[r].v[i] = from_float<T>(hat);
+                rd[r].v[i] = from_float<T>(dz);
+            }
         }
     }
     if (s.tx < s.columns) {
@@ -592,8 +597,8 @@ __global__ __launch_bounds__(1024) void backward_resident_kernel(const Args a)
         float v[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float hat, dz;
-            ch.template element<ACT, QUICK>(i, to_float(rx[r].v[i]), to_float(rd[r].v[i]), hat, dz);
+            float hat = to_float(rx[r].v[i]), dz = to_float(rd[r].v[i]);
+            if (QUICK) ch.template element<ACT, QUICK>(i, hat, dz, hat, dz);
             v[i] = ch.rstd[i] * (fmaf(dz, ch.gamma[i], -mean_dz[i]) - hat * mean_with_hat[i]);
         }
         store_floats<T, V>(dx + a.py.at(s.ty + r * s.rows, a.W, a.by_w, a.flat) + col, v);
