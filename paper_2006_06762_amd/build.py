@@ -39,8 +39,6 @@ FILE_FLAGS = {
     "conv_pieces.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "conv_stem.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-    "mm16_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-    "mm16_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

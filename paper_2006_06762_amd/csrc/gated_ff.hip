@@ -228,12 +228,30 @@ int splits_of(int64_t M, int64_t N, int64_t chunks)
     return (int)std::max<int64_t>(1, std::min<int64_t>({(512 + tiles - 1) / tiles, chunks / 4, 16}));
 }
 
+int64_t chunks_of(int64_t K) { return (K + mm16::BK - 1) / mm16::BK; }
+
+// The tile with the shortest estimated time: rounds of work-groups over the CUs, each with its chunks and ends (us). A tile of 256 takes a CU
+// for itself, of those of 128 it takes two; one alone is split over two groups of waves.
+mm16::Shape choose_shape(int64_t tiles256, int64_t tiles128, int64_t chunks)
+{
+    const double large = (double)((tiles256 + 255) / 256) * (1.7 * (double)chunks + 4.0);
+    const int64_t full = tiles128 / 512, rest = tiles128 % 512;
+    const double pair = 1.14 * (double)chunks + 4.0, alone = 0.60 * (double)chunks + 4.0;
+    if (tiles128 <= 256) return large < alone ? mm16::SHAPE_256 : mm16::SHAPE_128_TWICE;
+    const double small = (double)full * pair + (rest > 256 ? pair : rest > 0 ? 0.75 * (double)chunks + 4.0 : 0.0);
+    return large < small ? mm16::SHAPE_256 : mm16::SHAPE_128;
+}
+
 hipError_t launch(mm16::Form form, int dtype, bool aligned, mm16::Args& a, hipStream_t stream)
 {
     const int n_share = form == mm16::FORM_GATED ? 2 : 1;
-    int64_t tiles256 = 0;
-    for (int i = 0; i < a.problems; ++i) tiles256 += tiles_of(a.p[i].M, a.p[i].N, 256, 256 / n_share);
-    const int tile = a.splits == 1 && tiles256 >= 200 ? 256 : 128;
+    auto tiles = [&](int edge) {
+        int64_t n = 0;
+        for (int i = 0; i < a.problems; ++i) n += tiles_of(a.p[i].M, a.p[i].N, edge, edge / n_share);
+        return n * a.splits;
+    };
+    const mm16::Shape shape = choose_shape(tiles(256), tiles(128), chunks_of(a.p[0].K) * a.p[0].segments / a.splits);
+    const int tile = mm16::edge_of(shape);
     a.first_tile[0] = 0;
     for (int i = 0; i < a.problems; ++i) {
         a.p[i].tiles_m = (a.p[i].M + tile - 1) / tile;
@@ -241,7 +259,7 @@ hipError_t launch(mm16::Form form, int dtype, bool aligned, mm16::Args& a, hipSt
         a.first_tile[i + 1] = a.first_tile[i] + a.p[i].tiles_m * a.p[i].tiles_n;
     }
     a.band = 8;
-    return dtype == ANR_F16 ? mm16::launch_products_f16(form, tile, aligned, a, stream) : mm16::launch_products_bf16(form, tile, aligned, a, stream);
+    return dtype == ANR_F16 ? mm16::launch_products_f16(form, shape, aligned, a, stream) : mm16::launch_products_bf16(form, shape, aligned, a, stream);
 }
 
 // A product whose k may be shared: through `parts` where it is.
@@ -259,8 +277,6 @@ hipError_t launch_shared(mm16::Form form, int dtype, bool aligned, const mm16::P
         return launch_kernel(join_kernel<T>, grid_of(p.N, kThreads, p.M, 1), dim3(kThreads), 0, stream, parts, splits, static_cast<T*>(p.d), p.ldd, (int64_t)p.M, (int64_t)p.N);
     });
 }
-
-int64_t chunks_of(int64_t K) { return (K + mm16::BK - 1) / mm16::BK; }
 
 hipError_t forward_16(const GatedFfArgs& g, hipStream_t stream)
 {

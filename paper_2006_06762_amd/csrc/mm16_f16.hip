@@ -4,7 +4,7 @@
 namespace anr {
 namespace mm16 {
 
-hipError_t launch_products_f16(Form form, int tile, bool aligned, const Args& a, hipStream_t stream) { return launch_products<half_t>(form, tile, aligned, a, stream); }
+hipError_t launch_products_f16(Form form, Shape shape, bool aligned, const Args& a, hipStream_t stream) { return launch_products<half_t>(form, shape, aligned, a, stream); }
 
 }  // namespace mm16
 }  // namespace anr

@@ -84,6 +84,9 @@ struct Image {
 template <int BM, int BN, Kind XK, Kind WK>
 constexpr size_t lds_bytes() { return 2 * (size_t)(Image<XK, BM>::BYTES + Image<WK, BN>::BYTES); }
 
+// The units of a chunk in three parts.
+constexpr int part_of(int units, int part) { return (units * part + 2) / 3; }
+
 // Global -> registers -> LDS of one operand's chunk by NT threads.
 template <typename T, Kind KIND, int R, int NT, bool ALIGNED, bool PAIRED>
 struct Stager {
@@ -128,11 +131,12 @@ struct Stager {
     }
     __device__ __forceinline__ int matrix_of(int i) const { return PAIRED ? (which + i * (NT / ROW_UNITS) / 32) & 1 : 0; }
 
-    // chunk of k from k0 on, of segment `seg`
+    // units FIRST to LAST - 1 of the chunk of k from k0 on, of segment `seg`
+    template <int FIRST, int LAST>
     __device__ __forceinline__ void load(int k0, int seg)
     {
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
+        for (int i = FIRST; i < LAST; ++i) {
             const char* const b = base + ((PAIRED ? matrix_of(i) : seg) ? other : 0) + 2 * (KIND == K_ROWS ? (int64_t)k0 : k0 * ld);
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(b), 0, kExtent, 0x00020000);
             const int k = KIND == K_ROWS ? k0 + unit * 8 : k0 + first + i * (NT / ROW_UNITS);
@@ -150,10 +154,11 @@ struct Stager {
             }
         }
     }
+    template <int FIRST, int LAST>
     __device__ __forceinline__ void store(char* lds) const
     {
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
+        for (int i = FIRST; i < LAST; ++i) {
             const int r = first + i * (NT / ROW_UNITS);
             const int at = KIND == K_ROWS ? r * Image<KIND, R>::ROW + ((unit ^ (r & 7)) * 16) : r * Image<KIND, R>::ROW + unit * 16;
             *reinterpret_cast<u32x4*>(lds + at) = data[i];
@@ -213,15 +218,19 @@ __device__ __forceinline__ void device_activation(int act, F f)
     }
 }
 
-template <typename T, int BM, int BN, int WM, int WN, Kind XK, Kind WK, Epilogue EPI, bool ALIGNED>
-__global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void product_kernel(const Args args)
+// G groups of waves take a tile's chunks in turn, each with buffers and sums of its own, and join the sums in LDS: for products with
+// about as many tiles as CUs, whose work-groups are alone on theirs.
+template <typename T, int BM, int BN, int WM, int WN, int G, Kind XK, Kind WK, Epilogue EPI, bool ALIGNED>
+__global__ __launch_bounds__(64 * WM * WN * G, 64 * WM * WN * G / 256) void product_kernel(const Args args)
 {
     constexpr int NT = 64 * WM * WN, MB = BM / (32 * WM), NB = BN / (32 * WN);
     constexpr int XBYTES = Image<XK, BM>::BYTES, BUF = XBYTES + Image<WK, BN>::BYTES;
     constexpr bool PAIRED = EPI == GATED;
     constexpr int TILE_N = PAIRED ? BN / 2 : BN;                      // columns of D in a tile
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+    char* const lds = shared + group * 2 * BUF;
+    const int tid = threadIdx.x % NT, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
     // Work-group ids are dealt round-robin over the 8 XCDs, each with its own L2: every XCD gets a contiguous run of tiles,
@@ -251,16 +260,24 @@ __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void product_kern
         c0 = (int)((int64_t)all * split / args.splits);
         c1 = (int)((int64_t)all * (split + 1) / args.splits);
     }
-    auto load = [&](int c) {
+    // Chunks past the last one load zeros or what is not used: no branch in the loop
+    using SX = decltype(sx);
+    using SW = decltype(sw);
+    auto load = [&](int c, auto part) {
+        constexpr int P = decltype(part)::value;
         const int seg = !PAIRED && c >= chunks;
-        const int k0 = (c - (seg ? chunks : 0)) * BK;
-        sx.load(k0, seg);
-        sw.load(k0, seg);
+        const int k0 = G > 1 && c >= c1 ? K : (c - (seg ? chunks : 0)) * BK;
+        sx.template load<part_of(SX::UNITS, P), part_of(SX::UNITS, P + 1)>(k0, seg);
+        sw.template load<part_of(SW::UNITS, P), part_of(SW::UNITS, P + 1)>(k0, seg);
     };
-    auto store = [&](int buf) {
-        sx.store(lds + buf * BUF);
-        sw.store(lds + buf * BUF + XBYTES);
+    auto store = [&](int buf, auto part) {
+        constexpr int P = decltype(part)::value;
+        sx.template store<part_of(SX::UNITS, P), part_of(SX::UNITS, P + 1)>(lds + buf * BUF);
+        sw.template store<part_of(SW::UNITS, P), part_of(SW::UNITS, P + 1)>(lds + buf * BUF + XBYTES);
     };
+    using P0 = std::integral_constant<int, 0>;
+    using P1 = std::integral_constant<int, 1>;
+    using P2 = std::integral_constant<int, 2>;
 
     f32x16 acc[NB][MB];
 #pragma unroll
@@ -270,31 +287,89 @@ __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void product_kern
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[n][m][r] = 0.f;
 
-    if (c0 < c1) {
-        load(c0);
-        store(0);
-        if (c0 + 1 < c1) load(c0 + 1);
-        __syncthreads();
-#pragma unroll 1
-        for (int c = c0; c < c1; ++c) {
-            const char* const x = lds + ((c - c0) & 1) * BUF;
-            const char* const w = x + XBYTES;
+    // A chunk has four steps of 16 k.  The operands of a step are read from LDS while the one before it is multiplied; the next
+    // chunk's units go to the other buffer in the first three steps, each followed by the load of the unit of the chunk after that, and
+    // the barrier comes before the fourth, in which the first operands of the next chunk are read.
+    u32x4 xv[2][MB], wv[2][NB];
+    auto operands = [&](int set, int buf, int s) {
+        const char* const x = lds + buf * BUF;
 #pragma unroll
-            for (int s = 0; s < BK / 16; ++s) {
-                u32x4 xv[MB], wv[NB];
+        for (int n = 0; n < NB; ++n) wv[set][n] = operand<WK, BN>(x + XBYTES, (wn * NB + n) * 32, s, lane);
 #pragma unroll
-                for (int n = 0; n < NB; ++n) wv[n] = operand<WK, BN>(w, (wn * NB + n) * 32, s, lane);
+        for (int m = 0; m < MB; ++m) xv[set][m] = operand<XK, BM>(x, (wm * MB + m) * 32, s, lane);
+    };
+    auto multiply = [&](int set) {
 #pragma unroll
-                for (int m = 0; m < MB; ++m) xv[m] = operand<XK, BM>(x, (wm * MB + m) * 32, s, lane);
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
+            for (int m = 0; m < MB; ++m) acc[n][m] = mfma(wv[set][n], xv[set][m], acc[n][m], T{});
+    };
+    // what goes between the matrix instructions of a step: `reads` operands, then `units` stores and loads
+    constexpr int kReads = (XK == K_ROWS ? MB : 2 * MB) + (WK == K_ROWS ? NB : 2 * NB);
+    auto interleave = [&](auto units_c) {
+        constexpr int units = decltype(units_c)::value, all_ops = kReads + 2 * units, N_ = MB * NB;
+        int done = 0;
 #pragma unroll
-                    for (int m = 0; m < MB; ++m) acc[n][m] = mfma(wv[n], xv[m], acc[n][m], T{});
+        for (int i = 0; i < N_; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+#pragma unroll
+            for (; done < (i + 1) * all_ops / N_; ++done) {
+                if (done < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                else if ((done - kReads) % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+                else __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
             }
-            if (c + 1 < c1) store((c + 1 - c0) & 1);
-            if (c + 2 < c1) load(c + 2);
-            __syncthreads();
         }
+    };
+    if (c0 < c1) {
+        const int first = c0 + group, rounds = (c1 - c0 + G - 1) / G;
+        load(first, P0{});
+        load(first, P1{});
+        load(first, P2{});
+        store(0, P0{});
+        store(0, P1{});
+        store(0, P2{});
+        load(first + G, P0{});
+        load(first + G, P1{});
+        load(first + G, P2{});
+        __syncthreads();
+        operands(0, 0, 0);
+#pragma unroll 1
+        for (int r = 0; r < rounds; ++r) {
+            const int buf = r & 1, c = first + r * G;
+            auto step = [&](auto part) {
+                constexpr int S = decltype(part)::value;
+                operands((S + 1) & 1, buf, S + 1);
+                multiply(S & 1);
+                store(buf ^ 1, part);
+                load(c + 2 * G, part);
+                interleave(std::integral_constant<int, part_of(SX::UNITS, S + 1) - part_of(SX::UNITS, S) + part_of(SW::UNITS, S + 1) - part_of(SW::UNITS, S)>{});
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            step(P0{});
+            step(P1{});
+            step(P2{});
+            __syncthreads();
+            operands(0, buf ^ 1, 0);
+            multiply(1);
+            interleave(std::integral_constant<int, 0>{});
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __syncthreads();
+    if constexpr (G > 1) {
+        static_assert(G == 2 && (size_t)BM * BN * 4 <= 2 * G * (size_t)BUF, "the sums of one group fit the chunks' room");
+        f32x16* const other = reinterpret_cast<f32x16*>(shared) + (wave * NB * MB) * 64 + lane;
+        if (group == 1) {
+#pragma unroll
+            for (int i = 0; i < NB * MB; ++i) other[i * 64] = acc[i / MB][i % MB];
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int i = 0; i < NB * MB; ++i) acc[i / MB][i % MB] += other[i * 64];
+        }
+        __syncthreads();
+        if (group == 1) return;
     }
 
     // The sums leave through LDS, 32 rows of a wave at a time, so that eight lanes read and write 128 bytes of a row
@@ -352,16 +427,16 @@ __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void product_kern
             store8(d + (int64_t)row * N + col, v, N - col, N % 8 == 0);
         });
     } else if constexpr (EPI == GATED) {
-        static_assert(NB == 2, "a block of gate and one of up");
+        static_assert(NB % 2 == 0, "blocks of gate and of up");
         T* const d = static_cast<T*>(p.d);
         T *const gate = static_cast<T*>(args.gate), *const up = static_cast<T*>(args.up);
         const bool aligned = whole(d, p.ldd), aligned_pre = whole(gate, args.ld_pre) && whole(up, args.ld_pre);
-        const int col = n0 + wn * 32 + part * 8;
+        const int col = n0 + wn * NB * 16 + part * 8, in_lds = (part >> 2) * 256 + (part & 3) * 32;
         device_activation(args.act, [&](auto act) {
             emit([&](int row, const char* at) {
                 float g[8], u[8], h[8];
-                eight(at + part * 32, g);
-                eight(at + 128 + part * 32, u);
+                eight(at + in_lds, g);
+                eight(at + in_lds + 128, u);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) h[e] = activation<decltype(act)::value, true>(g[e]) * u[e];
                 if (gate) {

@@ -14,39 +14,52 @@ enum Form {
     FORM_WEIGHT_GRADS    // both operands columns of k
 };
 
-hipError_t launch_products_f16(Form form, int tile, bool aligned, const Args& a, hipStream_t stream);
-hipError_t launch_products_bf16(Form form, int tile, bool aligned, const Args& a, hipStream_t stream);
+// A work-group's tile, and whether two groups of waves share its k.
+enum Shape { SHAPE_256, SHAPE_128, SHAPE_128_TWICE };
+constexpr int edge_of(Shape s) { return s == SHAPE_256 ? 256 : 128; }
 
-template <typename T, int BM, int BN, int WM, int WN, Kind XK, Kind WK, Epilogue EPI, bool ALIGNED>
+hipError_t launch_products_f16(Form form, Shape shape, bool aligned, const Args& a, hipStream_t stream);
+hipError_t launch_products_bf16(Form form, Shape shape, bool aligned, const Args& a, hipStream_t stream);
+
+template <typename T, int BM, int BN, int WM, int WN, int G, Kind XK, Kind WK, Epilogue EPI, bool ALIGNED>
 hipError_t launch_one(const Args& a, hipStream_t stream)
 {
     static LdsLimit limit;
-    auto* const kernel = product_kernel<T, BM, BN, WM, WN, XK, WK, EPI, ALIGNED>;
-    constexpr size_t lds = lds_bytes<BM, BN, XK, WK>();
+    auto* const kernel = product_kernel<T, BM, BN, WM, WN, G, XK, WK, EPI, ALIGNED>;
+    constexpr size_t lds = G * lds_bytes<BM, BN, XK, WK>();
     const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit);
     if (e != hipSuccess) return e;
-    return launch_kernel(kernel, dim3((unsigned)(a.first_tile[a.problems] * a.splits)), dim3(64 * WM * WN), lds, stream, a);
+    return launch_kernel(kernel, dim3((unsigned)(a.first_tile[a.problems] * a.splits)), dim3(64 * WM * WN * G), lds, stream, a);
 }
 
-template <typename T, Kind XK, Kind WK, Epilogue EPI>
-hipError_t launch_tile(int tile, bool aligned, const Args& a, hipStream_t stream)
+// 256 x 256: with both operands rows of k four waves of 128 x 128 (gate and up of 8192 x 4096 -> 11264 in 1.17 ms, eight waves of 128 x 64,
+// which read half as much again from LDS, 1.46), else eight (operands turned in LDS: level, and the backward epilogue has no registers
+// beside 128 x 128 sums).
+template <typename T, Kind XK, Kind WK, Epilogue EPI, bool ALIGNED>
+hipError_t launch_shape(Shape shape, const Args& a, hipStream_t stream)
 {
-    if (tile == 256)
-        return aligned ? launch_one<T, 256, 256, 2, 4, XK, WK, EPI, true>(a, stream) : launch_one<T, 256, 256, 2, 4, XK, WK, EPI, false>(a, stream);
-    return aligned ? launch_one<T, 128, 128, 2, 2, XK, WK, EPI, true>(a, stream) : launch_one<T, 128, 128, 2, 2, XK, WK, EPI, false>(a, stream);
+    constexpr int WIDE = XK == K_ROWS && WK == K_ROWS ? 2 : 4;
+    if (shape == SHAPE_256) return launch_one<T, 256, 256, 2, WIDE, 1, XK, WK, EPI, ALIGNED>(a, stream);
+    if (shape == SHAPE_128_TWICE) return launch_one<T, 128, 128, 2, 2, 2, XK, WK, EPI, ALIGNED>(a, stream);
+    return launch_one<T, 128, 128, 2, 2, 1, XK, WK, EPI, ALIGNED>(a, stream);
+}
+template <typename T, Kind XK, Kind WK, Epilogue EPI>
+hipError_t launch_tile(Shape shape, bool aligned, const Args& a, hipStream_t stream)
+{
+    return aligned ? launch_shape<T, XK, WK, EPI, true>(shape, a, stream) : launch_shape<T, XK, WK, EPI, false>(shape, a, stream);
 }
 
 template <typename T>
-hipError_t launch_products(Form form, int tile, bool aligned, const Args& a, hipStream_t stream)
+hipError_t launch_products(Form form, Shape shape, bool aligned, const Args& a, hipStream_t stream)
 {
     switch (form) {
-        case FORM_GATED: return launch_tile<T, K_ROWS, K_ROWS, GATED>(tile, aligned, a, stream);
-        case FORM_HIDDEN_GRADS: return launch_tile<T, K_ROWS, K_COLUMNS, GATED_BACKWARD>(tile, aligned, a, stream);
-        case FORM_INPUT_GRAD: return a.splits > 1 ? launch_tile<T, K_ROWS, K_COLUMNS, PARTIAL>(tile, aligned, a, stream)
-                                                  : launch_tile<T, K_ROWS, K_COLUMNS, STORE>(tile, aligned, a, stream);
-        case FORM_WEIGHT_GRADS: return launch_tile<T, K_COLUMNS, K_COLUMNS, STORE>(tile, aligned, a, stream);
-        default: return a.splits > 1 ? launch_tile<T, K_ROWS, K_ROWS, PARTIAL>(tile, aligned, a, stream)
-                                     : launch_tile<T, K_ROWS, K_ROWS, STORE>(tile, aligned, a, stream);
+        case FORM_GATED: return launch_tile<T, K_ROWS, K_ROWS, GATED>(shape, aligned, a, stream);
+        case FORM_HIDDEN_GRADS: return launch_tile<T, K_ROWS, K_COLUMNS, GATED_BACKWARD>(shape, aligned, a, stream);
+        case FORM_INPUT_GRAD: return a.splits > 1 ? launch_tile<T, K_ROWS, K_COLUMNS, PARTIAL>(shape, aligned, a, stream)
+                                                  : launch_tile<T, K_ROWS, K_COLUMNS, STORE>(shape, aligned, a, stream);
+        case FORM_WEIGHT_GRADS: return launch_tile<T, K_COLUMNS, K_COLUMNS, STORE>(shape, aligned, a, stream);
+        default: return a.splits > 1 ? launch_tile<T, K_ROWS, K_ROWS, PARTIAL>(shape, aligned, a, stream)
+                                     : launch_tile<T, K_ROWS, K_ROWS, STORE>(shape, aligned, a, stream);
     }
 }
 
