@@ -68,6 +68,17 @@ struct GemmArgs {
     float eps;
 };
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t stream);
+
+// C = act(A.B^T) * (A.B2^T), element by element (B and B2 both N x K, row stride ldb; no batch), by the bf16-split GEMM: K and extents as
+// there. gate, up: where the two products go as well (row stride ld_pre), or null.
+struct GatedGemmArgs : GemmArgs {
+    const float* B2;
+    float *gate, *up;
+    int64_t ld_pre;
+    int act;             // anr_act
+};
+bool gemm_split_gated_takes(const GatedGemmArgs& a);
+hipError_t launch_gemm_split_gated(const GatedGemmArgs& a, hipStream_t stream);
 // The bf16-split GEMM alone (A.B with K >= 32, N >= 2, extents below 2^29 floats), and the edge of its tile and the
 // groups of waves in a work-group.
 hipError_t launch_gemm_split(const GemmArgs& a, hipStream_t stream);

@@ -154,6 +154,19 @@ inline auto with_activation(int act, F f)
     }
 }
 
+// f(std::integral_constant<int, ACT>) on the device.
+template <typename F>
+__device__ __forceinline__ void device_activation(int act, F f)
+{
+    switch (act) {
+        case ANR_ACT_RELU: f(std::integral_constant<int, ANR_ACT_RELU>{}); break;
+        case ANR_ACT_SILU: f(std::integral_constant<int, ANR_ACT_SILU>{}); break;
+        case ANR_ACT_GELU: f(std::integral_constant<int, ANR_ACT_GELU>{}); break;
+        case ANR_ACT_GELU_TANH: f(std::integral_constant<int, ANR_ACT_GELU_TANH>{}); break;
+        default: f(std::integral_constant<int, ANR_ACT_NONE>{}); break;
+    }
+}
+
 // f(T{}) for the element type of a descriptor.
 template <typename F>
 inline auto with_type(int dtype, F f)

@@ -131,7 +131,7 @@ __global__ __launch_bounds__(1024) void rows_kernel(const Args a)
                 static_cast<T*>(a.gate)[token * a.ld_pre + n] = from_float<T>(v[0]);
                 static_cast<T*>(a.up)[token * a.ld_pre + n] = from_float<T>(v[MATS - 1]);
             }
-            mm16::device_activation(a.act, [&](auto act) { out = activation<decltype(act)::value, sizeof(T) == 2>(v[0]) * v[MATS - 1]; });
+            device_activation(a.act, [&](auto act) { out = activation<decltype(act)::value, sizeof(T) == 2>(v[0]) * v[MATS - 1]; });
         }
         static_cast<T*>(a.d)[token * a.ldd + n] = from_float<T>(out);
     }

@@ -3,12 +3,14 @@
 //   few tokens     ff_rows_kernel.h: two launches, each reads its weights once
 //   16-bit types   mm16_kernel.h: gate, up, activation and product in one launch, then the down projection; backward
 //                  three (dh with dg, du and h where they are formed; dx; the weights' gradients together)
-//   float32        the library's GEMM (gemm.hip) and the kernels here
+//   float32        the library's GEMM (gemm.hip): gate, up, activation and product in one launch of its form for two matrices, the other
+//                  products with the kernels here around them
 #include <algorithm>
 
 #include "blocks_internal.h"
 #include "element_types.h"
 #include "ff_rows_kernel.h"
+#include "gemm_split_plan.h"
 #include "mm16_launch.h"
 
 namespace anr {
@@ -65,29 +67,38 @@ __global__ __launch_bounds__(kThreads) void hidden_gradients_kernel(const float*
     }
 }
 
-// out [C,R] = in [R,C] turned.
-__global__ __launch_bounds__(kThreads) void turn_kernel(const float* in, int64_t ld, float* out, int64_t R, int64_t C)
+// What a matrix [R,C] is laid out as: packed, or turned, [C,R].
+struct Layout {
+    const float* in;
+    int64_t ld, R, C;
+    float* out;
+    bool turned;
+};
+struct Layouts {
+    Layout l[3];
+};
+__global__ __launch_bounds__(kThreads) void lay_out_kernel(const Layouts all)
 {
     __shared__ float tile[32][33];
+    const Layout& l = all.l[blockIdx.z];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c0 = (int64_t)blockIdx.x * 32;
-    for (int64_t r0 = (int64_t)blockIdx.y * 32; r0 < R; r0 += (int64_t)gridDim.y * 32) {
+    if (c0 >= l.C) return;
+    for (int64_t r0 = (int64_t)blockIdx.y * 32; r0 < l.R; r0 += (int64_t)gridDim.y * 32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (r0 + y + 8 * i < R && c0 + x < C) tile[y + 8 * i][x] = in[(r0 + y + 8 * i) * ld + c0 + x];
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = r0 + y + 8 * i, c = c0 + x;
+            if (r >= l.R || c >= l.C) continue;
+            if (l.turned) tile[y + 8 * i][x] = l.in[r * l.ld + c];
+            else l.out[r * l.C + c] = l.in[r * l.ld + c];
+        }
+        if (!l.turned) continue;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (c0 + y + 8 * i < C && r0 + x < R) out[(c0 + y + 8 * i) * R + r0 + x] = tile[x][y + 8 * i];
+            if (c0 + y + 8 * i < l.C && r0 + x < l.R) l.out[(c0 + y + 8 * i) * l.R + r0 + x] = tile[x][y + 8 * i];
         __syncthreads();
     }
-}
-
-// out [R,C] packed = in [R,C].
-__global__ __launch_bounds__(kThreads) void pack_kernel(const float* in, int64_t ld, float* out, int64_t R, int64_t C)
-{
-    for (int64_t r = blockIdx.y; r < R; r += gridDim.y)
-        for (int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x; c < C; c += (int64_t)gridDim.x * kThreads) out[r * C + c] = in[r * ld + c];
 }
 
 // D [M,N] in T = the sum of the `splits` packed matrices at `parts`.
@@ -114,8 +125,9 @@ dim3 grid_of(int64_t columns, int64_t per, int64_t rows, int64_t rows_per)
     return dim3((unsigned)((columns + per - 1) / per), (unsigned)std::max<int64_t>(1, std::min<int64_t>((rows + rows_per - 1) / rows_per, 65535)));
 }
 
-// C [M,N] = A [M,K] B, B as [N,K] (nk) or [K,N].
-hipError_t gemm(const float* A, int64_t lda, const float* B, int64_t ldb, bool nk, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, hipStream_t stream)
+// C [M,N] = A [M,K] B, B as [N,K] (nk) or [K,N]; `batch` of them with these steps.
+hipError_t gemm(const float* A, int64_t lda, const float* B, int64_t ldb, bool nk, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, hipStream_t stream, int batch = 1,
+                int64_t step_a = 0, int64_t step_b = 0, int64_t step_c = 0)
 {
     GemmArgs g{};
     g.A = A;
@@ -127,9 +139,47 @@ hipError_t gemm(const float* A, int64_t lda, const float* B, int64_t ldb, bool n
     g.lda = lda;
     g.ldb = ldb;
     g.ldc = ldc;
-    g.batch = g.batch_inner = 1;
+    g.batch = batch;
+    g.batch_inner = 1;
+    g.sAo = step_a;
+    g.sBo = step_b;
+    g.sCo = step_c;
     g.b_is_nk = nk;
     return launch_gemm(g, stream);
+}
+
+// Parts of equal length that k is cut into, each a product of a batch, for products with few tiles: where the split GEMM's estimate for the batch
+// and the launch that joins its results (3 us and 5 TB/s) is 0.9 of that for the whole or less. A function of the extents alone.
+int parts_of_k(int64_t M, int64_t N, int64_t K)
+{
+    auto estimate = [&](int64_t parts) {
+        return gsplit::estimate_us(gsplit::kVariants[gsplit::choose_variant(M, N, K / parts, parts)], M, N, K / parts, parts) +
+               (parts > 1 ? 3.0 + (double)(parts + 1) * (double)M * (double)N * 4.0 / 5e6 : 0.0);
+    };
+    int best = 1;
+    double least = 0.9 * estimate(1);
+    for (const int parts : {2, 3, 4, 6, 8})
+        if (K % parts == 0 && K / parts >= 256 && estimate(parts) < least) {
+            best = parts;
+            least = estimate(parts);
+        }
+    return best;
+}
+size_t parts_bytes(int64_t M, int64_t N, int64_t K)
+{
+    const int n = parts_of_k(M, N, K);
+    return n > 1 ? (size_t)n * M * N * 4 : 0;
+}
+
+// gemm() of which k may be cut, through `parts` (parts_bytes()).
+hipError_t gemm_in_parts(const float* A, int64_t lda, const float* B, int64_t ldb, bool nk, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, float* parts, hipStream_t stream)
+{
+    const int n = parts_of_k(M, N, K);
+    if (n == 1) return gemm(A, lda, B, ldb, nk, C, ldc, M, N, K, stream);
+    const int64_t k = K / n;
+    const hipError_t e = gemm(A, lda, B, ldb, nk, parts, N, M, N, k, stream, n, k, nk ? k : k * ldb, M * N);
+    if (e != hipSuccess) return e;
+    return launch_kernel(join_kernel<float>, grid_of(N, kThreads, M, 1), dim3(kThreads), 0, stream, static_cast<const float*>(parts), n, C, ldc, M, N);
 }
 
 // ---- few tokens
@@ -344,24 +394,42 @@ hipError_t backward_16(const GatedFfArgs& g, hipStream_t stream)
 hipError_t forward_32(const GatedFfArgs& g, hipStream_t stream)
 {
     const anr_gated_ff_desc& d = g.d;
+    const size_t tf = whole_lines((size_t)d.T * d.F * 4) / 4;
     float* const h = static_cast<float*>(g.ws);
-    float* gate = static_cast<float*>(g.gate);
-    float* up = static_cast<float*>(g.up);
-    int64_t ld = d.ldpre;
-    if (!gate) {
-        gate = h + whole_lines((size_t)d.T * d.F * 4) / 4;
-        up = gate + whole_lines((size_t)d.T * d.F * 4) / 4;
-        ld = d.F;
+    GatedGemmArgs a{};
+    a.A = static_cast<const float*>(g.x);
+    a.B = static_cast<const float*>(g.w_gate);
+    a.B2 = static_cast<const float*>(g.w_up);
+    a.C = h;
+    a.M = (int)d.T;
+    a.N = (int)d.F;
+    a.K = (int)d.C;
+    a.lda = d.ldx;
+    a.ldb = d.ldw;
+    a.ldc = d.F;
+    a.batch = a.batch_inner = 1;
+    a.b_is_nk = true;
+    a.gate = static_cast<float*>(g.gate);
+    a.up = static_cast<float*>(g.up);
+    a.ld_pre = d.ldpre;
+    a.act = d.act;
+    hipError_t e = hipSuccess;
+    if (gemm_split_gated_takes(a)) {
+        e = launch_gemm_split_gated(a, stream);
+    } else {
+        float* const gate = g.gate ? a.gate : h + tf;
+        float* const up = g.gate ? a.up : h + 2 * tf;
+        const int64_t ld = g.gate ? d.ldpre : d.F;
+        e = gemm(a.A, d.ldx, a.B, d.ldw, true, gate, ld, d.T, d.F, d.C, stream);
+        if (e == hipSuccess) e = gemm(a.A, d.ldx, a.B2, d.ldw, true, up, ld, d.T, d.F, d.C, stream);
+        if (e == hipSuccess)
+            e = with_activation(d.act, [&](auto act) {
+                return launch_kernel(product_of_gate_kernel<decltype(act)::value>, grid_of(d.F, kThreads, d.T, 1), dim3(kThreads), 0, stream, static_cast<const float*>(gate),
+                                     static_cast<const float*>(up), ld, h, d.T, d.F);
+            });
     }
-    const float* const x = static_cast<const float*>(g.x);
-    hipError_t e = gemm(x, d.ldx, static_cast<const float*>(g.w_gate), d.ldw, true, gate, ld, d.T, d.F, d.C, stream);
-    if (e == hipSuccess) e = gemm(x, d.ldx, static_cast<const float*>(g.w_up), d.ldw, true, up, ld, d.T, d.F, d.C, stream);
-    if (e == hipSuccess)
-        e = with_activation(d.act, [&](auto act) {
-            return launch_kernel(product_of_gate_kernel<decltype(act)::value>, grid_of(d.F, kThreads, d.T, 1), dim3(kThreads), 0, stream, gate, up, ld, h, d.T, d.F);
-        });
     if (e != hipSuccess) return e;
-    return gemm(h, d.F, static_cast<const float*>(g.w_down), d.ld_down, true, static_cast<float*>(g.y), d.ldy, d.T, d.C, d.F, stream);
+    return gemm_in_parts(h, d.F, static_cast<const float*>(g.w_down), d.ld_down, true, static_cast<float*>(g.y), d.ldy, d.T, d.C, d.F, h + 3 * tf, stream);
 }
 
 hipError_t backward_32(const GatedFfArgs& g, hipStream_t stream)
@@ -375,24 +443,37 @@ hipError_t backward_32(const GatedFfArgs& g, hipStream_t stream)
     float* const turned = dgu + 2 * tf;                 // [2F, T]
     float* const weights = turned + 2 * tf;             // [2F, C], gate's and up's
     float* const dy_turned = weights + whole_lines((size_t)F * C * 8) / 4;
+    float* const parts = dy_turned + whole_lines((size_t)T * C * 4) / 4;
     const float *const dy = static_cast<const float*>(g.dy), *const x = static_cast<const float*>(g.x);
+    const float *const wg = static_cast<const float*>(g.w_gate), *const wu = static_cast<const float*>(g.w_up);
+    const bool one_tensor = wu == wg + F * d.ldw;       // (gate's and up's weights are rows of one matrix)
     hipError_t e = gemm(dy, d.ldy, static_cast<const float*>(g.w_down), d.ld_down, false, dh, F, T, F, C, stream);
     if (e == hipSuccess)
         e = with_activation(d.act, [&](auto act) {
             return launch_kernel(hidden_gradients_kernel<decltype(act)::value>, grid_of(F, 32, T, 32), dim3(kThreads), 0, stream, static_cast<const float*>(dh),
                                  static_cast<const float*>(g.gate), static_cast<const float*>(g.up), d.ldpre, dgu, turned, h, T, F);
         });
-    if (e == hipSuccess && g.dx) {
-        e = launch_kernel(pack_kernel, grid_of(C, kThreads, F, 1), dim3(kThreads), 0, stream, static_cast<const float*>(g.w_gate), d.ldw, weights, F, C);
-        if (e == hipSuccess) e = launch_kernel(pack_kernel, grid_of(C, kThreads, F, 1), dim3(kThreads), 0, stream, static_cast<const float*>(g.w_up), d.ldw, weights + F * C, F, C);
-        if (e == hipSuccess) e = gemm(dgu, 2 * F, weights, C, false, static_cast<float*>(g.dx), d.lddx, T, C, 2 * F, stream);
+    Layouts l{};
+    unsigned n = 0;
+    if (g.dx && !one_tensor) {
+        l.l[n++] = {wg, d.ldw, F, C, weights, false};
+        l.l[n++] = {wu, d.ldw, F, C, weights + F * C, false};
     }
-    if (e == hipSuccess && g.dw_gate) e = gemm(turned, T, x, d.ldx, false, static_cast<float*>(g.dw_gate), d.lddw, F, C, T, stream);
-    if (e == hipSuccess && g.dw_up) e = gemm(turned + F * T, T, x, d.ldx, false, static_cast<float*>(g.dw_up), d.lddw, F, C, T, stream);
-    if (e == hipSuccess && g.dw_down) {
-        e = launch_kernel(turn_kernel, grid_of(C, 32, T, 32), dim3(kThreads), 0, stream, dy, d.ldy, dy_turned, T, C);
-        if (e == hipSuccess) e = gemm(dy_turned, T, h, F, false, static_cast<float*>(g.dw_down), d.ld_ddown, C, F, T, stream);
+    if (g.dw_down) l.l[n++] = {dy, d.ldy, T, C, dy_turned, true};
+    if (e == hipSuccess && n > 0) {
+        dim3 grid = grid_of(C, 32, std::max(T, F), 32);
+        grid.z = n;
+        e = launch_kernel(lay_out_kernel, grid, dim3(kThreads), 0, stream, l);
     }
+    if (e == hipSuccess && g.dx)
+        e = gemm_in_parts(dgu, 2 * F, one_tensor ? wg : weights, one_tensor ? d.ldw : C, false, static_cast<float*>(g.dx), d.lddx, T, C, 2 * F, parts, stream);
+    float *const dwg = static_cast<float*>(g.dw_gate), *const dwu = static_cast<float*>(g.dw_up);
+    if (e == hipSuccess && dwg && dwu) {                // two products of one launch
+        e = gemm(turned, T, x, d.ldx, false, dwg, d.lddw, F, C, T, stream, 2, F * T, 0, dwu - dwg);
+    } else if (e == hipSuccess && (dwg || dwu)) {
+        e = gemm(dwg ? turned : turned + F * T, T, x, d.ldx, false, dwg ? dwg : dwu, d.lddw, F, C, T, stream);
+    }
+    if (e == hipSuccess && g.dw_down) e = gemm(dy_turned, T, h, F, false, static_cast<float*>(g.dw_down), d.ld_ddown, C, F, T, stream);
     return e;
 }
 
@@ -405,8 +486,8 @@ size_t gated_ff_workspace_bytes(const GatedFfArgs& g, bool backward)
     if (T == 0) return 0;
     if (d.dtype == ANR_F32) {
         const size_t tf = whole_lines(T * F * 4);
-        if (backward) return 6 * tf + whole_lines(F * C * 8) + whole_lines(T * C * 4);
-        return T <= kFewTokens ? tf : 3 * tf;
+        if (backward) return 6 * tf + whole_lines(F * C * 8) + whole_lines(T * C * 4) + parts_bytes(d.T, d.C, 2 * d.F);
+        return T <= kFewTokens ? tf : 3 * tf + parts_bytes(d.T, d.C, d.F);
     }
     const size_t tf = whole_lines(T * F * 2);
     const int splits = splits_of(d.T, d.C, (backward ? 2 : 1) * chunks_of(d.F));

@@ -439,6 +439,18 @@ hipError_t launch_split_any(const GemmArgs& a, hipStream_t stream)
     }
 }
 
+template <int BM, int WM, int WN, int NWG, bool SPEC>
+hipError_t launch_split_gated(const GatedGemmArgs& a, hipStream_t stream)
+{
+    const gsplit::Grid g{(a.M + BM - 1) / BM, (a.N + BM / 2 - 1) / (BM / 2), 8};
+    constexpr size_t lds_bytes = gsplit::lds_bytes<BM, BM, NWG, SPEC>();
+    auto kern = gsplit::gemm_split_gated_kernel<BM, BM, WM, WN, NWG, SPEC, 2>;
+    static LdsLimit granted;
+    const hipError_t e = lds_bytes > 48 * 1024 ? raise_lds_limit(reinterpret_cast<const void*>(kern), lds_bytes, granted) : hipSuccess;
+    if (e != hipSuccess) return e;
+    return launch_kernel(kern, dim3((unsigned)((int64_t)g.tiles_m * g.tiles_n)), dim3(64 * WM * WN * (SPEC ? 2 : NWG)), lds_bytes, stream, a, g);
+}
+
 hipError_t launch_pipe(const GemmArgs& a, hipStream_t stream)
 {
     static_assert(gpipe::KC == 32, "gemm_pipe_takes counts its chunks");
@@ -556,6 +568,24 @@ hipError_t launch_gemm(const GemmArgs& args, hipStream_t stream)
 
     if (a.softmax_rows) err = launch_softmax_rows(a, stream);
     return err;
+}
+
+// 32-bit byte offsets inside one matrix, and work-items below 2^32.
+bool gemm_split_gated_takes(const GatedGemmArgs& a)
+{
+    const int64_t lim = (int64_t)1 << 29;
+    return (int64_t)(a.M - 1) * a.lda + a.K < lim && (int64_t)(a.N - 1) * a.ldb + a.K < lim && ((int64_t)a.M + 63) / 64 * ((a.N + 31) / 32) < ((int64_t)1 << 22);
+}
+
+hipError_t launch_gemm_split_gated(const GatedGemmArgs& a, hipStream_t stream)
+{
+    switch (gsplit::choose_variant(a.M, 2 * (int64_t)a.N, a.K, 1)) {
+        case 0: return launch_split_gated<128, 2, 2, 1, false>(a, stream);
+        case 1: return launch_split_gated<128, 2, 2, 1, true>(a, stream);
+        case 2: return launch_split_gated<64, 2, 1, 1, false>(a, stream);
+        case 3: return launch_split_gated<64, 2, 1, 2, false>(a, stream);
+        default: return launch_split_gated<64, 2, 1, 4, false>(a, stream);
+    }
 }
 
 hipError_t launch_gemm_split(const GemmArgs& a, hipStream_t stream)

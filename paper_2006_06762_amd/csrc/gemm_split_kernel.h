@@ -36,6 +36,7 @@
 #include <type_traits>
 
 #include "anr_kernels.h"
+#include "element_types.h"
 #include "gemm_split_plan.h"
 #include "split_bf16.h"
 
@@ -63,9 +64,14 @@ struct Grid {
 
 // One tile of a work-group: as bf16 pieces, or PLAIN, with the fp32 instruction.  False if it met a value that the
 // pieces cannot carry: then nothing is stored.
-template <int BM, int BN, int WM, int WN, int NWG, bool SPEC, bool NT, bool FUSED, bool PLAIN>
-__device__ __forceinline__ bool compute_tile(const GemmArgs& p, const Grid& g, const int thread)
+// GatedGemmArgs in place of GemmArgs: B's tile is half rows of B and half as many of B2, which the lanes have side by side, and what is
+// stored is act of the one times the other.
+template <int BM, int BN, int WM, int WN, int NWG, bool SPEC, bool NT, bool FUSED, bool PLAIN, typename ARGS>
+__device__ __forceinline__ bool compute_tile(const ARGS& p, const Grid& g, const int thread)
 {
+    constexpr bool GATED = std::is_same<ARGS, GatedGemmArgs>::value;
+    static_assert(!GATED || NT, "rows of k");
+    constexpr int TILE_N = GATED ? BN / 2 : BN;      // columns of C
     constexpr int T = 64 * WM * WN;                  // threads of a wave group
     constexpr int MB = BM / (32 * WM);
     static_assert(BN == 64 * WN && BM == BN && T == 2 * BM,
@@ -103,7 +109,7 @@ __device__ __forceinline__ bool compute_tile(const GemmArgs& p, const Grid& g, c
     const int band_rows = min(g.group_m, g.tiles_m - band * g.group_m);
     const int in_band = id - band * g.group_m * g.tiles_n;
     const int tile_m = band * g.group_m + in_band % band_rows, tile_n = in_band / band_rows;
-    const int m0 = tile_m * BM, n0 = tile_n * BN;
+    const int m0 = tile_m * BM, n0 = tile_n * TILE_N;
 
     const int zo = mat / p.batch_inner, zi = mat - zo * p.batch_inner;
     const float* A = p.A + zo * p.sAo + zi * p.sAi;
@@ -115,6 +121,12 @@ __device__ __forceinline__ bool compute_tile(const GemmArgs& p, const Grid& g, c
     const uint32_t b_bytes = NT ? 4u * (uint32_t)((int64_t)(N - 1) * p.ldb + K) : 4u * (uint32_t)((int64_t)(K - 1) * p.ldb + N);
     const __amdgpu_buffer_rsrc_t arsrc =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(A), 0, (int)a_bytes, 0x00020000);
+    // GATED: the row of B's tile that a thread stages is one of B or B2 for a wave as a whole
+    const int bhalf = GATED ? __builtin_amdgcn_readfirstlane(tid >> 1) / (BN / 2) : 0;
+    if constexpr (GATED) {
+        static_assert(BN / 2 % 32 == 0, "a wave stages 32 rows");
+        B = bhalf ? p.B2 : B;
+    }
     const __amdgpu_buffer_rsrc_t brsrc =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(B), 0, (int)b_bytes, 0x00020000);
 
@@ -123,7 +135,7 @@ __device__ __forceinline__ bool compute_tile(const GemmArgs& p, const Grid& g, c
     const int at = tid & 1, arow = tid >> 1;
     const int bt = arow / (BN / 2), bpair = arow % (BN / 2);
     const uint32_t aoff = 4u * (uint32_t)((int64_t)unit_row(m0 + arow, M) * p.lda + unit_k(at, 0, 0));
-    const uint32_t boff = NT ? 4u * (uint32_t)((int64_t)unit_row(n0 + arow, N) * p.ldb + unit_k(at, 0, 0))
+    const uint32_t boff = NT ? 4u * (uint32_t)((int64_t)unit_row(n0 + (GATED ? arow - bhalf * (BN / 2) : arow), N) * p.ldb + unit_k(at, 0, 0))
                              : 4u * (uint32_t)((int64_t)piece_k(bt, at) * p.ldb + piece_col(n0 + 2 * bpair, N));
 
     float ra[2][8], rb[2][8];                        // rb: four k of the first column, then of the second (NT: as ra)
@@ -163,7 +175,8 @@ __device__ __forceinline__ bool compute_tile(const GemmArgs& p, const Grid& g, c
     uint32_t lost = 0;
     uint32_t sp[3][8];
     char* const wa = region + at * Plane<BM>::UNIT + arow * 16;
-    char* const wb = region + 3 * PA + (NT ? at * Plane<BN>::UNIT + ((arow & 1) * (BN / 2) + (arow >> 1)) * 16
+    const int brow = GATED ? arow : (arow & 1) * (BN / 2) + (arow >> 1);             // its place among the tile's columns (k-contiguous B)
+    char* const wb = region + 3 * PA + (NT ? at * Plane<BN>::UNIT + brow * 16
                                            : bt * Plane<BN>::UNIT + bpair * 16 + 8 * at);
     // k that an earlier chunk has counted and, of a K below 32, k past the end (in B's rows too: they run on into
     // the next one).  Zeros in A leave the NaN of an infinity in B, which ends the first try; the second one has zeros in
@@ -208,7 +221,7 @@ __device__ __forceinline__ bool compute_tile(const GemmArgs& p, const Grid& g, c
     constexpr int QA = BM * 16 + 64, QB = BN * 16 + 64;
     static_assert(4 * QA <= 3 * PA && 4 * QB <= 3 * PB, "fits the room of the pieces");
     char* const fa = region + at * QA + arow * 16;
-    char* const fb = region + 3 * PA + (NT ? at * QB + ((arow & 1) * (BN / 2) + (arow >> 1)) * 16 : (bt + 2 * at) * QB + bpair * 16);
+    char* const fb = region + 3 * PA + (NT ? at * QB + brow * 16 : (bt + 2 * at) * QB + bpair * 16);
     auto store_half = [&](auto f_c, int c) {         // half f of chunk c
         constexpr int f = decltype(f_c)::value;
         if (c * KC + KC > K) clear_uncounted(f_c, c);
@@ -419,6 +432,27 @@ __device__ __forceinline__ bool compute_tile(const GemmArgs& p, const Grid& g, c
     }
     if (stager || (NWG > 1 && wgrp > 0)) return true;
 
+    if constexpr (GATED) {
+        // gate's sum and up's of one column: 32 lanes write 128 bytes of a row
+        const int col = n0 + wn * 32 + r32;
+        if (col >= N) return true;
+        device_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int row = m0 + (wm * MB + mb) * 32 + 4 * h + 8 * (r / 4) + (r % 4);
+                    if (row >= M) continue;
+                    const float gate = acc[mb][0][r], up = acc[mb][1][r];
+                    if (p.gate) {
+                        __builtin_nontemporal_store(gate, p.gate + (int64_t)row * p.ld_pre + col);
+                        __builtin_nontemporal_store(up, p.up + (int64_t)row * p.ld_pre + col);
+                    }
+                    C[(int64_t)row * p.ldc + col] = activation<decltype(act)::value, false>(gate) * up;
+                }
+        });
+        return true;
+    }
     // accumulator register r of lane (h, r32): row 8*(r/4) + 4*h + r%4 of block mb, columns 2*(wn*32 + r32) + nb:
     // 32 lanes write 256 contiguous bytes of a row, and C is not read again (non-temporal)
     auto store_tile = [&](auto whole_c) {
@@ -463,6 +497,16 @@ __global__ __launch_bounds__(64 * WM * WN * (SPEC ? 2 : NWG), MINW) void gemm_sp
     if (compute_tile<BM, BN, WM, WN, NWG, SPEC, NT, FUSED, false>(p, g, thread)) return;
     asm("" : "+v"(thread));                          // nothing of the second try is held through the first
     compute_tile<BM, BN, WM, WN, NWG, SPEC, NT, FUSED, true>(p, g, thread);
+}
+
+// C = act(A.B^T) * (A.B2^T).
+template <int BM, int BN, int WM, int WN, int NWG, bool SPEC, int MINW>
+__global__ __launch_bounds__(64 * WM * WN * (SPEC ? 2 : NWG), MINW) void gemm_split_gated_kernel(const GatedGemmArgs p, const Grid g)
+{
+    int thread = threadIdx.x;
+    if (compute_tile<BM, BN, WM, WN, NWG, SPEC, true, false, false>(p, g, thread)) return;
+    asm("" : "+v"(thread));
+    compute_tile<BM, BN, WM, WN, NWG, SPEC, true, false, true>(p, g, thread);
 }
 
 }  // namespace gsplit

@@ -205,19 +205,6 @@ __device__ __forceinline__ void load8(const T* p, float (&v)[8], int in, bool al
     }
 }
 
-// f(std::integral_constant<int, ACT>) on the device.
-template <typename F>
-__device__ __forceinline__ void device_activation(int act, F f)
-{
-    switch (act) {
-        case ANR_ACT_RELU: f(std::integral_constant<int, ANR_ACT_RELU>{}); break;
-        case ANR_ACT_SILU: f(std::integral_constant<int, ANR_ACT_SILU>{}); break;
-        case ANR_ACT_GELU: f(std::integral_constant<int, ANR_ACT_GELU>{}); break;
-        case ANR_ACT_GELU_TANH: f(std::integral_constant<int, ANR_ACT_GELU_TANH>{}); break;
-        default: f(std::integral_constant<int, ANR_ACT_NONE>{}); break;
-    }
-}
-
 // G groups of waves take a tile's chunks in turn, each with buffers and sums of its own, and join the sums in LDS: for products with
 // about as many tiles as CUs, whose work-groups are alone on theirs.
 template <typename T, int BM, int BN, int WM, int WN, int G, Kind XK, Kind WK, Epilogue EPI, bool ALIGNED>
