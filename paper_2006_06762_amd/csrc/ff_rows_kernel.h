@@ -3,7 +3,7 @@
 //
 // Bound: reading W once.  A work-group takes 16 rows of W (of both matrices), its waves share the k in chunks of 128 bytes
 // a row and join their sums in LDS; W goes from memory straight into the operands of the matrix instructions, sixteen tokens wide
-// (which cost nothing here), without LDS: nothing of it is used twice.  A lane's part of a chunk are 32 bytes of a row, so
+// (which cost nothing here), without LDS: nothing of it is used twice.  A lane's part of a chunk are two units of a row, so
 // the order of k differs from memory's, in both operands alike.
 #pragma once
 #include "anr_kernels.h"
@@ -27,6 +27,7 @@ struct Args {
     int64_t ldx, ldw[2], ldd, ld_pre;
     int T, N, K;
     int act;
+    bool whole_rows;                // gated: D's rows go on in zeros to the end of their last 16 bytes
 };
 
 // Sixteen bytes of each operand.
@@ -46,6 +47,7 @@ __device__ __forceinline__ f32x4 multiply(u32x4 w, u32x4 x, f32x4 c, float)
     return c;
 }
 
+// ALIGNED: pointers and leading dimensions are whole 16-byte units, and a row of K elements goes on in zeros to the end of its last one.
 // Elements k .. k + 16 / sizeof(T) - 1 of the row at byte `row` of a matrix; those past K are zeros.
 template <typename T, bool ALIGNED>
 __device__ __forceinline__ u32x4 load_unit(__amdgpu_buffer_rsrc_t rsrc, uint32_t row, int k, int K)
@@ -92,7 +94,7 @@ __global__ __launch_bounds__(1024) void rows_kernel(const Args a)
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int k = (c + u * waves) * CHUNK + (2 * g + i) * E;
+                const int k = (c + u * waves) * CHUNK + (4 * i + g) * E;
 #pragma unroll
                 for (int m = 0; m < MATS; ++m) w[u][m][i] = load_unit<T, ALIGNED>(wr[m], wrow[m], k, a.K);
 #pragma unroll
@@ -124,6 +126,8 @@ __global__ __launch_bounds__(1024) void rows_kernel(const Args a)
             v[m] = 0.f;
             for (int w = 0; w < waves; ++w) v[m] += sums[(((w * TB + t) * MATS + m) * 4 + e) * 64 + l];
         }
+        constexpr int UNIT = 16 / sizeof(T);
+        if (GATED && a.whole_rows && token < a.T && n >= a.N && n < (a.N + UNIT - 1) / UNIT * UNIT) static_cast<T*>(a.d)[token * a.ldd + n] = from_float<T>(0.f);
         if (token >= a.T || n >= a.N) continue;
         float out = v[0];
         if (GATED) {

@@ -17,7 +17,10 @@ namespace anr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFewTokens = 64;                  // at most four blocks of sixteen (ff_rows_kernel.h)
+// Calls of few tokens (ff_rows_kernel.h): sixteen, and up to 64 while each work-group's pass over them costs less than the tiles of 128 tokens that
+// are mostly empty. us, T tokens so / in tiles: 1024 -> 2816 bf16, T = 64, 24 / 26, 2048 -> 5632, T = 32, 36 / 37, 64 52 / 37, 4096 -> 11264, T = 17,
+// 67 / 74, 32 87 / 75; float32 T = 64 43 / 51, 101 / 121, 285 / 386.
+bool few_tokens(const anr_gated_ff_desc& d) { return d.T <= 16 || (d.T <= 64 && (d.dtype == ANR_F32 || d.T * d.C * d.F <= (int64_t)600000000)); }
 
 size_t whole_lines(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
@@ -210,43 +213,119 @@ hipError_t launch_rows(const ffrows::Args& a, bool aligned, hipStream_t stream)
     return with(std::integral_constant<int, 4>{});
 }
 
-// 16-byte units: pointer, leading dimension and extent.
-bool whole_units(const void* p, int64_t ld, int64_t extent, int es) { return is_aligned16(p) && ld * es % 16 == 0 && extent * es % 16 == 0; }
+// Operands whose rows are no whole 16-byte units are copied first, to rows that are, with zeros behind their ends: a pass over the weights, which
+// the products read once (one token 1001 -> 2777 in bf16 34 us with loads of single elements, XX so) or far more often.
+struct Copy {
+    const void* in;
+    int64_t ld, R, C;
+    void* out;
+    int64_t ld_out;
+};
+struct Copies {
+    Copy c[5];
+};
+template <typename T>
+__global__ __launch_bounds__(kThreads) void copy_rows_kernel(const Copies all)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    const Copy& c = all.c[blockIdx.z];
+    const T* const in = static_cast<const T*>(c.in);
+    T* const out = static_cast<T*>(c.out);
+    const int64_t units = c.ld_out / E;
+    for (int64_t r = blockIdx.y; r < c.R; r += gridDim.y)
+        for (int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x; u < units; u += (int64_t)gridDim.x * kThreads) {
+            Pack<T, E> v;
+#pragma unroll
+            for (int i = 0; i < E; ++i) v.v[i] = u * E + i < c.C ? in[r * c.ld + u * E + i] : from_float<T>(0.f);
+            *reinterpret_cast<Pack<T, E>*>(out + r * c.ld_out + u * E) = v;
+        }
+}
+
+int64_t whole(int64_t n, int es) { return (n * es + 15) / 16 * 16 / es; }
+// Whether a call copies its operands: by the descriptor alone (pointers that are not aligned take the kernels of single elements).
+bool copies(const anr_gated_ff_desc& d, bool backward)
+{
+    const int es = element_bytes(d.dtype);
+    for (const int64_t n : {d.C, d.F, d.ldx, d.ldw, d.ld_down, backward ? d.ldy : 0})
+        if (n * es % 16 != 0) return true;
+    return false;
+}
+// A call's arguments with the copies in place of the operands; `at`: where they go, at the end the first byte behind them.
+struct Operands {
+    const void *x, *dy, *w_gate, *w_up, *w_down;
+    int64_t ldx, ldy, ldw, ld_down;
+};
+size_t copied_bytes(const anr_gated_ff_desc& d, bool backward)
+{
+    const size_t es = element_bytes(d.dtype), c = whole(d.C, (int)es), f = whole(d.F, (int)es);
+    return whole_lines(d.T * c * es) * (backward ? 2 : 1) + 2 * whole_lines(d.F * c * es) + whole_lines(d.C * f * es);
+}
+hipError_t operands_of(const GatedFfArgs& g, bool backward, char* at, Operands* o, hipStream_t stream)
+{
+    const anr_gated_ff_desc& d = g.d;
+    *o = {g.x, g.dy, g.w_gate, g.w_up, g.w_down, d.ldx, d.ldy, d.ldw, d.ld_down};
+    if (!copies(d, backward)) return hipSuccess;
+    const int es = element_bytes(d.dtype);
+    Copies all{};
+    unsigned n = 0;
+    auto copy = [&](const void*& p, int64_t ld, int64_t R, int64_t C) {
+        all.c[n++] = {p, ld, R, C, at, whole(C, es)};
+        p = at;
+        at += whole_lines((size_t)R * whole(C, es) * es);
+    };
+    copy(o->x, d.ldx, d.T, d.C);
+    if (backward) copy(o->dy, d.ldy, d.T, d.C);
+    copy(o->w_gate, d.ldw, d.F, d.C);
+    copy(o->w_up, d.ldw, d.F, d.C);
+    copy(o->w_down, d.ld_down, d.C, d.F);
+    o->ldx = o->ldw = whole(d.C, es);
+    if (backward) o->ldy = o->ldx;
+    o->ld_down = whole(d.F, es);
+    dim3 grid = grid_of(std::max(o->ldx, o->ld_down) * es / 16, kThreads, std::max({d.T, d.F, d.C}), 1);
+    grid.z = n;
+    return with_type(d.dtype, [&](auto t) { return launch_kernel(copy_rows_kernel<decltype(t)>, grid, dim3(kThreads), 0, stream, all); });
+}
+bool whole_rows(const void* p, int64_t ld, int es) { return is_aligned16(p) && ld * es % 16 == 0; }
 
 hipError_t forward_few(const GatedFfArgs& g, hipStream_t stream)
 {
     const anr_gated_ff_desc& d = g.d;
     const int es = element_bytes(d.dtype);
+    const int64_t F8 = whole(d.F, es);
+    Operands o;
+    const hipError_t copied = operands_of(g, false, static_cast<char*>(g.ws) + whole_lines((size_t)d.T * F8 * es), &o, stream);
+    if (copied != hipSuccess) return copied;
     return with_type(d.dtype, [&](auto t) {
         using T = decltype(t);
         ffrows::Args a{};
-        a.x = g.x;
-        a.w[0] = g.w_gate;
-        a.w[1] = g.w_up;
+        a.x = o.x;
+        a.w[0] = o.w_gate;
+        a.w[1] = o.w_up;
         a.d = g.ws;
         a.gate = g.gate;
         a.up = g.up;
-        a.ldx = d.ldx;
-        a.ldw[0] = a.ldw[1] = d.ldw;
-        a.ldd = d.F;
+        a.ldx = o.ldx;
+        a.ldw[0] = a.ldw[1] = o.ldw;
+        a.ldd = F8;
+        a.whole_rows = true;
         a.ld_pre = d.ldpre;
         a.T = (int)d.T;
         a.N = (int)d.F;
         a.K = (int)d.C;
         a.act = d.act;
-        hipError_t e = launch_rows<T, true>(a, whole_units(g.x, d.ldx, d.C, es) && whole_units(g.w_gate, d.ldw, d.C, es) && whole_units(g.w_up, d.ldw, d.C, es), stream);
+        hipError_t e = launch_rows<T, true>(a, whole_rows(o.x, o.ldx, es) && whole_rows(o.w_gate, o.ldw, es) && whole_rows(o.w_up, o.ldw, es), stream);
         if (e != hipSuccess) return e;
         ffrows::Args b{};
         b.x = g.ws;
-        b.w[0] = g.w_down;
+        b.w[0] = o.w_down;
         b.d = g.y;
-        b.ldx = d.F;
-        b.ldw[0] = d.ld_down;
+        b.ldx = F8;
+        b.ldw[0] = o.ld_down;
         b.ldd = d.ldy;
         b.T = (int)d.T;
         b.N = (int)d.C;
         b.K = (int)d.F;
-        return launch_rows<T, false>(b, whole_units(g.ws, d.F, d.F, es) && whole_units(g.w_down, d.ld_down, d.F, es), stream);
+        return launch_rows<T, false>(b, whole_rows(o.w_down, o.ld_down, es), stream);
     });
 }
 
@@ -270,26 +349,39 @@ mm16::Problem problem(const void* x, int64_t ldx, const void* w, int64_t ldw, vo
 
 int64_t tiles_of(int64_t M, int64_t N, int tile_m, int tile_n) { return ((M + tile_m - 1) / tile_m) * ((N + tile_n - 1) / tile_n); }
 
-// Work-groups that share a tile's k, for products with fewer tiles than CUs: as many as fill them, with four chunks each or more.
-int splits_of(int64_t M, int64_t N, int64_t chunks)
-{
-    const int64_t tiles = tiles_of(M, N, 128, 128);
-    if (tiles >= 256) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(512 + tiles - 1) / tiles, chunks / 4, 16}));
-}
-
 int64_t chunks_of(int64_t K) { return (K + mm16::BK - 1) / mm16::BK; }
 
 // The tile with the shortest estimated time: rounds of work-groups over the CUs, each with its chunks and ends (us). A tile of 256 takes a CU
 // for itself, of those of 128 it takes two; one alone is split over two groups of waves.
-mm16::Shape choose_shape(int64_t tiles256, int64_t tiles128, int64_t chunks)
+struct Choice {
+    mm16::Shape shape;
+    double us;
+};
+Choice choose_shape(int64_t tiles256, int64_t tiles128, int64_t chunks)
 {
     const double large = (double)((tiles256 + 255) / 256) * (1.7 * (double)chunks + 4.0);
     const int64_t full = tiles128 / 512, rest = tiles128 % 512;
     const double pair = 1.14 * (double)chunks + 4.0, alone = 0.60 * (double)chunks + 4.0;
-    if (tiles128 <= 256) return large < alone ? mm16::SHAPE_256 : mm16::SHAPE_128_TWICE;
-    const double small = (double)full * pair + (rest > 256 ? pair : rest > 0 ? 0.75 * (double)chunks + 4.0 : 0.0);
-    return large < small ? mm16::SHAPE_256 : mm16::SHAPE_128;
+    const bool twice = tiles128 <= 256;
+    const double small = twice ? alone : (double)full * pair + (rest > 256 ? pair : rest > 0 ? 0.75 * (double)chunks + 4.0 : 0.0);
+    if (large < small) return {mm16::SHAPE_256, large};
+    return {twice ? mm16::SHAPE_128_TWICE : mm16::SHAPE_128, small};
+}
+
+// Work-groups that share a tile's k, for products with few tiles: the number with the shortest estimated time, that of the launch that joins their
+// sums among it. A function of the extents alone.
+int splits_of(int64_t M, int64_t N, int64_t chunks)
+{
+    int best = 1;
+    double least = choose_shape(tiles_of(M, N, 256, 256), tiles_of(M, N, 128, 128), chunks).us;
+    for (int s = 2; s <= 16 && chunks / s >= 4; ++s) {
+        const double us = choose_shape(s * tiles_of(M, N, 256, 256), s * tiles_of(M, N, 128, 128), (chunks + s - 1) / s).us + 4.0 + 2.0 * s * (double)M * (double)N * 4.0 / 8e6;
+        if (us < least) {
+            least = us;
+            best = s;
+        }
+    }
+    return best;
 }
 
 hipError_t launch(mm16::Form form, int dtype, bool aligned, mm16::Args& a, hipStream_t stream)
@@ -300,7 +392,7 @@ hipError_t launch(mm16::Form form, int dtype, bool aligned, mm16::Args& a, hipSt
         for (int i = 0; i < a.problems; ++i) n += tiles_of(a.p[i].M, a.p[i].N, edge, edge / n_share);
         return n * a.splits;
     };
-    const mm16::Shape shape = choose_shape(tiles(256), tiles(128), chunks_of(a.p[0].K) * a.p[0].segments / a.splits);
+    const mm16::Shape shape = choose_shape(tiles(256), tiles(128), chunks_of(a.p[0].K) * a.p[0].segments / a.splits).shape;
     const int tile = mm16::edge_of(shape);
     a.first_tile[0] = 0;
     for (int i = 0; i < a.problems; ++i) {
@@ -331,33 +423,43 @@ hipError_t launch_shared(mm16::Form form, int dtype, bool aligned, const mm16::P
 hipError_t forward_16(const GatedFfArgs& g, hipStream_t stream)
 {
     const anr_gated_ff_desc& d = g.d;
+    const int64_t F8 = whole(d.F, 2);
     char* const ws = static_cast<char*>(g.ws);
+    const int splits = splits_of(d.T, d.C, chunks_of(d.F));
+    char* const parts = ws + whole_lines((size_t)d.T * F8 * 2);
+    Operands o;
+    hipError_t e = operands_of(g, false, parts + whole_lines(splits > 1 ? (size_t)splits * d.T * d.C * 4 : 0), &o, stream);
+    if (e != hipSuccess) return e;
     mm16::Args a{};
-    a.p[0] = problem(g.x, d.ldx, g.w_gate, d.ldw, ws, d.F, d.T, d.F, d.C);
-    a.p[0].w[1] = g.w_up;
+    a.p[0] = problem(o.x, o.ldx, o.w_gate, o.ldw, ws, F8, d.T, d.F, d.C);
+    a.p[0].w[1] = o.w_up;
     a.problems = a.splits = 1;
     a.act = d.act;
     a.gate = g.gate;
     a.up = g.up;
     a.ld_pre = d.ldpre;
-    const bool aligned = whole_units(g.x, d.ldx, d.C, 2) && whole_units(g.w_gate, d.ldw, d.C, 2) && whole_units(g.w_up, d.ldw, d.C, 2);
-    hipError_t e = launch(mm16::FORM_GATED, d.dtype, aligned, a, stream);
+    a.whole_rows = true;
+    e = launch(mm16::FORM_GATED, d.dtype, whole_rows(o.x, o.ldx, 2) && whole_rows(o.w_gate, o.ldw, 2) && whole_rows(o.w_up, o.ldw, 2), a, stream);
     if (e != hipSuccess) return e;
-    const mm16::Problem down = problem(ws, d.F, g.w_down, d.ld_down, g.y, d.ldy, d.T, d.C, d.F);
-    return launch_shared(mm16::FORM_ROWS, d.dtype, whole_units(ws, d.F, d.F, 2) && whole_units(g.w_down, d.ld_down, d.F, 2), down, splits_of(d.T, d.C, chunks_of(d.F)),
-                         reinterpret_cast<float*>(ws + whole_lines((size_t)d.T * d.F * 2)), stream);
+    const mm16::Problem down = problem(ws, F8, o.w_down, o.ld_down, g.y, d.ldy, d.T, d.C, d.F);
+    return launch_shared(mm16::FORM_ROWS, d.dtype, whole_rows(o.w_down, o.ld_down, 2), down, splits, reinterpret_cast<float*>(parts), stream);
 }
 
 hipError_t backward_16(const GatedFfArgs& g, hipStream_t stream)
 {
     const anr_gated_ff_desc& d = g.d;
-    const int64_t T = d.T, C = d.C, F = d.F;
+    const int64_t T = d.T, C = d.C, F = d.F, F8 = whole(F, 2);
     char* const dg = static_cast<char*>(g.ws);
-    char* const du = dg + 2 * F;                        // side by side: rows of 2 F
-    char* const h = dg + whole_lines((size_t)T * F * 4);
-    float* const parts = reinterpret_cast<float*>(h + whole_lines((size_t)T * F * 2));
+    char* const du = dg + 2 * F8;                       // side by side: rows of 2 F8
+    char* const h = dg + whole_lines((size_t)T * F8 * 4);
+    char* const parts = h + whole_lines((size_t)T * F8 * 2);
+    const int splits = splits_of(T, C, 2 * chunks_of(F));
+    Operands o;
+    hipError_t e = operands_of(g, true, parts + whole_lines(splits > 1 ? (size_t)splits * T * C * 4 : 0), &o, stream);
+    if (e != hipSuccess) return e;
+    const bool aligned_w = whole_rows(o.w_gate, o.ldw, 2) && whole_rows(o.w_up, o.ldw, 2), aligned_dy = whole_rows(o.dy, o.ldy, 2), aligned_x = whole_rows(o.x, o.ldx, 2);
     mm16::Args a{};
-    a.p[0] = problem(g.dy, d.ldy, g.w_down, d.ld_down, dg, 2 * F, T, F, C);
+    a.p[0] = problem(o.dy, o.ldy, o.w_down, o.ld_down, dg, 2 * F8, T, F, C);
     a.problems = a.splits = 1;
     a.act = d.act;
     a.gate = g.gate;
@@ -365,28 +467,23 @@ hipError_t backward_16(const GatedFfArgs& g, hipStream_t stream)
     a.ld_pre = d.ldpre;
     a.du = du;
     a.h = h;
-    a.ld_h = F;
-    hipError_t e = launch(mm16::FORM_HIDDEN_GRADS, d.dtype, whole_units(g.dy, d.ldy, C, 2) && whole_units(g.w_down, d.ld_down, F, 2), a, stream);
+    a.ld_h = F8;
+    a.whole_rows = true;
+    e = launch(mm16::FORM_HIDDEN_GRADS, d.dtype, aligned_dy && whole_rows(o.w_down, o.ld_down, 2), a, stream);
     if (e == hipSuccess && g.dx) {
-        mm16::Problem p = problem(dg, 2 * F, g.w_gate, d.ldw, g.dx, d.lddx, T, C, F);
+        mm16::Problem p = problem(dg, 2 * F8, o.w_gate, o.ldw, g.dx, d.lddx, T, C, F);
         p.x[1] = du;
-        p.w[1] = g.w_up;
+        p.w[1] = o.w_up;
         p.segments = 2;
-        const bool aligned = F % 8 == 0 && whole_units(g.w_gate, d.ldw, C, 2) && whole_units(g.w_up, d.ldw, C, 2);
-        e = launch_shared(mm16::FORM_INPUT_GRAD, d.dtype, aligned, p, splits_of(T, C, 2 * chunks_of(F)), parts, stream);
+        e = launch_shared(mm16::FORM_INPUT_GRAD, d.dtype, aligned_w, p, splits, reinterpret_cast<float*>(parts), stream);
     }
     if (e != hipSuccess || !(g.dw_gate || g.dw_up || g.dw_down)) return e;
     mm16::Args b{};
     b.splits = 1;
-    bool aligned = F % 8 == 0 && C % 8 == 0;
-    if (g.dw_gate) b.p[b.problems++] = problem(dg, 2 * F, g.x, d.ldx, g.dw_gate, d.lddw, F, C, T);
-    if (g.dw_up) b.p[b.problems++] = problem(du, 2 * F, g.x, d.ldx, g.dw_up, d.lddw, F, C, T);
-    if (g.dw_gate || g.dw_up) aligned = aligned && whole_units(g.x, d.ldx, C, 2);
-    if (g.dw_down) {
-        b.p[b.problems++] = problem(g.dy, d.ldy, h, F, g.dw_down, d.ld_ddown, C, F, T);
-        aligned = aligned && whole_units(g.dy, d.ldy, C, 2);
-    }
-    return launch(mm16::FORM_WEIGHT_GRADS, d.dtype, aligned, b, stream);
+    if (g.dw_gate) b.p[b.problems++] = problem(dg, 2 * F8, o.x, o.ldx, g.dw_gate, d.lddw, F, C, T);
+    if (g.dw_up) b.p[b.problems++] = problem(du, 2 * F8, o.x, o.ldx, g.dw_up, d.lddw, F, C, T);
+    if (g.dw_down) b.p[b.problems++] = problem(o.dy, o.ldy, h, F8, g.dw_down, d.ld_ddown, C, F, T);
+    return launch(mm16::FORM_WEIGHT_GRADS, d.dtype, (aligned_x || !(g.dw_gate || g.dw_up)) && (aligned_dy || !g.dw_down), b, stream);
 }
 
 // ---- float32 products
@@ -484,22 +581,22 @@ size_t gated_ff_workspace_bytes(const GatedFfArgs& g, bool backward)
     const anr_gated_ff_desc& d = g.d;
     const size_t T = (size_t)d.T, C = (size_t)d.C, F = (size_t)d.F;
     if (T == 0) return 0;
+    const size_t copied = copies(d, backward) ? copied_bytes(d, backward) : 0;
+    const size_t es = element_bytes(d.dtype), tf = whole_lines(T * whole(d.F, (int)es) * es);
+    if (!backward && few_tokens(d)) return tf + copied;
     if (d.dtype == ANR_F32) {
-        const size_t tf = whole_lines(T * F * 4);
         if (backward) return 6 * tf + whole_lines(F * C * 8) + whole_lines(T * C * 4) + parts_bytes(d.T, d.C, 2 * d.F);
-        return T <= kFewTokens ? tf : 3 * tf + parts_bytes(d.T, d.C, d.F);
+        return 3 * tf + parts_bytes(d.T, d.C, d.F);
     }
-    const size_t tf = whole_lines(T * F * 2);
     const int splits = splits_of(d.T, d.C, (backward ? 2 : 1) * chunks_of(d.F));
-    const size_t parts = splits > 1 ? (size_t)splits * T * C * 4 : 0;
-    if (backward) return whole_lines(T * F * 4) + tf + parts;
-    return T <= kFewTokens ? tf : tf + parts;
+    const size_t parts = whole_lines(splits > 1 ? (size_t)splits * T * C * 4 : 0);
+    return (backward ? whole_lines(T * whole(d.F, 2) * 4) : 0) + tf + parts + copied;
 }
 
 hipError_t launch_gated_ff(const GatedFfArgs& g, hipStream_t stream)
 {
     if (g.d.T == 0) return hipSuccess;
-    if (g.d.T <= kFewTokens) return forward_few(g, stream);
+    if (few_tokens(g.d)) return forward_few(g, stream);
     return g.d.dtype == ANR_F32 ? forward_32(g, stream) : forward_16(g, stream);
 }
 

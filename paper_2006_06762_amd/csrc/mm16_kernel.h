@@ -47,6 +47,9 @@ enum Epilogue {
     GATED_BACKWARD  // D is dh: gradients of gate and up, and h
 };
 
+// ALIGNED kernels read 16-byte units: pointers and leading dimensions are whole units, and where an extent is none, its rows go on in zeros
+// to the end of their last unit (zeros matter for k only).
+//
 // One product.  Two pointers of an operand: K_ROWS of GATED: gate's and up's weights; else the sum runs over
 // `segments` pairs of operands of K each.
 struct Problem {
@@ -72,6 +75,8 @@ struct Args {
     int64_t ld_pre;
     void *du, *h;
     int64_t ld_h;
+    // of D, du and h in the workspace (GATED, GATED_BACKWARD): their last unit is written whole, zeros behind N
+    bool whole_rows;
 };
 
 // An operand of R rows (its own index) in LDS.
@@ -123,7 +128,7 @@ struct Stager {
             }
             which = PAIRED ? __builtin_amdgcn_readfirstlane((first >> 5) & 1) : 0;
         } else {
-            const int column = ALIGNED ? min(unit * 8, own - 8) : unit * 8;
+            const int column = ALIGNED ? min(unit * 8, ((own + 7) & ~7) - 8) : unit * 8;
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) offset[i] = (uint32_t)((first + i * (NT / ROW_UNITS)) * ld * 2) + column * 2;
             which = 0;
@@ -203,6 +208,18 @@ __device__ __forceinline__ void load8(const T* p, float (&v)[8], int in, bool al
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < in ? to_float(p[i]) : 0.f;
     }
+}
+
+// store8 to the workspace: with whole_rows the last unit of a row whole, with zeros.
+template <typename T>
+__device__ __forceinline__ void store_workspace(T* p, float (&v)[8], int in, bool aligned, bool whole_rows)
+{
+    if (whole_rows && in > 0 && in < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < in ? v[i] : 0.f;
+        in = 8;
+    }
+    store8(p, v, in, aligned);
 }
 
 // G groups of waves take a tile's chunks in turn, each with buffers and sums of its own, and join the sums in LDS: for products with
@@ -418,6 +435,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 64 * WM * WN * G / 256) void prod
         T* const d = static_cast<T*>(p.d);
         T *const gate = static_cast<T*>(args.gate), *const up = static_cast<T*>(args.up);
         const bool aligned = whole(d, p.ldd), aligned_pre = whole(gate, args.ld_pre) && whole(up, args.ld_pre);
+        auto store_unit = [&](T* at, float (&v)[8], bool aligned) { store_workspace(at, v, N - (n0 + wn * NB * 16 + part * 8), aligned, args.whole_rows); };
         const int col = n0 + wn * NB * 16 + part * 8, in_lds = (part >> 2) * 256 + (part & 3) * 32;
         device_activation(args.act, [&](auto act) {
             emit([&](int row, const char* at) {
@@ -430,7 +448,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 64 * WM * WN * G / 256) void prod
                     store8(gate + (int64_t)row * args.ld_pre + col, g, N - col, aligned_pre);
                     store8(up + (int64_t)row * args.ld_pre + col, u, N - col, aligned_pre);
                 }
-                store8(d + (int64_t)row * p.ldd + col, h, N - col, aligned);
+                store_unit(d + (int64_t)row * p.ldd + col, h, aligned);
             });
         });
     } else {
@@ -439,6 +457,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 64 * WM * WN * G / 256) void prod
         const T *const gate = static_cast<const T*>(args.gate), *const up = static_cast<const T*>(args.up);
         const bool aligned = whole(d, p.ldd) && whole(du, p.ldd) && whole(h, args.ld_h), aligned_pre = whole(gate, args.ld_pre) && whole(up, args.ld_pre);
         const int col = n0 + wn * NB * 32 + part * 8;
+        auto store_unit = [&](T* at, float (&v)[8], bool aligned) { store_workspace(at, v, N - col, aligned, args.whole_rows); };
         device_activation(args.act, [&](auto act) {
             emit([&](int row, const char* at) {
                 float g[8], u[8], dh[8], hh[8];
@@ -453,9 +472,9 @@ __global__ __launch_bounds__(64 * WM * WN * G, 64 * WM * WN * G / 256) void prod
                     g[e] = dh[e] * u[e] * slope;
                     u[e] = dh[e] * a;
                 }
-                store8(d + (int64_t)row * p.ldd + col, g, N - col, aligned);
-                store8(du + (int64_t)row * p.ldd + col, u, N - col, aligned);
-                store8(h + (int64_t)row * args.ld_h + col, hh, N - col, aligned);
+                store_unit(d + (int64_t)row * p.ldd + col, g, aligned);
+                store_unit(du + (int64_t)row * p.ldd + col, u, aligned);
+                store_unit(h + (int64_t)row * args.ld_h + col, hh, aligned);
             });
         });
     }
