@@ -39,19 +39,19 @@ __device__ __forceinline__ Pack<T, V> pack_floats(const float (&in)[V])
     return a;
 }
 
-// A store that goes past L2 (see stg4_nt) where it is `streaming`: neighbouring lanes write whole lines then.
-template <typename T, int V>
-__device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& a, bool streaming)
+// A store that goes past L2 (see stg4_nt) where STREAMING: neighbouring lanes write whole lines then.
+template <bool STREAMING, typename T, int V>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& a)
 {
-    if constexpr (sizeof(T) * V == 16) {
-        if (streaming) {
-            asm volatile("" ::: "memory");           // (or the two stores become one, an ordinary one)
-            __builtin_nontemporal_store(__builtin_bit_cast(f32x4, a), reinterpret_cast<f32x4*>(p));
-            asm volatile("" ::: "memory");
-            return;
-        }
-    }
-    *reinterpret_cast<Pack<T, V>*>(p) = a;
+    if constexpr (STREAMING && sizeof(T) * V == 16) __builtin_nontemporal_store(__builtin_bit_cast(f32x4, a), reinterpret_cast<f32x4*>(p));
+    else *reinterpret_cast<Pack<T, V>*>(p) = a;
+}
+// f(std::true_type{}) or f(std::false_type{}): a loop of its own for each (in one loop the compiler makes the two stores one, an ordinary one).
+template <typename F>
+__device__ __forceinline__ void by_streaming(bool streaming, F f)
+{
+    if (streaming) f(std::true_type{});
+    else f(std::false_type{});
 }
 
 template <typename T, int V>

@@ -47,19 +47,42 @@ __device__ __forceinline__ f32x4 multiply(u32x4 w, u32x4 x, f32x4 c, float)
     return c;
 }
 
-// ALIGNED: pointers and leading dimensions are whole 16-byte units, and a row of K elements goes on in zeros to the end of its last one.
-// Elements k .. k + 16 / sizeof(T) - 1 of the row at byte `row` of a matrix; those past K are zeros.
+// A matrix that a lane reads rows of.
+struct Source {
+    const char* base;
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ void init(const void* p)
+    {
+        base = static_cast<const char*>(p);
+        rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, kExtent, 0x00020000);
+    }
+};
+
+// Elements k .. k + 16 / sizeof(T) - 1 of the row at byte `row` of a matrix; those past K are zeros.  ALIGNED: pointers, leading dimensions
+// and K are whole 16-byte units, but for rows that go on in zeros to the end of their last one.  Else a row's last unit starts so far ahead that
+// it ends with the row, and what the unit before it has is cleared: other elements of k in its place, in both operands alike.
 template <typename T, bool ALIGNED>
-__device__ __forceinline__ u32x4 load_unit(__amdgpu_buffer_rsrc_t rsrc, uint32_t row, int k, int K)
+__device__ __forceinline__ u32x4 load_unit(const Source& s, uint32_t row, int k, int K)
 {
     constexpr int E = 16 / sizeof(T);
-    if (ALIGNED) return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(k < K ? row + k * (int)sizeof(T) : kNowhere), 0, 0));
+    if (ALIGNED) return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(s.rsrc, (int)(k < K ? row + k * (int)sizeof(T) : kNowhere), 0, 0));
     u32x4 v = {0, 0, 0, 0};
+    if (K >= E) {
+        struct __attribute__((packed, aligned(2))) Loose { u32x4 v; };
+        const int start = min(k, K - E), counted = k < K ? k - start : E;
+        v = reinterpret_cast<const Loose*>(s.base + row + start * (int)sizeof(T))->v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (sizeof(T) == 4) v[j] = j < counted ? 0u : v[j];
+            else v[j] &= (2 * j < counted ? 0u : 0x0000ffffu) | (2 * j + 1 < counted ? 0u : 0xffff0000u);
+        }
+        return v;
+    }
 #pragma unroll
     for (int j = 0; j < E; ++j) {
         const int at = (int)(k + j < K ? row + (k + j) * (int)sizeof(T) : kNowhere);
-        if (sizeof(T) == 4) v[j * (int)sizeof(T) / 4] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0);
-        else v[j / 2] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0) << (16 * (j & 1));
+        if (sizeof(T) == 4) v[j * (int)sizeof(T) / 4] = __builtin_amdgcn_raw_buffer_load_b32(s.rsrc, at, 0, 0);
+        else v[j / 2] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(s.rsrc, at, 0, 0) << (16 * (j & 1));
     }
     return v;
 }
@@ -72,14 +95,14 @@ __global__ __launch_bounds__(1024) void rows_kernel(const Args a)
     extern __shared__ __attribute__((aligned(16))) float sums[];       // [wave][TB][MATS][4][64]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int n0 = blockIdx.x * 16, r = lane & 15, g = lane >> 4;
-    __amdgpu_buffer_rsrc_t wr[MATS];
+    Source wr[MATS], xr;
     uint32_t wrow[MATS], xrow[TB];
 #pragma unroll
     for (int m = 0; m < MATS; ++m) {
-        wr[m] = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(static_cast<const T*>(a.w[m]) + n0 * a.ldw[m]), 0, kExtent, 0x00020000);
+        wr[m].init(static_cast<const T*>(a.w[m]) + n0 * a.ldw[m]);
         wrow[m] = (uint32_t)(min(r, a.N - 1 - n0) * a.ldw[m] * sizeof(T));
     }
-    const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(a.x), 0, kExtent, 0x00020000);
+    xr.init(a.x);
 #pragma unroll
     for (int t = 0; t < TB; ++t) xrow[t] = (uint32_t)(min(t * 16 + r, a.T - 1) * a.ldx * sizeof(T));
     f32x4 acc[MATS][TB];

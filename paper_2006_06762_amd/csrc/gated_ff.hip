@@ -213,8 +213,8 @@ hipError_t launch_rows(const ffrows::Args& a, bool aligned, hipStream_t stream)
     return with(std::integral_constant<int, 4>{});
 }
 
-// Operands whose rows are no whole 16-byte units are copied first, to rows that are, with zeros behind their ends: a pass over the weights, which
-// the products read once (one token 1001 -> 2777 in bf16 34 us with loads of single elements, XX so) or far more often.
+// 16-bit operands whose rows are no whole 16-byte units are copied first, to rows that are, with zeros behind their ends: 1024 tokens 1001 -> 2777
+// took 175 us with loads of single elements where they are used, 76 so.
 struct Copy {
     const void* in;
     int64_t ld, R, C;
@@ -234,9 +234,14 @@ __global__ __launch_bounds__(kThreads) void copy_rows_kernel(const Copies all)
     const int64_t units = c.ld_out / E;
     for (int64_t r = blockIdx.y; r < c.R; r += gridDim.y)
         for (int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x; u < units; u += (int64_t)gridDim.x * kThreads) {
+            struct __attribute__((packed, aligned(2))) Loose { Pack<T, E> v; };
             Pack<T, E> v;
+            if (u * E + E <= c.C) {
+                v = reinterpret_cast<const Loose*>(in + r * c.ld + u * E)->v;
+            } else {
 #pragma unroll
-            for (int i = 0; i < E; ++i) v.v[i] = u * E + i < c.C ? in[r * c.ld + u * E + i] : from_float<T>(0.f);
+                for (int i = 0; i < E; ++i) v.v[i] = u * E + i < c.C ? in[r * c.ld + u * E + i] : from_float<T>(0.f);
+            }
             *reinterpret_cast<Pack<T, E>*>(out + r * c.ld_out + u * E) = v;
         }
 }
@@ -292,20 +297,18 @@ hipError_t forward_few(const GatedFfArgs& g, hipStream_t stream)
     const anr_gated_ff_desc& d = g.d;
     const int es = element_bytes(d.dtype);
     const int64_t F8 = whole(d.F, es);
-    Operands o;
-    const hipError_t copied = operands_of(g, false, static_cast<char*>(g.ws) + whole_lines((size_t)d.T * F8 * es), &o, stream);
-    if (copied != hipSuccess) return copied;
+    auto units = [&](const void* p, int64_t ld, int64_t K) { return whole_rows(p, ld, es) && K * es % 16 == 0; };
     return with_type(d.dtype, [&](auto t) {
         using T = decltype(t);
         ffrows::Args a{};
-        a.x = o.x;
-        a.w[0] = o.w_gate;
-        a.w[1] = o.w_up;
+        a.x = g.x;
+        a.w[0] = g.w_gate;
+        a.w[1] = g.w_up;
         a.d = g.ws;
         a.gate = g.gate;
         a.up = g.up;
-        a.ldx = o.ldx;
-        a.ldw[0] = a.ldw[1] = o.ldw;
+        a.ldx = d.ldx;
+        a.ldw[0] = a.ldw[1] = d.ldw;
         a.ldd = F8;
         a.whole_rows = true;
         a.ld_pre = d.ldpre;
@@ -313,19 +316,19 @@ hipError_t forward_few(const GatedFfArgs& g, hipStream_t stream)
         a.N = (int)d.F;
         a.K = (int)d.C;
         a.act = d.act;
-        hipError_t e = launch_rows<T, true>(a, whole_rows(o.x, o.ldx, es) && whole_rows(o.w_gate, o.ldw, es) && whole_rows(o.w_up, o.ldw, es), stream);
+        const hipError_t e = launch_rows<T, true>(a, units(g.x, d.ldx, d.C) && units(g.w_gate, d.ldw, d.C) && units(g.w_up, d.ldw, d.C), stream);
         if (e != hipSuccess) return e;
         ffrows::Args b{};
         b.x = g.ws;
-        b.w[0] = o.w_down;
+        b.w[0] = g.w_down;
         b.d = g.y;
         b.ldx = F8;
-        b.ldw[0] = o.ld_down;
+        b.ldw[0] = d.ld_down;
         b.ldd = d.ldy;
         b.T = (int)d.T;
         b.N = (int)d.C;
         b.K = (int)d.F;
-        return launch_rows<T, false>(b, whole_rows(o.w_down, o.ld_down, es), stream);
+        return launch_rows<T, false>(b, units(g.w_down, d.ld_down, d.F), stream);
     });
 }
 
@@ -581,15 +584,14 @@ size_t gated_ff_workspace_bytes(const GatedFfArgs& g, bool backward)
     const anr_gated_ff_desc& d = g.d;
     const size_t T = (size_t)d.T, C = (size_t)d.C, F = (size_t)d.F;
     if (T == 0) return 0;
-    const size_t copied = copies(d, backward) ? copied_bytes(d, backward) : 0;
     const size_t es = element_bytes(d.dtype), tf = whole_lines(T * whole(d.F, (int)es) * es);
-    if (!backward && few_tokens(d)) return tf + copied;
+    if (!backward && few_tokens(d)) return tf;
     if (d.dtype == ANR_F32) {
         if (backward) return 6 * tf + whole_lines(F * C * 8) + whole_lines(T * C * 4) + parts_bytes(d.T, d.C, 2 * d.F);
         return 3 * tf + parts_bytes(d.T, d.C, d.F);
     }
     const int splits = splits_of(d.T, d.C, (backward ? 2 : 1) * chunks_of(d.F));
-    const size_t parts = whole_lines(splits > 1 ? (size_t)splits * T * C * 4 : 0);
+    const size_t parts = whole_lines(splits > 1 ? (size_t)splits * T * C * 4 : 0), copied = copies(d, backward) ? copied_bytes(d, backward) : 0;
     return (backward ? whole_lines(T * whole(d.F, 2) * 4) : 0) + tf + parts + copied;
 }
 

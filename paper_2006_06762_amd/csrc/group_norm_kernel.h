@@ -241,14 +241,16 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
         from_table<V>(shared, s.tx * V, mean);
         from_table<V>(shared + table, s.tx * V, scale);
         from_table<V>(shared + 2 * table, s.tx * V, shift);
+        by_streaming(a.streaming, [&](auto streaming) {
 #pragma unroll 4
-        for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
-            float v[V];
-            load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
+            for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
+                float v[V];
+                load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = activation<ACT, QUICK>(fmaf(v[i] - mean[i], scale[i], shift[i]));
-            store_pack(y + a.py.at(p, a.W, a.by_w, a.flat) + col * V, pack_floats<T, V>(v), a.streaming);
-        }
+                for (int i = 0; i < V; ++i) v[i] = activation<ACT, QUICK>(fmaf(v[i] - mean[i], scale[i], shift[i]));
+                store_pack<decltype(streaming)::value>(y + a.py.at(p, a.W, a.by_w, a.flat) + col * V, pack_floats<T, V>(v));
+            }
+        });
     }
 }
 
@@ -402,19 +404,21 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
         float mean_dz[V], mean_with_hat[V];
         from_table<V>(shared + 4 * table, s.tx * V, mean_dz);
         from_table<V>(shared + 5 * table, s.tx * V, mean_with_hat);
+        by_streaming(a.streaming, [&](auto streaming) {
 #pragma unroll 2
-        for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
-            float v[V], d[V];
-            load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
-            load_floats<T, V>(dy + a.pdy.at(p, a.W, a.by_w, a.flat) + col * V, d);
+            for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
+                float v[V], d[V];
+                load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
+                load_floats<T, V>(dy + a.pdy.at(p, a.W, a.by_w, a.flat) + col * V, d);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float hat, dz;
-                ch.template element<ACT, QUICK>(i, v[i], d[i], hat, dz);
-                v[i] = ch.rstd[i] * (fmaf(dz, ch.gamma[i], -mean_dz[i]) - hat * mean_with_hat[i]);
+                for (int i = 0; i < V; ++i) {
+                    float hat, dz;
+                    ch.template element<ACT, QUICK>(i, v[i], d[i], hat, dz);
+                    v[i] = ch.rstd[i] * (fmaf(dz, ch.gamma[i], -mean_dz[i]) - hat * mean_with_hat[i]);
+                }
+                store_pack<decltype(streaming)::value>(dx + a.py.at(p, a.W, a.by_w, a.flat) + col * V, pack_floats<T, V>(v));
             }
-            store_pack(dx + a.py.at(p, a.W, a.by_w, a.flat) + col * V, pack_floats<T, V>(v), a.streaming);
-        }
+        });
     }
     if (s.n == 0 && s.slab == 0) parameter_gradients(a);
 }

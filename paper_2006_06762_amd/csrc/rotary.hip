@@ -29,7 +29,6 @@ struct RotaryKernelArgs {
     int pair_columns, columns;      // columns of V pairs; with those of V dimensions (adjacent: of 2 V) that are copied
     int rest;                       // first dimension that is copied
     int group_tokens, group_heads;  // of a work-group
-    bool streaming;
     FastDiv by_columns, by_heads, by_s, by_pairs;
 };
 
@@ -53,7 +52,8 @@ __device__ __forceinline__ void turn_of(double pos, float freq, float& c, float&
 }
 
 // ADJACENT: the V pairs of a column are 2 V dimensions in a row, else two runs of V.
-template <typename T, int V, bool ADJACENT>
+// STREAMING: stores go past L2.
+template <typename T, int V, bool ADJACENT, bool STREAMING>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKernelArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) float lds[];      // cosines of [tokens][pairs], then the sines
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKernelArgs
                 out = pack_floats<T, 2 * V>(y);
             }
             if (ADJACENT && V > 1) {
-                store_pack(to + at[j].first, out, a.streaming);
+                store_pack<STREAMING>(to + at[j].first, out);
             } else {
                 Pack<T, V> lo, hi;
 #pragma unroll
@@ -158,8 +158,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKernelArgs
                     lo.v[i] = out.v[i];
                     hi.v[i] = out.v[V + i];
                 }
-                store_pack(to + at[j].first, lo, a.streaming);
-                if (!at[j].copied) store_pack(to + at[j].second, hi, a.streaming);
+                store_pack<STREAMING>(to + at[j].first, lo);
+                if (!at[j].copied) store_pack<STREAMING>(to + at[j].second, hi);
             }
         }
     }
@@ -212,10 +212,10 @@ hipError_t launch_rotary(const RotaryArgs& g, hipStream_t stream)
         // Stores past L2 where they cover runs of 64 bytes: 33 k tokens of 16 heads, past L2 / not, TB/s: float32 halves of 64 pairs 6.4 / 4.9, of 32 6.2 /
         // 5.6, of 16 4.9 / 5.6, bf16 of 64 6.1 / 5.5, of 32 4.9 / 5.1, of 16 3.1 / 4.1; adjacent 36 4.9 / 4.3; 8 k tokens of 8 heads, float32 of 16 4.4 / 3.7.
         constexpr int LINE = 64 / (int)sizeof(T);
-        a.streaming = adjacent || (d.pairing == ANR_ROTARY_HALVES && a.pairs % LINE == 0);
+        bool streaming = adjacent || (d.pairing == ANR_ROTARY_HALVES && a.pairs % LINE == 0);
         if (d.pairing == ANR_ROTARY_SECTION_HALVES) {
-            a.streaming = true;
-            for (int i = 0; i < d.axes; ++i) a.streaming = a.streaming && d.section[i] % LINE == 0;
+            streaming = true;
+            for (int i = 0; i < d.axes; ++i) streaming = streaming && d.section[i] % LINE == 0;
         }
         auto launch = [&](auto kernel, int pairs_per_column, int copied) {
             RotaryKernelArgs b = a;
@@ -237,8 +237,9 @@ hipError_t launch_rotary(const RotaryArgs& g, hipStream_t stream)
             return launch_kernel(kernel, dim3((unsigned)blocks, (unsigned)((heads + b.group_heads - 1) / b.group_heads)), dim3(kThreads),
                                  sizeof(float) * 2 * (size_t)b.group_tokens * a.pairs, stream, b);
         };
-        if (!whole) return adjacent ? launch(rotary_kernel<T, 1, true>, 1, 1) : launch(rotary_kernel<T, 1, false>, 1, 1);
-        return adjacent ? launch(rotary_kernel<T, UNIT / 2, true>, UNIT / 2, UNIT) : launch(rotary_kernel<T, UNIT, false>, UNIT, UNIT);
+        if (!whole) return adjacent ? launch(rotary_kernel<T, 1, true, false>, 1, 1) : launch(rotary_kernel<T, 1, false, false>, 1, 1);
+        if (adjacent) return launch(rotary_kernel<T, UNIT / 2, true, true>, UNIT / 2, UNIT);
+        return streaming ? launch(rotary_kernel<T, UNIT, false, true>, UNIT, UNIT) : launch(rotary_kernel<T, UNIT, false, false>, UNIT, UNIT);
     });
 }
 
