@@ -123,8 +123,8 @@ __device__ __forceinline__ float activation_and_slope(float z, float& slope)
         return z < 0.f ? 0.f : z;
     }
     if (ACT == ANR_ACT_SILU) {
-        const float s = sigmoid<QUICK>(z), rest = 1.f - s;
-        slope = rest == 0.f || s == 0.f ? s : s * fmaf(z, rest, 1.f);
+        const float s = sigmoid<QUICK>(z);
+        slope = s * fmaf(__builtin_amdgcn_fmed3f(z, -128.f, 128.f), 1.f - s, 1.f);     // (s is 0 or 1 where z is cut)
         return z * s;
     }
     if (ACT == ANR_ACT_GELU) {

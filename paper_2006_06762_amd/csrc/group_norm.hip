@@ -129,12 +129,10 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
         a.slabs = 1;
         a.slab_pixels = a.HW;
     }
-    const size_t partial = p.resident ? 0 : sizeof(float) * 2 * (size_t)g.N * a.slabs * (backward ? (size_t)g.C : (size_t)g.groups);
-    const size_t sums = backward ? sizeof(float) * 2 * (size_t)g.N * g.C : 0;
-    p.bytes = partial + sums + (backward ? sizeof(float) * 2 * (size_t)g.N * g.groups : 0);
+    const size_t of_groups = p.resident ? 0 : sizeof(float) * 2 * (size_t)g.N * a.slabs * g.groups;
+    p.bytes = of_groups + (backward ? sizeof(float) * 2 * (size_t)g.N * a.slabs * g.C : 0);
     a.ws = static_cast<float*>(g.ws);
-    a.sums = a.ws + partial / sizeof(float);
-    a.group_sums = a.sums + sums / sizeof(float);
+    a.sums = a.ws + of_groups / sizeof(float);
     return p;
 }
 
@@ -237,8 +235,8 @@ hipError_t launch_group_norm_backward(const GroupNormArgs& g, hipStream_t stream
             constexpr int V = decltype(v)::value;
             return with_activation(g.act, [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
-                static LdsLimit limit, limit_groups, limit_apply;
-                const size_t lds = sizeof(float) * 2 * p.args.chunk, apply_lds = sizeof(float) * 6 * (size_t)p.table;
+                static LdsLimit limit, limit_apply;
+                const size_t apply_lds = sizeof(float) * std::max<size_t>(6 * (size_t)p.table + 2 * (size_t)(p.args.chunk / p.args.cg), kThreads);
                 if constexpr (V > 1) {
                     if (p.resident) {
                         auto launch = [&](auto kernel, LdsLimit& held) {
@@ -252,13 +250,11 @@ hipError_t launch_group_norm_backward(const GroupNormArgs& g, hipStream_t stream
                     }
                 }
                 hipError_t e = p.lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(backward_sums_kernel<T, V, ACT>), p.lds, limit) : hipSuccess;
-                if (e == hipSuccess && lds > 65536) e = raise_lds_limit(reinterpret_cast<const void*>(backward_groups_kernel), lds, limit_groups);
                 if (e == hipSuccess) e = launch_kernel(backward_sums_kernel<T, V, ACT>, grid, dim3(kThreads), p.lds, stream, p.args);
-                if (e == hipSuccess) e = launch_kernel(backward_groups_kernel, dim3(1, p.chunks, g.N), dim3(kThreads), lds, stream, p.args);
                 if (e != hipSuccess) return e;
                 if (!g.y) return launch_kernel(backward_parameters_kernel, dim3(1, p.chunks, 1), dim3(kThreads), 0, stream, p.args);
                 if (apply_lds > 65536) e = raise_lds_limit(reinterpret_cast<const void*>(backward_apply_kernel<T, V, ACT>), apply_lds, limit_apply);
-                return e != hipSuccess ? e : launch_kernel(backward_apply_kernel<T, V, ACT>, grid, dim3(kThreads), apply_lds, stream, p.args);
+                return e != hipSuccess ? e : launch_kernel(backward_apply_kernel<T, V, ACT>, dim3(grid.x + (g.dgamma || g.dbeta ? 1 : 0), grid.y, grid.z), dim3(kThreads), apply_lds, stream, p.args);
             });
         });
     });

@@ -38,9 +38,8 @@ struct Args {
     const void *gamma, *beta;
     void *dgamma, *dbeta;
     float *mean, *rstd;
-    float* ws;                      // partial sums of the slabs
-    float* sums;                    // backward: sums of a channel over an image's slabs, [N][2][C]
-    float* group_sums;              // backward: [N][groups][2]
+    float* ws;                      // mean and M2 (backward: the two sums) of each group over the slabs, [N][slabs][groups][2]
+    float* sums;                    // backward: sums of each channel over the slabs, [N][slabs][2][C]
     Pixels px, pdy, py;
     FastDiv by_w, by_cg;
     float eps;
@@ -286,7 +285,19 @@ struct Channels {
     }
 };
 
-// First kernel of the backward pass: sums of dz and dz xhat of each channel over the slab.
+// From the chunk's sums of dz gamma and dz gamma xhat of each channel ([2][channels]) those of its groups over the slab.
+__device__ __forceinline__ void group_parts(const Args& a, const Place& s, const float* channel, int threads)
+{
+    float* const out = a.ws + 2 * (((int64_t)s.n * a.slabs + s.slab) * a.groups + s.c0 / a.cg);
+    for (int e = threadIdx.x; e < 2 * (s.channels / a.cg); e += threads) {
+        const float* const from = channel + (e & 1) * s.channels + (e >> 1) * a.cg;
+        float sum = 0.f;
+        for (int c = 0; c < a.cg; ++c) sum += from[c];
+        out[e] = sum;
+    }
+}
+
+// First kernel of the backward pass: sums of dz and dz xhat over the slab, of each channel and, with gamma, of each group.
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void backward_sums_kernel(const Args a)
 {
@@ -328,63 +339,74 @@ __global__ __launch_bounds__(kThreads) void backward_sums_kernel(const Args a)
         }
     }
     __syncthreads();
-    float* const out = a.ws + ((int64_t)s.n * a.slabs + s.slab) * 2 * a.C + s.c0;
+    float* const out = a.sums + ((int64_t)s.n * a.slabs + s.slab) * 2 * a.C + s.c0;
     for (int e = threadIdx.x; e < 2 * s.channels; e += kThreads) {
         const int which = e >= s.channels, c = e - which * s.channels;
         float sum = 0.f;
         for (int r = 0; r < s.rows; ++r) sum += lds[(2 * r + which) * s.channels + c];
         out[(int64_t)which * a.C + c] = sum;
-    }
-}
-
-// Second kernel: sums over an image's slabs, and those of its groups with gamma.
-__global__ __launch_bounds__(kThreads) void backward_groups_kernel(const Args a)
-{
-    extern __shared__ __attribute__((aligned(16))) float lds[];      // [2][channels]
-    const int n = blockIdx.z, c0 = blockIdx.y * a.chunk, channels = min(a.chunk, a.C - c0);
-    const float* const in = a.ws + (int64_t)n * a.slabs * 2 * a.C + c0;
-    for (int e = threadIdx.x; e < 2 * channels; e += kThreads) {
-        const int which = e >= channels, c = e - which * channels;
-        float sum = 0.f;
-#pragma unroll 8
-        for (int i = 0; i < a.slabs; ++i) sum += in[((int64_t)i * 2 + which) * a.C + c];
-        a.sums[((int64_t)n * 2 + which) * a.C + c0 + c] = sum;
-        lds[e] = sum * parameter(a.gamma, c0 + c, a.param_dtype, 1.f);
+        lds[which * s.channels + c] = sum * parameter(a.gamma, s.c0 + c, a.param_dtype, 1.f);      // (row 0, which this thread alone reads)
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * (channels / a.cg); e += kThreads) {
-        const int which = e & 1, g = e >> 1;
-        float sum = 0.f;
-        for (int c = 0; c < a.cg; ++c) sum += lds[which * channels + g * a.cg + c];
-        a.group_sums[((int64_t)n * a.groups + c0 / a.cg + g) * 2 + which] = sum / ((float)a.HW * (float)a.cg);
-    }
+    group_parts(a, s, lds, kThreads);
 }
 
-// dgamma and dbeta of the chunk: sums over the images.
-__device__ __forceinline__ void parameter_gradients(const Args& a)
+// dgamma and dbeta of the chunk: sums over the images' slabs, which the threads of a channel share.
+__device__ __forceinline__ void parameter_gradients(const Args& a, float* lds, int threads)
 {
-    const int c0 = blockIdx.y * a.chunk, channels = min(a.chunk, a.C - c0);
-    for (int e = threadIdx.x; e < 2 * channels; e += kThreads) {
+    const int c0 = blockIdx.y * a.chunk, channels = min(a.chunk, a.C - c0), sums = 2 * channels;
+    const int64_t parts = (int64_t)a.N * a.slabs;
+    for (int base = 0; base < sums; base += threads) {
+        const int here = min(sums - base, threads), shares = threads / here, share = threadIdx.x / here, e = base + threadIdx.x - share * here;
         const int which = e >= channels, c = c0 + e - which * channels;
-        void* const out = which ? a.dgamma : a.dbeta;
-        if (!out) continue;
         float sum = 0.f;
-#pragma unroll 16
-        for (int n = 0; n < a.N; ++n) sum += a.sums[((int64_t)n * 2 + which) * a.C + c];
+        if (share < shares) {
+#pragma unroll 8
+            for (int64_t i = share; i < parts; i += shares) sum += a.sums[(i * 2 + which) * a.C + c];
+        }
+        __syncthreads();
+        lds[threadIdx.x] = sum;
+        __syncthreads();
+        void* const out = which ? a.dgamma : a.dbeta;
+        if (share > 0 || !out) continue;
+        for (int i = 1; i < shares; ++i) sum += lds[i * here + threadIdx.x];
         store_any(out, c, a.param_dtype, sum);
     }
 }
 
-__global__ __launch_bounds__(kThreads) void backward_parameters_kernel(const Args a) { parameter_gradients(a); }
+__global__ __launch_bounds__(kThreads) void backward_parameters_kernel(const Args a)
+{
+    __shared__ float lds[kThreads];
+    parameter_gradients(a, lds, kThreads);
+}
 
-// Third kernel: dx, and in the first slab of the first image the parameters' gradients.
+// Second kernel: dx, and in work-groups of their own, behind the first image's slabs, the parameters' gradients.
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
-    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, and those of the group's two means
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, those of the group's two means, and [groups] of the means
+    if ((int)blockIdx.x == a.slabs) {
+        if (blockIdx.z == 0) parameter_gradients(a, shared, kThreads);
+        return;
+    }
     const Place s(a, V);
     const int table = table_floats(min(s.channels, kThreads * V));
+    float* const means = shared + 6 * table;
+    for (int g = threadIdx.x >> 6; g < s.channels / a.cg; g += kThreads / 64) {
+        const float* const at = a.ws + 2 * ((int64_t)s.n * a.slabs * a.groups + s.c0 / a.cg + g);
+        float dz = 0.f, with_hat = 0.f;
+        for (int i = threadIdx.x & 63; i < a.slabs; i += 64) {
+            dz += at[2 * (int64_t)i * a.groups];
+            with_hat += at[2 * (int64_t)i * a.groups + 1];
+        }
+        dz = wave_sum(dz);
+        with_hat = wave_sum(with_hat);
+        if ((threadIdx.x & 63) == 0) {
+            means[2 * g] = dz / ((float)a.HW * (float)a.cg);
+            means[2 * g + 1] = with_hat / ((float)a.HW * (float)a.cg);
+        }
+    }
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     const T* const dy = static_cast<const T*>(a.dy) + s.n * a.pdy.sn + s.c0;
     T* const dx = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
@@ -393,9 +415,9 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
         __syncthreads();
         channel_tables(a, s, first, here, shared, table, kThreads);
         for (int c = threadIdx.x; c < here; c += kThreads) {
-            const float* const at = a.group_sums + ((int64_t)s.n * a.groups + s.c0 / a.cg + a.by_cg.div(first + c)) * 2;
-            shared[4 * table + c] = at[0];
-            shared[5 * table + c] = at[1];
+            const int g = a.by_cg.div(first + c);
+            shared[4 * table + c] = means[2 * g];
+            shared[5 * table + c] = means[2 * g + 1];
         }
         __syncthreads();
         if (col >= s.columns) continue;
@@ -420,7 +442,6 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
             }
         });
     }
-    if (s.n == 0 && s.slab == 0) parameter_gradients(a);
 }
 
 // ---- resident: a work-group holds its chunk of an image, at most R vectors of four channels a thread (of eight, the
