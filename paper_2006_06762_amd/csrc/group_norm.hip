@@ -124,7 +124,7 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
         const int resident_rows = p.resident / held_columns, each = (a.HW + resident_rows - 1) / resident_rows;
         p.held = each <= 4 ? 4 : each <= 8 ? 8 : 16;
         const size_t groups = a.chunk / a.cg;
-        p.resident_lds = sizeof(float) * (backward ? 6 * (size_t)table_floats(a.chunk) + table_floats(2 * groups) + 2 * (size_t)resident_rows * a.chunk
+        p.resident_lds = sizeof(float) * (backward ? 6 * (size_t)table_floats(a.chunk) + table_floats(2 * groups) + 2 * (size_t)resident_rows * a.chunk + p.resident
                                                    : 3 * (size_t)table_floats(a.chunk) + table_floats(groups) + (size_t)resident_rows * a.chunk);
         a.slabs = 1;
         a.slab_pixels = a.HW;

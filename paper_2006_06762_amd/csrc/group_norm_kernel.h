@@ -547,7 +547,7 @@ __global__ __launch_bounds__(1024) void backward_resident_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
     constexpr int V = kHeldChannels;
-    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, [2][channels], [groups] of two means, [rows][2][channels]
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, [2][channels], [groups] of two means, [rows][2][channels], [threads]
     const int threads = blockDim.x;
     const Place s(a, V, threads);
     const int table = table_floats(s.channels), groups = s.channels / a.cg;
@@ -592,11 +592,21 @@ __global__ __launch_bounds__(1024) void backward_resident_kernel(const Args a)
         }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * s.channels; e += threads) {
+    // the threads of a channel share the rows
+    float* const shares_of = part + 2 * s.rows * s.channels;
+    for (int base = 0; base < 2 * s.channels; base += threads) {
+        const int here = min(2 * s.channels - base, threads), shares = threads / here, share = threadIdx.x / here, e = base + threadIdx.x - share * here;
         const int which = e >= s.channels, c = e - which * s.channels;
         float v = 0.f;
-#pragma unroll 8
-        for (int r = 0; r < s.rows; ++r) v += part[(2 * r + which) * s.channels + c];
+        if (share < shares) {
+#pragma unroll 4
+            for (int r = share; r < s.rows; r += shares) v += part[(2 * r + which) * s.channels + c];
+        }
+        __syncthreads();
+        shares_of[threadIdx.x] = v;
+        __syncthreads();
+        if (share > 0) continue;
+        for (int i = 1; i < shares; ++i) v += shares_of[i * here + threadIdx.x];
         a.sums[((int64_t)s.n * 2 + which) * a.C + s.c0 + c] = v;
         total[which * table + c] = v * shared[2 * table + c];
     }
