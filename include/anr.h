@@ -320,7 +320,8 @@ typedef struct {
 /* y = act((x - mean) rstd gamma + beta) with the mean and rstd = 1/sqrt(var + eps)
  * (var: the mean square difference) of each group of each image over its pixels and
  * channels.  gamma, beta: C each, NULL for ones and zeros.  mean, rstd: [N, groups]
- * float32 outputs for a backward call, or NULL.  eps is finite and not negative. */
+ * float32 outputs for a backward call, or NULL.  eps is finite and not negative.  y may be
+ * x itself, with the same strides. */
 anr_status anr_group_norm(const anr_group_norm_desc *desc, const void *x, const void *gamma, const void *beta,
                           float eps, void *y, float *mean, float *rstd, void *ws, size_t ws_bytes, void *hip_stream);
 
@@ -328,7 +329,7 @@ anr_status anr_group_norm(const anr_group_norm_desc *desc, const void *x, const 
  * xhat = (x - mean) rstd and dz = dy act'(xhat gamma + beta), dgamma = sum dz xhat and
  * dbeta = sum dz over images and pixels, and dx = rstd (dz gamma - a - xhat b) with the
  * group's means a of dz gamma and b of dz gamma xhat.  dx, dgamma, dbeta: NULL for what is
- * not wanted, not all three. */
+ * not wanted, not all three.  dx may be x or dy itself, with the same strides. */
 anr_status anr_group_norm_backward(const anr_group_norm_desc *desc, const void *dy, const void *x, const void *gamma,
                                    const void *beta, const float *mean, const float *rstd, void *dx, void *dgamma,
                                    void *dbeta, void *ws, size_t ws_bytes, void *hip_stream);

@@ -130,9 +130,9 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
         a.slab_pixels = a.HW;
     }
     const size_t of_groups = p.resident ? 0 : sizeof(float) * 2 * (size_t)g.N * a.slabs * g.groups;
-    p.bytes = of_groups + (backward ? sizeof(float) * 2 * (size_t)g.N * a.slabs * g.C : 0);
+    p.bytes = of_groups + (backward ? sizeof(float) * 2 * (size_t)g.N * a.slabs * g.C : of_groups / (2 * (size_t)a.slabs));
     a.ws = static_cast<float*>(g.ws);
-    a.sums = a.ws + of_groups / sizeof(float);
+    a.first = a.sums = a.ws + of_groups / sizeof(float);
     return p;
 }
 

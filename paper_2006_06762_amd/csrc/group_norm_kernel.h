@@ -39,6 +39,7 @@ struct Args {
     void *dgamma, *dbeta;
     float *mean, *rstd;
     float* ws;                      // mean and M2 (backward: the two sums) of each group over the slabs, [N][slabs][groups][2]
+    float* first;                   // forward: the value that each group's are relative to, [N][groups] (x may be overwritten in place)
     float* sums;                    // backward: sums of each channel over the slabs, [N][slabs][2][C]
     Pixels px, pdy, py;
     FastDiv by_w, by_cg;
@@ -190,6 +191,7 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(const Args a)
             float* const at = a.ws + 2 * (((int64_t)s.n * a.slabs + s.slab) * a.groups + s.c0 / a.cg + g);
             at[0] = mean;
             at[1] = q;
+            if (s.slab == 0) a.first[(int64_t)s.n * a.groups + s.c0 / a.cg + g] = to_float(x[g * a.cg]);
         }
     }
 }
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
         }
         const float rstd = 1.f / sqrtf(wave_sum(q) / ((float)a.HW * (float)a.cg) + a.eps);
         if (lane == 0) {
-            const float whole = mean + to_float(static_cast<const T*>(a.x)[s.n * a.px.sn + s.c0 + g * a.cg]);
+            const float whole = mean + a.first[(int64_t)s.n * a.groups + g0 + g];
             lds[2 * g] = whole;
             lds[2 * g + 1] = rstd;
             if (s.slab == 0 && a.mean) a.mean[(int64_t)s.n * a.groups + g0 + g] = whole;

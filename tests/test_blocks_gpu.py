@@ -176,6 +176,24 @@ def test_group_norm_without_what_is_not_wanted(anr):
     assert torch.equal(y3, y.flatten(2))
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("shape", [(2, 64, 9, 7, 8), (2, 64, 90, 70, 8), (1, 30, 70, 90, 3), (1, 2560, 9, 60, 2)])
+def test_group_norm_in_place(anr, t, shape):
+    N, C, H, W, groups = shape
+    r = rng(11)
+    x, dy = images(r.normal(size=(N, C, H, W)) + 3, TYPES[t]), images(r.normal(size=(N, C, H, W)), TYPES[t])
+    mean, rstd = nans(N, groups, dtype=torch.float32), nans(N, groups, dtype=torch.float32)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    anr.group_norm(x, groups, y, act=anr.ANR_ACT_SILU, mean=mean, rstd=rstd)
+    anr.group_norm_backward(dy, x, groups, None, None, mean, rstd, dx, act=anr.ANR_ACT_SILU)
+    for _ in range(3):
+        z, d, e = (torch.empty_like(x).copy_(v) for v in (x, dy, x))
+        anr.group_norm(z, groups, z, act=anr.ANR_ACT_SILU)
+        anr.group_norm_backward(d, x, groups, None, None, mean, rstd, d, act=anr.ANR_ACT_SILU)
+        anr.group_norm_backward(dy, e, groups, None, None, mean, rstd, e, act=anr.ANR_ACT_SILU)
+        assert torch.equal(z, y) and torch.equal(d, dx) and torch.equal(e, dx)
+
+
 def test_group_norm_of_one_value_everywhere(anr):
     x = images(np.full((2, 16, 5, 5), 3.0), torch.bfloat16)
     y, mean, rstd = torch.empty_like(x), nans(2, 2, dtype=torch.float32), nans(2, 2, dtype=torch.float32)
@@ -540,6 +558,33 @@ def test_gated_ff_slope_is_that_of_the_forward_pass(anr):
         size = float((grads[i].double() * v.double()).abs().sum())
         # roundings of 720 outputs of about 2^-22 over the step, as a random sum; the third derivative's part, step^2
         assert abs(got - want) <= size * (step ** 2 + 720 ** 0.5 * 2.0 ** -21 / step), i
+
+
+def test_gated_ff_offsets_beyond_32_bits(anr):
+    """Four million tokens: operands of more than 2^31 bytes, in float32 more than the split GEMM's offsets reach."""
+    T, C, F = (1 << 22) - 1, 136, 16
+    for t in (torch.float32, torch.bfloat16):
+        r = rng(41)
+        wg, wu, wd = (matrix(r, *s, t, 0.1) for s in ((F, C), (F, C), (C, F)))
+        x, y = torch.zeros(T, C, dtype=t, device="cuda"), torch.empty(T, C, dtype=t, device="cuda")
+        gate, up = torch.empty(T, F, dtype=t, device="cuda"), torch.empty(T, F, dtype=t, device="cuda")
+        x[-5:] = matrix(r, 5, C, t)
+        anr.gated_ff(x, wg, wu, wd, y, gate=gate, up=up)
+        small = torch.zeros(70, C, dtype=t, device="cuda")
+        small[-5:] = x[-5:]
+        want = anr.gated_ff(small, wg, wu, wd, torch.empty_like(small))
+        # (the same products by another kernel: roundings of sums of 136 and 16 products, and of h)
+        size = 1e-4 if t is torch.float32 else 2e-2
+        assert torch.allclose(y[-5:].float(), want[-5:].float(), rtol=size, atol=size) and not y[:-5].any()
+        dx, dw = torch.empty_like(y), [torch.empty_like(v) for v in (wg, wu, wd)]
+        anr.gated_ff_backward(x, x, wg, wu, wd, gate, up, dx, *dw)
+        g, u = gate[-70:].contiguous(), up[-70:].contiguous()
+        dsmall, dwsmall = torch.empty_like(small), [torch.empty_like(v) for v in (wg, wu, wd)]
+        anr.gated_ff_backward(small, small, wg, wu, wd, g, u, dsmall, *dwsmall)
+        assert torch.allclose(dx[-5:].float(), dsmall[-5:].float(), rtol=size, atol=size) and not dx[:-5].any()
+        assert all(torch.allclose(a.float(), b.float(), rtol=size, atol=size) for a, b in zip(dw, dwsmall))
+        del x, y, gate, up, dx
+        torch.cuda.empty_cache()
 
 
 def test_gated_ff_refuses(anr):
