@@ -6,10 +6,12 @@
 // (v_mfma_f32_32x32x16), and walks k in chunks of 64: global -> registers -> LDS -> operands, with two LDS buffers, so that
 // one is multiplied while the other is filled and the loads of the chunk after that are on their way.
 //
-// LDS.  K_ROWS: 128 bytes of k per row, 16-byte units exchanged by row (unit ^ row % 8), so that eight rows' same unit, which an
-// operand read takes together, lie in different banks.  K_COLUMNS: rows of k as they come, 64 bytes apart from the next
-// one beyond their length; ds_read_b64_tr_b16 turns 4 k x 16 columns as it reads, each lane gets four k of its column,
-// and the four rows of such a read are in different banks.
+// LDS.  K_ROWS: 128 bytes of k per row, 16-byte units exchanged by pairs of rows (unit ^ row / 2 % 8): two rows fill the 64
+// banks, and sixteen rows' same unit, which an operand read takes together, lie in different ones (exchanged by row % 8, rows
+// eight apart met in theirs: gate and up of 4096 x 1024 -> 2816 with tiles of 128 in 61 us, so 58; with tiles of 256, which
+// wait for the matrix pipes, no difference).  K_COLUMNS: rows of k as they come, 64 bytes apart from the next one beyond
+// their length; ds_read_b64_tr_b16 turns 4 k x 16 columns as it reads, each lane gets four k of its column, and the four
+// rows of such a read are in different banks.
 //
 // W is the instruction's first operand: register r of a lane is then n = 8 (r / 4) + 4 (lane / 32) + r % 4 of the block and
 // m = lane % 32: four neighbouring columns of a row of D.
@@ -165,7 +167,7 @@ struct Stager {
 #pragma unroll
         for (int i = FIRST; i < LAST; ++i) {
             const int r = first + i * (NT / ROW_UNITS);
-            const int at = KIND == K_ROWS ? r * Image<KIND, R>::ROW + ((unit ^ (r & 7)) * 16) : r * Image<KIND, R>::ROW + unit * 16;
+            const int at = KIND == K_ROWS ? r * Image<KIND, R>::ROW + ((unit ^ ((r >> 1) & 7)) * 16) : r * Image<KIND, R>::ROW + unit * 16;
             *reinterpret_cast<u32x4*>(lds + at) = data[i];
         }
     }
@@ -177,7 +179,7 @@ __device__ __forceinline__ u32x4 operand(const char* lds, int row0, int step, in
 {
     if (KIND == K_ROWS) {
         const int r = row0 + (lane & 31), u = 2 * step + (lane >> 5);
-        return *reinterpret_cast<const u32x4*>(lds + r * Image<KIND, R>::ROW + ((u ^ (r & 7)) * 16));
+        return *reinterpret_cast<const u32x4*>(lds + r * Image<KIND, R>::ROW + ((u ^ ((r >> 1) & 7)) * 16));
     }
     typedef __attribute__((address_space(3))) s16x4 lds_t;
     const int j = lane & 15;
