@@ -304,7 +304,8 @@ anr_status anr_nrm(const anr_nrm_desc *desc, const float *x, float *out,
  * x_stride is x's; y_stride that of y, or of dy in the backward call; dx_stride that
  * of dx.  Every stride >= 1 for an extent above 1 and no view overlaps itself.
  * Channels are cut into `groups` equal runs; C / groups <= 8192.  param_dtype is the
- * type of gamma, beta, dgamma and dbeta: float32 or `dtype`.
+ * type of gamma, beta, dgamma and dbeta: float32 or `dtype`.  N <= 65535, H W <= 2^30,
+ * C <= 2^20.
  */
 typedef struct {
     int32_t N, H, W, C;
@@ -366,7 +367,7 @@ typedef struct {
 } anr_rotary_desc;
 
 /* q_out and k_out: turned q and k; each may be its input itself, with the same strides.  k
- * and k_out may be NULL where Hk is 0.  D <= 2048. */
+ * and k_out may be NULL where Hk is 0.  D <= 2048, B S < 2^24. */
 anr_status anr_rotary(const anr_rotary_desc *desc, const void *q, const void *k, const void *positions,
                       const float *inv_freq, void *q_out, void *k_out, void *ws, size_t ws_bytes, void *hip_stream);
 

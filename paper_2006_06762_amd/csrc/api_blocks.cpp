@@ -9,7 +9,8 @@
 
 namespace {
 
-constexpr int64_t kFarStride = (int64_t)1 << 40;       // strides below it: no product here or in the launchers overflows
+// A stride of 2^40 elements, or one that takes its extent beyond 2^58: below both no offset, nor the sum of three, overflows.
+bool far(int64_t stride, int64_t extent) { return stride >= (int64_t)1 << 40 || stride >= ((int64_t)1 << 58) / extent; }
 
 bool valid_type(int t) { return t == ANR_F32 || t == ANR_F16 || t == ANR_BF16; }
 bool valid_act(int a) { return a >= ANR_ACT_NONE && a <= ANR_ACT_GELU_TANH; }
@@ -46,7 +47,8 @@ anr_status check_group_norm(const anr_group_norm_desc* d, bool backward, anr::Gr
     if (!d) return ANR_ERR_NULL;
     if (d->N < 0 || d->H < 0 || d->W < 0 || d->C < 1 || d->groups < 1 || d->C % d->groups != 0) return ANR_ERR_INVALID_ARG;
     if (!valid_act(d->act) || !valid_type(d->dtype) || (d->param_dtype != ANR_F32 && d->param_dtype != d->dtype)) return ANR_ERR_INVALID_ARG;
-    if (d->N > 65535 || d->C > 1 << 22 || d->C / d->groups > 8192 || (int64_t)d->H * d->W >= (int64_t)1 << 31) return ANR_ERR_UNSUPPORTED;
+    // chunks of channels and images are extents of the grid; pixels are counted in 32 bits, a step beyond the last one too
+    if (d->N > 65535 || d->C > 1 << 20 || d->C / d->groups > 8192 || (int64_t)d->H * d->W > (int64_t)1 << 30) return ANR_ERR_UNSUPPORTED;
     const int64_t extent[3] = {d->N, d->H, d->W};
     const int64_t* const in[3] = {d->x_stride, d->y_stride, d->dx_stride};
     int64_t* const out[3] = {a->xs, backward ? a->dys : a->ys, a->ys};
@@ -60,7 +62,7 @@ anr_status check_group_norm(const anr_group_norm_desc* d, bool backward, anr::Gr
             for (int i = 0; i < 3; ++i) {
                 if (extent[i] <= 1) continue;
                 if (s[i] < 1) return ANR_ERR_INVALID_ARG;
-                if (s[i] >= kFarStride) return ANR_ERR_UNSUPPORTED;
+                if (far(s[i], extent[i])) return ANR_ERR_UNSUPPORTED;
             }
             if (!apart(extent, s, d->C)) return ANR_ERR_INVALID_ARG;
         }
@@ -81,6 +83,8 @@ anr_status check_group_norm(const anr_group_norm_desc* d, bool backward, anr::Gr
     return ANR_OK;
 }
 
+bool same_strides(const int64_t* a, const int64_t* b) { return a[0] == b[0] && a[1] == b[1] && a[2] == b[2]; }
+
 bool empty(const anr::GroupNormArgs& a) { return a.N == 0 || a.H == 0 || a.W == 0; }
 
 // ---- rotary positions
@@ -96,8 +100,8 @@ anr_status check_rotary(const anr_rotary_desc* d, anr_rotary_desc* out)
     }
     if (2 * pairs > d->D || !valid_type(d->dtype) || d->pairing < ANR_ROTARY_HALVES || d->pairing > ANR_ROTARY_SECTION_HALVES) return ANR_ERR_INVALID_ARG;
     if (d->inverse < 0 || d->inverse > 1 || d->pos_type < ANR_POS_I32 || d->pos_type > ANR_POS_F32 || d->reserved != 0) return ANR_ERR_INVALID_ARG;
-    // tokens are counted in 32 bits
-    if (d->D > 2048 || (int64_t)d->H + d->Hk > 65536 || (int64_t)d->B * d->S >= (int64_t)1 << 31) return ANR_ERR_UNSUPPORTED;
+    // a grid has 2^32 threads, of which a token can take 256
+    if (d->D > 2048 || (int64_t)d->H + d->Hk > 65536 || (int64_t)d->B * d->S >= (int64_t)1 << 24) return ANR_ERR_UNSUPPORTED;
     *out = *d;
     int64_t* const strides[4] = {out->q_stride, out->k_stride, out->q_out_stride, out->k_out_stride};
     for (int t = 0; t < 4; ++t) {
@@ -115,15 +119,18 @@ anr_status check_rotary(const anr_rotary_desc* d, anr_rotary_desc* out)
                 continue;
             }
             if (s[i] < 0) return ANR_ERR_INVALID_ARG;
-            if (s[i] >= kFarStride) return ANR_ERR_UNSUPPORTED;
+            if (far(s[i], extent[i])) return ANR_ERR_UNSUPPORTED;
         }
         if (t >= 2 && !apart(extent, given, d->D)) return ANR_ERR_INVALID_ARG;
     }
     const int64_t extent[3] = {d->axes, d->B, d->S};
     for (int i = 0; i < 3; ++i) {
-        if (extent[i] <= 1) out->pos_stride[i] = 0;
+        if (extent[i] <= 1) {
+            out->pos_stride[i] = 0;
+            continue;
+        }
         if (out->pos_stride[i] < 0) return ANR_ERR_INVALID_ARG;
-        if (out->pos_stride[i] >= kFarStride) return ANR_ERR_UNSUPPORTED;
+        if (far(out->pos_stride[i], extent[i])) return ANR_ERR_UNSUPPORTED;
     }
     return ANR_OK;
 }
@@ -192,6 +199,7 @@ anr_status anr_group_norm(const anr_group_norm_desc* d, const void* x, const voi
     if (!element_aligned(x, d->dtype) || !element_aligned(y, d->dtype) || !element_aligned(gamma, d->param_dtype) || !element_aligned(beta, d->param_dtype) ||
         !element_aligned(mean, ANR_F32) || !element_aligned(rstd, ANR_F32))
         return ANR_ERR_INVALID_ARG;
+    if (x && x == y && !same_strides(a.xs, a.ys)) return ANR_ERR_INVALID_ARG;
     st = check_workspace(ws, ws_bytes, anr::group_norm_workspace_bytes(a, false));
     if (st != ANR_OK) return st;
     a.x = x;
@@ -217,6 +225,7 @@ anr_status anr_group_norm_backward(const anr_group_norm_desc* d, const void* dy,
         !element_aligned(beta, d->param_dtype) || !element_aligned(dgamma, d->param_dtype) || !element_aligned(dbeta, d->param_dtype) || !element_aligned(mean, ANR_F32) ||
         !element_aligned(rstd, ANR_F32))
         return ANR_ERR_INVALID_ARG;
+    if (dx && ((dx == x && !same_strides(a.xs, a.ys)) || (dx == dy && !same_strides(a.dys, a.ys)))) return ANR_ERR_INVALID_ARG;
     st = check_workspace(ws, ws_bytes, anr::group_norm_workspace_bytes(a, true));
     if (st != ANR_OK) return st;
     a.dy = dy;
@@ -247,8 +256,7 @@ anr_status anr_rotary(const anr_rotary_desc* d, const void* q, const void* k, co
     if (!element_aligned(q, d->dtype) || !element_aligned(k, d->dtype) || !element_aligned(q_out, d->dtype) || !element_aligned(k_out, d->dtype) ||
         !element_aligned(inv_freq, ANR_F32) || (reinterpret_cast<uintptr_t>(positions) & (d->pos_type == ANR_POS_I64 ? 7 : 3)) != 0)
         return ANR_ERR_INVALID_ARG;
-    for (int i = 0; i < 3; ++i)
-        if ((q && q == q_out && a.d.q_stride[i] != a.d.q_out_stride[i]) || (k && k == k_out && a.d.k_stride[i] != a.d.k_out_stride[i])) return ANR_ERR_INVALID_ARG;
+    if ((q && q == q_out && !same_strides(a.d.q_stride, a.d.q_out_stride)) || (k && k == k_out && !same_strides(a.d.k_stride, a.d.k_out_stride))) return ANR_ERR_INVALID_ARG;
     a.q = q;
     a.k = k;
     a.positions = positions;

@@ -167,6 +167,40 @@ def test_workspace_size_refuses_what_the_calls_refuse():
             B.workspace_size(op, d)
 
 
+def test_extents_and_strides_whose_offsets_overflow():
+    """Views of more than 2^58 elements, and extents beyond the grids' and the kernels' counters, by calls and sizes alike."""
+    big = [(B.ANR_OP_GROUP_NORM, norm_desc(N=1, H=1, W=1 << 29, C=4, x_stride=(1, 1, 1 << 39))),
+           (B.ANR_OP_GROUP_NORM, norm_desc(N=1, H=1 << 29, W=1, C=4, y_stride=(1, 1 << 39, 1))),
+           (B.ANR_OP_GROUP_NORM_BACKWARD, norm_desc(N=60000, H=1, W=1, C=4, dx_stride=((1 << 40) - 1000000, 1, 4), x_stride=(1 << 43, 1, 4))),
+           (B.ANR_OP_GROUP_NORM, norm_desc(N=1, H=1 << 15, W=(1 << 15) + 1, C=4)),
+           (B.ANR_OP_GROUP_NORM_BACKWARD, norm_desc(C=(1 << 20) + 4, groups=(1 << 20) + 4)),
+           (B.ANR_OP_ROTARY, rotary_desc(B=1, S=(1 << 24) - 1, q_stride=(1, 1 << 39, 32))),
+           (B.ANR_OP_ROTARY, rotary_desc(B=1, S=(1 << 24) - 1, pos_stride=(0, 0, 1 << 39))),
+           (B.ANR_OP_ROTARY, rotary_desc(B=1 << 12, S=1 << 12))]
+    for op, d in big:
+        with pytest.raises(B.AnrError) as e:
+            B.workspace_size(op, d)
+        assert e.value.status == UNSUPPORTED, op
+    assert norm(big[0][1]) == UNSUPPORTED and norm_backward(big[4][1]) == UNSUPPORTED and rotary(big[5][1]) == UNSUPPORTED
+    B.workspace_size(B.ANR_OP_GROUP_NORM, norm_desc(N=1, H=1 << 15, W=1 << 15, C=4))
+    B.workspace_size(B.ANR_OP_GROUP_NORM, norm_desc(C=1 << 20, groups=1 << 20))
+    B.workspace_size(B.ANR_OP_ROTARY, rotary_desc(B=1, S=(1 << 24) - 1))
+
+
+def test_group_norm_in_place_takes_the_same_strides():
+    P2 = ctypes.c_void_p(0x20000)
+    wide = (960, 240, 48)
+    d = norm_desc(x_stride=wide)
+    assert norm(d) == INVALID and norm(d, y=P2) == WORKSPACE
+    assert norm(norm_desc(x_stride=wide, y_stride=wide)) == WORKSPACE
+    assert norm_backward(d, x=P, dy=P2, dx=P) == INVALID and norm_backward(d, x=P, dy=P2, dx=P2) == WORKSPACE
+    d = norm_desc(y_stride=wide)                                   # dy's
+    assert norm_backward(d, x=P, dy=P2, dx=P2) == INVALID and norm_backward(d, x=P, dy=P2, dx=P) == WORKSPACE
+    # the strides of single extents say nothing
+    d = norm_desc(N=1, H=1, W=5, x_stride=(7, 9, 24))
+    assert norm(d) == WORKSPACE
+
+
 def test_binding_refuses_host_tensors_and_other_types():
     x = torch.zeros(2, 8, 3, 3).to(memory_format=torch.channels_last)
     with pytest.raises(TypeError):

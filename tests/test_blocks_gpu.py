@@ -516,6 +516,29 @@ def test_gated_ff_without_what_is_not_wanted(anr):
                     assert all(torch.equal(part[j], every[j]) for j in keep)
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("T,C,F", [(130, 64, 96), (77, 35, 51)])
+def test_gated_ff_halves_of_one_tensor_in_either_order(anr, t, T, C, F):
+    """Gate's and up's weights, pre-activations and gradients as halves of one tensor, the second before the first too."""
+    r, t = rng(47), TYPES[t]
+    x, wd, dy = matrix(r, T, C, t), matrix(r, C, F, t, F ** -0.5), matrix(r, T, C, t)
+    weights, results = matrix(r, 2 * F, C, t, C ** -0.5), []
+    for first in (None, 0, 1):
+        if first is None:
+            wg, wu = weights[:F].clone(), weights[F:].clone()
+            gate, up, dwg, dwu = empty_matrix(T, F, t), empty_matrix(T, F, t), empty_matrix(F, C, t), empty_matrix(F, C, t)
+        else:
+            both = weights if first == 0 else torch.cat([weights[F:], weights[:F]])
+            pre, grads = empty_matrix(2 * T, F, t), empty_matrix(2 * F, C, t)
+            (wg, wu), (gate, up), (dwg, dwu) = ((v[n:], v[:n])[::1 if first else -1] for v, n in ((both, F), (pre, T), (grads, F)))
+        y, dx, dwd = empty_matrix(T, C, t), empty_matrix(T, C, t), empty_matrix(C, F, t)
+        anr.gated_ff(x, wg, wu, wd, y, anr.ANR_ACT_SILU, gate, up)
+        anr.gated_ff_backward(dy, x, wg, wu, wd, gate, up, dx, dwg, dwu, dwd, anr.ANR_ACT_SILU)
+        results.append([v.clone() for v in (y, gate, up, dx, dwg, dwu, dwd)])
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+
+
 def test_gated_ff_of_no_tokens(anr):
     for t in TYPES.values():
         r = rng(38)
