@@ -304,7 +304,7 @@ anr_status anr_nrm(const anr_nrm_desc *desc, const float *x, float *out,
  * x_stride is x's; y_stride that of y, or of dy in the backward call; dx_stride that
  * of dx.  Every stride >= 1 for an extent above 1 and no view overlaps itself.
  * Channels are cut into `groups` equal runs; C / groups <= 8192.  param_dtype is the
- * type of gamma, beta, dgamma and dbeta: float32 or `dtype`.  N <= 65535, H W <= 2^30,
+ * type of gamma, beta, dgamma and dbeta: float32 or `dtype`.  N < 65535, H W <= 2^30,
  * C <= 2^20.
  */
 typedef struct {

@@ -48,7 +48,7 @@ anr_status check_group_norm(const anr_group_norm_desc* d, bool backward, anr::Gr
     if (d->N < 0 || d->H < 0 || d->W < 0 || d->C < 1 || d->groups < 1 || d->C % d->groups != 0) return ANR_ERR_INVALID_ARG;
     if (!valid_act(d->act) || !valid_type(d->dtype) || (d->param_dtype != ANR_F32 && d->param_dtype != d->dtype)) return ANR_ERR_INVALID_ARG;
     // chunks of channels and images are extents of the grid; pixels are counted in 32 bits, a step beyond the last one too
-    if (d->N > 65535 || d->C > 1 << 20 || d->C / d->groups > 8192 || (int64_t)d->H * d->W > (int64_t)1 << 30) return ANR_ERR_UNSUPPORTED;
+    if (d->N >= 65535 || d->C > 1 << 20 || d->C / d->groups > 8192 || (int64_t)d->H * d->W > (int64_t)1 << 30) return ANR_ERR_UNSUPPORTED;
     const int64_t extent[3] = {d->N, d->H, d->W};
     const int64_t* const in[3] = {d->x_stride, d->y_stride, d->dx_stride};
     int64_t* const out[3] = {a->xs, backward ? a->dys : a->ys, a->ys};

@@ -40,6 +40,13 @@ int common_multiple(int a, int b)
 // Strides that keep 16-byte units whole.
 bool whole_units(const void* p, const int64_t* s, int V) { return is_aligned16(p) && s[0] % V == 0 && s[1] % V == 0 && s[2] % V == 0; }
 
+// Vectors that a thread of a full work-group holds of a chunk, which has at most 256 columns of them.
+int held_by(const Args& a)
+{
+    const int rows = kResidentThreads / (a.chunk / kHeldChannels);
+    return (a.HW + rows - 1) / rows;
+}
+
 // Where the resident kernels run: a chunk of an image fits the registers of a work-group (vectors of four channels a thread).
 // Timed with groups of 8 and 10 channels of 256 and 320, batch 1 to 32, SiLU, against the kernels that read twice (us, resident / not):
 // forward, 16 bits, 14^2 7.9 / 14, 28^2 (12 to 16 vectors) 14 / 15; float32 20^2 10 / 15, 28^2 (7) 14.5 / 15.5, but 40^2 (13) 19 / 13
@@ -47,11 +54,9 @@ bool whole_units(const void* p, const int64_t* s, int V) { return is_aligned16(p
 // 22 / 19. So: eight vectors, and sixteen in the forward pass of 16-bit types or with work-groups for most CUs.
 bool resident_pays(const GroupNormArgs& g, const Args& a, bool backward, int64_t work_groups)
 {
-    const int columns = a.chunk / kHeldChannels;
-    if (columns > 256) return false;
-    const int rows = kResidentThreads / columns;
+    if (a.chunk / kHeldChannels > 256) return false;
     const int most = !backward && (g.dtype != ANR_F32 || work_groups >= 192) ? 16 : 8;
-    return (a.HW + rows - 1) / rows <= most;
+    return held_by(a) <= most;
 }
 
 Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
@@ -91,16 +96,20 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
     auto chunk_of = [&](int bytes) { return std::min(g.C, least * std::max(1, (bytes / es + least - 1) / least)); };
     a.chunk = chunk_of(128);
     p.chunks = (g.C + a.chunk - 1) / a.chunk;
-    // Resident kernels with work-groups for less than every CU take chunks of 64 bytes, float32 ones only where there are fewer still: 20^2 x 256
-    // float32 backward, batch 1, 14.8 -> 11.0 us, 28^2 18.6 -> 12.4, batch 16 18.8 -> 20; bf16 20^2 14.8 -> 13.0, batch 16 15.9 -> 13.7, 28^2
-    // 22 -> 17 (19 for the kernels that read twice).
-    if (vector && chunk_of(64) < a.chunk && (int64_t)p.chunks * g.N < (g.dtype == ANR_F32 ? 128 : 256) &&
-        (g.dtype != ANR_F32 || resident_pays(g, a, backward, (int64_t)p.chunks * g.N))) {
+    // Resident kernels take chunks of 64 bytes where work-groups of 128 would be half the CUs or fewer: the backward pass, and the forward one where a thread
+    // has more than four vectors. 256 channels, chunks of 128 / 64 bytes, forward and backward (us): float32 14^2 x 16 images 9.2 9.9 / 9.8 10.0, 20^2 x 1
+    // 10.0 10.5 / 10.7 10.0, 28^2 x 1 12.8 14.3 / 11.8 11.5, x 16 15.8 18.6 / 15.2 16.4; bf16 14^2 x 32 8.0 11.7 / 8.6 10.4, 20^2 x 16 9.7 15.5 / 9.0
+    // 12.4, 48 images (more than half the CUs) 11.1 18.1 / 17.2 18.9. Of maps that only the halves hold, those of 16-bit types with 64 work-groups, forward:
+    // against the kernels that read twice bf16 36^2 x 16 17.3 / 15.1, but 40^2 x 1 12.2 / 14.0, and backward 28^2 x 16 15.6 / 17.4.
+    const int64_t work_groups = (int64_t)p.chunks * g.N;
+    if (vector && chunk_of(64) < a.chunk && work_groups <= 128 &&
+        (resident_pays(g, a, backward, work_groups) ? backward || held_by(a) > 4 : !backward && g.dtype != ANR_F32 && work_groups >= 64)) {
         Args half = a;
         half.chunk = chunk_of(64);
-        if (resident_pays(g, half, backward, (int64_t)p.chunks * g.N)) {
+        if (resident_pays(g, half, backward, work_groups)) {
             a.chunk = half.chunk;
             p.chunks = (g.C + a.chunk - 1) / a.chunk;
+            a.halves = true;
         }
     }
     const int line = 128 / es;
@@ -113,6 +122,9 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
     int64_t slabs = std::min((1024 + others - 1) / others, (int64_t)a.HW / ((es == 4 ? 4 : 8) * rows));
     slabs = std::max(slabs, std::min((256 + others - 1) / others, (int64_t)a.HW / (2 * rows)));
     slabs = std::max<int64_t>(1, std::min<int64_t>(slabs, 128));
+    // Work-groups go round-robin to the eight XCDs: those that share the lines at a chunk's ends to the same one (4 x 95 x 63 x 320 bf16, chunks of 160 bytes,
+    // 29 / 24 slabs, forward 21.7 / 20.4 us, backward 27.8 / 25.3; level where chunks are whole lines).
+    if (slabs > 8) slabs = slabs / 8 * 8;
     a.slab_pixels = (int)((a.HW + slabs - 1) / slabs);
     a.slabs = (a.HW + a.slab_pixels - 1) / a.slab_pixels;
     p.lds = sizeof(float) * (2 * (size_t)rows * a.chunk + (backward ? 4 : 1) * (size_t)p.table);
@@ -254,7 +266,7 @@ hipError_t launch_group_norm_backward(const GroupNormArgs& g, hipStream_t stream
                 if (e != hipSuccess) return e;
                 if (!g.y) return launch_kernel(backward_parameters_kernel, dim3(1, p.chunks, 1), dim3(kThreads), 0, stream, p.args);
                 if (apply_lds > 65536) e = raise_lds_limit(reinterpret_cast<const void*>(backward_apply_kernel<T, V, ACT>), apply_lds, limit_apply);
-                return e != hipSuccess ? e : launch_kernel(backward_apply_kernel<T, V, ACT>, dim3(grid.x + (g.dgamma || g.dbeta ? 1 : 0), grid.y, grid.z), dim3(kThreads), apply_lds, stream, p.args);
+                return e != hipSuccess ? e : launch_kernel(backward_apply_kernel<T, V, ACT>, dim3(grid.x, grid.y, grid.z + (g.dgamma || g.dbeta ? 1 : 0)), dim3(kThreads), apply_lds, stream, p.args);
             });
         });
     });

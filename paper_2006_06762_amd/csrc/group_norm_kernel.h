@@ -47,6 +47,7 @@ struct Args {
     int N, HW, W, C, groups, cg, flat, param_dtype;
     int chunk;                      // channels of a chunk: whole groups
     int slabs, slab_pixels;
+    bool halves;                    // resident: a chunk's pixel is half a line
     bool streaming;                 // y's stores go past L2: a chunk's pixel is whole lines of 128 bytes
 };
 
@@ -58,7 +59,16 @@ struct Place {
     {
         slab = blockIdx.x;
         n = blockIdx.z;
-        c0 = blockIdx.y * a.chunk;
+        int c = blockIdx.y;
+        if (a.halves) {                 // of sixteen work-groups i and i + 8, which one XCD has, take neighbouring halves
+            const int chunks = (int)gridDim.y, i = c + chunks * n, of16 = i & ~15;
+            if (of16 + 16 <= chunks * a.N) {
+                const int j = of16 + 2 * (i & 7) + ((i >> 3) & 1);
+                n = j / chunks;
+                c = j - n * chunks;
+            }
+        }
+        c0 = c * a.chunk;
         channels = min(a.chunk, a.C - c0);
         p0 = slab * a.slab_pixels;
         p1 = min(a.HW, p0 + a.slab_pixels);
@@ -382,14 +392,15 @@ __global__ __launch_bounds__(kThreads) void backward_parameters_kernel(const Arg
     parameter_gradients(a, lds, kThreads);
 }
 
-// Second kernel: dx, and in work-groups of their own, behind the first image's slabs, the parameters' gradients.
+// Second kernel: dx, and in work-groups of their own, behind the last image's, the parameters' gradients (behind the slabs, where they moved the others to
+// other XCDs than those whose L2 has what the first kernel read there, 2 x 96^2 x 320 in float32 took 32 us, so 27).
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
     extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, those of the group's two means, and [groups] of the means
-    if ((int)blockIdx.x == a.slabs) {
-        if (blockIdx.z == 0) parameter_gradients(a, shared, kThreads);
+    if ((int)blockIdx.z == a.N) {
+        if (blockIdx.x == 0) parameter_gradients(a, shared, kThreads);
         return;
     }
     const Place s(a, V);
