@@ -152,7 +152,9 @@ hipError_t gemm(const float* A, int64_t lda, const float* B, int64_t ldb, bool n
 }
 
 // Parts of equal length that k is cut into, each a product of a batch, for products with few tiles: where the split GEMM's estimate for the batch
-// and the launch that joins its results (3 us and 5 TB/s) is 0.9 of that for the whole or less. A function of the extents alone.
+// and the launch that joins its results (3 us and 5 TB/s) is 0.97 of that for the whole or less. (Blocks whose down product or dx lies between 0.9 and
+// 0.97, whole / in parts, us: backward 777 and 1024 tokens of 1024 -> 2816 297 / 278, 344 / 325, 2048 640 / 606, its forward pass 283 / 267, backward 4096
+// of 512 -> 1536 397 / 377; forward 4096 of 640 -> 2560 318 / 324.) A function of the extents alone.
 int parts_of_k(int64_t M, int64_t N, int64_t K)
 {
     auto estimate = [&](int64_t parts) {
@@ -160,7 +162,7 @@ int parts_of_k(int64_t M, int64_t N, int64_t K)
                (parts > 1 ? 3.0 + (double)(parts + 1) * (double)M * (double)N * 4.0 / 5e6 : 0.0);
     };
     int best = 1;
-    double least = 0.9 * estimate(1);
+    double least = 0.97 * estimate(1);
     for (const int parts : {2, 3, 4, 6, 8})
         if (K % parts == 0 && K / parts >= 256 && estimate(parts) < least) {
             best = parts;
