@@ -133,6 +133,14 @@ def test_group_norm_views(anr, t, spare, crop):
         assert torch.allclose(whole.double().sum(), inside, rtol=1e-9, atol=1e-6)
 
 
+@pytest.mark.parametrize("t,shape", [("f32", (3, 96, 20, 20, 12)), ("f32", (5, 160, 28, 28, 20)), ("bf16", (3, 192, 20, 20, 24)), ("f16", (2, 640, 23, 19, 32)),
+                                     ("bf16", (16, 256, 36, 36, 32))])
+def test_group_norm_chunks_of_half_a_line(anr, t, shape):
+    """Maps that work-groups hold with few of these: whole sixteens of them change places, what is left does not."""
+    N, C, H, W, groups = shape
+    norm_case(anr, 21, N, C, H, W, groups, "silu", TYPES[t])
+
+
 def test_group_norm_values_far_from_zero(anr):
     """A mean of a thousand spreads costs no bits of the spread."""
     norm_case(anr, 4, 1, 32, 40, 40, 4, "none", torch.float32, shift=0.0)
@@ -192,6 +200,30 @@ def test_group_norm_in_place(anr, t, shape):
         anr.group_norm_backward(d, x, groups, None, None, mean, rstd, d, act=anr.ANR_ACT_SILU)
         anr.group_norm_backward(dy, e, groups, None, None, mean, rstd, e, act=anr.ANR_ACT_SILU)
         assert torch.equal(z, y) and torch.equal(d, dx) and torch.equal(e, dx)
+
+
+@pytest.mark.parametrize("C,t", [(3, torch.float32), (8, torch.bfloat16)])
+def test_group_norm_most_images(anr, C, t):
+    """As many images as a call takes: those of the last half as in a call of their own, and a sum over them that is exact."""
+    N, half = 65534, 32767
+    x = torch.randn(N, 2, C, device="cuda").to(t).transpose(1, 2)
+    y, part, mean, rstd = torch.empty_like(x), torch.empty_like(x[half:]), nans(N, 1, dtype=torch.float32), nans(N, 1, dtype=torch.float32)
+    anr.group_norm(x, 1, y, mean=mean, rstd=rstd)
+    anr.group_norm(x[half:], 1, part)
+    assert torch.equal(y[half:], part) and torch.isfinite(y).all()
+    dy, dx, dbeta = torch.ones_like(x), torch.empty_like(x), nans(C, dtype=torch.float32)
+    anr.group_norm_backward(dy, x, 1, None, None, mean, rstd, dx, None, dbeta)
+    anr.group_norm_backward(dy[half:], x[half:], 1, None, None, mean[half:], rstd[half:], part)
+    assert torch.equal(dx[half:], part) and (dbeta == 2 * N).all()
+
+
+def test_group_norm_most_channels(anr):
+    C = 1 << 20
+    x = torch.randn(1, 2, C, device="cuda").transpose(1, 2)
+    y, part = torch.empty_like(x), torch.empty(1, 2, 64, device="cuda").transpose(1, 2)
+    anr.group_norm(x, C, y)
+    anr.group_norm(x[:, -64:], 64, part)
+    assert torch.equal(y[:, -64:], part) and torch.isfinite(y).all()
 
 
 def test_group_norm_of_one_value_everywhere(anr):
@@ -364,6 +396,20 @@ def test_rotary_offsets_beyond_32_bits(anr):
     want = O.rotary(host(tail), host(pos)[:, None, -3:], host(freq), (64,), "adjacent", False)
     within("q", q[:, -3:], want, 8 * U * 5, torch.bfloat16)
     assert not q[:, :-3].any()
+    del q
+    torch.cuda.empty_cache()
+
+
+def test_rotary_most_tokens(anr):
+    """A work-group for each of as many tokens as a call takes (257 pairs: more than half of what one has angles for)."""
+    S, D = (1 << 24) - 1, 514
+    q = torch.zeros(1, S, 1, D, dtype=torch.bfloat16, device="cuda")
+    q[:, -3:] = torch.randn(1, 3, 1, D, device="cuda")
+    tail = q[:, -3:].clone()
+    freq, pos = torch.rand(257, device="cuda"), torch.arange(S, dtype=torch.int32, device="cuda")[None]
+    anr.rotary(q, None, pos, freq, q, None, None, anr.ANR_ROTARY_HALVES)
+    within("q", q[:, -3:], O.rotary(host(tail), host(pos[:, None, -3:]), host(freq), (257,), "halves", False), 8 * U * 5, torch.bfloat16)
+    assert not q[:, :1000].any() and not q[:, -1003:-3].any()
     del q
     torch.cuda.empty_cache()
 
