@@ -47,16 +47,20 @@ int held_by(const Args& a)
     return (a.HW + rows - 1) / rows;
 }
 
-// Where the resident kernels run: a chunk of an image fits the registers of a work-group (vectors of four channels a thread).
-// Timed with groups of 8 and 10 channels of 256 and 320, batch 1 to 32, SiLU, against the kernels that read twice (us, resident / not):
-// forward, 16 bits, 14^2 7.9 / 14, 28^2 (12 to 16 vectors) 14 / 15; float32 20^2 10 / 15, 28^2 (7) 14.5 / 15.5, but 40^2 (13) 19 / 13
-// with 8 work-groups, 23 / 21 with 128, 28 / 32 with 256. Backward, float32 28^2 19 / 19 to 28 / 30; 16 bits 20^2 (7) 15 / 22, 28^2 (13)
-// 22 / 19. So: eight vectors, and sixteen in the forward pass of 16-bit types or with work-groups for most CUs.
+// Where the resident kernels run: a chunk of an image fits the registers of a work-group (vectors of four channels a thread), and all work-groups the
+// CUs at once, at 1024 threads each. 256 channels, groups of 8, SiLU, against the kernels that read twice (us, resident / not):
+// forward, 16 bits, 20^2 x 16 images (7 vectors) 9.0 / 13.3, 28^2 x 64 (13) 17 / 22; float32 20^2 x 16 (4) 10.8 / 12.3, but 24^2 x 4 (5) 11.3 / 9.7, 28^2 x 1
+// (7) 11.8 / 10.2, x 16 15.1 / 14.7, with work-groups for most CUs 28^2 x 24 17.1 / 18.0, 32^2 x 32 20.6 / 24.7, 40^2 x 28 (13) 27.6 / 30.1.
+// Backward, float32 28^2 x 1 11.5 / 12.3, x 32 23.0 / 29.5, 24^2 x 4 11.0 / 10.3; 16 bits 20^2 x 16 12.3 / 13.6, x 64 19.8 / 21.6, 28^2 x 16 (13) 22 / 19.
+// More than fit at once: float32 20^2 x 40 21.3 / 16.3, 23.1 / 20.3, 10^2 x 128 27.8 / 15.1; bf16 14^2 x 128 16.1 / 17.3, 21.1 / 19.7, 7^2 x 256 22.6 / 16.1
+// (512 of 448 threads fit: float32 7^2 x 64 7.5 / 10.4).
 bool resident_pays(const GroupNormArgs& g, const Args& a, bool backward, int64_t work_groups)
 {
-    if (a.chunk / kHeldChannels > 256) return false;
-    const int most = !backward && (g.dtype != ANR_F32 || work_groups >= 192) ? 16 : 8;
-    return held_by(a) <= most;
+    const int columns = a.chunk / kHeldChannels;
+    if (columns > 256) return false;
+    const int64_t threads = std::min<int64_t>(kResidentThreads, ((int64_t)a.HW * columns + 63) / 64 * 64);
+    if (work_groups * threads > 256 * kResidentThreads) return false;
+    return held_by(a) <= (backward ? 8 : g.dtype != ANR_F32 || work_groups >= 192 ? 16 : 4);
 }
 
 Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
@@ -97,10 +101,10 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
     a.chunk = chunk_of(128);
     p.chunks = (g.C + a.chunk - 1) / a.chunk;
     // Resident kernels take chunks of 64 bytes where work-groups of 128 would be half the CUs or fewer: the backward pass, and the forward one where a thread
-    // has more than four vectors. 256 channels, chunks of 128 / 64 bytes, forward and backward (us): float32 14^2 x 16 images 9.2 9.9 / 9.8 10.0, 20^2 x 1
-    // 10.0 10.5 / 10.7 10.0, 28^2 x 1 12.8 14.3 / 11.8 11.5, x 16 15.8 18.6 / 15.2 16.4; bf16 14^2 x 32 8.0 11.7 / 8.6 10.4, 20^2 x 16 9.7 15.5 / 9.0
-    // 12.4, 48 images (more than half the CUs) 11.1 18.1 / 17.2 18.9. Of maps that only the halves hold, those of 16-bit types with 64 work-groups, forward:
-    // against the kernels that read twice bf16 36^2 x 16 17.3 / 15.1, but 40^2 x 1 12.2 / 14.0, and backward 28^2 x 16 15.6 / 17.4.
+    // has more than four vectors. 256 channels, chunks of 128 / 64 bytes (us): backward, float32 14^2 x 16 images 9.9 / 10.0, 20^2 x 1 10.5 / 10.0, 28^2 x 1
+    // 14.3 / 11.5, x 16 18.6 / 16.4; bf16 14^2 x 32 11.7 / 10.4, 20^2 x 16 15.5 / 12.4. Forward, bf16 14^2 x 32 8.0 / 8.6, 20^2 x 16 9.7 / 9.0, x 48 (more
+    // than half the CUs) 11.1 / 17.2, 28^2 x 16 14.0 / 11.3. Of maps that only the halves hold, those of 16-bit types with 64 work-groups, forward: against the
+    // kernels that read twice bf16 36^2 x 16 17.3 / 15.1, but 40^2 x 1 12.2 / 14.0, and backward 28^2 x 16 15.6 / 17.4.
     const int64_t work_groups = (int64_t)p.chunks * g.N;
     if (vector && chunk_of(64) < a.chunk && work_groups <= 128 &&
         (resident_pays(g, a, backward, work_groups) ? backward || held_by(a) > 4 : !backward && g.dtype != ANR_F32 && work_groups >= 64)) {

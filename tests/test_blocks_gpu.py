@@ -218,12 +218,20 @@ def test_group_norm_most_images(anr, C, t):
 
 
 def test_group_norm_most_channels(anr):
+    """As many channels as a call takes, each a group of two values, which a call of few of them gives too. (Not to the bit: calls of other sizes
+    run other kernels.)  With d their difference, held to u d, the mean is d / 2 from the first, its sum with that is rounded to u max|x| and a value's
+    distance from it to u d / 2; the squares, their mean, the root and the two products are off by at most 10 u of 1."""
     C = 1 << 20
     x = torch.randn(1, 2, C, device="cuda").transpose(1, 2)
     y, part = torch.empty_like(x), torch.empty(1, 2, 64, device="cuda").transpose(1, 2)
     anr.group_norm(x, C, y)
     anr.group_norm(x[:, -64:], 64, part)
-    assert torch.equal(y[:, -64:], part) and torch.isfinite(y).all()
+    x64 = host(x)
+    rstd = 1 / np.sqrt(x64.var(axis=2, keepdims=True) + 1e-5)
+    want = (x64 - x64.mean(axis=2, keepdims=True)) * rstd
+    bound = U * np.abs(x64).max(axis=2, keepdims=True) * rstd + 14 * U
+    within("y", y, want, np.broadcast_to(bound, want.shape), torch.float32)
+    within("part", part, want[:, -64:], np.broadcast_to(bound, want.shape)[:, -64:], torch.float32)
 
 
 def test_group_norm_of_one_value_everywhere(anr):
