@@ -15,11 +15,10 @@
 #pragma once
 #include "anr_kernels.h"
 #include "element_types.h"
+#include "group_norm_plan.h"
 
 namespace anr {
 namespace gnorm {
-
-constexpr int kThreads = 256;
 
 // Offsets of pixels; flat: one stride from pixel to pixel.
 struct Pixels {
@@ -72,9 +71,9 @@ struct Place {
         channels = min(a.chunk, a.C - c0);
         p0 = slab * a.slab_pixels;
         p1 = min(a.HW, p0 + a.slab_pixels);
-        columns = channels / V;
+        columns = columns_of(channels, V);
         const int wide = min(columns, threads);
-        rows = threads / wide;
+        rows = rows_of(channels, V, threads);
         ty = threadIdx.x / wide;
         tx = ty < rows ? threadIdx.x - ty * wide : columns;          // (threads that are left over have no column)
     }
@@ -114,16 +113,13 @@ __device__ __forceinline__ void from_table(const float* table, int c, float (&ou
     }
 }
 
-// Floats of a table in LDS: whole 16-byte units.
-__device__ __host__ __forceinline__ constexpr int table_floats(int channels) { return (channels + 3) & ~3; }
-
 // First kernel of the forward pass: mean and M2 of each group of the chunk over the slab.
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void stats_kernel(const Args a)
 {
     extern __shared__ __attribute__((aligned(16))) float shared[];   // the table, then [rows][channels] of (mean, M2)
     const Place s(a, V);
-    float* const lds = shared + table_floats(min(s.channels, kThreads * V));
+    float* const lds = shared + table_floats(table_channels(s.channels, V));
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     const int first = s.p0 + s.ty;
     const int mine = s.tx < s.columns && first < s.p1 ? (s.p1 - first + s.rows - 1) / s.rows : 0;
@@ -213,7 +209,7 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
     constexpr bool QUICK = sizeof(T) == 2;
     extern __shared__ __attribute__((aligned(16))) float shared[];   // tables of mean, scale and shift, then [groups] of (mean, rstd)
     const Place s(a, V);
-    const int table = table_floats(min(s.channels, kThreads * V));
+    const int table = table_floats(table_channels(s.channels, V));
     float* const lds = shared + 3 * table;
     const int groups = s.channels / a.cg, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g0 = s.c0 / a.cg;
     for (int g = wave; g < groups; g += kThreads / 64) {
@@ -316,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void backward_sums_kernel(const Args a)
     constexpr bool QUICK = sizeof(T) == 2;
     extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, then [rows][2][channels]
     const Place s(a, V);
-    const int table = table_floats(min(s.channels, kThreads * V));
+    const int table = table_floats(table_channels(s.channels, V));
     float* const lds = shared + 4 * table;
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     const T* const dy = static_cast<const T*>(a.dy) + s.n * a.pdy.sn + s.c0;
@@ -404,7 +400,7 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
         return;
     }
     const Place s(a, V);
-    const int table = table_floats(min(s.channels, kThreads * V));
+    const int table = table_floats(table_channels(s.channels, V));
     float* const means = shared + 6 * table;
     for (int g = threadIdx.x >> 6; g < s.channels / a.cg; g += kThreads / 64) {
         const float* const at = a.ws + 2 * ((int64_t)s.n * a.slabs * a.groups + s.c0 / a.cg + g);
@@ -457,9 +453,7 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
     }
 }
 
-// ---- resident: a work-group holds its chunk of an image, at most R vectors of four channels a thread (of eight, the
-// constants of 16-bit types' channels left no registers for the data)
-constexpr int kHeldChannels = 4;
+// ---- resident: a work-group holds its chunk of an image, at most R vectors of kHeldChannels channels a thread
 
 // Sums over the work-group's rows and each group's channels of a value per channel and thread; the results of group g at
 // result[g].  `part`: [rows][channels].

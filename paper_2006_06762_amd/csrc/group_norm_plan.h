@@ -1,0 +1,164 @@
+// What the group norm's kernels (group_norm_kernel.h) divide and lay out how: plain arithmetic without a device in it, so that a CPU program
+// can hold what a launch asks for against what its work-groups use.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace anr {
+namespace gnorm {
+
+constexpr int kThreads = 256;                // of the kernels that read twice
+constexpr int kResidentThreads = 1024;
+constexpr int kHeldChannels = 4;             // of a vector of the resident kernels (of eight, the constants of 16-bit types' channels left no registers for the data)
+
+// Floats of a table in LDS: whole 16-byte units.
+constexpr int table_floats(int channels) { return (channels + 3) & ~3; }
+
+// Threads of a work-group on `channels` channels: columns of V of them by rows of pixels.  A chunk of fewer channels has more rows, and rows x
+// channels may be more than a wider one's: 100 channels of 256 threads are 2 rows, 60 are 4.
+constexpr int columns_of(int channels, int V) { return channels / V; }
+constexpr int rows_of(int channels, int V, int threads) { return threads / (columns_of(channels, V) < threads ? columns_of(channels, V) : threads); }
+
+// Channels that the tables of the kernels that read twice hold at a time.
+constexpr int table_channels(int channels, int V) { return channels < kThreads * V ? channels : kThreads * V; }
+
+// Floats of LDS that a work-group on `channels` channels uses: of the kernels that sum (a table and two numbers a channel and row; backward four
+// tables), of the resident ones, of those that apply.
+constexpr size_t sums_lds_floats(bool backward, int channels, int V)
+{
+    return (backward ? 4 : 1) * (size_t)table_floats(table_channels(channels, V)) + 2 * (size_t)rows_of(channels, V, kThreads) * channels;
+}
+constexpr size_t resident_lds_floats(bool backward, int channels, int cg, int threads)
+{
+    const size_t groups = channels / cg, part = (size_t)rows_of(channels, kHeldChannels, threads) * channels;
+    return backward ? 6 * (size_t)table_floats(channels) + table_floats(2 * groups) + 2 * part + threads : 3 * (size_t)table_floats(channels) + table_floats(groups) + part;
+}
+constexpr size_t apply_lds_floats(bool backward, int channels, int cg, int V)
+{
+    const size_t floats = (backward ? 6 : 3) * (size_t)table_floats(table_channels(channels, V)) + 2 * (size_t)(channels / cg);
+    return backward && floats < (size_t)kThreads ? (size_t)kThreads : floats;        // (the parameters' gradients take a float a thread)
+}
+
+// A call, and how its kernels divide it.
+struct Shape {
+    int N, HW, C, groups;
+    int es;                         // bytes of an element
+    bool vector;                    // loads of 16 bytes, else of single elements
+    bool backward;
+};
+struct Division {
+    int V;                          // channels of a thread of the kernels that read twice
+    int chunk, chunks;              // channels of a chunk, whole groups; the last may have fewer
+    bool halves;                    // resident: a chunk's pixel is half a line
+    int slabs, slab_pixels;
+    int resident;                   // threads of the resident kernel, or 0
+    int held;                       // its vectors a thread: 4, 8 or 16
+    size_t sums_lds, apply_lds, resident_lds;    // bytes a launch asks for
+};
+
+inline int common_multiple(int a, int b)
+{
+    int x = a, y = b;
+    while (y) {
+        const int r = x % y;
+        x = y;
+        y = r;
+    }
+    return a / x * b;
+}
+
+// Whether loads of 16 bytes can be: whole units of a pixel, and a chunk of whole groups and units that LDS holds.
+inline bool vector_possible(int C, int groups, int es)
+{
+    const int V = 16 / es;
+    return C % V == 0 && std::min(common_multiple(C / groups, V), C) <= 8192;
+}
+
+// Vectors that a thread of a full work-group holds of a chunk, which has at most 256 columns of them.
+inline int held_by(const Shape& s, int chunk)
+{
+    const int rows = rows_of(chunk, kHeldChannels, kResidentThreads);
+    return (s.HW + rows - 1) / rows;
+}
+
+// Where the resident kernels run: a chunk of an image fits the registers of a work-group (vectors of four channels a thread), and all work-groups the
+// CUs at once, at 1024 threads each. 256 channels, groups of 8, SiLU, against the kernels that read twice (us, resident / not):
+// forward, 16 bits, 20^2 x 16 images (7 vectors) 9.0 / 13.3, 28^2 x 64 (13) 17 / 22; float32 20^2 x 16 (4) 10.8 / 12.3, but 24^2 x 4 (5) 11.3 / 9.7, 28^2 x 1
+// (7) 11.8 / 10.2, x 16 15.1 / 14.7, with work-groups for most CUs 28^2 x 24 17.1 / 18.0, 32^2 x 32 20.6 / 24.7, 40^2 x 28 (13) 27.6 / 30.1.
+// Backward, float32 28^2 x 1 11.5 / 12.3, x 32 23.0 / 29.5, 24^2 x 4 11.0 / 10.3; 16 bits 20^2 x 16 12.3 / 13.6, x 64 19.8 / 21.6, 28^2 x 16 (13) 22 / 19.
+// More than fit at once: float32 20^2 x 40 21.3 / 16.3, 23.1 / 20.3, 10^2 x 128 27.8 / 15.1; bf16 14^2 x 128 16.1 / 17.3, 21.1 / 19.7, 7^2 x 256 22.6 / 16.1
+// (512 of 448 threads fit: float32 7^2 x 64 7.5 / 10.4).
+inline bool resident_pays(const Shape& s, int chunk, int64_t work_groups)
+{
+    const int columns = columns_of(chunk, kHeldChannels);
+    if (columns > 256) return false;
+    const int64_t threads = std::min<int64_t>(kResidentThreads, ((int64_t)s.HW * columns + 63) / 64 * 64);
+    if (work_groups * threads > 256 * kResidentThreads) return false;
+    return held_by(s, chunk) <= (s.backward ? 8 : s.es == 2 || work_groups >= 192 ? 16 : 4);
+}
+
+// f(channels) of the larger of a full chunk and the last one.
+template <typename F>
+size_t of_chunks(const Division& d, int C, F f)
+{
+    const int last = C - (d.chunks - 1) * d.chunk;
+    return std::max<size_t>(f(d.chunk), f(last));
+}
+
+inline Division divide(const Shape& s)
+{
+    Division d{};
+    d.V = s.vector ? 16 / s.es : 1;
+    const int cg = s.C / s.groups;
+    // Whole groups and whole units, at least a line of 128 bytes of a pixel.
+    const int least = std::min(common_multiple(cg, d.V), s.C);
+    auto chunk_of = [&](int bytes) { return std::min(s.C, least * std::max(1, (bytes / s.es + least - 1) / least)); };
+    auto take = [&](int chunk) {
+        d.chunk = chunk;
+        d.chunks = (s.C + chunk - 1) / chunk;
+    };
+    take(chunk_of(128));
+    // Resident kernels take chunks of 64 bytes where work-groups of 128 would be half the CUs or fewer: the backward pass, and the forward one where a thread
+    // has more than four vectors. 256 channels, chunks of 128 / 64 bytes (us): backward, float32 14^2 x 16 images 9.9 / 10.0, 20^2 x 1 10.5 / 10.0, 28^2 x 1
+    // 14.3 / 11.5, x 16 18.6 / 16.4; bf16 14^2 x 32 11.7 / 10.4, 20^2 x 16 15.5 / 12.4. Forward, bf16 14^2 x 32 8.0 / 8.6, 20^2 x 16 9.7 / 9.0, x 48 (more
+    // than half the CUs) 11.1 / 17.2, 28^2 x 16 14.0 / 11.3. Of maps that only the halves hold, those of 16-bit types with 64 work-groups, forward: against the
+    // kernels that read twice bf16 36^2 x 16 17.3 / 15.1, but 40^2 x 1 12.2 / 14.0, and backward 28^2 x 16 15.6 / 17.4.
+    const int64_t work_groups = (int64_t)d.chunks * s.N;
+    if (s.vector && chunk_of(64) < d.chunk && work_groups <= 128 &&
+        (resident_pays(s, d.chunk, work_groups) ? s.backward || held_by(s, d.chunk) > 4 : !s.backward && s.es == 2 && work_groups >= 64) &&
+        resident_pays(s, chunk_of(64), work_groups)) {
+        take(chunk_of(64));
+        d.halves = true;
+    }
+    const int rows = rows_of(d.chunk, d.V, kThreads);
+    // Slabs: about four work-groups per CU as far as each thread has eight pixels (float32: four), one per CU as far as it has two, and at
+    // most 128 that are joined. (Eight or four, backward, 320 channels: float32 8 x 56^2 47 / 36 us, bf16 34 / 35, 4 x 95 x 63 32 / 34.)
+    const int64_t others = (int64_t)d.chunks * s.N;
+    int64_t slabs = std::min((1024 + others - 1) / others, (int64_t)s.HW / ((s.es == 4 ? 4 : 8) * rows));
+    slabs = std::max(slabs, std::min((256 + others - 1) / others, (int64_t)s.HW / (2 * rows)));
+    slabs = std::max<int64_t>(1, std::min<int64_t>(slabs, 128));
+    // Work-groups go round-robin to the eight XCDs: those that share the lines at a chunk's ends to the same one (4 x 95 x 63 x 320 bf16, chunks of 160 bytes,
+    // 29 / 24 slabs, forward 21.7 / 20.4 us, backward 27.8 / 25.3; level where chunks are whole lines).
+    if (slabs > 8) slabs = slabs / 8 * 8;
+    d.slab_pixels = (int)((s.HW + slabs - 1) / slabs);
+    d.slabs = (s.HW + d.slab_pixels - 1) / d.slab_pixels;
+    d.sums_lds = sizeof(float) * of_chunks(d, s.C, [&](int channels) { return sums_lds_floats(s.backward, channels, d.V); });
+    d.apply_lds = sizeof(float) * of_chunks(d, s.C, [&](int channels) { return apply_lds_floats(s.backward, channels, cg, d.V); });
+    if (s.vector && resident_pays(s, d.chunk, others)) {
+        const int columns = columns_of(d.chunk, kHeldChannels);
+        const int64_t vectors = (int64_t)s.HW * columns;
+        d.resident = (int)std::min<int64_t>(kResidentThreads, (vectors + 63) / 64 * 64);
+        d.resident = std::max(d.resident, (columns + 63) / 64 * 64);
+        const int resident_rows = rows_of(d.chunk, kHeldChannels, d.resident), each = (s.HW + resident_rows - 1) / resident_rows;
+        d.held = each <= 4 ? 4 : each <= 8 ? 8 : 16;
+        d.resident_lds = sizeof(float) * of_chunks(d, s.C, [&](int channels) { return resident_lds_floats(s.backward, channels, cg, d.resident); });
+        d.slabs = 1;
+        d.slab_pixels = s.HW;
+    }
+    return d;
+}
+
+}  // namespace gnorm
+}  // namespace anr
