@@ -60,10 +60,18 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
     a.slabs = p.d.slabs;
     a.slab_pixels = p.d.slab_pixels;
     a.streaming = a.chunk % line == 0 && (reinterpret_cast<uintptr_t>(g.y) & 127) == 0 && g.ys[0] % line == 0 && g.ys[1] % line == 0 && g.ys[2] % line == 0;
-    const size_t of_groups = p.d.resident ? 0 : sizeof(float) * 2 * (size_t)g.N * a.slabs * g.groups;
-    p.bytes = of_groups + (backward ? sizeof(float) * 2 * (size_t)g.N * a.slabs * g.C : of_groups / (2 * (size_t)a.slabs));
-    a.ws = static_cast<float*>(g.ws);
-    a.first = a.sums = a.ws + of_groups / sizeof(float);
+    a.values = (double)a.HW * (double)a.cg;
+    if (backward) {
+        const size_t of_groups = p.d.resident ? 0 : 2 * (size_t)g.N * a.slabs * g.groups;
+        p.bytes = sizeof(float) * (of_groups + 2 * (size_t)g.N * a.slabs * g.C);
+        a.ws = static_cast<float*>(g.ws);
+        a.sums = a.ws + of_groups;
+    } else if (!p.d.resident) {
+        const size_t of_groups = 2 * (size_t)g.N * a.slabs * g.groups;
+        p.bytes = sizeof(double) * of_groups + sizeof(float) * (size_t)g.N * g.groups;
+        a.stats = static_cast<double*>(g.ws);
+        a.first = reinterpret_cast<float*>(a.stats + of_groups);
+    }
     return p;
 }
 

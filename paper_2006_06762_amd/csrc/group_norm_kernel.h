@@ -4,12 +4,15 @@
 // chunk of whole groups (at least 128 bytes of a pixel's channels, so that lines are used whole) of a slab of pixels; its
 // threads are columns of V channels by rows of pixels, and a thread keeps the sums of its V channels over its pixels.
 //
-// The statistics of a thread are mean and sum of squared differences M2, from blocks of four pixels that are joined by
-//     d = mean_b - mean_a,  mean = mean_a + d n_b / n,  M2 = M2_a + M2_b + d^2 n_a n_b / n,
-// Values are taken relative to one of their own, the group's first in the image, so that a mean far from zero costs no bits
-// (M2 by joins feels the rounding of the means that it joins: without this, values at 4096 spreads gave an rstd 4e-6 off).  Many of them are joined in two passes, mean = sum n_i mean_i / n and
-// M2 = sum M2_i + n_i (mean_i - mean)^2: threads of a work-group through LDS, slabs through the workspace, where the
-// work-groups of the second kernel join them again each for itself (fewer launches than a kernel that does).
+// The statistics are sums in 64 bits, whose additions the vector units do at the rate of 32 bits: of the values (resident kernels, which then sum
+// the squared differences from the mean), or, where x is read once for both, of each value's difference from one of the group's own, the
+// first in the image, and of its square.  The mean square difference is then s2 / n - (s1 / n)^2, which loses the factor by which its
+// second part exceeds it; that is (first - mean)^2 over the variance, at most n since the first value is one of the n: less than 2^-24 is lost
+// below 2^28 values whatever they are.  (Means and squared differences in 32 bits, joined block by block, felt a first value that
+// lies 1000 spreads out, 2e-5 of a spread in y, and grew with the number of joins.)  The mean is kept as two floats, its rounded value and the rest.
+//
+// Sums are joined by the threads of a work-group through LDS, those of slabs through the workspace, where the work-groups of the second
+// kernel join them each for itself (fewer launches than a kernel that does), always in the same order.
 //
 // Where a work-group can hold a chunk of an image in its registers (resident kernels), it is read once, in one launch.
 #pragma once
@@ -37,7 +40,9 @@ struct Args {
     const void *gamma, *beta;
     void *dgamma, *dbeta;
     float *mean, *rstd;
-    float* ws;                      // mean and M2 (backward: the two sums) of each group over the slabs, [N][slabs][groups][2]
+    double* stats;                  // forward: the two sums of each group over the slabs, [N][slabs][groups][2]
+    double values;                  // of a group
+    float* ws;                      // backward: the two sums of each group over the slabs, [N][slabs][groups][2]
     float* first;                   // forward: the value that each group's are relative to, [N][groups] (x may be overwritten in place)
     float* sums;                    // backward: sums of each channel over the slabs, [N][slabs][2][C]
     Pixels px, pdy, py;
@@ -79,7 +84,8 @@ struct Place {
     }
 };
 
-__device__ __forceinline__ float wave_sum(float v)
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v)
 {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
@@ -113,90 +119,67 @@ __device__ __forceinline__ void from_table(const float* table, int c, float (&ou
     }
 }
 
-// First kernel of the forward pass: mean and M2 of each group of the chunk over the slab.
+// A mean as its rounded value and the rest.
+__device__ __forceinline__ void two_floats(double mean, float& high, float& low)
+{
+    high = (float)mean;
+    low = (float)(mean - (double)high);
+}
+
+// First kernel of the forward pass: the two sums of each group of the chunk over the slab.
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void stats_kernel(const Args a)
 {
-    extern __shared__ __attribute__((aligned(16))) float shared[];   // the table, then [rows][channels] of (mean, M2)
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the table, then the sums, [2][V][rows][columns] in 64 bits
     const Place s(a, V);
-    float* const lds = shared + table_floats(table_channels(s.channels, V));
+    const int table = table_floats(table_channels(s.channels, V)), all = s.rows * s.channels;
+    double* const lds = reinterpret_cast<double*>(shared + table);
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
-    const int first = s.p0 + s.ty;
-    const int mine = s.tx < s.columns && first < s.p1 ? (s.p1 - first + s.rows - 1) / s.rows : 0;
     for (int base = 0; base < s.columns; base += kThreads) {         // (one round but for groups of thousands of channels)
         const int here = min(s.channels - base * V, kThreads * V), col = base + s.tx;
         __syncthreads();
         origins(a, x, base * V, here, shared, kThreads);
         __syncthreads();
         if (col >= s.columns) continue;
-        float mean[V], m2[V], origin[V];
+        double sum[V], squares[V];
+        float origin[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.f;
+        for (int i = 0; i < V; ++i) sum[i] = squares[i] = 0.;
         from_table<V>(shared, s.tx * V, origin);
         const T* const xc = x + col * V;
-        int k = 0;
-        for (; k + 4 <= mine; k += 4) {
-            float v[4][V];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                load_floats<T, V>(xc + a.px.at(first + (k + u) * s.rows, a.W, a.by_w, a.flat), v[u]);
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[u][i] -= origin[i];
-            }
-            const float n = (float)k, share = 4.f / (n + 4.f), weight = n * share;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float m = 0.25f * ((v[0][i] + v[1][i]) + (v[2][i] + v[3][i]));
-                float q = 0.f;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) q = fmaf(v[u][i] - m, v[u][i] - m, q);
-                const float d = m - mean[i];
-                m2[i] += fmaf(d * d, weight, q);
-                mean[i] = fmaf(d, share, mean[i]);
-            }
-        }
-        for (; k < mine; ++k) {
+#pragma unroll 4
+        for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
             float v[V];
-            load_floats<T, V>(xc + a.px.at(first + k * s.rows, a.W, a.by_w, a.flat), v);
-            const float share = 1.f / (float)(k + 1);
+            load_floats<T, V>(xc + a.px.at(p, a.W, a.by_w, a.flat), v);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                v[i] -= origin[i];
-                const float d = v[i] - mean[i];
-                mean[i] = fmaf(d, share, mean[i]);
-                m2[i] = fmaf(d, v[i] - mean[i], m2[i]);
+                const double d = (double)v[i] - (double)origin[i];
+                sum[i] += d;
+                squares[i] = fma(d, d, squares[i]);
             }
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float* const at = lds + 2 * (s.ty * s.channels + col * V + i);
-            at[0] = mean[i];
-            at[1] = m2[i];
+            const int at = (i * s.rows + s.ty) * s.columns + col;
+            lds[at] = sum[i];
+            lds[all + at] = squares[i];
         }
     }
     __syncthreads();
     const int groups = s.channels / a.cg, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int pixels = s.p1 - s.p0;
     for (int g = wave; g < groups; g += kThreads / 64) {
-        float sum = 0.f;
+        double sum = 0., squares = 0.;
         for (int e = lane; e < s.rows * a.cg; e += 64) {
-            const int row = a.by_cg.div(e), c = g * a.cg + e - row * a.cg;
-            const int count = pixels > row ? (pixels - row + s.rows - 1) / s.rows : 0;
-            sum = fmaf((float)count, lds[2 * (row * s.channels + c)], sum);
+            const int row = a.by_cg.div(e), c = g * a.cg + e - row * a.cg, at = (c % V * s.rows + row) * s.columns + c / V;
+            sum += lds[at];
+            squares += lds[all + at];
         }
-        const float mean = wave_sum(sum) / ((float)pixels * (float)a.cg);
-        float q = 0.f;
-        for (int e = lane; e < s.rows * a.cg; e += 64) {
-            const int row = a.by_cg.div(e), c = g * a.cg + e - row * a.cg;
-            const int count = pixels > row ? (pixels - row + s.rows - 1) / s.rows : 0;
-            const float d = lds[2 * (row * s.channels + c)] - mean;
-            q += fmaf((float)count * d, d, lds[2 * (row * s.channels + c) + 1]);
-        }
-        q = wave_sum(q);
+        sum = wave_sum(sum);
+        squares = wave_sum(squares);
         if (lane == 0) {
-            float* const at = a.ws + 2 * (((int64_t)s.n * a.slabs + s.slab) * a.groups + s.c0 / a.cg + g);
-            at[0] = mean;
-            at[1] = q;
+            double* const at = a.stats + 2 * (((int64_t)s.n * a.slabs + s.slab) * a.groups + s.c0 / a.cg + g);
+            at[0] = sum;
+            at[1] = squares;
             if (s.slab == 0) a.first[(int64_t)s.n * a.groups + s.c0 / a.cg + g] = to_float(x[g * a.cg]);
         }
     }
@@ -207,27 +190,27 @@ template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
-    extern __shared__ __attribute__((aligned(16))) float shared[];   // tables of mean, scale and shift, then [groups] of (mean, rstd)
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // tables of mean, scale and shift, then [groups] of (mean, rest of the mean, rstd)
     const Place s(a, V);
     const int table = table_floats(table_channels(s.channels, V));
     float* const lds = shared + 3 * table;
     const int groups = s.channels / a.cg, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g0 = s.c0 / a.cg;
     for (int g = wave; g < groups; g += kThreads / 64) {
-        const float* const at = a.ws + 2 * ((int64_t)s.n * a.slabs * a.groups + g0 + g);
-        float sum = 0.f;
-        for (int i = lane; i < a.slabs; i += 64) sum = fmaf((float)(min(a.HW, (i + 1) * a.slab_pixels) - i * a.slab_pixels), at[2 * (int64_t)i * a.groups], sum);
-        const float mean = wave_sum(sum) / (float)a.HW;              // (relative to the group's first value)
-        float q = 0.f;
+        const double* const at = a.stats + 2 * ((int64_t)s.n * a.slabs * a.groups + g0 + g);
+        double sum = 0., squares = 0.;
         for (int i = lane; i < a.slabs; i += 64) {
-            const float pixels = (float)(min(a.HW, (i + 1) * a.slab_pixels) - i * a.slab_pixels), d = at[2 * (int64_t)i * a.groups] - mean;
-            q += fmaf(pixels * (float)a.cg * d, d, at[2 * (int64_t)i * a.groups + 1]);
+            sum += at[2 * (int64_t)i * a.groups];
+            squares += at[2 * (int64_t)i * a.groups + 1];
         }
-        const float rstd = 1.f / sqrtf(wave_sum(q) / ((float)a.HW * (float)a.cg) + a.eps);
+        const double mean = wave_sum(sum) / a.values, var = wave_sum(squares) / a.values - mean * mean;    // (the mean relative to the first value)
+        const float rstd = 1.f / sqrtf((float)((var < 0. ? 0. : var) + (double)a.eps));
         if (lane == 0) {
-            const float whole = mean + a.first[(int64_t)s.n * a.groups + g0 + g];
-            lds[2 * g] = whole;
-            lds[2 * g + 1] = rstd;
-            if (s.slab == 0 && a.mean) a.mean[(int64_t)s.n * a.groups + g0 + g] = whole;
+            float high, low;
+            two_floats(mean + (double)a.first[(int64_t)s.n * a.groups + g0 + g], high, low);
+            lds[3 * g] = high;
+            lds[3 * g + 1] = low;
+            lds[3 * g + 2] = rstd;
+            if (s.slab == 0 && a.mean) a.mean[(int64_t)s.n * a.groups + g0 + g] = high;
             if (s.slab == 0 && a.rstd) a.rstd[(int64_t)s.n * a.groups + g0 + g] = rstd;
         }
     }
@@ -238,9 +221,10 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(const Args a)
         __syncthreads();
         for (int c = threadIdx.x; c < here; c += kThreads) {
             const int g = a.by_cg.div(first + c);
-            shared[c] = lds[2 * g];
-            shared[table + c] = lds[2 * g + 1] * parameter(a.gamma, s.c0 + first + c, a.param_dtype, 1.f);
-            shared[2 * table + c] = parameter(a.beta, s.c0 + first + c, a.param_dtype, 0.f);
+            const float scale = lds[3 * g + 2] * parameter(a.gamma, s.c0 + first + c, a.param_dtype, 1.f);
+            shared[c] = lds[3 * g];
+            shared[table + c] = scale;
+            shared[2 * table + c] = fmaf(-lds[3 * g + 1], scale, parameter(a.beta, s.c0 + first + c, a.param_dtype, 0.f));
         }
         __syncthreads();
         if (col >= s.columns) continue;
@@ -455,10 +439,10 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
 
 // ---- resident: a work-group holds its chunk of an image, at most R vectors of kHeldChannels channels a thread
 
-// Sums over the work-group's rows and each group's channels of a value per channel and thread; the results of group g at
-// result[g].  `part`: [rows][channels].
-template <int V>
-__device__ __forceinline__ void group_sums_of(const Args& a, const Place& s, const float (&v)[V], float* part, float* result, int threads)
+// Means over the work-group's rows and each group's channels of what a thread has summed of each channel; that of group g at
+// result[g].  (By a division: that of equal values is that value.)  `part`: [rows][channels].
+template <typename S, int V>
+__device__ __forceinline__ void group_means_of(const Args& a, const Place& s, const S (&v)[V], S* part, S* result, int threads)
 {
     if (s.tx < s.columns) {
 #pragma unroll
@@ -467,13 +451,13 @@ __device__ __forceinline__ void group_sums_of(const Args& a, const Place& s, con
     __syncthreads();
     const int groups = s.channels / a.cg, lane = threadIdx.x & 63, entries = s.rows * a.cg;
     for (int g = threadIdx.x >> 6; g < groups; g += threads >> 6) {
-        float sum = 0.f;
+        S sum = 0;
         for (int e = lane; e < entries; e += 64) {
             const int row = a.by_cg.div(e);
             sum += part[row * s.channels + g * a.cg + e - row * a.cg];
         }
         sum = wave_sum(sum);
-        if (lane == 0) result[g] = sum;
+        if (lane == 0) result[g] = sum / (S)a.values;
     }
     __syncthreads();
 }
@@ -483,67 +467,77 @@ __global__ __launch_bounds__(1024) void resident_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
     constexpr int V = kHeldChannels;
-    extern __shared__ __attribute__((aligned(16))) float shared[];   // tables of origin, scale and shift, [groups], [rows][channels]
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // tables of scale and shift, then [groups] and [rows][channels] in 64 bits
     const int threads = blockDim.x;
     const Place s(a, V, threads);
     const int table = table_floats(s.channels), groups = s.channels / a.cg;
-    float *const result = shared + 3 * table, *const part = result + table_floats(groups);
+    double *const result = reinterpret_cast<double*>(shared + 2 * table), *const part = result + table_floats(groups);
+    float *const result32 = reinterpret_cast<float*>(result), *const part32 = reinterpret_cast<float*>(part);
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     const int col = min(s.tx, s.columns - 1) * V, mine = s.tx < s.columns && s.ty < a.HW ? (a.HW - s.ty + s.rows - 1) / s.rows : 0;
-    Pack<T, V> raw[R];
+    using Raw = Pack<T, V>;
+    Raw raw[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) raw[r] = *reinterpret_cast<const Pack<T, V>*>(x + a.px.at(min(s.ty + r * s.rows, a.HW - 1), a.W, a.by_w, a.flat) + col);
-    origins(a, x, 0, s.channels, shared, threads);
+    for (int r = 0; r < R; ++r) raw[r] = *reinterpret_cast<const Raw*>(x + a.px.at(min(s.ty + r * s.rows, a.HW - 1), a.W, a.by_w, a.flat) + col);
     for (int c = threadIdx.x; c < s.channels; c += threads) {
-        shared[table + c] = parameter(a.gamma, s.c0 + c, a.param_dtype, 1.f);
-        shared[2 * table + c] = parameter(a.beta, s.c0 + c, a.param_dtype, 0.f);
+        shared[c] = parameter(a.gamma, s.c0 + c, a.param_dtype, 1.f);
+        shared[table + c] = parameter(a.beta, s.c0 + c, a.param_dtype, 0.f);
     }
-    __syncthreads();
-    float origin[V], sum[V];
-    from_table<V>(shared, col, origin);
+    double total[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum[i] = 0.f;
+    for (int i = 0; i < V; ++i) total[i] = 0.;
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] += r < mine ? to_float(raw[r].v[i]) - origin[i] : 0.f;
-    group_sums_of<V>(a, s, sum, part, result, threads);
-    const float count = 1.f / ((float)a.HW * (float)a.cg);
-    float mean[V];                                                   // relative to the origin
+        for (int i = 0; i < V; ++i) total[i] += r < mine ? (double)to_float(raw[r].v[i]) : 0.;
+    if constexpr (QUICK && R == 16) {                                 // (what is held are the 16 bits: the floats, kept from sum to sum, do not fit the registers)
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            u32x2 bits = __builtin_bit_cast(u32x2, raw[r]);
+            asm("" : "+v"(bits));
+            raw[r] = __builtin_bit_cast(Raw, bits);
+        }
+    }
+    group_means_of<double, V>(a, s, total, part, result, threads);
+    float high[V], low[V], sum[V];                                   // the mean, and its rest
     int group[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         group[i] = a.by_cg.div(col + i);
-        mean[i] = result[group[i]] * count;
+        two_floats(result[group[i]], high[i], low[i]);
         sum[i] = 0.f;
     }
-    const float own_mean = threadIdx.x < groups ? result[threadIdx.x] * count : 0.f;
+    const float own_mean = threadIdx.x < groups ? (float)result[threadIdx.x] : 0.f;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float d = to_float(raw[r].v[i]) - origin[i] - mean[i];
+            const float d = to_float(raw[r].v[i]) - high[i] - low[i];
             sum[i] = r < mine ? fmaf(d, d, sum[i]) : sum[i];
         }
-    group_sums_of<V>(a, s, sum, part, result, threads);
+    group_means_of<float, V>(a, s, sum, part32, result32, threads);
     if (threadIdx.x < groups) {
         const int64_t g = (int64_t)s.n * a.groups + s.c0 / a.cg + threadIdx.x;
-        if (a.mean) a.mean[g] = own_mean + shared[threadIdx.x * a.cg];
-        if (a.rstd) a.rstd[g] = 1.f / sqrtf(result[threadIdx.x] * count + a.eps);
+        if (a.mean) a.mean[g] = own_mean;
+        if (a.rstd) a.rstd[g] = 1.f / sqrtf(result32[threadIdx.x] + a.eps);
     }
     float scale[V], shift[V];
-    from_table<V>(shared + table, col, scale);
-    from_table<V>(shared + 2 * table, col, shift);
+    from_table<V>(shared, col, scale);
+    from_table<V>(shared + table, col, shift);
 #pragma unroll
-    for (int i = 0; i < V; ++i) scale[i] *= 1.f / sqrtf(result[group[i]] * count + a.eps);
+    for (int i = 0; i < V; ++i) {
+        scale[i] *= 1.f / sqrtf(result32[group[i]] + a.eps);
+        shift[i] = fmaf(-low[i], scale[i], shift[i]);
+    }
     T* const y = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if (r >= mine) continue;
         float v[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = activation<ACT, QUICK>(fmaf(to_float(raw[r].v[i]) - origin[i] - mean[i], scale[i], shift[i]));
+        for (int i = 0; i < V; ++i) v[i] = activation<ACT, QUICK>(fmaf(to_float(raw[r].v[i]) - high[i], scale[i], shift[i]));
         store_floats<T, V>(y + a.py.at(s.ty + r * s.rows, a.W, a.by_w, a.flat) + col, v);
     }
 }

@@ -28,7 +28,7 @@ static void sums(const Shape& s, int channels, int V)
             if (col >= t.columns) continue;
             touch((size_t)tx * V + V - 1 + (s.backward ? 3 * table : 0));
             if (s.backward) touch((size_t)tables + (size_t)(2 * ty + 1) * channels + (size_t)col * V + V - 1);
-            else touch((size_t)tables + 2 * ((size_t)ty * channels + (size_t)col * V + V - 1) + 1);
+            else touch((size_t)tables + 2 * ((size_t)t.rows * channels + (size_t)((V - 1) * t.rows + ty) * t.columns + col) + 1);
         }
         for (int e = tid; s.backward && e < 2 * channels; e += 256) touch((size_t)tables + (size_t)(2 * (t.rows - 1) + (e >= channels)) * channels + e % channels);
     }
@@ -38,7 +38,7 @@ static void apply(const Shape& s, int channels, int V, int cg)
 {
     const int tables = s.backward ? 6 : 3, table = (std::min(channels, 256 * V) + 3) / 4 * 4;
     touch((size_t)tables * table - 1);
-    touch((size_t)tables * table + 2 * (channels / cg) - 1);
+    touch((size_t)tables * table + (s.backward ? 2 : 3) * (channels / cg) - 1);
     if (s.backward) touch(255);                      // the parameters' gradients: a float a thread
 }
 
@@ -46,10 +46,11 @@ static void resident(const Shape& s, int channels, int cg, int threads)
 {
     const int table = (channels + 3) / 4 * 4, groups = channels / cg;
     const Threads t(channels, 4, threads);
-    const size_t before = s.backward ? 6 * (size_t)table + (2 * groups + 3) / 4 * 4 : 3 * (size_t)table + (groups + 3) / 4 * 4;
+    const size_t before = s.backward ? 6 * (size_t)table + (2 * groups + 3) / 4 * 4 : 2 * (size_t)table + 2 * ((groups + 3) / 4 * 4);
     for (int tid = 0; tid < threads; ++tid) {
         const int ty = tid / t.wide, tx = ty < t.rows ? tid - ty * t.wide : t.columns;
-        if (tx < t.columns) touch(before + (s.backward ? (size_t)(2 * ty + 1) : (size_t)ty) * channels + (size_t)tx * 4 + 3);
+        const size_t at = (s.backward ? (size_t)(2 * ty + 1) : (size_t)ty) * channels + (size_t)tx * 4 + 3;
+        if (tx < t.columns) touch(before + (s.backward ? at : 2 * at + 1));         // (forward: 64 bits)
         if (s.backward) touch(before + 2 * (size_t)t.rows * channels + tid);
     }
 }

@@ -15,3 +15,36 @@ def test_a_last_chunk_of_fewer_channels(anr, t, shape, spare):
     """Whose work-groups have more rows of threads than those of a full chunk."""
     N, C, H, W, groups = shape
     norm_case(anr, 80, N, C, H, W, groups, "silu", TYPES[t], spare=spare)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("shape", [(1, 512, 7, 7, 32), (3, 64, 20, 20, 8), (1, 32, 128, 128, 4), (2, 30, 40, 31, 3), (24, 256, 28, 28, 32)])
+@pytest.mark.parametrize("centre,first", [(0, 100), (0, -1000), (0, 60000), (500, 0), (500, -400)])
+def test_statistics_do_not_depend_on_where_a_group_starts(anr, t, shape, centre, first):
+    """The first value of each group far from the others, and all of them far from zero: maps that a work-group holds and others, vectors and single
+    elements.  The mean is a sum in 64 bits, rounded once; the variance one too, or sums in 32 bits of at most 16, 64 and 6 squares after each other, each of a
+    difference off by 2 u; its root halves that and adds three roundings: 64 u.  y: a difference and a product, and a float's last place of the two terms."""
+    N, C, H, W, groups = shape
+    r = rng(81)
+    a = r.normal(size=(N, C, H, W)) + centre
+    a[:, ::C // groups, 0, 0] += first
+    x, gamma, beta = images(a, TYPES[t]), dev(r.normal(size=C) * 0.3 + 1, torch.float32), dev(r.normal(size=C) * 0.3, torch.float32)
+    y, mean, rstd = torch.empty_like(x), nans(N, groups, dtype=torch.float32), nans(N, groups, dtype=torch.float32)
+    anr.group_norm(x, groups, y, gamma, beta, 1e-5, anr.ANR_ACT_NONE, mean, rstd)
+    b = host(beta).reshape(1, C, 1, 1)
+    want, m64, r64, z = O.group_norm(host(x), groups, host(gamma), host(beta), 1e-5, "none")
+    largest = np.abs(host(x).reshape(N, groups, -1)).max(2)
+    within("mean", mean, m64, 2.0 ** -40 * largest, torch.float32)
+    within("rstd", rstd, r64, 64 * U * r64, torch.float32)
+    within("y", y, want, 70 * U * np.abs(z - b) + 4 * U * (np.abs(z) + np.abs(b)), TYPES[t])
+
+
+def test_the_mean_of_values_that_cancel(anr):
+    """Halves of opposite sign and a small rest: the sum is exact in 64 bits, the mean's distance from a value of 1000 four roundings off."""
+    for edge in (12, 24, 100):
+        x = torch.full((2, 64, edge, edge), 1000.0, device="cuda").contiguous(memory_format=torch.channels_last)
+        x[:, :, ::2] = -1000.0
+        x[:, :, 5, 7] += 2.0 ** -10
+        mean, want = nans(2, 8, dtype=torch.float32), 2.0 ** -10 / edge ** 2
+        anr.group_norm(x, 8, torch.empty_like(x), mean=mean)
+        assert (np.abs(host(mean) - want) <= U * want + 4 * 1000 * 2.0 ** -53).all(), edge
