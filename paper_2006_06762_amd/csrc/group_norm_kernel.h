@@ -277,27 +277,17 @@ struct Channels {
     }
 };
 
-// From the chunk's sums of dz gamma and dz gamma xhat of each channel ([2][channels]) those of its groups over the slab.
-__device__ __forceinline__ void group_parts(const Args& a, const Place& s, const float* channel, int threads)
-{
-    float* const out = a.ws + 2 * (((int64_t)s.n * a.slabs + s.slab) * a.groups + s.c0 / a.cg);
-    for (int e = threadIdx.x; e < 2 * (s.channels / a.cg); e += threads) {
-        const float* const from = channel + (e & 1) * s.channels + (e >> 1) * a.cg;
-        float sum = 0.f;
-        for (int c = 0; c < a.cg; ++c) sum += from[c];
-        out[e] = sum;
-    }
-}
-
-// First kernel of the backward pass: sums of dz and dz xhat over the slab, of each channel and, with gamma, of each group.
+// First kernel of the backward pass: sums of dz and dz xhat over the slab, of each channel and, with gamma, of each group.  A thread adds 32 pixels in
+// 32 bits and those sums in 64, in its place in LDS: one after another in 32 bits, 1500 pixels of one value were 250 units of the last
+// place off, and the number of pixels has no bound.
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void backward_sums_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
-    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, then [rows][2][channels]
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, then the sums, [2][V][rows][columns] in 64 bits
     const Place s(a, V);
-    const int table = table_floats(table_channels(s.channels, V));
-    float* const lds = shared + 4 * table;
+    const int table = table_floats(table_channels(s.channels, V)), all = s.rows * s.channels;
+    double* const lds = reinterpret_cast<double*>(shared + 4 * table);
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
     const T* const dy = static_cast<const T*>(a.dy) + s.n * a.pdy.sn + s.c0;
     for (int base = 0; base < s.columns; base += kThreads) {
@@ -308,53 +298,69 @@ __global__ __launch_bounds__(kThreads) void backward_sums_kernel(const Args a)
         if (col >= s.columns) continue;
         Channels<V> ch;
         ch.load(shared, table, s.tx * V);
-        float sum[V], with_hat[V];
+        int p = s.p0 + s.ty;
+        auto add = [&](auto first) {
+            float sum[V], with_hat[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] = with_hat[i] = 0.f;
+            for (int i = 0; i < V; ++i) sum[i] = with_hat[i] = 0.f;
+            const int end = min(s.p1, p + 32 * s.rows);
 #pragma unroll 4
-        for (int p = s.p0 + s.ty; p < s.p1; p += s.rows) {
-            float v[V], d[V];
-            load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
-            load_floats<T, V>(dy + a.pdy.at(p, a.W, a.by_w, a.flat) + col * V, d);
+            for (; p < end; p += s.rows) {
+                float v[V], d[V];
+                load_floats<T, V>(x + a.px.at(p, a.W, a.by_w, a.flat) + col * V, v);
+                load_floats<T, V>(dy + a.pdy.at(p, a.W, a.by_w, a.flat) + col * V, d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float hat, dz;
+                    ch.template element<ACT, QUICK>(i, v[i], d[i], hat, dz);
+                    sum[i] += dz;
+                    with_hat[i] = fmaf(dz, hat, with_hat[i]);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                float hat, dz;
-                ch.template element<ACT, QUICK>(i, v[i], d[i], hat, dz);
-                sum[i] += dz;
-                with_hat[i] = fmaf(dz, hat, with_hat[i]);
+                double* const at = lds + (i * s.rows + s.ty) * s.columns + col;
+                at[0] = (double)sum[i] + (decltype(first)::value ? 0. : at[0]);
+                at[all] = (double)with_hat[i] + (decltype(first)::value ? 0. : at[all]);
             }
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            lds[(2 * s.ty) * s.channels + col * V + i] = sum[i];
-            lds[(2 * s.ty + 1) * s.channels + col * V + i] = with_hat[i];
-        }
+        };
+        add(std::true_type{});
+        while (p < s.p1) add(std::false_type{});
     }
     __syncthreads();
     float* const out = a.sums + ((int64_t)s.n * a.slabs + s.slab) * 2 * a.C + s.c0;
-    for (int e = threadIdx.x; e < 2 * s.channels; e += kThreads) {
-        const int which = e >= s.channels, c = e - which * s.channels;
-        float sum = 0.f;
-        for (int r = 0; r < s.rows; ++r) sum += lds[(2 * r + which) * s.channels + c];
-        out[(int64_t)which * a.C + c] = sum;
-        lds[which * s.channels + c] = sum * parameter(a.gamma, s.c0 + c, a.param_dtype, 1.f);      // (row 0, which this thread alone reads)
+    auto first_row = [&](int which, int c) { return which * all + c % V * s.rows * s.columns + c / V; };
+    for (int e = threadIdx.x; e < 2 * s.channels; e += kThreads) {   // neighbouring threads take neighbouring columns
+        const int which = e >= s.channels, i = (e - which * s.channels) / s.columns, col = e - which * s.channels - i * s.columns, c = col * V + i;
+        double* const at = lds + which * all + i * s.rows * s.columns + col;
+        double sum = 0.;
+#pragma unroll 8
+        for (int r = 0; r < s.rows; ++r) sum += at[r * s.columns];
+        out[(int64_t)which * a.C + c] = (float)sum;
+        at[0] = sum * (double)parameter(a.gamma, s.c0 + c, a.param_dtype, 1.f);      // (row 0, which this thread alone reads)
     }
     __syncthreads();
-    group_parts(a, s, lds, kThreads);
+    float* const of_groups = a.ws + 2 * (((int64_t)s.n * a.slabs + s.slab) * a.groups + s.c0 / a.cg);
+    for (int e = threadIdx.x; e < 2 * (s.channels / a.cg); e += kThreads) {
+        double sum = 0.;
+#pragma unroll 8
+        for (int c = (e >> 1) * a.cg; c < ((e >> 1) + 1) * a.cg; ++c) sum += lds[first_row(e & 1, c)];
+        of_groups[e] = (float)sum;
+    }
 }
 
-// dgamma and dbeta of the chunk: sums over the images' slabs, which the threads of a channel share.
-__device__ __forceinline__ void parameter_gradients(const Args& a, float* lds, int threads)
+// dgamma and dbeta of the chunk: sums over the images' slabs, which the threads of a channel share, in 64 bits (there are as many as images).
+__device__ __forceinline__ void parameter_gradients(const Args& a, double* lds, int threads)
 {
     const int c0 = blockIdx.y * a.chunk, channels = min(a.chunk, a.C - c0), sums = 2 * channels;
     const int64_t parts = (int64_t)a.N * a.slabs;
     for (int base = 0; base < sums; base += threads) {
         const int here = min(sums - base, threads), shares = threads / here, share = threadIdx.x / here, e = base + threadIdx.x - share * here;
         const int which = e >= channels, c = c0 + e - which * channels;
-        float sum = 0.f;
+        double sum = 0.;
         if (share < shares) {
 #pragma unroll 8
-            for (int64_t i = share; i < parts; i += shares) sum += a.sums[(i * 2 + which) * a.C + c];
+            for (int64_t i = share; i < parts; i += shares) sum += (double)a.sums[(i * 2 + which) * a.C + c];
         }
         __syncthreads();
         lds[threadIdx.x] = sum;
@@ -362,13 +368,13 @@ __device__ __forceinline__ void parameter_gradients(const Args& a, float* lds, i
         void* const out = which ? a.dgamma : a.dbeta;
         if (share > 0 || !out) continue;
         for (int i = 1; i < shares; ++i) sum += lds[i * here + threadIdx.x];
-        store_any(out, c, a.param_dtype, sum);
+        store_any(out, c, a.param_dtype, (float)sum);
     }
 }
 
 __global__ __launch_bounds__(kThreads) void backward_parameters_kernel(const Args a)
 {
-    __shared__ float lds[kThreads];
+    __shared__ double lds[kThreads];
     parameter_gradients(a, lds, kThreads);
 }
 
@@ -380,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
     constexpr bool QUICK = sizeof(T) == 2;
     extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, those of the group's two means, and [groups] of the means
     if ((int)blockIdx.z == a.N) {
-        if (blockIdx.x == 0) parameter_gradients(a, shared, kThreads);
+        if (blockIdx.x == 0) parameter_gradients(a, reinterpret_cast<double*>(shared), kThreads);
         return;
     }
     const Place s(a, V);
@@ -396,8 +402,8 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
         dz = wave_sum(dz);
         with_hat = wave_sum(with_hat);
         if ((threadIdx.x & 63) == 0) {
-            means[2 * g] = dz / ((float)a.HW * (float)a.cg);
-            means[2 * g + 1] = with_hat / ((float)a.HW * (float)a.cg);
+            means[2 * g] = dz / (float)a.values;
+            means[2 * g + 1] = with_hat / (float)a.values;
         }
     }
     const T* const x = static_cast<const T*>(a.x) + s.n * a.px.sn + s.c0;
@@ -548,7 +554,7 @@ __global__ __launch_bounds__(1024) void backward_resident_kernel(const Args a)
 {
     constexpr bool QUICK = sizeof(T) == 2;
     constexpr int V = kHeldChannels;
-    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, [2][channels], [groups] of two means, [rows][2][channels], [threads]
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // the tables, [2][channels], [groups] of two means, [rows][2][channels], [threads] in 64 bits
     const int threads = blockDim.x;
     const Place s(a, V, threads);
     const int table = table_floats(s.channels), groups = s.channels / a.cg;
@@ -594,29 +600,29 @@ __global__ __launch_bounds__(1024) void backward_resident_kernel(const Args a)
     }
     __syncthreads();
     // the threads of a channel share the rows
-    float* const shares_of = part + 2 * s.rows * s.channels;
+    double* const shares_of = reinterpret_cast<double*>(part + 2 * s.rows * s.channels);
     for (int base = 0; base < 2 * s.channels; base += threads) {
         const int here = min(2 * s.channels - base, threads), shares = threads / here, share = threadIdx.x / here, e = base + threadIdx.x - share * here;
         const int which = e >= s.channels, c = e - which * s.channels;
-        float v = 0.f;
+        double v = 0.;
         if (share < shares) {
 #pragma unroll 4
-            for (int r = share; r < s.rows; r += shares) v += part[(2 * r + which) * s.channels + c];
+            for (int r = share; r < s.rows; r += shares) v += (double)part[(2 * r + which) * s.channels + c];
         }
         __syncthreads();
         shares_of[threadIdx.x] = v;
         __syncthreads();
         if (share > 0) continue;
         for (int i = 1; i < shares; ++i) v += shares_of[i * here + threadIdx.x];
-        a.sums[((int64_t)s.n * 2 + which) * a.C + s.c0 + c] = v;
-        total[which * table + c] = v * shared[2 * table + c];
+        a.sums[((int64_t)s.n * 2 + which) * a.C + s.c0 + c] = (float)v;
+        total[which * table + c] = (float)v * shared[2 * table + c];
     }
     if (!a.y) return;
     __syncthreads();
     for (int e = threadIdx.x; e < 2 * groups; e += threads) {
-        float v = 0.f;
-        for (int c = 0; c < a.cg; ++c) v += total[(e & 1) * table + (e >> 1) * a.cg + c];
-        means[e] = v / ((float)a.HW * (float)a.cg);
+        double v = 0.;
+        for (int c = 0; c < a.cg; ++c) v += (double)total[(e & 1) * table + (e >> 1) * a.cg + c];
+        means[e] = (float)(v / a.values);
     }
     __syncthreads();
     float mean_dz[V], mean_with_hat[V];

@@ -25,20 +25,20 @@ constexpr int rows_of(int channels, int V, int threads) { return threads / (colu
 constexpr int table_channels(int channels, int V) { return channels < kThreads * V ? channels : kThreads * V; }
 
 // Floats of LDS that a work-group on `channels` channels uses: of the kernels that sum (a table and two numbers of 64 bits a channel and row; backward four
-// tables and two floats), of the resident ones, of those that apply.
+// tables), of the resident ones, of those that apply.
 constexpr size_t sums_lds_floats(bool backward, int channels, int V)
 {
-    return (backward ? 4 : 1) * (size_t)table_floats(table_channels(channels, V)) + (backward ? 2 : 4) * (size_t)rows_of(channels, V, kThreads) * channels;
+    return (backward ? 4 : 1) * (size_t)table_floats(table_channels(channels, V)) + 4 * (size_t)rows_of(channels, V, kThreads) * channels;
 }
 constexpr size_t resident_lds_floats(bool backward, int channels, int cg, int threads)
 {
     const size_t groups = channels / cg, part = (size_t)rows_of(channels, kHeldChannels, threads) * channels;
-    return backward ? 6 * (size_t)table_floats(channels) + table_floats(2 * groups) + 2 * part + threads : 2 * (size_t)table_floats(channels) + 2 * ((size_t)table_floats(groups) + part);
+    return backward ? 6 * (size_t)table_floats(channels) + table_floats(2 * groups) + 2 * part + 2 * (size_t)threads : 2 * (size_t)table_floats(channels) + 2 * ((size_t)table_floats(groups) + part);
 }
 constexpr size_t apply_lds_floats(bool backward, int channels, int cg, int V)
 {
     const size_t floats = (backward ? 6 : 3) * (size_t)table_floats(table_channels(channels, V)) + (backward ? 2 : 3) * (size_t)(channels / cg);
-    return backward && floats < (size_t)kThreads ? (size_t)kThreads : floats;        // (the parameters' gradients take a float a thread)
+    return backward && floats < (size_t)2 * kThreads ? (size_t)2 * kThreads : floats;        // (the parameters' gradients take 64 bits a thread)
 }
 
 // A call, and how its kernels divide it.

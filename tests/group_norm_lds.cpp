@@ -27,10 +27,8 @@ static void sums(const Shape& s, int channels, int V)
             for (int c = tid; c < here; c += 256) touch(s.backward ? 3 * (size_t)table + c : (size_t)c);
             if (col >= t.columns) continue;
             touch((size_t)tx * V + V - 1 + (s.backward ? 3 * table : 0));
-            if (s.backward) touch((size_t)tables + (size_t)(2 * ty + 1) * channels + (size_t)col * V + V - 1);
-            else touch((size_t)tables + 2 * ((size_t)t.rows * channels + (size_t)((V - 1) * t.rows + ty) * t.columns + col) + 1);
+            touch((size_t)tables + 2 * ((size_t)t.rows * channels + (size_t)((V - 1) * t.rows + ty) * t.columns + col) + 1);      // (64 bits)
         }
-        for (int e = tid; s.backward && e < 2 * channels; e += 256) touch((size_t)tables + (size_t)(2 * (t.rows - 1) + (e >= channels)) * channels + e % channels);
     }
 }
 
@@ -39,7 +37,7 @@ static void apply(const Shape& s, int channels, int V, int cg)
     const int tables = s.backward ? 6 : 3, table = (std::min(channels, 256 * V) + 3) / 4 * 4;
     touch((size_t)tables * table - 1);
     touch((size_t)tables * table + (s.backward ? 2 : 3) * (channels / cg) - 1);
-    if (s.backward) touch(255);                      // the parameters' gradients: a float a thread
+    if (s.backward) touch(2 * 255 + 1);              // the parameters' gradients: 64 bits a thread
 }
 
 static void resident(const Shape& s, int channels, int cg, int threads)
@@ -51,7 +49,7 @@ static void resident(const Shape& s, int channels, int cg, int threads)
         const int ty = tid / t.wide, tx = ty < t.rows ? tid - ty * t.wide : t.columns;
         const size_t at = (s.backward ? (size_t)(2 * ty + 1) : (size_t)ty) * channels + (size_t)tx * 4 + 3;
         if (tx < t.columns) touch(before + (s.backward ? at : 2 * at + 1));         // (forward: 64 bits)
-        if (s.backward) touch(before + 2 * (size_t)t.rows * channels + tid);
+        if (s.backward) touch(before + 2 * (size_t)t.rows * channels + 2 * tid + 1);
     }
 }
 

@@ -48,3 +48,52 @@ def test_the_mean_of_values_that_cancel(anr):
         mean, want = nans(2, 8, dtype=torch.float32), 2.0 ** -10 / edge ** 2
         anr.group_norm(x, 8, torch.empty_like(x), mean=mean)
         assert (np.abs(host(mean) - want) <= U * want + 4 * 1000 * 2.0 ** -53).all(), edge
+
+
+def gradients_of_long_sums(anr, x, dy, groups, k):
+    """dbeta, dgamma and dx of a norm without activation and parameters within k u of the sums of their terms' magnitudes, and what xhat's roundings make:
+    a difference, to u of its terms, and a product.  In 64 bits on the GPU (the CPU takes minutes)."""
+    N, C, S = x.shape
+    mean, rstd = nans(N, groups, dtype=torch.float32), nans(N, groups, dtype=torch.float32)
+    anr.group_norm(x, groups, torch.empty_like(x), mean=mean, rstd=rstd)
+    dx, dgamma, dbeta = torch.empty_like(x), nans(C, dtype=torch.float32), nans(C, dtype=torch.float32)
+    anr.group_norm_backward(dy, x, groups, None, None, mean, rstd, dx, dgamma, dbeta)
+    of_group = lambda v: v.double().repeat_interleave(C // groups, 1)[:, :, None]  # noqa: E731
+    means = lambda v: of_group(v.reshape(N, groups, -1).mean(2))  # noqa: E731
+    m, s, d = of_group(mean), of_group(rstd), dy.double()
+    hat = (x.double() - m) * s
+    ehat = 4 * U * (hat.abs() + (x.double().abs() + m.abs()) * s)
+    half = HALF[x.dtype]
+
+    def close(name, got, want, bound, half):
+        over = ((got.double() - want).abs() - bound - half * (want.abs() + bound)).max().item()
+        assert over <= 0, "%s: %g over the bound" % (name, over)
+
+    close("dbeta", dbeta, d.sum((0, 2)), k * U * d.abs().sum((0, 2)), U)
+    close("dgamma", dgamma, (d * hat).sum((0, 2)), k * U * (d * hat).abs().sum((0, 2)) + (d.abs() * ehat).sum((0, 2)), U)
+    dhat = means((d * hat).abs())
+    close("dx", dx, s * (d - means(d) - hat * means(d * hat)), s * (k * U * (d.abs() + means(d.abs()) + hat.abs() * dhat) + ehat * dhat + hat.abs() * means(d.abs() * ehat)), half)
+
+
+@pytest.mark.parametrize("t,C,S", [("f32", 3, 1 << 24), ("f32", 4, 1 << 23), ("bf16", 8, 1 << 23), ("f16", 30, 1 << 20)])
+def test_gradients_of_one_large_map(anr, t, C, S):
+    """A gradient that is the same everywhere, of no whole number: sums of 32 in 32 bits, of those in 64, rounded, of at most eight slabs a lane and six joins, and
+    four roundings of the terms: 50 u."""
+    x = torch.randn(1, S, C, device="cuda").to(TYPES[t]).transpose(1, 2)
+    gradients_of_long_sums(anr, x, torch.full_like(x, 0.7), 1, 50)
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("t,C", [("f32", 3), ("f32", 4), ("bf16", 8), ("f16", 5)])
+def test_gradients_of_the_most_images(anr, t, C):
+    """The parameters' sums over 65534 images of two pixels, 50 u as above."""
+    x = torch.randn(65534, 2, C, device="cuda").to(TYPES[t]).transpose(1, 2)
+    gradients_of_long_sums(anr, x, torch.full_like(x, 0.7), 1, 50)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("shape", [(1, 8192, 2, 1, 1), (2, 8192, 9, 5, 1), (1, 8184, 3, 1, 1), (1, 8191, 3, 2, 1)])
+def test_the_widest_groups(anr, t, shape):
+    """Whose sums take all of a CU's shared memory."""
+    N, C, H, W, groups = shape
+    norm_case(anr, 82, N, C, H, W, groups, "silu", TYPES[t])
