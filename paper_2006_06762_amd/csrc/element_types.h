@@ -81,17 +81,25 @@ __device__ __forceinline__ float sigmoid(float z)
     return 1.f / (1.f + expf(-z));
 }
 
-// Phi(z), and exp(-z^2 / 2).  QUICK: by Abramowitz and Stegun's formula 7.1.26, erf to 1.5e-7, which shares the exponential; else by the
-// library's erf.
+// Phi(z), and exp(-z^2 / 2).  QUICK: by Abramowitz and Stegun's formula 7.1.26, erf to 1.5e-7, which shares the exponential; else, for float32, to 10 u of
+// itself (u = 2^-24) and z^2 / 4 more below -1 for the rounding of the exponential's argument: within a unit of zero as 0.5 + z P(z^2), and what lies beyond a
+// = |z| otherwise as exp(-a^2 / 2) t P(1 - 2 k t) with t = 1 / (a + k), k = 3.58, polynomials of least relative error over [1, 14] (1 u) and [0, 1].
+// 0.5 (1 + erf), which has few bits left below -4 and none below -6, took longer: norm backward, 4 x 128^2 x 256, 69.9 us, so 68.2, with erfc 77.9;
+// forward 39.4, 39.3, 42.1, but 8 x 56^2 x 320 24.1, 25.0, 26.8.
 template <bool QUICK>
 __device__ __forceinline__ float normal_below(float z, float& bell)
 {
+    const float a = fabsf(z);
     if (!QUICK) {
-        bell = expf(-0.5f * z * z);
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f));
+        const float w = z * z;
+        bell = expf(-0.5f * w);
+        const float middle = fmaf(z, fmaf(w, fmaf(w, fmaf(w, fmaf(w, fmaf(w, -7.65420373e-6f, 1.13486356e-4f), -1.18632987e-3f), 9.97332297e-3f), -0.0664903596f), 0.398942292f), 0.5f);
+        const float t = __builtin_amdgcn_rcpf(a + 3.58f), q = fmaf(-7.16f, t, 1.f);
+        const float tail = fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, -0.00334144803f, 0.00508789485f), 0.0234102663f), -0.127396584f), 0.327804804f), -0.573150635f), 0.746405363f) * t * bell;
+        return a < 1.f ? middle : z > 0.f ? 1.f - tail : tail;             // (a NaN's tail is one)
     }
     bell = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, a, 1.f));
     const float tail = 0.5f * bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
     return z > 0.f ? 1.f - tail : tail;                                    // (a NaN's tail is one)
 }
