@@ -495,7 +495,7 @@ __global__ __launch_bounds__(1024) void resident_kernel(const Args a)
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int i = 0; i < V; ++i) total[i] += r < mine ? (double)to_float(raw[r].v[i]) : 0.;
+        for (int i = 0; i < V; ++i) total[i] += (double)(r < mine ? to_float(raw[r].v[i]) : 0.f);
     if constexpr (QUICK && R == 16) {                                 // (what is held are the 16 bits: the floats, kept from sum to sum, do not fit the registers)
         typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
