@@ -51,6 +51,7 @@ Plan make_plan_with(const GroupNormArgs& g, bool backward, bool vector)
     a.W = g.W;
     a.by_w = make_fastdiv(g.W);
     a.by_cg = make_fastdiv(a.cg);
+    a.by_each = make_fastdiv(a.cg % kHeldChannels == 0 ? a.cg / kHeldChannels : a.cg);
 
     const int es = element_bytes(g.dtype), line = 128 / es;
     p.vector = vector;

@@ -47,6 +47,7 @@ struct Args {
     float* sums;                    // backward: sums of each channel over the slabs, [N][slabs][2][C]
     Pixels px, pdy, py;
     FastDiv by_w, by_cg;
+    FastDiv by_each;                // resident: sums of a group in a row of threads, one a thread where its channels are of one group
     float eps;
     int N, HW, W, C, groups, cg, flat, param_dtype;
     int chunk;                      // channels of a chunk: whole groups
@@ -446,21 +447,30 @@ __global__ __launch_bounds__(kThreads) void backward_apply_kernel(const Args a)
 // ---- resident: a work-group holds its chunk of an image, at most R vectors of kHeldChannels channels a thread
 
 // Means over the work-group's rows and each group's channels of what a thread has summed of each channel; that of group g at
-// result[g].  (By a division: that of equal values is that value.)  `part`: [rows][channels].
+// result[g].  (By a division: that of equal values is that value.)  `part`: [rows][channels], or a place a thread where its channels are of one group.
 template <typename S, int V>
 __device__ __forceinline__ void group_means_of(const Args& a, const Place& s, const S (&v)[V], S* part, S* result, int threads)
 {
+    const bool whole = a.cg % V == 0;
+    const int width = whole ? s.columns : s.channels, each = whole ? a.cg / V : a.cg;       // of a row, of a group in it
     if (s.tx < s.columns) {
+        if (whole) {
+            S sum = v[0];
 #pragma unroll
-        for (int i = 0; i < V; ++i) part[s.ty * s.channels + s.tx * V + i] = v[i];
+            for (int i = 1; i < V; ++i) sum += v[i];
+            part[s.ty * width + s.tx] = sum;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) part[s.ty * width + s.tx * V + i] = v[i];
+        }
     }
     __syncthreads();
-    const int groups = s.channels / a.cg, lane = threadIdx.x & 63, entries = s.rows * a.cg;
+    const int groups = s.channels / a.cg, lane = threadIdx.x & 63, entries = s.rows * each;
     for (int g = threadIdx.x >> 6; g < groups; g += threads >> 6) {
         S sum = 0;
         for (int e = lane; e < entries; e += 64) {
-            const int row = a.by_cg.div(e);
-            sum += part[row * s.channels + g * a.cg + e - row * a.cg];
+            const int row = a.by_each.div(e);
+            sum += part[row * width + g * each + e - row * each];
         }
         sum = wave_sum(sum);
         if (lane == 0) result[g] = sum / (S)a.values;
@@ -507,11 +517,9 @@ __global__ __launch_bounds__(1024) void resident_kernel(const Args a)
     }
     group_means_of<double, V>(a, s, total, part, result, threads);
     float high[V], low[V], sum[V];                                   // the mean, and its rest
-    int group[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        group[i] = a.by_cg.div(col + i);
-        two_floats(result[group[i]], high[i], low[i]);
+        two_floats(result[a.by_cg.div(col + i)], high[i], low[i]);
         sum[i] = 0.f;
     }
     const float own_mean = threadIdx.x < groups ? (float)result[threadIdx.x] : 0.f;
@@ -534,7 +542,7 @@ __global__ __launch_bounds__(1024) void resident_kernel(const Args a)
     from_table<V>(shared + table, col, shift);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        scale[i] *= 1.f / sqrtf(result32[group[i]] + a.eps);
+        scale[i] *= 1.f / sqrtf(result32[a.by_cg.div(col + i)] + a.eps);
         shift[i] = fmaf(-low[i], scale[i], shift[i]);
     }
     T* const y = static_cast<T*>(a.y) + s.n * a.py.sn + s.c0;
