@@ -17,10 +17,16 @@ namespace anr {
 namespace {
 
 constexpr int kThreads = 256;
-// Calls of few tokens (ff_rows_kernel.h): sixteen, and up to 64 while each work-group's pass over them costs less than the tiles of 128 tokens that
-// are mostly empty. us, T tokens so / in tiles: 1024 -> 2816 bf16, T = 64, 24 / 26, 2048 -> 5632, T = 32, 36 / 37, 64 52 / 37, 4096 -> 11264, T = 17,
-// 67 / 74, 32 87 / 75; float32 T = 64 43 / 51, 101 / 121, 285 / 386.
-bool few_tokens(const anr_gated_ff_desc& d) { return d.T <= 16 || (d.T <= 64 && (d.dtype == ANR_F32 || d.T * d.C * d.F <= (int64_t)600000000)); }
+// Calls of few tokens (ff_rows_kernel.h): sixteen, in float32 32, and up to 64 while each work-group's pass over them costs less than the tiles of 128 tokens that
+// are mostly empty. us, T tokens so / in tiles: 16 bits, 1024 -> 2816 T = 17 15.4 / 21.6, 48 21.9 / 22.8, 64 23.9 / 23.6, 1536 -> 4096 33 24.7 / 26.4, 40 26.5 /
+// 26.5, 48 28.2 / 27.0, 2048 -> 5632 17 29.3 / 29.5, 20 30.7 / 29.0, 64 51.7 / 32.5, 2560 -> 6912 17 40.1 / 41.3, 20 42.7 / 41.6, 4096 -> 11264 17 73.7 / 67.4, 64
+// 140 / 73; float32, 1024 -> 2816 17 24 / 40, 48 38 / 41, 64 43.5 / 41.3, 1536 -> 4096 32 38 / 51, 48 51.8 / 51.3, 2048 -> 5632 17 60 / 69, 32 75.8 / 73.0, 64
+// 116 / 75, 2560 -> 6912 32 97 / 88, 4096 -> 11264 17 144 / 210, 32 185 / 215, 48 246 / 217.
+bool few_tokens(const anr_gated_ff_desc& d)
+{
+    const bool f32 = d.dtype == ANR_F32;
+    return d.T <= (f32 ? 32 : 16) || (d.T <= 64 && d.T * d.C * d.F <= (int64_t)(f32 ? 150000000 : 220000000));
+}
 
 size_t whole_lines(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
