@@ -521,16 +521,10 @@ hipError_t backward_16(const GatedFfArgs& g, hipStream_t stream)
 
 // ---- float32 products
 
-hipError_t forward_32(const GatedFfArgs& g, hipStream_t stream)
+// Gate, up, activation and product in one launch: what it multiplies, and whether it runs, by the descriptor alone.
+GatedGemmArgs gated_product(const anr_gated_ff_desc& d)
 {
-    const anr_gated_ff_desc& d = g.d;
-    const size_t tf = whole_lines((size_t)d.T * d.F * 4) / 4;
-    float* const h = static_cast<float*>(g.ws);
     GatedGemmArgs a{};
-    a.A = static_cast<const float*>(g.x);
-    a.B = static_cast<const float*>(g.w_gate);
-    a.B2 = static_cast<const float*>(g.w_up);
-    a.C = h;
     a.M = (int)d.T;
     a.N = (int)d.F;
     a.K = (int)d.C;
@@ -539,12 +533,27 @@ hipError_t forward_32(const GatedFfArgs& g, hipStream_t stream)
     a.ldc = d.F;
     a.batch = a.batch_inner = 1;
     a.b_is_nk = true;
-    a.gate = static_cast<float*>(g.gate);
-    a.up = static_cast<float*>(g.up);
     a.ld_pre = d.ldpre;
     a.act = d.act;
+    return a;
+}
+// Of the workspace: h, and gate and up where they are products of their own.
+int hidden_matrices(const anr_gated_ff_desc& d) { return gemm_split_gated_takes(gated_product(d)) ? 1 : 3; }
+
+hipError_t forward_32(const GatedFfArgs& g, hipStream_t stream)
+{
+    const anr_gated_ff_desc& d = g.d;
+    const size_t tf = whole_lines((size_t)d.T * d.F * 4) / 4;
+    float* const h = static_cast<float*>(g.ws);
+    GatedGemmArgs a = gated_product(d);
+    a.A = static_cast<const float*>(g.x);
+    a.B = static_cast<const float*>(g.w_gate);
+    a.B2 = static_cast<const float*>(g.w_up);
+    a.C = h;
+    a.gate = static_cast<float*>(g.gate);
+    a.up = static_cast<float*>(g.up);
     hipError_t e = hipSuccess;
-    if (gemm_split_gated_takes(a)) {
+    if (hidden_matrices(d) == 1) {
         e = launch_gemm_split_gated(a, stream);
     } else {
         float* const gate = g.gate ? a.gate : h + tf;
@@ -559,7 +568,7 @@ hipError_t forward_32(const GatedFfArgs& g, hipStream_t stream)
             });
     }
     if (e != hipSuccess) return e;
-    return gemm_in_parts(h, d.F, static_cast<const float*>(g.w_down), d.ld_down, true, static_cast<float*>(g.y), d.ldy, d.T, d.C, d.F, h + 3 * tf, stream);
+    return gemm_in_parts(h, d.F, static_cast<const float*>(g.w_down), d.ld_down, true, static_cast<float*>(g.y), d.ldy, d.T, d.C, d.F, h + hidden_matrices(d) * tf, stream);
 }
 
 hipError_t backward_32(const GatedFfArgs& g, hipStream_t stream)
@@ -618,7 +627,7 @@ size_t gated_ff_workspace_bytes(const GatedFfArgs& g, bool backward)
     if (!backward && few_tokens(d)) return tf;
     if (d.dtype == ANR_F32) {
         if (backward) return 6 * tf + whole_lines(F * C * 8) + whole_lines(T * C * 4) + parts_bytes(d.T, d.C, 2 * d.F);
-        return 3 * tf + parts_bytes(d.T, d.C, d.F);
+        return hidden_matrices(d) * tf + parts_bytes(d.T, d.C, d.F);
     }
     const int splits = splits_of(d.T, d.C, (backward ? 2 : 1) * chunks_of(d.F));
     const size_t parts = whole_lines(splits > 1 ? (size_t)splits * T * C * 4 : 0), copied = copies(d, backward) ? copied_bytes(d, backward) : 0;
