@@ -85,18 +85,19 @@ inline int held_by(const Shape& s, int chunk)
 
 // Where the resident kernels run: a chunk of an image fits the registers of a work-group (vectors of four channels a thread), and all work-groups the
 // CUs at once, at 1024 threads each. 256 channels, groups of 8, SiLU, against the kernels that read twice (us, resident / not):
-// forward, 16 bits, 20^2 x 16 images (7 vectors) 9.0 / 13.3, 28^2 x 64 (13) 17 / 22; float32 20^2 x 16 (4) 10.8 / 12.3, but 24^2 x 4 (5) 11.3 / 9.7, 28^2 x 1
-// (7) 11.8 / 10.2, x 16 15.1 / 14.7, with work-groups for most CUs 28^2 x 24 17.1 / 18.0, 32^2 x 32 20.6 / 24.7, 40^2 x 28 (13) 27.6 / 30.1.
-// Backward, float32 28^2 x 1 11.5 / 12.3, x 32 23.0 / 29.5, 24^2 x 4 11.0 / 10.3; 16 bits 20^2 x 16 12.3 / 13.6, x 64 19.8 / 21.6, 28^2 x 16 (13) 22 / 19.
-// More than fit at once: float32 20^2 x 40 21.3 / 16.3, 23.1 / 20.3, 10^2 x 128 27.8 / 15.1; bf16 14^2 x 128 16.1 / 17.3, 21.1 / 19.7, 7^2 x 256 22.6 / 16.1
-// (512 of 448 threads fit: float32 7^2 x 64 7.5 / 10.4).
+// forward, 16 bits, 20^2 x 16 images (7 vectors) 8.1 / 11.8, 28^2 x 64 (13) 17.7 / 21.0; float32 20^2 x 16 (4) 9.4 / 11.4, with work-groups for half the CUs
+// 24^2 x 16 (5) 10.1 / 12.1, 28^2 x 16 12.0 / 13.6, 40^2 x 16 (13) 16.9 / 19.0, 40^2 x 28 26.6 / 29.1, but for fewer 24^2 x 4 8.8 / 8.8, 28^2 x 1 (7) 9.3 / 9.5, 32^2
+// x 4 (8) 10.4 / 9.3, 40^2 x 8 14.9 / 14.1, x 1 12.5 / 8.8.
+// Backward, float32 28^2 x 1 11.4 / 11.1, x 32 23.5 / 29.3, 24^2 x 4 10.9 / 10.4; 16 bits 20^2 x 16 12.6 / 12.3, x 64 20.2 / 23.9, 14^2 x 32 10.6 / 12.2.
+// More than fit at once, forward and backward: float32 20^2 x 40 18.2 / 15.1, 23.6 / 20.7, 10^2 x 128 23.4 / 14.1, 26.5 / 17.6; bf16 14^2 x 128 14.9 / 15.8, 23.9 /
+// 19.9, 7^2 x 256 21.7 / 15.5, 28.8 / 20.0 (512 of 448 threads fit: float32 7^2 x 64 6.8 / 9.4, 8.9 / 10.5).
 inline bool resident_pays(const Shape& s, int chunk, int64_t work_groups)
 {
     const int columns = columns_of(chunk, kHeldChannels);
     if (columns > 256) return false;
     const int64_t threads = std::min<int64_t>(kResidentThreads, ((int64_t)s.HW * columns + 63) / 64 * 64);
     if (work_groups * threads > 256 * kResidentThreads) return false;
-    return held_by(s, chunk) <= (s.backward ? 8 : s.es == 2 || work_groups >= 192 ? 16 : 4);
+    return held_by(s, chunk) <= (s.backward ? 8 : s.es == 2 || work_groups >= 128 ? 16 : 4);
 }
 
 // f(channels) of the larger of a full chunk and the last one.
@@ -121,10 +122,10 @@ inline Division divide(const Shape& s)
     };
     take(chunk_of(128));
     // Resident kernels take chunks of 64 bytes where work-groups of 128 would be half the CUs or fewer: the backward pass, and the forward one where a thread
-    // has more than four vectors. 256 channels, chunks of 128 / 64 bytes (us): backward, float32 14^2 x 16 images 9.9 / 10.0, 20^2 x 1 10.5 / 10.0, 28^2 x 1
-    // 14.3 / 11.5, x 16 18.6 / 16.4; bf16 14^2 x 32 11.7 / 10.4, 20^2 x 16 15.5 / 12.4. Forward, bf16 14^2 x 32 8.0 / 8.6, 20^2 x 16 9.7 / 9.0, x 48 (more
-    // than half the CUs) 11.1 / 17.2, 28^2 x 16 14.0 / 11.3. Of maps that only the halves hold, those of 16-bit types with 64 work-groups, forward: against the
-    // kernels that read twice bf16 36^2 x 16 17.3 / 15.1, but 40^2 x 1 12.2 / 14.0, and backward 28^2 x 16 15.6 / 17.4.
+    // has more than four vectors. 256 channels, chunks of 128 / 64 bytes (us): backward, float32 14^2 x 16 images 10.0 / 9.8, 20^2 x 1 10.7 / 10.0, 28^2 x 1
+    // 14.6 / 11.4, x 16 19.0 / 16.5; bf16 14^2 x 32 11.9 / 10.6, 20^2 x 16 15.8 / 12.6. Forward, bf16 14^2 x 32 (4 vectors) 7.6 / 7.5, 20^2 x 16 9.6 / 8.1, x 48 (more
+    // than half the CUs) 10.7 / 14.4, 28^2 x 16 14.7 / 10.3. Of maps that only the halves hold, those of 16-bit types with 64 work-groups, forward: against the
+    // kernels that read twice bf16 36^2 x 16 15.0 / 16.2, but 40^2 x 1 14.3 / 10.6, float32 52^2 x 8 21.5 / 17.7.
     const int64_t work_groups = (int64_t)d.chunks * s.N;
     if (s.vector && chunk_of(64) < d.chunk && work_groups <= 128 &&
         (resident_pays(s, d.chunk, work_groups) ? s.backward || held_by(s, d.chunk) > 4 : !s.backward && s.es == 2 && work_groups >= 64) &&

@@ -97,3 +97,9 @@ def test_the_widest_groups(anr, t, shape):
     """Whose sums take all of a CU's shared memory."""
     N, C, H, W, groups = shape
     norm_case(anr, 82, N, C, H, W, groups, "silu", TYPES[t])
+
+
+@pytest.mark.parametrize("shape", [(16, 256, 24, 24, 32), (16, 256, 28, 28, 32), (4, 1024, 32, 32, 32), (16, 320, 23, 29, 32), (8, 512, 40, 40, 64)])
+def test_float32_maps_held_by_half_the_work_groups(anr, shape):
+    N, C, H, W, groups = shape
+    norm_case(anr, 83, N, C, H, W, groups, "silu", torch.float32)
