@@ -135,14 +135,15 @@ inline Division divide(const Shape& s)
     }
     const int rows = rows_of(d.chunk, d.V, kThreads);
     // Slabs: about four work-groups per CU as far as each thread has eight pixels (float32: four), one per CU as far as it has two, and at
-    // most 128 that are joined. (Eight or four, backward, 320 channels: float32 8 x 56^2 47 / 36 us, bf16 34 / 35, 4 x 95 x 63 32 / 34.)
+    // most 128 that are joined. (Eight or four, backward, 320 channels: bf16 8 x 64^2 27.8 / 35.8 us, 4 x 95 x 63 22.6 / 25.9.)
     const int64_t others = (int64_t)d.chunks * s.N;
     int64_t slabs = std::min((1024 + others - 1) / others, (int64_t)s.HW / ((s.es == 4 ? 4 : 8) * rows));
     slabs = std::max(slabs, std::min((256 + others - 1) / others, (int64_t)s.HW / (2 * rows)));
     slabs = std::max<int64_t>(1, std::min<int64_t>(slabs, 128));
-    // Work-groups go round-robin to the eight XCDs: those that share the lines at a chunk's ends to the same one (4 x 95 x 63 x 320 bf16, chunks of 160 bytes,
-    // 29 / 24 slabs, forward 21.7 / 20.4 us, backward 27.8 / 25.3; level where chunks are whole lines).
-    if (slabs > 8) slabs = slabs / 8 * 8;
+    // Work-groups go round-robin to the eight XCDs: those that share the lines at a chunk's ends to the same one. As it comes / down to eights / to the nearest
+    // eight, bf16, chunks of 160 bytes: 4 x 95 x 63 x 320 (29 slabs) forward 19.7 / 18.3 / 17.6 us, backward 27.0 / 25.2 / 22.6, 8 x 56^2 x 320 (15) 20.4 / 21.2 / 18.9,
+    // 28.0 / 30.5 / 22.9; level where chunks are whole lines.
+    if (slabs > 8) slabs = (slabs + 4) / 8 * 8;
     d.slab_pixels = (int)((s.HW + slabs - 1) / slabs);
     d.slabs = (s.HW + d.slab_pixels - 1) / d.slab_pixels;
     d.sums_lds = sizeof(float) * of_chunks(d, s.C, [&](int channels) { return sums_lds_floats(s.backward, channels, d.V); });
