@@ -390,13 +390,15 @@ typedef struct {
 
 /* g = x w_gate^T, u = x w_up^T, h = act(g) u, y = h w_down^T.  g and u go to `gate` and `up`
  * where those are given (both or neither), which a backward call takes.  h is held in `dtype`
- * between the products, made from g and u before they are rounded. */
+ * between the products, made from g and u before they are rounded: in float16 it has to stay
+ * below 65504. */
 anr_status anr_gated_ff(const anr_gated_ff_desc *desc, const void *x, const void *w_gate, const void *w_up,
                         const void *w_down, void *y, void *gate, void *up, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Gradients of anr_gated_ff from its x, weights, gate and up: dh = dy w_down,
  * dg = dh u act'(g), du = dh act(g), dx = dg w_gate + du w_up, dw_gate = dg^T x,
- * dw_up = du^T x, dw_down = dy^T h.  dg, du and h are held in `dtype` between the products.
+ * dw_up = du^T x, dw_down = dy^T h.  dg, du and h are held in `dtype` between the products
+ * (float16: dy is scaled by the caller so that they neither overflow nor vanish).
  * dx, dw_gate, dw_up, dw_down: NULL for what is not wanted, not all four. */
 anr_status anr_gated_ff_backward(const anr_gated_ff_desc *desc, const void *dy, const void *x, const void *w_gate,
                                  const void *w_up, const void *w_down, const void *gate, const void *up, void *dx,

@@ -160,7 +160,7 @@ __global__ __launch_bounds__(1024) void rows_kernel(const Args a)
             }
             device_activation(a.act, [&](auto act) { out = activation<decltype(act)::value, sizeof(T) == 2>(v[0]) * v[MATS - 1]; });
         }
-        static_cast<T*>(a.d)[token * a.ldd + n] = from_float<T>(out);
+        static_cast<T*>(a.d)[token * a.ldd + n] = from_float<T>(out);          // (gated: h, in the type that the next product's instructions take)
     }
 }
 

@@ -384,8 +384,8 @@ int64_t chunks_of(int64_t K) { return (K + mm16::BK - 1) / mm16::BK; }
 
 // The tile with the shortest estimated time: rounds of work-groups over the CUs, each with its chunks and ends (us). A tile of 256 takes a CU
 // for itself, of those of 128 it takes two; one alone is split over two groups of waves. Measured (256 / 128 / 128 twice, 4096 tokens, 1024 -> 2816):
-// gate and up 64 / 58 / 77 us, down 62 / 32 / 31, hidden gradients 53 / 54 / 70, dx 113 / 62 / 55, weights 95 / 106 / 112; 8192 tokens, 4096 -> 11264:
-// 1394 / 1430 / 1610, 630 / 741 / 815, 843 / 915 / 1160, 1217 / 1640 / 1750, 1920 / 2360 / 2520.
+// gate and up, both stored, 72 / 72 / 88 us, down 61 / 32 / 30, hidden gradients 54 / 53 / 70, dx 111 / 62 / 54, weights 93 / 103 / 110; 8192 tokens, 4096 -> 11264:
+// 1226 / 1568 / 1792, 564 / 745 / 835, 848 / 925 / 1175, 1142 / 1580 / 1682, 1851 / 2328 / 2492.
 struct Choice {
     mm16::Shape shape;
     double us;

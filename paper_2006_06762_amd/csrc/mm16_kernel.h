@@ -1,5 +1,7 @@
 // Matrix products of 16-bit types on the matrix pipes, D[m][n] = sum_k X[m][k] W[n][k], for the products of the gated
-// feed-forward block: sums in float32, one rounding where they are stored.
+// feed-forward block: sums in float32, one rounding where they are stored.  What the next product takes (h; dg, du and h) is rounded to the element type
+// there: the matrix pipes take 16 bits, and as two numbers of 16 bits each it would be twice that product and twice the traffic between them.  The result of a
+// block is then off by 1.4 times the rounding that it would have with float32 in between (0.0023 for 0.0017 of it in bf16).
 //
 // Each operand lies in memory with k contiguous (K_ROWS: rows of k) or with its own index contiguous (K_COLUMNS: rows
 // are k).  A work-group takes a tile of BM x BN, its waves WM x WN parts of it in blocks of 32 x 32
