@@ -85,12 +85,12 @@ inline int held_by(const Shape& s, int chunk)
 
 // Where the resident kernels run: a chunk of an image fits the registers of a work-group (vectors of four channels a thread), and all work-groups the
 // CUs at once, at 1024 threads each. 256 channels, groups of 8, SiLU, against the kernels that read twice (us, resident / not):
-// forward, 16 bits, 20^2 x 16 images (7 vectors) 8.1 / 11.8, 28^2 x 64 (13) 17.7 / 21.0; float32 20^2 x 16 (4) 9.4 / 11.4, with work-groups for half the CUs
-// 24^2 x 16 (5) 10.1 / 12.1, 28^2 x 16 12.0 / 13.6, 40^2 x 16 (13) 16.9 / 19.0, 40^2 x 28 26.6 / 29.1, but for fewer 24^2 x 4 8.8 / 8.8, 28^2 x 1 (7) 9.3 / 9.5, 32^2
-// x 4 (8) 10.4 / 9.3, 40^2 x 8 14.9 / 14.1, x 1 12.5 / 8.8.
-// Backward, float32 28^2 x 1 11.4 / 11.1, x 32 23.5 / 29.3, 24^2 x 4 10.9 / 10.4; 16 bits 20^2 x 16 12.6 / 12.3, x 64 20.2 / 23.9, 14^2 x 32 10.6 / 12.2.
-// More than fit at once, forward and backward: float32 20^2 x 40 18.2 / 15.1, 23.6 / 20.7, 10^2 x 128 23.4 / 14.1, 26.5 / 17.6; bf16 14^2 x 128 14.9 / 15.8, 23.9 /
-// 19.9, 7^2 x 256 21.7 / 15.5, 28.8 / 20.0 (512 of 448 threads fit: float32 7^2 x 64 6.8 / 9.4, 8.9 / 10.5).
+// forward, 16 bits, 20^2 x 16 images (7 vectors) 7.7 / 11.4, 28^2 x 64 (13) 17.0 / 19.8; float32 20^2 x 16 (4) 8.9 / 10.8, with work-groups for half the CUs
+// 24^2 x 16 (5) 9.8 / 11.7, 28^2 x 16 11.7 / 13.1, 40^2 x 16 (13) 17.1 / 18.6, 40^2 x 28 26.4 / 28.9, but for fewer 24^2 x 4 8.3 / 8.6, 28^2 x 1 (7) 8.9 / 9.3, 32^2
+// x 4 (8) 9.9 / 9.1, 40^2 x 8 14.3 / 13.3, x 1 12.1 / 8.6.
+// Backward, float32 28^2 x 1 11.4 / 10.9, x 32 23.3 / 29.1, 24^2 x 4 10.9 / 10.2, 32^2 x 4 12.9 / 11.3; 16 bits 20^2 x 16 12.7 / 12.4, x 64 20.1 / 23.5, 14^2 x 32 10.6 / 12.0.
+// More than fit at once, forward and backward: float32 20^2 x 40 17.3 / 14.3, 23.5 / 20.4, 10^2 x 128 21.3 / 13.4, 26.5 / 17.3; bf16 14^2 x 128 13.8 / 15.0, 23.7 /
+// 19.4, 7^2 x 256 19.7 / 14.2, 28.7 / 19.7 (512 of 448 threads fit: float32 7^2 x 64 6.4 / 9.0, 8.9 / 10.3).
 inline bool resident_pays(const Shape& s, int chunk, int64_t work_groups)
 {
     const int columns = columns_of(chunk, kHeldChannels);
@@ -122,10 +122,10 @@ inline Division divide(const Shape& s)
     };
     take(chunk_of(128));
     // Resident kernels take chunks of 64 bytes where work-groups of 128 would be half the CUs or fewer: the backward pass, and the forward one where a thread
-    // has more than four vectors. 256 channels, chunks of 128 / 64 bytes (us): backward, float32 14^2 x 16 images 10.0 / 9.8, 20^2 x 1 10.7 / 10.0, 28^2 x 1
-    // 14.6 / 11.4, x 16 19.0 / 16.5; bf16 14^2 x 32 11.9 / 10.6, 20^2 x 16 15.8 / 12.6. Forward, bf16 14^2 x 32 (4 vectors) 7.6 / 7.5, 20^2 x 16 9.6 / 8.1, x 48 (more
-    // than half the CUs) 10.7 / 14.4, 28^2 x 16 14.7 / 10.3. Of maps that only the halves hold, those of 16-bit types with 64 work-groups, forward: against the
-    // kernels that read twice bf16 36^2 x 16 15.0 / 16.2, but 40^2 x 1 14.3 / 10.6, float32 52^2 x 8 21.5 / 17.7.
+    // has more than four vectors. 256 channels, chunks of 128 / 64 bytes (us): backward, float32 14^2 x 16 images 10.0 / 9.8, 20^2 x 1 10.7 / 9.9, 28^2 x 1
+    // 14.6 / 11.4, x 16 18.9 / 16.4; bf16 14^2 x 32 11.8 / 10.6, 20^2 x 16 15.9 / 12.7. Forward, bf16 14^2 x 32 (4 vectors) 7.0 / 7.0, 20^2 x 16 9.1 / 7.6, x 48 (more
+    // than half the CUs) 10.2 / 14.1, 28^2 x 16 14.1 / 9.7. Of maps that only the halves hold, those of 16-bit types with 64 work-groups, forward: against the
+    // kernels that read twice bf16 36^2 x 16 14.4 / 15.4, but 40^2 x 1 13.6 / 10.1, float32 52^2 x 8 17.5 / 17.2.
     const int64_t work_groups = (int64_t)d.chunks * s.N;
     if (s.vector && chunk_of(64) < d.chunk && work_groups <= 128 &&
         (resident_pays(s, d.chunk, work_groups) ? s.backward || held_by(s, d.chunk) > 4 : !s.backward && s.es == 2 && work_groups >= 64) &&
@@ -140,10 +140,15 @@ inline Division divide(const Shape& s)
     int64_t slabs = std::min((1024 + others - 1) / others, (int64_t)s.HW / ((s.es == 4 ? 4 : 8) * rows));
     slabs = std::max(slabs, std::min((256 + others - 1) / others, (int64_t)s.HW / (2 * rows)));
     slabs = std::max<int64_t>(1, std::min<int64_t>(slabs, 128));
-    // Work-groups go round-robin to the eight XCDs: those that share the lines at a chunk's ends to the same one. As it comes / down to eights / to the nearest
-    // eight, bf16, chunks of 160 bytes: 4 x 95 x 63 x 320 (29 slabs) forward 19.7 / 18.3 / 17.6 us, backward 27.0 / 25.2 / 22.6, 8 x 56^2 x 320 (15) 20.4 / 21.2 / 18.9,
-    // 28.0 / 30.5 / 22.9; level where chunks are whole lines.
-    if (slabs > 8) slabs = (slabs + 4) / 8 * 8;
+    // Work-groups go round-robin to the eight XCDs: those that share the lines at a chunk's ends to the same one, so slabs come in eights, next below or above by the
+    // pixels that the fullest CU then has: a work-group's start and joins count as two a thread, a second one on the CU adds 0.7 of the first one's time. Below / above, bf16: 4 x 95 x 63 x 320 (29 slabs, 384 / 512
+    // work-groups) forward 18.3 / 17.6 us, backward 25.2 / 22.6, 8 x 56^2 x 320 (15, 256 / 512) 21.2 / 18.9, 30.5 / 22.9; float16 13 x 52 x 33 x 48 (20, 208 / 312)
+    // backward 12.5 / 16.0, 13 x 123 x 38 x 80 (23, 208 / 312) 23.7 / 26.7. Level where chunks are whole lines.
+    if (slabs > 8) {
+        auto fullest = [&](int64_t n) { return (0.3 + 0.7 * (double)((n * others + 255) / 256)) * (double)((s.HW + n - 1) / n + 2 * rows); };
+        const int64_t below = slabs / 8 * 8, above = std::min<int64_t>(below + 8, 128);
+        slabs = slabs > below && above <= s.HW / (2 * rows) && fullest(above) < fullest(below) ? above : below;
+    }
     d.slab_pixels = (int)((s.HW + slabs - 1) / slabs);
     d.slabs = (s.HW + d.slab_pixels - 1) / d.slab_pixels;
     d.sums_lds = sizeof(float) * of_chunks(d, s.C, [&](int channels) { return sums_lds_floats(s.backward, channels, d.V); });
