@@ -135,18 +135,21 @@ inline Division divide(const Shape& s)
     }
     const int rows = rows_of(d.chunk, d.V, kThreads);
     // Slabs: about four work-groups per CU as far as each thread has eight pixels (float32: four), one per CU as far as it has two, and at
-    // most 128 that are joined. (Eight or four, backward, 320 channels: bf16 8 x 64^2 27.8 / 35.8 us, 4 x 95 x 63 22.6 / 25.9.)
+    // most 128 that are joined, 256 where those are less than two work-groups per CU: one map of 1024^2, forward and backward, 128 / 256 slabs, 64 channels bf16
+    // 215 / 125 us, 367 / 215, float32 211 / 170, 450 / 291, 256^2 x 64 bf16 24.5 / 24.2, 29.5 / 24.6, but two maps of 256^2 x 64 float32 (four work-groups a slab) 26.9 /
+    // 29.8, 36.8 / 46.5. (Eight or four, backward, 320 channels: bf16 8 x 64^2 27.8 / 35.8 us, 4 x 95 x 63 22.6 / 25.9.)
     const int64_t others = (int64_t)d.chunks * s.N;
     int64_t slabs = std::min((1024 + others - 1) / others, (int64_t)s.HW / ((s.es == 4 ? 4 : 8) * rows));
     slabs = std::max(slabs, std::min((256 + others - 1) / others, (int64_t)s.HW / (2 * rows)));
-    slabs = std::max<int64_t>(1, std::min<int64_t>(slabs, 128));
+    const int64_t most = others <= 2 ? 256 : 128;
+    slabs = std::max<int64_t>(1, std::min(slabs, most));
     // Work-groups go round-robin to the eight XCDs: those that share the lines at a chunk's ends to the same one, so slabs come in eights, next below or above by the
     // pixels that the fullest CU then has: a work-group's start and joins count as two a thread, a second one on the CU adds 0.7 of the first one's time. Below / above, bf16: 4 x 95 x 63 x 320 (29 slabs, 384 / 512
     // work-groups) forward 18.3 / 17.6 us, backward 25.2 / 22.6, 8 x 56^2 x 320 (15, 256 / 512) 21.2 / 18.9, 30.5 / 22.9; float16 13 x 52 x 33 x 48 (20, 208 / 312)
     // backward 12.5 / 16.0, 13 x 123 x 38 x 80 (23, 208 / 312) 23.7 / 26.7. Level where chunks are whole lines.
     if (slabs > 8) {
         auto fullest = [&](int64_t n) { return (0.3 + 0.7 * (double)((n * others + 255) / 256)) * (double)((s.HW + n - 1) / n + 2 * rows); };
-        const int64_t below = slabs / 8 * 8, above = std::min<int64_t>(below + 8, 128);
+        const int64_t below = slabs / 8 * 8, above = std::min(below + 8, most);
         slabs = slabs > below && above <= s.HW / (2 * rows) && fullest(above) < fullest(below) ? above : below;
     }
     d.slab_pixels = (int)((s.HW + slabs - 1) / slabs);

@@ -103,3 +103,10 @@ def test_the_widest_groups(anr, t, shape):
 def test_float32_maps_held_by_half_the_work_groups(anr, shape):
     N, C, H, W, groups = shape
     norm_case(anr, 83, N, C, H, W, groups, "silu", torch.float32)
+
+
+@pytest.mark.parametrize("t,shape", [("bf16", (1, 64, 300, 400, 8)), ("f32", (1, 64, 280, 330, 4)), ("f32", (2, 32, 250, 300, 32)), ("f16", (1, 5, 500, 401, 5))])
+def test_as_many_slabs_as_are_joined(anr, t, shape):
+    """One image, or two, of one or two chunks."""
+    N, C, H, W, groups = shape
+    norm_case(anr, 84, N, C, H, W, groups, "none", TYPES[t])
