@@ -79,11 +79,12 @@ typedef enum {
     ANR_OP_GEMM = 0, ANR_OP_CONV2D = 1, ANR_OP_CONV_BN_RELU = 2, ANR_OP_DWCONV = 3,
     ANR_OP_TBG = 4, ANR_OP_TBS = 5, ANR_OP_NRM = 6,
     ANR_OP_GROUP_NORM = 7, ANR_OP_GROUP_NORM_BACKWARD = 8, ANR_OP_ROTARY = 9,
-    ANR_OP_GATED_FF = 10, ANR_OP_GATED_FF_BACKWARD = 11
+    ANR_OP_GATED_FF = 10, ANR_OP_GATED_FF_BACKWARD = 11,
+    ANR_OP_RMS_NORM = 12, ANR_OP_RMS_NORM_BACKWARD = 13, ANR_OP_RMS_NORM_Q8 = 14
 } anr_op;
 
-/* Types of the elements of group norm, rotary positions and the gated feed-forward
- * block.  The operators above take float32 only. */
+/* Types of the elements of the operators of a transformer block (from group norm on).  The
+ * operators above take float32 only. */
 typedef enum { ANR_F32 = 0, ANR_F16 = 1, ANR_BF16 = 2 } anr_dtype;
 
 /* Activations: z; max(z, 0) (a NaN stays one); z sigmoid(z); z Phi(z) with the normal
@@ -403,6 +404,44 @@ anr_status anr_gated_ff(const anr_gated_ff_desc *desc, const void *x, const void
 anr_status anr_gated_ff_backward(const anr_gated_ff_desc *desc, const void *dy, const void *x, const void *w_gate,
                                  const void *w_up, const void *w_down, const void *gate, const void *up, void *dx,
                                  void *dw_gate, void *dw_up, void *dw_down, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Root-mean-square norm of T tokens of C channels, with the residual's addition.  Row-major,
+ * leading dimensions in elements, 0 for packed: x (ldx); residual, or dh in the backward
+ * call (ld_residual); h, or dx (ldh); y, dy or q (ldy).  param_dtype is the type of gamma and
+ * dgamma: float32 or `dtype`.  C <= 32768, T < 2^31.  Outputs of the forward calls may be x
+ * or residual itself, dx may be dy, x or dh itself, with the same leading dimension; two
+ * outputs are never the same.
+ */
+typedef struct {
+    int64_t T, C;
+    int32_t dtype;       /* anr_dtype */
+    int32_t param_dtype; /* anr_dtype */
+    int64_t ldx, ld_residual, ldh, ldy;
+} anr_rms_norm_desc;
+
+/* y = h rstd gamma with h = x + residual (x alone where residual is NULL) and
+ * rstd = 1/sqrt(m + eps), m the mean of h^2 over a token's channels.  gamma: C, NULL for ones.
+ * h: where the sum goes, rounded to `dtype` (y is made from the sum before that), or NULL;
+ * NULL where there is no residual.  rstd: T floats for a backward call, or NULL.  eps is
+ * finite and not negative.  m is formed in float32: magnitudes up to 2^60. */
+anr_status anr_rms_norm(const anr_rms_norm_desc *desc, const void *x, const void *residual, const void *gamma, float eps,
+                        void *h, void *y, float *rstd, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Gradients of anr_rms_norm: x is what was normed (its h where it had a residual), rstd what
+ * it wrote.  With hat = x rstd: dx = rstd (dy gamma - hat a) + dh with the token's mean a of
+ * dy gamma hat, and dgamma = sum of dy hat over the tokens.  dh: the gradient that reaches the
+ * sum by its other way, or NULL; dx is then that of x and of residual alike.  dx, dgamma: NULL
+ * for what is not wanted, not both. */
+anr_status anr_rms_norm_backward(const anr_rms_norm_desc *desc, const void *dy, const void *x, const void *gamma,
+                                 const float *rstd, const void *dh, void *dx, void *dgamma, void *ws, size_t ws_bytes,
+                                 void *hip_stream);
+
+/* anr_rms_norm with y in 8 bits: scale[t] = (largest |y| of token t) / 127 and q = y / scale to
+ * the nearest whole number, ties to even (y is not rounded before that).  A token of zeros has
+ * scale and q zero.  One with an infinity or NaN has a NaN as its scale and q zero. */
+anr_status anr_rms_norm_q8(const anr_rms_norm_desc *desc, const void *x, const void *residual, const void *gamma,
+                           float eps, void *h, int8_t *q, float *scale, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Bytes of device workspace `op` (an anr_op) needs for `desc` (the matching
  * descriptor type): a function of the descriptor only, enough for any pointer

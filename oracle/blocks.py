@@ -95,3 +95,23 @@ def gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, activation):
     dh = dy @ w_down
     dg, du = dh * up * slope, dh * a
     return dg @ w_gate + du @ w_up, dg.T @ x, du.T @ x, dy.T @ (a * up)
+
+
+def rms_norm(x, residual, gamma, eps):
+    """x [T,C]; (h, y, rstd [T])."""
+    h = x if residual is None else x + residual
+    rstd = 1 / np.sqrt((h * h).mean(1) + eps)
+    return h, h * rstd[:, None] * gamma, rstd
+
+
+def rms_norm_backward(dy, x, gamma, rstd, dh):
+    """(dx, dgamma, and for error bounds: hat, each row's mean of |dy gamma hat|)."""
+    hat, dhat = x * rstd[:, None], dy * gamma
+    dx = rstd[:, None] * (dhat - hat * (dhat * hat).mean(1, keepdims=True))
+    return dx if dh is None else dx + dh, (dy * hat).sum(0), hat, np.abs(dhat * hat).mean(1, keepdims=True)
+
+
+def in_8_bits(v):
+    """(v / scale before it is rounded, scale) of rows of values; zeros where a row has none but zeros."""
+    scale = np.abs(v).max(1) / 127
+    return np.divide(v, scale[:, None], out=np.zeros_like(v), where=scale[:, None] > 0), scale

@@ -2,8 +2,8 @@
 extension module ``_native`` (csrc/binding_native.cpp).
 
 Function names and arguments mirror ``include/anr.h``.  Every tensor argument
-is a torch CUDA tensor (float32; group norm, rotary positions and the gated
-feed-forward block also float16 and bfloat16); torch is used for device memory and for the
+is a torch CUDA tensor (float32; the operators of a transformer block, from group
+norm on, also float16 and bfloat16, and int8 for what is held in 8 bits); torch is used for device memory and for the
 current HIP stream, nothing else.  There is no CPU path: if the library has not
 been built, importing this module raises.
 """
@@ -32,6 +32,7 @@ ANR_OK, ANR_ERR_NULL, ANR_ERR_INVALID_ARG, ANR_ERR_UNSUPPORTED, ANR_ERR_WORKSPAC
 ANR_LAYOUT_NCHW = 0
 ANR_OP_GEMM, ANR_OP_CONV2D, ANR_OP_CONV_BN_RELU, ANR_OP_DWCONV, ANR_OP_TBG, ANR_OP_TBS, ANR_OP_NRM = range(7)
 ANR_OP_GROUP_NORM, ANR_OP_GROUP_NORM_BACKWARD, ANR_OP_ROTARY, ANR_OP_GATED_FF, ANR_OP_GATED_FF_BACKWARD = range(7, 12)
+ANR_OP_RMS_NORM, ANR_OP_RMS_NORM_BACKWARD, ANR_OP_RMS_NORM_Q8 = range(12, 15)
 ANR_F32, ANR_F16, ANR_BF16 = range(3)
 ANR_ACT_NONE, ANR_ACT_RELU, ANR_ACT_SILU, ANR_ACT_GELU, ANR_ACT_GELU_TANH = range(5)
 ANR_ROTARY_HALVES, ANR_ROTARY_ADJACENT, ANR_ROTARY_SECTION_HALVES = range(3)
@@ -40,7 +41,8 @@ ANR_POS_I32, ANR_POS_I64, ANR_POS_F32 = range(3)
 EXPORTS = ("anr_gemm", "anr_conv2d", "anr_conv2d_noalloc", "anr_conv2d_packed_size", "anr_conv2d_pack_weights",
            "anr_conv2d_packed", "anr_conv_bn_relu_packed", "anr_conv_bn_relu", "anr_dwconv", "anr_tbg", "anr_tbs", "anr_nrm",
            "anr_workspace_size", "anr_conv2d_fast_workspace_size", "anr_conv2d_route", "anr_status_string", "anr_version", "anr_last_hip_error",
-           "anr_last_hip_error_string", "anr_group_norm", "anr_group_norm_backward", "anr_rotary", "anr_gated_ff", "anr_gated_ff_backward")
+           "anr_last_hip_error_string", "anr_group_norm", "anr_group_norm_backward", "anr_rotary", "anr_gated_ff", "anr_gated_ff_backward",
+           "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8")
 
 
 class GemmDesc(ctypes.Structure):
@@ -103,6 +105,11 @@ class GatedFfDesc(ctypes.Structure):
                 ("ldw", ctypes.c_int64), ("ld_down", ctypes.c_int64), ("lddw", ctypes.c_int64), ("ld_ddown", ctypes.c_int64)]
 
 
+class RmsNormDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("C", ctypes.c_int64), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+                ("ldx", ctypes.c_int64), ("ld_residual", ctypes.c_int64), ("ldh", ctypes.c_int64), ("ldy", ctypes.c_int64)]
+
+
 _vp = ctypes.c_void_p
 _lib.anr_gemm.argtypes = [ctypes.POINTER(GemmDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_conv2d.argtypes = [ctypes.POINTER(ConvDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
@@ -123,13 +130,16 @@ _lib.anr_group_norm_backward.argtypes = [ctypes.POINTER(GroupNormDesc)] + [_vp] 
 _lib.anr_rotary.argtypes = [ctypes.POINTER(RotaryDesc)] + [_vp] * 7 + [ctypes.c_size_t, _vp]
 _lib.anr_gated_ff.argtypes = [ctypes.POINTER(GatedFfDesc)] + [_vp] * 8 + [ctypes.c_size_t, _vp]
 _lib.anr_gated_ff_backward.argtypes = [ctypes.POINTER(GatedFfDesc)] + [_vp] * 12 + [ctypes.c_size_t, _vp]
+_lib.anr_rms_norm.argtypes = [ctypes.POINTER(RmsNormDesc), _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.anr_rms_norm_backward.argtypes = [ctypes.POINTER(RmsNormDesc)] + [_vp] * 8 + [ctypes.c_size_t, _vp]
+_lib.anr_rms_norm_q8.argtypes = [ctypes.POINTER(RmsNormDesc), _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_workspace_size.argtypes = [ctypes.c_int, _vp, ctypes.POINTER(ctypes.c_size_t)]
 _lib.anr_conv2d_fast_workspace_size.argtypes = [ctypes.POINTER(ConvDesc), ctypes.POINTER(ctypes.c_size_t)]
 _lib.anr_conv2d_route.argtypes = [ctypes.POINTER(ConvDesc), ctypes.POINTER(ConvRoute)]
 for _name in ("anr_gemm", "anr_conv2d", "anr_conv2d_noalloc", "anr_conv2d_packed_size", "anr_conv2d_pack_weights",
               "anr_conv2d_packed", "anr_conv_bn_relu_packed", "anr_conv_bn_relu", "anr_dwconv", "anr_tbg", "anr_tbs",
               "anr_workspace_size", "anr_conv2d_fast_workspace_size", "anr_group_norm", "anr_group_norm_backward", "anr_rotary",
-              "anr_gated_ff", "anr_gated_ff_backward"):
+              "anr_gated_ff", "anr_gated_ff_backward", "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8"):
     getattr(_lib, _name).restype = ctypes.c_int
 _lib.anr_status_string.argtypes = [ctypes.c_int]
 _lib.anr_status_string.restype = ctypes.c_char_p
@@ -190,6 +200,9 @@ _fast.anr_group_norm_backward.argtypes = [_vp] * 11 + [_sz, _vp]
 _fast.anr_rotary.argtypes = [_vp] * 8 + [_sz, _vp]
 _fast.anr_gated_ff.argtypes = [_vp] * 9 + [_sz, _vp]
 _fast.anr_gated_ff_backward.argtypes = [_vp] * 13 + [_sz, _vp]
+_fast.anr_rms_norm.argtypes = [_vp] * 4 + [_fl] + [_vp] * 4 + [_sz, _vp]
+_fast.anr_rms_norm_backward.argtypes = [_vp] * 9 + [_sz, _vp]
+_fast.anr_rms_norm_q8.argtypes = [_vp] * 4 + [_fl] + [_vp] * 4 + [_sz, _vp]
 
 _pack_gemm = struct.Struct("@10q").pack
 _pack_conv = struct.Struct("@14i8q2i").pack
@@ -198,8 +211,9 @@ _pack_nrm = struct.Struct("@5q").pack
 _pack_group_norm = struct.Struct("@8i9q").pack
 _pack_rotary = struct.Struct("@15i15q").pack
 _pack_gated_ff = struct.Struct("@3q2i8q").pack
-assert [struct.calcsize(f) for f in ("@10q", "@14i8q2i", "@4i12q", "@5q", "@8i9q", "@15i15q", "@3q2i8q")] == \
-    [ctypes.sizeof(t) for t in (GemmDesc, ConvDesc, TbgDesc, NrmDesc, GroupNormDesc, RotaryDesc, GatedFfDesc)]
+_pack_rms_norm = struct.Struct("@2q2i4q").pack
+assert [struct.calcsize(f) for f in ("@10q", "@14i8q2i", "@4i12q", "@5q", "@8i9q", "@15i15q", "@3q2i8q", "@2q2i4q")] == \
+    [ctypes.sizeof(t) for t in (GemmDesc, ConvDesc, TbgDesc, NrmDesc, GroupNormDesc, RotaryDesc, GatedFfDesc, RmsNormDesc)]
 _NO_STRIDES = (0, 0, 0, 0)
 _f32 = torch.float32
 
@@ -687,15 +701,56 @@ def _gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, dx=None, dw_gate=N
     return dx, dw_gate, dw_up, dw_down
 
 
+def _rms_norm_forward(x, gamma, residual, h, y, y_type):
+    """The descriptor and the addresses (x, residual, gamma, h, y) of a forward call."""
+    dtype, (T, C) = _dtype(x), _matrix("x", x)
+    if h is not None and residual is None:
+        raise ValueError("h belongs to a residual")
+    param = _param_dtype(x, gamma)
+    t = x.dtype
+    xs, rs, hs, ys = _rows("x", x, (T, C), t), _rows("residual", residual, (T, C), t), _rows("h", h, (T, C), t), _rows("y" if y_type is t else "q", y, (T, C), y_type)
+    d = _pack_rms_norm(T, C, dtype, _DTYPES[param], xs[1], rs[1], hs[1], ys[1])
+    return d, (xs[0], rs[0], _vector("gamma", gamma, (C,), param), hs[0], ys[0])
+
+
+def _rms_norm(x, y, gamma=None, eps=1e-6, residual=None, h=None, rstd=None):
+    """y = h * rstd * gamma with h = x + residual and rstd = 1/sqrt(mean(h^2) + eps) over each row; x, residual, h, y [T,C].  h: where the sum goes;
+    rstd: float32 [T], for a backward pass."""
+    d, (x_, r_, g_, h_, y_) = _rms_norm_forward(x, gamma, residual, h, y, x.dtype)
+    _check(_fast.anr_rms_norm(d, x_, r_, g_, eps, h_, y_, _vector("rstd", rstd, x.shape[:1], _f32), None, 0, _stream()), "anr_rms_norm")
+    return y
+
+
+def _rms_norm_q8(x, q, scale, gamma=None, eps=1e-6, residual=None, h=None):
+    """rms_norm with its result in 8 bits: q int8 [T,C], scale float32 [T], y = q * scale."""
+    d, (x_, r_, g_, h_, q_) = _rms_norm_forward(x, gamma, residual, h, q, torch.int8)
+    _check(_fast.anr_rms_norm_q8(d, x_, r_, g_, eps, h_, q_, _vector("scale", scale, x.shape[:1], _f32), None, 0, _stream()), "anr_rms_norm_q8")
+    return q, scale
+
+
+def _rms_norm_backward(dy, x, gamma, rstd, dx=None, dgamma=None, dh=None, ws=None):
+    """Gradients of rms_norm, into those of dx and dgamma that are given, from what it normed (its h where it had a residual) and the rstd that it
+    wrote.  dh: the gradient that reaches the sum by its other way; dx is then that of x and of residual alike."""
+    dtype, (T, C) = _dtype(x), _matrix("x", x)
+    param = _param_dtype(x, gamma, dgamma)
+    t = x.dtype
+    dys, xs, dhs, dxs = _rows("dy", dy, (T, C), t), _rows("x", x, (T, C), t), _rows("dh", dh, (T, C), t), _rows("dx", dx, (T, C), t)
+    d = _pack_rms_norm(T, C, dtype, _DTYPES[param], xs[1], dhs[1], dxs[1], dys[1])
+    args = (dys[0], xs[0], _vector("gamma", gamma, (C,), param), _vector("rstd", rstd, (T,), _f32), dhs[0], dxs[0], _vector("dgamma", dgamma, (C,), param))
+    _with_workspace(_fast.anr_rms_norm_backward, "anr_rms_norm_backward", ANR_OP_RMS_NORM_BACKWARD, d, args, ws, RmsNormDesc)
+    return dx, dgamma
+
+
 # The operators as programs call them: the functions above without Python's part in the usual case.
 _OPERATORS = ("gemm", "conv2d", "conv_bn_relu", "conv2d_packed", "conv_bn_relu_packed", "dwconv", "tbg", "tbs", "nrm", "group_norm",
-              "group_norm_backward", "rotary", "gated_ff", "gated_ff_backward")
+              "group_norm_backward", "rotary", "gated_ff", "gated_ff_backward", "rms_norm", "rms_norm_backward", "rms_norm_q8")
 for _name in _OPERATORS:
     globals()["_" + _name].__name__ = globals()["_" + _name].__qualname__ = _name      # (what their errors say)
 _native.setup(tuple(globals()["_" + n] for n in _OPERATORS),
               tuple(ctypes.cast(getattr(_fast, "anr_" + n), _vp).value for n in _OPERATORS),
               ctypes.cast(_fast.anr_conv2d_fast_workspace_size, _vp).value, ctypes.cast(_fast.anr_workspace_size, _vp).value)
 from paper_2006_06762_amd._native import (gemm, conv2d, conv_bn_relu, conv2d_packed, conv_bn_relu_packed, dwconv, tbg, tbs,  # noqa: E402
-                                          nrm, group_norm, group_norm_backward, rotary, gated_ff, gated_ff_backward)
+                                          nrm, group_norm, group_norm_backward, rotary, gated_ff, gated_ff_backward, rms_norm, rms_norm_backward,
+                                          rms_norm_q8)
 for _name in _OPERATORS:
     globals()[_name].__module__ = __name__          # (where a pickle of one finds it again, in a process that has not imported torch)

@@ -154,6 +154,62 @@ anr_status check_gated_ff(const anr_gated_ff_desc* d, anr_gated_ff_desc* out)
     return ANR_OK;
 }
 
+// ---- root-mean-square norm
+
+// Leading dimensions of matrices of T rows: 0 is packed; those of a single row say nothing.
+anr_status fill_leading(int64_t T, int n, int64_t* const* ld, const int64_t* least)
+{
+    for (int i = 0; i < n; ++i) {
+        if (*ld[i] == 0) *ld[i] = least[i];
+        if (T <= 1 && *ld[i] >= 0) *ld[i] = least[i];
+        if (*ld[i] < least[i]) return ANR_ERR_INVALID_ARG;
+        if (far(*ld[i], T > 0 ? T : 1)) return ANR_ERR_UNSUPPORTED;
+    }
+    return ANR_OK;
+}
+
+anr_status check_rms_norm(const anr_rms_norm_desc* d, anr_rms_norm_desc* out)
+{
+    if (!d) return ANR_ERR_NULL;
+    if (d->T < 0 || d->C < 1 || !valid_type(d->dtype) || (d->param_dtype != ANR_F32 && d->param_dtype != d->dtype)) return ANR_ERR_INVALID_ARG;
+    // a row is held in the registers of one work-group
+    if (d->C > 32768 || d->T >= (int64_t)1 << 31) return ANR_ERR_UNSUPPORTED;
+    *out = *d;
+    int64_t* const ld[4] = {&out->ldx, &out->ld_residual, &out->ldh, &out->ldy};
+    const int64_t least[4] = {d->C, d->C, d->C, d->C};
+    return fill_leading(d->T, 4, ld, least);
+}
+
+// Whether an output is one of the inputs with another leading dimension.
+struct Matrix {
+    const void* p;
+    int64_t ld;
+};
+bool crossed(Matrix out, std::initializer_list<Matrix> inputs)
+{
+    for (const Matrix& in : inputs)
+        if (out.p && out.p == in.p && out.ld != in.ld) return true;
+    return false;
+}
+
+// What the two forward calls have in common.
+anr_status rms_norm_forward_args(const anr_rms_norm_desc* d, const void* x, const void* residual, const void* gamma, float eps, void* h, void* y, anr::RmsNormArgs* a)
+{
+    const anr_status st = check_rms_norm(d, &a->d);
+    if (st != ANR_OK) return st;
+    if (!std::isfinite(eps) || eps < 0.f || (h && !residual)) return ANR_ERR_INVALID_ARG;
+    if (d->T > 0 && (!x || !y)) return ANR_ERR_NULL;
+    if (!element_aligned(x, d->dtype) || !element_aligned(residual, d->dtype) || !element_aligned(h, d->dtype) || !element_aligned(gamma, d->param_dtype)) return ANR_ERR_INVALID_ARG;
+    if (crossed({h, a->d.ldh}, {{x, a->d.ldx}, {residual, a->d.ld_residual}}) || (h && h == y)) return ANR_ERR_INVALID_ARG;
+    a->x = x;
+    a->residual = residual;
+    a->gamma = gamma;
+    a->eps = eps;
+    a->h = h;
+    a->y = y;
+    return ANR_OK;
+}
+
 }  // namespace
 
 namespace anr {
@@ -163,6 +219,7 @@ anr_status blocks_workspace_size(int op, const void* desc, size_t* bytes)
     GroupNormArgs gn{};
     RotaryArgs r{};
     GatedFfArgs ff{};
+    RmsNormArgs rn{};
     anr_status st = ANR_ERR_INVALID_ARG;
     switch (op) {
         case ANR_OP_GROUP_NORM:
@@ -178,6 +235,12 @@ anr_status blocks_workspace_size(int op, const void* desc, size_t* bytes)
         case ANR_OP_GATED_FF_BACKWARD:
             st = check_gated_ff(static_cast<const anr_gated_ff_desc*>(desc), &ff.d);
             if (st == ANR_OK) *bytes = gated_ff_workspace_bytes(ff, op == ANR_OP_GATED_FF_BACKWARD);
+            break;
+        case ANR_OP_RMS_NORM:
+        case ANR_OP_RMS_NORM_Q8:
+        case ANR_OP_RMS_NORM_BACKWARD:
+            st = check_rms_norm(static_cast<const anr_rms_norm_desc*>(desc), &rn.d);
+            if (st == ANR_OK) *bytes = op == ANR_OP_RMS_NORM_BACKWARD ? rms_norm_backward_workspace_bytes(rn) : 0;
             break;
         default: break;
     }
@@ -314,6 +377,56 @@ anr_status anr_gated_ff_backward(const anr_gated_ff_desc* d, const void* dy, con
     a.dw_down = dw_down;
     a.ws = ws;
     return anr::launch_result(anr::launch_gated_ff_backward(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+anr_status anr_rms_norm(const anr_rms_norm_desc* d, const void* x, const void* residual, const void* gamma, float eps, void* h, void* y, float* rstd, void* ws,
+                        size_t ws_bytes, void* hip_stream)
+{
+    (void)ws; (void)ws_bytes;
+    anr::RmsNormArgs a{};
+    const anr_status st = rms_norm_forward_args(d, x, residual, gamma, eps, h, y, &a);
+    if (st != ANR_OK) return st;
+    if (!element_aligned(y, d->dtype) || !element_aligned(rstd, ANR_F32)) return ANR_ERR_INVALID_ARG;
+    if (crossed({y, a.d.ldy}, {{x, a.d.ldx}, {residual, a.d.ld_residual}})) return ANR_ERR_INVALID_ARG;
+    a.rstd = rstd;
+    return anr::launch_result(anr::launch_rms_norm(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+anr_status anr_rms_norm_q8(const anr_rms_norm_desc* d, const void* x, const void* residual, const void* gamma, float eps, void* h, int8_t* q, float* scale, void* ws,
+                           size_t ws_bytes, void* hip_stream)
+{
+    (void)ws; (void)ws_bytes;
+    anr::RmsNormArgs a{};
+    const anr_status st = rms_norm_forward_args(d, x, residual, gamma, eps, h, q, &a);
+    if (st != ANR_OK) return st;
+    if (d->T > 0 && !scale) return ANR_ERR_NULL;
+    if (!element_aligned(scale, ANR_F32) || (q && (q == x || q == residual))) return ANR_ERR_INVALID_ARG;
+    a.scale = scale;
+    return anr::launch_result(anr::launch_rms_norm_q8(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+anr_status anr_rms_norm_backward(const anr_rms_norm_desc* d, const void* dy, const void* x, const void* gamma, const float* rstd, const void* dh, void* dx, void* dgamma,
+                                 void* ws, size_t ws_bytes, void* hip_stream)
+{
+    anr::RmsNormArgs a{};
+    anr_status st = check_rms_norm(d, &a.d);
+    if (st != ANR_OK) return st;
+    if (d->T > 0 && (!dy || !x || !rstd || (!dx && !dgamma))) return ANR_ERR_NULL;
+    for (const void* p : {dy, x, dh, static_cast<const void*>(dx)})
+        if (!element_aligned(p, d->dtype)) return ANR_ERR_INVALID_ARG;
+    if (!element_aligned(gamma, d->param_dtype) || !element_aligned(dgamma, d->param_dtype) || !element_aligned(rstd, ANR_F32)) return ANR_ERR_INVALID_ARG;
+    if (crossed({dx, a.d.ldh}, {{dy, a.d.ldy}, {x, a.d.ldx}, {dh, a.d.ld_residual}})) return ANR_ERR_INVALID_ARG;
+    st = check_workspace(ws, ws_bytes, anr::rms_norm_backward_workspace_bytes(a));
+    if (st != ANR_OK) return st;
+    a.dy = dy;
+    a.x = x;
+    a.gamma = gamma;
+    a.rstd = const_cast<float*>(rstd);
+    a.residual = dh;
+    a.h = dx;
+    a.dgamma = dgamma;
+    a.ws = ws;
+    return anr::launch_result(anr::launch_rms_norm_backward(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

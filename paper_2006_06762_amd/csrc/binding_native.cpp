@@ -23,7 +23,8 @@
 namespace {
 
 // ---- what binding.py hands over (setup): its functions, the library's entry points
-enum Op { GEMM, CONV2D, CONV_BN_RELU, CONV2D_PACKED, CONV_BN_RELU_PACKED, DWCONV, TBG, TBS, NRM, GROUP_NORM, GROUP_NORM_BACKWARD, ROTARY, GATED_FF, GATED_FF_BACKWARD, OPS };
+enum Op { GEMM, CONV2D, CONV_BN_RELU, CONV2D_PACKED, CONV_BN_RELU_PACKED, DWCONV, TBG, TBS, NRM, GROUP_NORM, GROUP_NORM_BACKWARD, ROTARY, GATED_FF, GATED_FF_BACKWARD, RMS_NORM, RMS_NORM_BACKWARD, RMS_NORM_Q8,
+          OPS };
 PyObject* g_python[OPS];
 using Call3 = anr_status (*)(const void*, const void*, const void*, void*, void*, size_t, void*);
 using CallBn = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, float, void*, void*, size_t, void*);
@@ -34,6 +35,8 @@ using CallRotary = anr_status (*)(const void*, const void*, const void*, const v
 using CallFf = anr_status (*)(const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, size_t, void*);
 using CallFfBackward = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, void*,
                                       size_t, void*);
+using CallRmsNorm = anr_status (*)(const void*, const void*, const void*, const void*, float, void*, void*, void*, void*, size_t, void*);
+using CallRmsNormBackward = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, size_t, void*);
 using CallFastSize = anr_status (*)(const void*, size_t*);
 using CallSize = anr_status (*)(int, const void*, size_t*);
 void* g_entry[OPS];
@@ -579,6 +582,75 @@ bool run_gated_ff_backward(PyObject* const* a)
                                                data_or_null(dwu), data_or_null(dwd), ws.ptr, ws.bytes, t.s.stream);
 }
 
+// What the calls of a root-mean-square norm have in common: x, its type and extents, the parameters' type.
+struct RmsNorm {
+    Tensors t;
+    const at::Tensor* x = nullptr;
+    at::ScalarType type, param = at::kFloat;
+    anr_rms_norm_desc d{};
+
+    bool init(PyObject* x_, std::initializer_list<PyObject*> parameters)
+    {
+        x = plain_memory(x_);
+        if (!x || x->dim() != 2) return false;
+        type = x->scalar_type();
+        d.dtype = type_code(type);
+        if (d.dtype < 0) return false;
+        bool given = false;
+        for (PyObject* const o : parameters) {
+            if (absent(o)) continue;
+            const at::Tensor* const v = plain_memory(o);
+            if (!v || (given && v->scalar_type() != param)) return false;
+            param = v->scalar_type();
+            given = true;
+        }
+        if (param != at::kFloat && param != type) return false;
+        d.param_dtype = type_code(param);
+        d.T = x->size(0);
+        d.C = x->size(1);
+        return matrix(x_, &d.ldx) != nullptr;
+    }
+    const at::Tensor* matrix(PyObject* o, int64_t* ld) { return t.matrix(o, type, d.T, d.C, ld); }
+    const at::Tensor* vector(PyObject* o) { return t.packed(o, param, {d.C}); }
+    const at::Tensor* statistic(PyObject* o) { return t.packed(o, at::kFloat, {d.T}); }
+};
+
+bool run_rms_norm(PyObject* const* a)
+{
+    RmsNorm n;
+    if ((a[3] && !PyFloat_CheckExact(a[3])) || (!absent(a[5]) && absent(a[4])) || !n.init(a[0], {a[2]})) return false;
+    const at::Tensor *y = n.matrix(a[1], &n.d.ldy), *residual = n.matrix(a[4], &n.d.ld_residual), *h = n.matrix(a[5], &n.d.ldh);
+    const at::Tensor *gamma = n.vector(a[2]), *rstd = n.statistic(a[6]);
+    return n.t.fine && y &&
+           accepted<CallRmsNorm>(RMS_NORM, &n.d, data(n.x), data_or_null(residual), data_or_null(gamma), a[3] ? (float)PyFloat_AS_DOUBLE(a[3]) : 1e-6f, data_or_null(h), data(y),
+                                 data_or_null(rstd), nullptr, 0, n.t.s.stream);
+}
+
+bool run_rms_norm_q8(PyObject* const* a)
+{
+    RmsNorm n;
+    if ((a[4] && !PyFloat_CheckExact(a[4])) || (!absent(a[6]) && absent(a[5])) || !n.init(a[0], {a[3]})) return false;
+    const at::Tensor *q = n.t.matrix(a[1], at::kChar, n.d.T, n.d.C, &n.d.ldy), *residual = n.matrix(a[5], &n.d.ld_residual), *h = n.matrix(a[6], &n.d.ldh);
+    const at::Tensor *gamma = n.vector(a[3]), *scale = n.statistic(a[2]);
+    return n.t.fine && q && scale &&
+           accepted<CallRmsNorm>(RMS_NORM_Q8, &n.d, data(n.x), data_or_null(residual), data_or_null(gamma), a[4] ? (float)PyFloat_AS_DOUBLE(a[4]) : 1e-6f, data_or_null(h), data(q),
+                                 data(scale), nullptr, 0, n.t.s.stream);
+}
+
+bool run_rms_norm_backward(PyObject* const* a)
+{
+    RmsNorm n;
+    if ((a[7] && a[7] != Py_None) || !n.init(a[1], {a[2], a[5]})) return false;
+    const at::Tensor *dy = n.matrix(a[0], &n.d.ldy), *dx = n.matrix(a[4], &n.d.ldh), *dh = n.matrix(a[6], &n.d.ld_residual);
+    const at::Tensor *gamma = n.vector(a[2]), *rstd = n.statistic(a[3]), *dgamma = n.vector(a[5]);
+    if (!n.t.fine || !dy || !rstd) return false;
+    size_t need = 0;
+    if (g_size(ANR_OP_RMS_NORM_BACKWARD, &n.d, &need) != ANR_OK) return false;
+    const Workspace ws(need, n.t.s);
+    return ws.here && accepted<CallRmsNormBackward>(RMS_NORM_BACKWARD, &n.d, data(dy), data(n.x), data_or_null(gamma), data(rstd), data_or_null(dh), data_or_null(dx),
+                                                    data_or_null(dgamma), ws.ptr, ws.bytes, n.t.s.stream);
+}
+
 // Parameters of each operator, the required ones first, and which of them it returns.
 const char* const kGemm[] = {"A", "B", "C"};
 const char* const kConv[] = {"x", "w", "y", "stride", "pad", "ws", "dil", "groups", "route"};
@@ -592,6 +664,9 @@ const char* const kNormBackward[] = {"dy", "x", "groups", "gamma", "beta", "mean
 const char* const kRotary[] = {"q", "k", "positions", "inv_freq", "q_out", "k_out", "sections", "pairing", "inverse"};
 const char* const kFf[] = {"x", "w_gate", "w_up", "w_down", "y", "act", "gate", "up", "ws"};
 const char* const kFfBackward[] = {"dy", "x", "w_gate", "w_up", "w_down", "gate", "up", "dx", "dw_gate", "dw_up", "dw_down", "act", "ws"};
+const char* const kRmsNorm[] = {"x", "y", "gamma", "eps", "residual", "h", "rstd"};
+const char* const kRmsNormBackward[] = {"dy", "x", "gamma", "rstd", "dx", "dgamma", "dh", "ws"};
+const char* const kRmsNormQ8[] = {"x", "q", "scale", "gamma", "eps", "residual", "h"};
 
 // The parameters `result` to `last`: one of them itself, more as a tuple.
 PyObject* returned(PyObject* const* a, int result, int last)
@@ -639,6 +714,9 @@ ANR_OPERATOR_OF(py_group_norm_backward, GROUP_NORM_BACKWARD, kNormBackward, 7, 7
 ANR_OPERATOR_OF(py_rotary, ROTARY, kRotary, 6, 4, 5, run_rotary(a))
 ANR_OPERATOR(py_gated_ff, GATED_FF, kFf, 5, 4, run_gated_ff(a))
 ANR_OPERATOR_OF(py_gated_ff_backward, GATED_FF_BACKWARD, kFfBackward, 7, 7, 10, run_gated_ff_backward(a))
+ANR_OPERATOR(py_rms_norm, RMS_NORM, kRmsNorm, 2, 1, run_rms_norm(a))
+ANR_OPERATOR_OF(py_rms_norm_backward, RMS_NORM_BACKWARD, kRmsNormBackward, 4, 4, 5, run_rms_norm_backward(a))
+ANR_OPERATOR_OF(py_rms_norm_q8, RMS_NORM_Q8, kRmsNormQ8, 3, 1, 2, run_rms_norm_q8(a))
 #undef ANR_OPERATOR
 #undef ANR_OPERATOR_OF
 
@@ -709,6 +787,17 @@ PyMethodDef g_methods[] = {
     {"gated_ff_backward", as_cfunction(py_gated_ff_backward), METH_FASTCALL | METH_KEYWORDS,
      "gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, dx=None, dw_gate=None, dw_up=None, dw_down=None, act=2, ws=None)\n--\n\n"
      "Gradients of gated_ff, into those of dx, dw_gate, dw_up and dw_down that are given, from its arguments and the gate and up that it wrote."},
+    {"rms_norm", as_cfunction(py_rms_norm), METH_FASTCALL | METH_KEYWORDS,
+     "rms_norm(x, y, gamma=None, eps=1e-06, residual=None, h=None, rstd=None)\n--\n\n"
+     "y = h * rstd * gamma with h = x + residual and rstd = 1/sqrt(mean(h^2) + eps) over each row; x, residual, h, y [T,C].  h: where the sum goes;\n"
+     "rstd: float32 [T], for a backward pass."},
+    {"rms_norm_backward", as_cfunction(py_rms_norm_backward), METH_FASTCALL | METH_KEYWORDS,
+     "rms_norm_backward(dy, x, gamma, rstd, dx=None, dgamma=None, dh=None, ws=None)\n--\n\n"
+     "Gradients of rms_norm, into those of dx and dgamma that are given, from what it normed (its h where it had a residual) and the rstd that it\n"
+     "wrote.  dh: the gradient that reaches the sum by its other way; dx is then that of x and of residual alike."},
+    {"rms_norm_q8", as_cfunction(py_rms_norm_q8), METH_FASTCALL | METH_KEYWORDS,
+     "rms_norm_q8(x, q, scale, gamma=None, eps=1e-06, residual=None, h=None)\n--\n\n"
+     "rms_norm with its result in 8 bits: q int8 [T,C], scale float32 [T], y = q * scale."},
     {"setup", py_setup, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

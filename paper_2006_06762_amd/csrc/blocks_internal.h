@@ -1,5 +1,5 @@
 // Launch interface between the C-ABI layer and the operators of a transformer block (group norm, rotary positions, gated
-// feed-forward).  As in anr_kernels.h: arguments are validated, launchers neither allocate nor synchronise.
+// feed-forward, root-mean-square norm).  As in anr_kernels.h: arguments are validated, launchers neither allocate nor synchronise.
 #pragma once
 #include "anr.h"
 #include "anr_kernels.h"
@@ -42,6 +42,21 @@ struct GatedFfArgs {
 size_t gated_ff_workspace_bytes(const GatedFfArgs& a, bool backward);
 hipError_t launch_gated_ff(const GatedFfArgs& a, hipStream_t stream);
 hipError_t launch_gated_ff_backward(const GatedFfArgs& a, hipStream_t stream);
+
+struct RmsNormArgs {
+    const void *x, *residual, *gamma;   // residual: dh in the backward call (both may be null)
+    void *h, *y;                        // h: dx in the backward call; y: q in 8 bits
+    float *rstd, *scale;                // rstd: output of the forward (may be null), input of the backward call
+    float eps;
+    const void* dy;
+    void* dgamma;
+    anr_rms_norm_desc d;                // leading dimensions filled in
+    void* ws;
+};
+size_t rms_norm_backward_workspace_bytes(const RmsNormArgs& a);
+hipError_t launch_rms_norm(const RmsNormArgs& a, hipStream_t stream);
+hipError_t launch_rms_norm_q8(const RmsNormArgs& a, hipStream_t stream);
+hipError_t launch_rms_norm_backward(const RmsNormArgs& a, hipStream_t stream);
 
 // The status of a launch, noted for anr_last_hip_error (api.cpp).
 anr_status launch_result(hipError_t e);

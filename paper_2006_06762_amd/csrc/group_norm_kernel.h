@@ -19,6 +19,7 @@
 #include "anr_kernels.h"
 #include "element_types.h"
 #include "group_norm_plan.h"
+#include "wave_join.h"
 
 namespace anr {
 namespace gnorm {
@@ -84,34 +85,6 @@ struct Place {
         tx = ty < rows ? threadIdx.x - ty * wide : columns;          // (threads that are left over have no column)
     }
 };
-
-// A lane's value from another one of its row of 16, or (ROWS: a mask of the rows that take it, zero in the others) the last one of a row before.
-template <int CONTROL, int ROWS, typename T>
-__device__ __forceinline__ T of_lane(T v)
-{
-    constexpr int WORDS = sizeof(T) / 4;
-    struct Words { int w[WORDS]; } from = __builtin_bit_cast(Words, v), to;
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) to.w[i] = __builtin_amdgcn_update_dpp(0, from.w[i], CONTROL, ROWS, 0xf, false);
-    return __builtin_bit_cast(T, to);
-}
-
-// The sum over a wave, by lanes that read each other's registers.
-template <typename T>
-__device__ __forceinline__ T wave_sum(T v)
-{
-    v += of_lane<0xb1, 0xf>(v);         // pairs: quad_perm 1, 0, 3, 2
-    v += of_lane<0x4e, 0xf>(v);         // fours: quad_perm 2, 3, 0, 1
-    v += of_lane<0x141, 0xf>(v);        // eights: row_half_mirror
-    v += of_lane<0x140, 0xf>(v);        // sixteens: row_mirror
-    v += of_lane<0x142, 0xa>(v);        // row_bcast 15: rows 1 and 3 hold two rows
-    v += of_lane<0x143, 0xc>(v);        // row_bcast 31: row 3 holds all
-    constexpr int WORDS = sizeof(T) / 4;
-    struct Words { int w[WORDS]; } all = __builtin_bit_cast(Words, v);
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) all.w[i] = __builtin_amdgcn_readlane(all.w[i], 63);
-    return __builtin_bit_cast(T, all);
-}
 
 // Parameter i of gamma or beta.
 __device__ __forceinline__ float parameter(const void* p, int i, int dtype, float absent) { return p ? load_any(p, i, dtype) : absent; }

@@ -1,0 +1,148 @@
+// Root-mean-square norm (rms_norm_kernel.h): which kernels a call runs.
+#include <algorithm>
+
+#include "blocks_internal.h"
+#include "rms_norm_kernel.h"
+#include "rows_plan.h"
+
+namespace anr {
+namespace {
+
+using rmsnorm::Args;
+using rows::Plan;
+
+constexpr int kMostGroups = 1 << 20;             // of a launch: rows beyond them are taken in turn
+// Work-groups of a backward pass, each of which leaves a line of sums.
+constexpr int kLines = 512;
+
+template <typename T>
+constexpr int values_of(int64_t C) { return C >= 16 / (int)sizeof(T) ? 16 / (int)sizeof(T) : 1; }
+
+// f(V, U, WHOLE) as constants for rows of C elements T, by a plan.
+template <typename T, typename F>
+hipError_t with_rows(int64_t C, const Plan& p, F f)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    if (C < V) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::true_type{});
+    auto of = [&](auto u) { return C % V == 0 ? f(std::integral_constant<int, V>{}, u, std::true_type{}) : f(std::integral_constant<int, V>{}, u, std::false_type{}); };
+    switch (p.units) {
+        case 1: return of(std::integral_constant<int, 1>{});
+        case 2: return of(std::integral_constant<int, 2>{});
+        case 4: return of(std::integral_constant<int, 4>{});
+        default:
+            if constexpr (V == 4) return of(std::integral_constant<int, 8>{});
+            else return of(std::integral_constant<int, 4>{});
+    }
+}
+
+template <typename F>
+hipError_t with_types(const RmsNormArgs& a, F f)
+{
+    return with_type(a.d.dtype, [&](auto t) {
+        using T = decltype(t);
+        if (a.d.param_dtype == ANR_F32) return f(t, 0.f);
+        return f(t, T{});
+    });
+}
+
+template <typename T>
+Plan plan(const anr_rms_norm_desc& d)
+{
+    const int V = values_of<T>(d.C);
+    return rows::plan_of((d.C + V - 1) / V, rows::kHeld / V, d.T);
+}
+
+Args arguments(const RmsNormArgs& g)
+{
+    Args a{};
+    a.x = g.x;
+    a.gamma = g.gamma;
+    a.T = g.d.T;
+    a.C = (int)g.d.C;
+    a.ldx = g.d.ldx;
+    a.ld_residual = g.d.ld_residual;
+    a.ldh = g.d.ldh;
+    a.ldy = g.d.ldy;
+    return a;
+}
+
+bool whole_units(const void* p, int64_t ld, int es) { return !p || (is_aligned16(p) && ld * es % 16 == 0); }
+
+template <bool QUANTIZED>
+hipError_t launch_forward(const RmsNormArgs& g, hipStream_t stream)
+{
+    if (g.d.T == 0) return hipSuccess;
+    Args a = arguments(g);
+    a.residual = g.residual;
+    a.h = g.h;
+    a.y = g.y;
+    a.eps = g.eps;
+    a.rstd = g.rstd;
+    a.scale = g.scale;
+    const int es = element_bytes(g.d.dtype);
+    return with_types(g, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        const Plan of = plan<T>(g.d);
+        return with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
+            constexpr int V = decltype(v)::value, U = decltype(u)::value;
+            constexpr bool WHOLE = decltype(whole)::value;
+            a.streaming = V > 1 && whole_units(a.h, a.ldh, es) && (QUANTIZED || whole_units(a.y, a.ldy, es)) && g.d.C * es % 16 == 0;
+            const int64_t groups = std::min<int64_t>((a.T + of.rows - 1) / of.rows, kMostGroups);
+            return launch_kernel(rmsnorm::forward_kernel<T, P, V, U, WHOLE, QUANTIZED, 1024>, dim3((unsigned)groups), dim3(64 * of.waves, of.rows), 0, stream, a);
+        });
+    });
+}
+
+template <typename T>
+int lines_of(const anr_rms_norm_desc& d)
+{
+    const Plan of = plan<T>(d);
+    return (int)std::min<int64_t>((d.T + of.rows - 1) / of.rows, kLines);
+}
+int lines(const anr_rms_norm_desc& d)
+{
+    return with_type(d.dtype, [&](auto t) { return lines_of<decltype(t)>(d); });
+}
+
+}  // namespace
+
+size_t rms_norm_backward_workspace_bytes(const RmsNormArgs& g) { return g.d.T == 0 ? 0 : (size_t)lines(g.d) * g.d.C * sizeof(float); }
+
+hipError_t launch_rms_norm(const RmsNormArgs& g, hipStream_t stream) { return launch_forward<false>(g, stream); }
+hipError_t launch_rms_norm_q8(const RmsNormArgs& g, hipStream_t stream) { return launch_forward<true>(g, stream); }
+
+hipError_t launch_rms_norm_backward(const RmsNormArgs& g, hipStream_t stream)
+{
+    Args a = arguments(g);
+    a.dy = g.dy;
+    a.dh = g.residual;
+    a.h = g.h;
+    a.rstd_in = g.rstd;
+    a.sums = g.dgamma ? static_cast<float*>(g.ws) : nullptr;
+    const int es = element_bytes(g.d.dtype), n = g.d.T == 0 ? 0 : lines(g.d);
+    if (n > 0) {
+        const hipError_t e = with_types(g, [&](auto t, auto p) {
+            using T = decltype(t);
+            using P = decltype(p);
+            const Plan of = plan<T>(g.d);
+            return with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
+                constexpr int V = decltype(v)::value, U = decltype(u)::value;
+                constexpr bool WHOLE = decltype(whole)::value;
+                a.streaming = V > 1 && a.h && whole_units(a.h, a.ldh, es) && g.d.C * es % 16 == 0;
+                return launch_kernel(rmsnorm::backward_kernel<T, P, V, U, WHOLE, 1024>, dim3((unsigned)n), dim3(64 * of.waves, of.rows), (size_t)(of.rows - 1) * g.d.C * sizeof(float),
+                                     stream, a);
+            });
+        });
+        if (e != hipSuccess) return e;
+    }
+    if (!g.dgamma) return hipSuccess;
+    const unsigned groups = (unsigned)((g.d.C + rmsnorm::kJoinColumns - 1) / rmsnorm::kJoinColumns);
+    return with_type(g.d.param_dtype, [&](auto p) {
+        using P = decltype(p);
+        return launch_kernel(rmsnorm::join_kernel<P>, dim3(groups), dim3(rmsnorm::kJoinColumns * rmsnorm::kJoinRuns), 0, stream, static_cast<const float*>(g.ws), n, (int)g.d.C,
+                             static_cast<P*>(g.dgamma));
+    });
+}
+
+}  // namespace anr

@@ -1,0 +1,219 @@
+// Root-mean-square norm of rows with the residual's addition, and its gradients.  h = x + residual, rstd = 1 / sqrt(mean(h^2) + eps),
+// y = h rstd gamma: a row is read once, held in registers (rows_device.h) and summed by the waves that have it.
+//
+// In 8 bits the largest |y| of a row is rstd times that of |h gamma|, which is found with the sum of the squares in one go, and y is the same
+// number of its steps as h gamma of its own.
+//
+// Backward, with dhat = dy gamma and hat = x rstd: dx = rstd (dhat - hat mean(dhat hat)) + dh, and dgamma = sum over the rows of dy hat.  A
+// work-group goes over several rows and sums dgamma of its columns in registers; a second launch joins the work-groups' sums in their order.
+#pragma once
+#include "anr_kernels.h"
+#include "rows_device.h"
+
+namespace anr {
+namespace rmsnorm {
+
+struct Args {
+    const void *x, *residual, *gamma;
+    void *h, *y;                    // y: q where the output is in 8 bits
+    float *rstd, *scale;
+    float eps;
+    int64_t T;
+    int C;
+    int64_t ldx, ld_residual, ldh, ldy;
+    bool streaming;                 // the outputs' rows are whole aligned units
+    // backward
+    const void *dy, *dh;            // (dx goes to h)
+    const float* rstd_in;
+    float* sums;                    // [work-groups][C], or null: no dgamma
+};
+
+// P: gamma's type.  U units of a thread.
+template <typename T, typename P, int V, int U, bool WHOLE, bool QUANTIZED, int THREADS>
+__global__ __launch_bounds__(THREADS) void forward_kernel(const Args a)
+{
+    using namespace rows;
+    const int threads = blockDim.x, t = threadIdx.x, C = a.C;
+    Raw<P, V> g[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (a.gamma) g[u].load(static_cast<const P*>(a.gamma) + Unit<V, WHOLE>(t + u * threads, C).start);
+        else g[u].fill(from_float<P>(1.f));
+    }
+    int round = 0;
+    for (int64_t first = (int64_t)blockIdx.x * blockDim.y; first < a.T; first += (int64_t)gridDim.x * blockDim.y, round ^= 1) {
+        const int64_t row = first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1;      // (rows past the end repeat the last one and store nothing)
+        const bool in = first + threadIdx.y < a.T;
+        Raw<T, V> x[U], r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u].load(static_cast<const T*>(a.x) + row * a.ldx + Unit<V, WHOLE>(t + u * threads, C).start);
+        if (a.residual) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) r[u].load(static_cast<const T*>(a.residual) + row * a.ld_residual + Unit<V, WHOLE>(t + u * threads, C).start);
+        }
+        float h[U][V];
+        Joined of{0.f, 0u};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const Unit<V, WHOLE> unit(t + u * threads, C);
+            x[u].floats(h[u]);
+            if (a.residual) {
+                float v[V];
+                r[u].floats(v);
+#pragma unroll
+                for (int j = 0; j < V; ++j) h[u][j] += v[j];
+            }
+            float gamma[V];
+            if (QUANTIZED) g[u].floats(gamma);
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (WHOLE || unit.counts(j)) sum = fmaf(h[u][j], h[u][j], sum);
+                if (QUANTIZED) of.largest = max(of.largest, magnitude(h[u][j] * gamma[j]));
+            }
+            if (!WHOLE || unit.in()) of.sum += sum;
+        }
+        of = join_row(of, round);
+        const float rstd = 1.f / sqrtf(of.sum / (float)C + a.eps);
+        if (!in) continue;
+        const Steps steps(of.largest, rstd);
+        if (t == 0) {
+            if (a.rstd) a.rstd[row] = rstd;
+            if (QUANTIZED) a.scale[row] = steps.step;
+        }
+        by_streaming(a.streaming, [&](auto streaming) {
+            constexpr bool S = decltype(streaming)::value;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const Unit<V, WHOLE> unit(t + u * threads, C);
+                if (!unit.in()) continue;
+                if (a.h) store<S>(static_cast<T*>(a.h) + row * a.ldh + unit.start, h[u]);
+                float gamma[V], y[V];
+                g[u].floats(gamma);
+#pragma unroll
+                for (int j = 0; j < V; ++j) y[j] = QUANTIZED ? h[u][j] * gamma[j] : h[u][j] * rstd * gamma[j];
+                if (QUANTIZED) store_steps<V>(static_cast<int8_t*>(a.y) + row * a.ldy + unit.start, y, steps);
+                else store<S>(static_cast<T*>(a.y) + row * a.ldy + unit.start, y);
+            }
+        });
+    }
+}
+
+template <typename T, typename P, int V, int U, bool WHOLE, int THREADS>
+__global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
+{
+    using namespace rows;
+    extern __shared__ float shared[];            // rows of a work-group beyond the first: their sums, [rows - 1][C]
+    const int threads = blockDim.x, t = threadIdx.x, C = a.C;
+    Raw<P, V> g[U];
+    float sums[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (a.gamma) g[u].load(static_cast<const P*>(a.gamma) + Unit<V, WHOLE>(t + u * threads, C).start);
+        else g[u].fill(from_float<P>(1.f));
+#pragma unroll
+        for (int j = 0; j < V; ++j) sums[u][j] = 0.f;
+    }
+    int round = 0;
+    for (int64_t first = (int64_t)blockIdx.x * blockDim.y; first < a.T; first += (int64_t)gridDim.x * blockDim.y, round ^= 1) {
+        const int64_t row = first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1;
+        const bool in = first + threadIdx.y < a.T;
+        Raw<T, V> x[U], dy[U], dh[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int start = Unit<V, WHOLE>(t + u * threads, C).start;
+            dy[u].load(static_cast<const T*>(a.dy) + row * a.ldy + start);
+            x[u].load(static_cast<const T*>(a.x) + row * a.ldx + start);
+        }
+        if (a.dh) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) dh[u].load(static_cast<const T*>(a.dh) + row * a.ld_residual + Unit<V, WHOLE>(t + u * threads, C).start);
+        }
+        const float rstd = a.rstd_in[row];
+        Joined along{0.f, 0u};                   // sum of dhat x
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const Unit<V, WHOLE> unit(t + u * threads, C);
+            float xv[V], dv[V], gamma[V], sum = 0.f;
+            x[u].floats(xv);
+            dy[u].floats(dv);
+            g[u].floats(gamma);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float hat = xv[j] * rstd;
+                if (WHOLE || unit.counts(j)) sum = fmaf(dv[j] * gamma[j], hat, sum);
+                if (in) sums[u][j] = fmaf(dv[j], hat, sums[u][j]);
+            }
+            if (!WHOLE || unit.in()) along.sum += sum;
+        }
+        if (!a.h) continue;
+        along = join_row(along, round);
+        if (!in) continue;
+        const float part = along.sum / (float)C;
+        by_streaming(a.streaming, [&](auto streaming) {
+            constexpr bool S = decltype(streaming)::value;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const Unit<V, WHOLE> unit(t + u * threads, C);
+                if (!unit.in()) continue;
+                float xv[V], dv[V], gamma[V], extra[V];
+                x[u].floats(xv);
+                dy[u].floats(dv);
+                g[u].floats(gamma);
+                if (a.dh) dh[u].floats(extra);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    dv[j] = rstd * fmaf(-xv[j] * rstd, part, dv[j] * gamma[j]);
+                    if (a.dh) dv[j] += extra[j];
+                }
+                store<S>(static_cast<T*>(a.h) + row * a.ldh + unit.start, dv);
+            }
+        });
+    }
+    if (!a.sums) return;
+    // the rows of a work-group, then one line of the workspace
+    if (blockDim.y > 1) {
+        if (threadIdx.y > 0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const Unit<V, WHOLE> unit(t + u * threads, C);
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (unit.counts(j)) shared[(threadIdx.y - 1) * C + unit.start + j] = sums[u][j];
+            }
+        }
+        __syncthreads();
+        if (threadIdx.y > 0) return;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const Unit<V, WHOLE> unit(t + u * threads, C);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (unit.counts(j)) {
+                float sum = sums[u][j];
+                for (int y = 1; y < (int)blockDim.y; ++y) sum += shared[(y - 1) * C + unit.start + j];
+                a.sums[(int64_t)blockIdx.x * C + unit.start + j] = sum;
+            }
+    }
+}
+
+// dgamma = the sum of `lines` lines of C floats: 32 columns of a work-group by 32 runs of lines, joined in LDS.
+constexpr int kJoinColumns = 32, kJoinRuns = 32;
+template <typename P>
+__global__ __launch_bounds__(kJoinColumns* kJoinRuns) void join_kernel(const float* sums, int lines, int C, P* dgamma)
+{
+    __shared__ float parts[kJoinRuns][kJoinColumns];
+    const int x = threadIdx.x % kJoinColumns, run = threadIdx.x / kJoinColumns, column = blockIdx.x * kJoinColumns + x;
+    float sum = 0.f;
+    if (column < C)
+        for (int i = run; i < lines; i += kJoinRuns) sum += sums[(int64_t)i * C + column];
+    parts[run][x] = sum;
+    __syncthreads();
+    if (run > 0 || column >= C) return;
+    for (int i = 1; i < kJoinRuns; ++i) sum += parts[i][x];
+    dgamma[column] = from_float<P>(sum);
+}
+
+}  // namespace rmsnorm
+}  // namespace anr

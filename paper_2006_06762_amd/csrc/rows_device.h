@@ -1,0 +1,158 @@
+// Rows of C values that the threads of one or more waves hold in registers, for operators that go over a row more than once but read it
+// once: sums or largest values of the row, then every value of it again.
+//
+// Unit i of a row are its V values (16 bytes) from i V on; a thread has units t, t + threads, and so on, so that a wave reads 1 KB at a time.
+// The last unit of a row whose length is no whole number of units starts so far ahead that it ends with the row: its first values are another
+// unit's too, which both compute and store alike, and which only the sums have to leave out.  No load stands under a branch.  Values that
+// start at any element's address are read and written 16 bytes at a time as well, which the memory pipes take.
+// Rows of less than one unit have units of one value.
+#pragma once
+#include "element_types.h"
+#include "wave_join.h"
+
+namespace anr {
+namespace rows {
+
+constexpr int kMostWaves = 16;                   // of a row
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// V values as they lie in memory, at any element's address.
+template <typename T, int V>
+struct Raw {
+    static constexpr int BYTES = sizeof(T) * V;
+    static constexpr int WORDS = BYTES >= 4 ? BYTES / 4 : 1;
+    uint32_t w[WORDS];
+
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (V == 1) {
+            w[0] = 0;
+            __builtin_memcpy(w, p, sizeof(T));
+        } else {
+            struct __attribute__((packed, aligned(sizeof(T)))) Loose { uint32_t w[WORDS]; };
+            const Loose l = *reinterpret_cast<const Loose*>(p);
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) w[i] = l.w[i];
+        }
+    }
+    __device__ __forceinline__ void fill(T v)
+    {
+        T a[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) a[i] = v;
+        w[0] = 0;
+        __builtin_memcpy(w, a, sizeof a);
+    }
+    __device__ __forceinline__ void floats(float (&out)[V]) const
+    {
+        T a[V];
+        __builtin_memcpy(a, w, sizeof a);
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[i] = to_float(a[i]);
+    }
+};
+
+// STREAMING: past L2 (see stg4_nt), for 16-byte units that neighbouring lanes write whole lines of.
+template <bool STREAMING, typename T, int V>
+__device__ __forceinline__ void store(T* p, const float (&v)[V])
+{
+    const Pack<T, V> a = pack_floats<T, V>(v);
+    if constexpr (STREAMING && sizeof(T) * V >= 16) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) * V / 16; ++i) {
+            u32x4 w;
+            __builtin_memcpy(&w, reinterpret_cast<const char*>(&a) + 16 * i, 16);
+            __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p) + i);
+        }
+    } else {
+        struct __attribute__((packed, aligned(sizeof(T)))) Loose { T v[V]; };
+        Loose l;
+#pragma unroll
+        for (int i = 0; i < V; ++i) l.v[i] = a.v[i];
+        *reinterpret_cast<Loose*>(p) = l;
+    }
+}
+
+// Where unit i of a row of C values starts, and how many of its values another unit counts (V: all of them, it is past the end).
+template <int V, bool WHOLE>
+struct Unit {
+    int start, counted;
+    __device__ __forceinline__ Unit(int i, int C)
+    {
+        const int64_t own = (int64_t)i * V;
+        start = (int)(own < C - V ? own : C - V);
+        counted = WHOLE ? (own < C ? 0 : V) : (int)(own - start < V ? own - start : V);
+    }
+    __device__ __forceinline__ bool in() const { return counted < V; }
+    __device__ __forceinline__ bool counts(int j) const { return WHOLE ? counted == 0 : j >= counted; }
+};
+
+// The bits of |v|, whose order as whole numbers is that of the magnitudes, infinity and NaN above all others.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+constexpr uint32_t kInfinite = 0x7f800000u;
+
+// A row in 8 bits: whole steps of `step`, the largest magnitude of the row being 127 of them.  Rows of zeros have the step zero; an infinity or NaN makes the
+// step NaN and the values zeros, so that whatever is made of the row is NaN.  Rows that lie low in float32's range are raised before they are
+// divided by their step, whose inverse would leave it at the other end.
+struct Steps {
+    float raise, inverse;
+    float step;                     // of rows whose values are multiplied by `factor` afterwards
+    __device__ __forceinline__ Steps(uint32_t largest, float factor)
+    {
+        const float most = __builtin_bit_cast(float, largest);
+        const bool fine = largest < kInfinite;
+        raise = most < 0x1p-60f ? 0x1p64f : 1.f;
+        inverse = fine && largest != 0 ? 127.f / (most * raise) : 0.f;
+        step = fine ? most * factor / 127.f : __builtin_nanf("");
+    }
+    __device__ __forceinline__ int operator()(float v) const
+    {
+        return inverse == 0.f ? 0 : (int)__builtin_amdgcn_fmed3f(rintf(v * raise * inverse), -127.f, 127.f);
+    }
+};
+
+// V of them at any address.
+template <int V>
+__device__ __forceinline__ void store_steps(int8_t* p, const float (&v)[V], const Steps& steps)
+{
+    if constexpr (V == 1) {
+        p[0] = (int8_t)steps(v[0]);
+    } else {
+        struct __attribute__((packed, aligned(1))) Loose { uint32_t w[V / 4]; };
+        Loose l;
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+            const uint32_t a = steps(v[4 * i]), b = steps(v[4 * i + 1]), c = steps(v[4 * i + 2]), d = steps(v[4 * i + 3]);
+            l.w[i] = (a & 0xff) | (b & 0xff) << 8 | (c & 0xff) << 16 | d << 24;
+        }
+        *reinterpret_cast<Loose*>(p) = l;
+    }
+}
+
+// A sum and a largest magnitude over the waves of a row (blockDim.x threads; a work-group has blockDim.y rows). `round` alternates from call to call, so that one
+// barrier is enough.
+struct Joined {
+    float sum;
+    uint32_t largest;
+};
+__device__ __forceinline__ Joined join_row(Joined v, int round)
+{
+    __shared__ Joined parts[2][kMostWaves];
+    v.sum = wave_sum(v.sum);
+    v.largest = wave_max(v.largest);
+    const int waves = blockDim.x >> 6;
+    if (waves == 1) return v;
+    const int first = threadIdx.y * waves, wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) parts[round][first + wave] = v;
+    __syncthreads();
+    v = parts[round][first];
+    for (int i = 1; i < waves; ++i) {
+        v.sum += parts[round][first + i].sum;
+        v.largest = max(v.largest, parts[round][first + i].largest);
+    }
+    return v;
+}
+
+}  // namespace rows
+}  // namespace anr

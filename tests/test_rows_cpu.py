@@ -1,0 +1,107 @@
+"""Root-mean-square norm without a GPU: layout of the descriptor, what is refused, what workspaces are asked for, and that no refused call
+launches anything."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2006_06762_amd import binding as B  # noqa: E402
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P, P2, P3, ODD = (ctypes.c_void_p(v) for v in (0x10000, 0x20000, 0x30000, 0x10001))      # never dereferenced: validation fails first
+OK, NULL, INVALID, UNSUPPORTED, WORKSPACE = B.ANR_OK, B.ANR_ERR_NULL, B.ANR_ERR_INVALID_ARG, B.ANR_ERR_UNSUPPORTED, B.ANR_ERR_WORKSPACE
+
+
+def layout_of(tmp_path, fields):
+    """(sizes and offsets as C has them, as the binding has them)."""
+    text = '#include <stdio.h>\n#include <stddef.h>\n#include "anr.h"\nint main(void) {\n'
+    want = []
+    for c, t in fields.items():
+        text += 'printf("%%zu ", sizeof(%s));\n' % c
+        want.append(ctypes.sizeof(t))
+        for n, *_ in t._fields_:
+            text += 'printf("%%zu ", offsetof(%s, %s));\n' % (c, n)
+            want.append(getattr(t, n).offset)
+    (tmp_path / "l.c").write_text(text + "return 0; }")
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), str(tmp_path / "l.c"), "-o", str(tmp_path / "l")], check=True)
+    return [int(v) for v in subprocess.run([str(tmp_path / "l")], check=True, capture_output=True, text=True).stdout.split()], want
+
+
+def test_rms_norm_layout_matches_c(tmp_path):
+    got, want = layout_of(tmp_path, {"anr_rms_norm_desc": B.RmsNormDesc})
+    assert got == want
+
+
+def norm_desc(**kw):
+    return B.RmsNormDesc(**dict(dict(T=9, C=40, dtype=B.ANR_BF16, param_dtype=B.ANR_BF16), **kw))
+
+
+def norm(d, x=P, residual=None, gamma=P, eps=1e-6, h=None, y=P2, rstd=None):
+    return B.raw().anr_rms_norm(ctypes.byref(d) if d else None, x, residual, gamma, ctypes.c_float(eps), h, y, rstd, None, 0, None)
+
+
+def norm_q8(d, x=P, residual=None, gamma=P, eps=1e-6, h=None, y=P2, scale=P3):
+    return B.raw().anr_rms_norm_q8(ctypes.byref(d) if d else None, x, residual, gamma, ctypes.c_float(eps), h, y, scale, None, 0, None)
+
+
+def norm_backward(d, dy=P, x=P2, gamma=P, rstd=P, dh=None, dx=P3, dgamma=P, ws=None, size=0):
+    return B.raw().anr_rms_norm_backward(ctypes.byref(d) if d else None, dy, x, gamma, rstd, dh, dx, dgamma, ws, size, None)
+
+
+def test_rms_norm_refusals():
+    for call in (norm, norm_q8, norm_backward):
+        assert call(None) == NULL
+        for field, bad in (("T", -1), ("C", 0), ("dtype", 3), ("dtype", -1), ("param_dtype", B.ANR_F16), ("ldx", 39), ("ldx", -40), ("ld_residual", 1), ("ldh", 39), ("ldy", 39)):
+            assert call(norm_desc(**{field: bad})) == INVALID, (call, field, bad)
+        for field, bad in (("C", 32769), ("T", 1 << 31), ("ldx", 1 << 40), ("ldy", 1 << 55)):
+            assert call(norm_desc(**{field: bad})) == UNSUPPORTED, (call, field, bad)
+        assert call(norm_desc(), x=None) == NULL and call(norm_desc(), x=ODD) == INVALID and call(norm_desc(), gamma=ODD) == INVALID
+    for call in (norm, norm_q8):
+        assert call(norm_desc(), y=None) == NULL
+        for eps in (-1e-9, float("nan"), float("inf")):
+            assert call(norm_desc(), eps=eps) == INVALID
+        assert call(norm_desc(), h=P3) == INVALID                                    # a sum without a residual
+        assert call(norm_desc(), residual=P3, h=ODD) == INVALID and call(norm_desc(), residual=ODD) == INVALID
+        assert call(norm_desc(), residual=P3, h=P2) == INVALID                       # two outputs in one place
+        assert call(norm_desc(ldx=48), residual=P3, h=P) == INVALID                  # in place with another leading dimension
+        assert call(norm_desc(ld_residual=48), residual=P3, h=P3) == INVALID
+    assert norm(norm_desc(), y=ODD) == INVALID and norm(norm_desc(), rstd=ctypes.c_void_p(0x10002)) == INVALID
+    assert norm(norm_desc(ldy=48), y=P) == INVALID and norm(norm_desc(ldy=48), residual=P2) == INVALID
+    assert norm_q8(norm_desc(), scale=None) == NULL and norm_q8(norm_desc(), scale=ctypes.c_void_p(0x10002)) == INVALID
+    assert norm_q8(norm_desc(), y=P) == INVALID and norm_q8(norm_desc(), residual=P2) == INVALID
+    for name in ("dy", "rstd"):
+        assert norm_backward(norm_desc(), **{name: None}) == NULL
+    assert norm_backward(norm_desc(), dx=None, dgamma=None) == NULL
+    for name in ("dy", "rstd", "dh", "dx", "dgamma"):
+        assert norm_backward(norm_desc(), **{name: ODD}) == INVALID, name
+    for field, name in (("ldy", "dy"), ("ldx", "x"), ("ld_residual", "dh")):
+        assert norm_backward(norm_desc(**{field: 48}), **{name: P3}) == INVALID, field
+    d = norm_desc(T=5000)
+    need = B.workspace_size(B.ANR_OP_RMS_NORM_BACKWARD, d)
+    assert need > 0 and need % 4 == 0
+    assert norm_backward(d) == WORKSPACE and norm_backward(d, ws=P, size=need - 1) == WORKSPACE and norm_backward(d, ws=ctypes.c_void_p(0x10008), size=need) == INVALID
+    for op in (B.ANR_OP_RMS_NORM, B.ANR_OP_RMS_NORM_Q8):
+        assert B.workspace_size(op, d) == 0
+    # nothing to do is no error and no launch
+    d = norm_desc(T=0)
+    assert norm(d, None, y=None) == OK and norm_q8(d, None, y=None, scale=None) == OK and norm_backward(d, None, None, None, None, None, None, None) == OK
+    assert B.workspace_size(B.ANR_OP_RMS_NORM_BACKWARD, d) == 0
+    # the leading dimensions of a single row say nothing
+    assert B.workspace_size(B.ANR_OP_RMS_NORM, norm_desc(T=1, ldx=1, ldy=1 << 60)) == 0
+
+
+def test_rms_norm_binding_refuses():
+    x, g = torch.zeros(4, 8), torch.zeros(8)
+    for args, kw, error in (((x, x), {}, TypeError), ((x.double(), x), {}, TypeError), ((x[0], x), {}, ValueError), ((x, x, g.half()), {}, TypeError),
+                            ((x, x), {"h": x}, ValueError)):
+        with pytest.raises(error):
+            B.rms_norm(*args, **kw)
+    with pytest.raises(TypeError):
+        B.rms_norm_q8(x, x.char(), g[:4])
+    with pytest.raises(ValueError):
+        B.rms_norm_q8(x, x.char(), g[:4], h=x)
+    with pytest.raises(TypeError):
+        B.rms_norm_backward(x, x, g, g[:4], x, g.half())
