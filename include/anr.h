@@ -80,7 +80,8 @@ typedef enum {
     ANR_OP_TBG = 4, ANR_OP_TBS = 5, ANR_OP_NRM = 6,
     ANR_OP_GROUP_NORM = 7, ANR_OP_GROUP_NORM_BACKWARD = 8, ANR_OP_ROTARY = 9,
     ANR_OP_GATED_FF = 10, ANR_OP_GATED_FF_BACKWARD = 11,
-    ANR_OP_RMS_NORM = 12, ANR_OP_RMS_NORM_BACKWARD = 13, ANR_OP_RMS_NORM_Q8 = 14
+    ANR_OP_RMS_NORM = 12, ANR_OP_RMS_NORM_BACKWARD = 13, ANR_OP_RMS_NORM_Q8 = 14,
+    ANR_OP_QUANTIZE_ROWS = 15, ANR_OP_DEQUANTIZE_ROWS = 16
 } anr_op;
 
 /* Types of the elements of the operators of a transformer block (from group norm on).  The
@@ -442,6 +443,28 @@ anr_status anr_rms_norm_backward(const anr_rms_norm_desc *desc, const void *dy, 
  * scale and q zero.  One with an infinity or NaN has a NaN as its scale and q zero. */
 anr_status anr_rms_norm_q8(const anr_rms_norm_desc *desc, const void *x, const void *residual, const void *gamma,
                            float eps, void *h, int8_t *q, float *scale, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * T rows of C values in 8 bits, each with a scale of its own: tokens in front of a product of 8-bit
+ * integers, or weights as [outputs, inputs].  Row-major, leading dimensions in elements, 0 for
+ * packed: x, or y in the way back (ldx), up (ld_up), q (ldq).  C <= 2^20, T < 2^31.
+ */
+typedef struct {
+    int64_t T, C;
+    int32_t act;         /* anr_act; ANR_ACT_NONE in the way back */
+    int32_t dtype;       /* anr_dtype of x, up and y */
+    int64_t ldx, ld_up, ldq;
+} anr_rows_q8_desc;
+
+/* v = act(x) up (act(x) where up is NULL), scale[t] = (largest |v| of row t) / 127 and q = v / scale
+ * to the nearest whole number, ties to even.  A row of zeros has scale and q zero; one with an
+ * infinity or NaN has a NaN as its scale and q zero. */
+anr_status anr_quantize_rows(const anr_rows_q8_desc *desc, const void *x, const void *up, int8_t *q, float *scale,
+                             void *ws, size_t ws_bytes, void *hip_stream);
+
+/* y = q scale[t]. */
+anr_status anr_dequantize_rows(const anr_rows_q8_desc *desc, const int8_t *q, const float *scale, void *y,
+                               void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Bytes of device workspace `op` (an anr_op) needs for `desc` (the matching
  * descriptor type): a function of the descriptor only, enough for any pointer

@@ -32,7 +32,7 @@ ANR_OK, ANR_ERR_NULL, ANR_ERR_INVALID_ARG, ANR_ERR_UNSUPPORTED, ANR_ERR_WORKSPAC
 ANR_LAYOUT_NCHW = 0
 ANR_OP_GEMM, ANR_OP_CONV2D, ANR_OP_CONV_BN_RELU, ANR_OP_DWCONV, ANR_OP_TBG, ANR_OP_TBS, ANR_OP_NRM = range(7)
 ANR_OP_GROUP_NORM, ANR_OP_GROUP_NORM_BACKWARD, ANR_OP_ROTARY, ANR_OP_GATED_FF, ANR_OP_GATED_FF_BACKWARD = range(7, 12)
-ANR_OP_RMS_NORM, ANR_OP_RMS_NORM_BACKWARD, ANR_OP_RMS_NORM_Q8 = range(12, 15)
+ANR_OP_RMS_NORM, ANR_OP_RMS_NORM_BACKWARD, ANR_OP_RMS_NORM_Q8, ANR_OP_QUANTIZE_ROWS, ANR_OP_DEQUANTIZE_ROWS = range(12, 17)
 ANR_F32, ANR_F16, ANR_BF16 = range(3)
 ANR_ACT_NONE, ANR_ACT_RELU, ANR_ACT_SILU, ANR_ACT_GELU, ANR_ACT_GELU_TANH = range(5)
 ANR_ROTARY_HALVES, ANR_ROTARY_ADJACENT, ANR_ROTARY_SECTION_HALVES = range(3)
@@ -42,7 +42,7 @@ EXPORTS = ("anr_gemm", "anr_conv2d", "anr_conv2d_noalloc", "anr_conv2d_packed_si
            "anr_conv2d_packed", "anr_conv_bn_relu_packed", "anr_conv_bn_relu", "anr_dwconv", "anr_tbg", "anr_tbs", "anr_nrm",
            "anr_workspace_size", "anr_conv2d_fast_workspace_size", "anr_conv2d_route", "anr_status_string", "anr_version", "anr_last_hip_error",
            "anr_last_hip_error_string", "anr_group_norm", "anr_group_norm_backward", "anr_rotary", "anr_gated_ff", "anr_gated_ff_backward",
-           "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8")
+           "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8", "anr_quantize_rows", "anr_dequantize_rows")
 
 
 class GemmDesc(ctypes.Structure):
@@ -110,6 +110,11 @@ class RmsNormDesc(ctypes.Structure):
                 ("ldx", ctypes.c_int64), ("ld_residual", ctypes.c_int64), ("ldh", ctypes.c_int64), ("ldy", ctypes.c_int64)]
 
 
+class RowsQ8Desc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("C", ctypes.c_int64), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("ldx", ctypes.c_int64), ("ld_up", ctypes.c_int64), ("ldq", ctypes.c_int64)]
+
+
 _vp = ctypes.c_void_p
 _lib.anr_gemm.argtypes = [ctypes.POINTER(GemmDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_conv2d.argtypes = [ctypes.POINTER(ConvDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
@@ -133,13 +138,16 @@ _lib.anr_gated_ff_backward.argtypes = [ctypes.POINTER(GatedFfDesc)] + [_vp] * 12
 _lib.anr_rms_norm.argtypes = [ctypes.POINTER(RmsNormDesc), _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_rms_norm_backward.argtypes = [ctypes.POINTER(RmsNormDesc)] + [_vp] * 8 + [ctypes.c_size_t, _vp]
 _lib.anr_rms_norm_q8.argtypes = [ctypes.POINTER(RmsNormDesc), _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.anr_quantize_rows.argtypes = [ctypes.POINTER(RowsQ8Desc)] + [_vp] * 5 + [ctypes.c_size_t, _vp]
+_lib.anr_dequantize_rows.argtypes = [ctypes.POINTER(RowsQ8Desc)] + [_vp] * 4 + [ctypes.c_size_t, _vp]
 _lib.anr_workspace_size.argtypes = [ctypes.c_int, _vp, ctypes.POINTER(ctypes.c_size_t)]
 _lib.anr_conv2d_fast_workspace_size.argtypes = [ctypes.POINTER(ConvDesc), ctypes.POINTER(ctypes.c_size_t)]
 _lib.anr_conv2d_route.argtypes = [ctypes.POINTER(ConvDesc), ctypes.POINTER(ConvRoute)]
 for _name in ("anr_gemm", "anr_conv2d", "anr_conv2d_noalloc", "anr_conv2d_packed_size", "anr_conv2d_pack_weights",
               "anr_conv2d_packed", "anr_conv_bn_relu_packed", "anr_conv_bn_relu", "anr_dwconv", "anr_tbg", "anr_tbs",
               "anr_workspace_size", "anr_conv2d_fast_workspace_size", "anr_group_norm", "anr_group_norm_backward", "anr_rotary",
-              "anr_gated_ff", "anr_gated_ff_backward", "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8"):
+              "anr_gated_ff", "anr_gated_ff_backward", "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8",
+              "anr_quantize_rows", "anr_dequantize_rows"):
     getattr(_lib, _name).restype = ctypes.c_int
 _lib.anr_status_string.argtypes = [ctypes.c_int]
 _lib.anr_status_string.restype = ctypes.c_char_p
@@ -203,6 +211,8 @@ _fast.anr_gated_ff_backward.argtypes = [_vp] * 13 + [_sz, _vp]
 _fast.anr_rms_norm.argtypes = [_vp] * 4 + [_fl] + [_vp] * 4 + [_sz, _vp]
 _fast.anr_rms_norm_backward.argtypes = [_vp] * 9 + [_sz, _vp]
 _fast.anr_rms_norm_q8.argtypes = [_vp] * 4 + [_fl] + [_vp] * 4 + [_sz, _vp]
+_fast.anr_quantize_rows.argtypes = [_vp] * 6 + [_sz, _vp]
+_fast.anr_dequantize_rows.argtypes = [_vp] * 5 + [_sz, _vp]
 
 _pack_gemm = struct.Struct("@10q").pack
 _pack_conv = struct.Struct("@14i8q2i").pack
@@ -212,8 +222,9 @@ _pack_group_norm = struct.Struct("@8i9q").pack
 _pack_rotary = struct.Struct("@15i15q").pack
 _pack_gated_ff = struct.Struct("@3q2i8q").pack
 _pack_rms_norm = struct.Struct("@2q2i4q").pack
-assert [struct.calcsize(f) for f in ("@10q", "@14i8q2i", "@4i12q", "@5q", "@8i9q", "@15i15q", "@3q2i8q", "@2q2i4q")] == \
-    [ctypes.sizeof(t) for t in (GemmDesc, ConvDesc, TbgDesc, NrmDesc, GroupNormDesc, RotaryDesc, GatedFfDesc, RmsNormDesc)]
+_pack_rows_q8 = struct.Struct("@2q2i3q").pack
+assert [struct.calcsize(f) for f in ("@10q", "@14i8q2i", "@4i12q", "@5q", "@8i9q", "@15i15q", "@3q2i8q", "@2q2i4q", "@2q2i3q")] == \
+    [ctypes.sizeof(t) for t in (GemmDesc, ConvDesc, TbgDesc, NrmDesc, GroupNormDesc, RotaryDesc, GatedFfDesc, RmsNormDesc, RowsQ8Desc)]
 _NO_STRIDES = (0, 0, 0, 0)
 _f32 = torch.float32
 
@@ -741,9 +752,29 @@ def _rms_norm_backward(dy, x, gamma, rstd, dx=None, dgamma=None, dh=None, ws=Non
     return dx, dgamma
 
 
+def _quantize_rows(x, q, scale, act=ANR_ACT_NONE, up=None):
+    """q int8 [T,C] and scale float32 [T]: rows of act(x) * up (act(x) without up) in 8 bits, whose values are q * scale.  x and up [T,C]; for weights as
+    [outputs, inputs] a scale for each output."""
+    dtype, (T, C) = _dtype(x), _matrix("x", x)
+    xs, us, qs = _rows("x", x, (T, C), x.dtype), _rows("up", up, (T, C), x.dtype), _rows("q", q, (T, C), torch.int8)
+    d = _pack_rows_q8(T, C, act, dtype, xs[1], us[1], qs[1])
+    _check(_fast.anr_quantize_rows(d, xs[0], us[0], qs[0], _vector("scale", scale, (T,), _f32), None, 0, _stream()), "anr_quantize_rows")
+    return q, scale
+
+
+def _dequantize_rows(q, scale, y):
+    """y = q * scale; q int8 [T,C], scale float32 [T], y [T,C]."""
+    dtype, (T, C) = _dtype(y), _matrix("q", q)
+    qs, ys = _rows("q", q, (T, C), torch.int8), _rows("y", y, (T, C), y.dtype)
+    d = _pack_rows_q8(T, C, ANR_ACT_NONE, dtype, ys[1], 0, qs[1])
+    _check(_fast.anr_dequantize_rows(d, qs[0], _vector("scale", scale, (T,), _f32), ys[0], None, 0, _stream()), "anr_dequantize_rows")
+    return y
+
+
 # The operators as programs call them: the functions above without Python's part in the usual case.
 _OPERATORS = ("gemm", "conv2d", "conv_bn_relu", "conv2d_packed", "conv_bn_relu_packed", "dwconv", "tbg", "tbs", "nrm", "group_norm",
-              "group_norm_backward", "rotary", "gated_ff", "gated_ff_backward", "rms_norm", "rms_norm_backward", "rms_norm_q8")
+              "group_norm_backward", "rotary", "gated_ff", "gated_ff_backward", "rms_norm", "rms_norm_backward", "rms_norm_q8",
+              "quantize_rows", "dequantize_rows")
 for _name in _OPERATORS:
     globals()["_" + _name].__name__ = globals()["_" + _name].__qualname__ = _name      # (what their errors say)
 _native.setup(tuple(globals()["_" + n] for n in _OPERATORS),
@@ -751,6 +782,6 @@ _native.setup(tuple(globals()["_" + n] for n in _OPERATORS),
               ctypes.cast(_fast.anr_conv2d_fast_workspace_size, _vp).value, ctypes.cast(_fast.anr_workspace_size, _vp).value)
 from paper_2006_06762_amd._native import (gemm, conv2d, conv_bn_relu, conv2d_packed, conv_bn_relu_packed, dwconv, tbg, tbs,  # noqa: E402
                                           nrm, group_norm, group_norm_backward, rotary, gated_ff, gated_ff_backward, rms_norm, rms_norm_backward,
-                                          rms_norm_q8)
+                                          rms_norm_q8, quantize_rows, dequantize_rows)
 for _name in _OPERATORS:
     globals()[_name].__module__ = __name__          # (where a pickle of one finds it again, in a process that has not imported torch)

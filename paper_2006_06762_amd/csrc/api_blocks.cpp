@@ -210,6 +210,19 @@ anr_status rms_norm_forward_args(const anr_rms_norm_desc* d, const void* x, cons
     return ANR_OK;
 }
 
+// ---- rows in 8 bits
+
+anr_status check_rows_q8(const anr_rows_q8_desc* d, bool back, anr_rows_q8_desc* out)
+{
+    if (!d) return ANR_ERR_NULL;
+    if (d->T < 0 || d->C < 1 || !valid_type(d->dtype) || !valid_act(d->act) || (back && d->act != ANR_ACT_NONE)) return ANR_ERR_INVALID_ARG;
+    if (d->C > 1 << 20 || d->T >= (int64_t)1 << 31) return ANR_ERR_UNSUPPORTED;
+    *out = *d;
+    int64_t* const ld[3] = {&out->ldx, &out->ldq, &out->ld_up};
+    const int64_t least[3] = {d->C, d->C, d->C};
+    return fill_leading(d->T, back ? 2 : 3, ld, least);
+}
+
 }  // namespace
 
 namespace anr {
@@ -220,6 +233,7 @@ anr_status blocks_workspace_size(int op, const void* desc, size_t* bytes)
     RotaryArgs r{};
     GatedFfArgs ff{};
     RmsNormArgs rn{};
+    RowsQ8Args rq{};
     anr_status st = ANR_ERR_INVALID_ARG;
     switch (op) {
         case ANR_OP_GROUP_NORM:
@@ -241,6 +255,11 @@ anr_status blocks_workspace_size(int op, const void* desc, size_t* bytes)
         case ANR_OP_RMS_NORM_BACKWARD:
             st = check_rms_norm(static_cast<const anr_rms_norm_desc*>(desc), &rn.d);
             if (st == ANR_OK) *bytes = op == ANR_OP_RMS_NORM_BACKWARD ? rms_norm_backward_workspace_bytes(rn) : 0;
+            break;
+        case ANR_OP_QUANTIZE_ROWS:
+        case ANR_OP_DEQUANTIZE_ROWS:
+            st = check_rows_q8(static_cast<const anr_rows_q8_desc*>(desc), op == ANR_OP_DEQUANTIZE_ROWS, &rq.d);
+            if (st == ANR_OK) *bytes = 0;
             break;
         default: break;
     }
@@ -427,6 +446,35 @@ anr_status anr_rms_norm_backward(const anr_rms_norm_desc* d, const void* dy, con
     a.dgamma = dgamma;
     a.ws = ws;
     return anr::launch_result(anr::launch_rms_norm_backward(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+anr_status anr_quantize_rows(const anr_rows_q8_desc* d, const void* x, const void* up, int8_t* q, float* scale, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    (void)ws; (void)ws_bytes;
+    anr::RowsQ8Args a{};
+    const anr_status st = check_rows_q8(d, false, &a.d);
+    if (st != ANR_OK) return st;
+    if (d->T > 0 && (!x || !q || !scale)) return ANR_ERR_NULL;
+    if (!element_aligned(x, d->dtype) || !element_aligned(up, d->dtype) || !element_aligned(scale, ANR_F32) || (q && (q == x || q == up))) return ANR_ERR_INVALID_ARG;
+    a.x = x;
+    a.up = up;
+    a.q = q;
+    a.scale = scale;
+    return anr::launch_result(anr::launch_quantize_rows(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+anr_status anr_dequantize_rows(const anr_rows_q8_desc* d, const int8_t* q, const float* scale, void* y, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    (void)ws; (void)ws_bytes;
+    anr::RowsQ8Args a{};
+    const anr_status st = check_rows_q8(d, true, &a.d);
+    if (st != ANR_OK) return st;
+    if (d->T > 0 && (!q || !scale || !y)) return ANR_ERR_NULL;
+    if (!element_aligned(y, d->dtype) || !element_aligned(scale, ANR_F32) || (y && y == q)) return ANR_ERR_INVALID_ARG;
+    a.x = y;
+    a.q = const_cast<int8_t*>(q);
+    a.scale = const_cast<float*>(scale);
+    return anr::launch_result(anr::launch_dequantize_rows(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

@@ -24,7 +24,7 @@ namespace {
 
 // ---- what binding.py hands over (setup): its functions, the library's entry points
 enum Op { GEMM, CONV2D, CONV_BN_RELU, CONV2D_PACKED, CONV_BN_RELU_PACKED, DWCONV, TBG, TBS, NRM, GROUP_NORM, GROUP_NORM_BACKWARD, ROTARY, GATED_FF, GATED_FF_BACKWARD, RMS_NORM, RMS_NORM_BACKWARD, RMS_NORM_Q8,
-          OPS };
+          QUANTIZE_ROWS, DEQUANTIZE_ROWS, OPS };
 PyObject* g_python[OPS];
 using Call3 = anr_status (*)(const void*, const void*, const void*, void*, void*, size_t, void*);
 using CallBn = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, float, void*, void*, size_t, void*);
@@ -37,6 +37,7 @@ using CallFfBackward = anr_status (*)(const void*, const void*, const void*, con
                                       size_t, void*);
 using CallRmsNorm = anr_status (*)(const void*, const void*, const void*, const void*, float, void*, void*, void*, void*, size_t, void*);
 using CallRmsNormBackward = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, size_t, void*);
+using CallQuantize = anr_status (*)(const void*, const void*, const void*, void*, void*, void*, size_t, void*);
 using CallFastSize = anr_status (*)(const void*, size_t*);
 using CallSize = anr_status (*)(int, const void*, size_t*);
 void* g_entry[OPS];
@@ -651,6 +652,38 @@ bool run_rms_norm_backward(PyObject* const* a)
                                                     data_or_null(dgamma), ws.ptr, ws.bytes, n.t.s.stream);
 }
 
+bool run_quantize_rows(PyObject* const* a)
+{
+    Tensors t;
+    const at::Tensor* const x = plain_memory(a[0]);
+    anr_rows_q8_desc d{};
+    if (!x || x->dim() != 2) return false;
+    const at::ScalarType type = x->scalar_type();
+    d.dtype = type_code(type);
+    if (d.dtype < 0 || (a[3] && !int32(a[3], &d.act))) return false;
+    d.T = x->size(0);
+    d.C = x->size(1);
+    t.matrix(a[0], type, d.T, d.C, &d.ldx);
+    const at::Tensor *q = t.matrix(a[1], at::kChar, d.T, d.C, &d.ldq), *up = t.matrix(a[4], type, d.T, d.C, &d.ld_up), *scale = t.packed(a[2], at::kFloat, {d.T});
+    return t.fine && q && scale && accepted<CallQuantize>(QUANTIZE_ROWS, &d, data(x), data_or_null(up), data(q), data(scale), nullptr, 0, t.s.stream);
+}
+
+bool run_dequantize_rows(PyObject* const* a)
+{
+    Tensors t;
+    const at::Tensor *q = plain_memory(a[0]), *y = plain_memory(a[2]);
+    anr_rows_q8_desc d{};
+    if (!q || !y || q->dim() != 2) return false;
+    d.dtype = type_code(y->scalar_type());
+    if (d.dtype < 0) return false;
+    d.T = q->size(0);
+    d.C = q->size(1);
+    t.matrix(a[0], at::kChar, d.T, d.C, &d.ldq);
+    t.matrix(a[2], y->scalar_type(), d.T, d.C, &d.ldx);
+    const at::Tensor* const scale = t.packed(a[1], at::kFloat, {d.T});
+    return t.fine && scale && accepted<Call3>(DEQUANTIZE_ROWS, &d, data(q), data(scale), data(y), nullptr, 0, t.s.stream);
+}
+
 // Parameters of each operator, the required ones first, and which of them it returns.
 const char* const kGemm[] = {"A", "B", "C"};
 const char* const kConv[] = {"x", "w", "y", "stride", "pad", "ws", "dil", "groups", "route"};
@@ -667,6 +700,8 @@ const char* const kFfBackward[] = {"dy", "x", "w_gate", "w_up", "w_down", "gate"
 const char* const kRmsNorm[] = {"x", "y", "gamma", "eps", "residual", "h", "rstd"};
 const char* const kRmsNormBackward[] = {"dy", "x", "gamma", "rstd", "dx", "dgamma", "dh", "ws"};
 const char* const kRmsNormQ8[] = {"x", "q", "scale", "gamma", "eps", "residual", "h"};
+const char* const kQuantize[] = {"x", "q", "scale", "act", "up"};
+const char* const kDequantize[] = {"q", "scale", "y"};
 
 // The parameters `result` to `last`: one of them itself, more as a tuple.
 PyObject* returned(PyObject* const* a, int result, int last)
@@ -717,6 +752,8 @@ ANR_OPERATOR_OF(py_gated_ff_backward, GATED_FF_BACKWARD, kFfBackward, 7, 7, 10, 
 ANR_OPERATOR(py_rms_norm, RMS_NORM, kRmsNorm, 2, 1, run_rms_norm(a))
 ANR_OPERATOR_OF(py_rms_norm_backward, RMS_NORM_BACKWARD, kRmsNormBackward, 4, 4, 5, run_rms_norm_backward(a))
 ANR_OPERATOR_OF(py_rms_norm_q8, RMS_NORM_Q8, kRmsNormQ8, 3, 1, 2, run_rms_norm_q8(a))
+ANR_OPERATOR_OF(py_quantize_rows, QUANTIZE_ROWS, kQuantize, 3, 1, 2, run_quantize_rows(a))
+ANR_OPERATOR(py_dequantize_rows, DEQUANTIZE_ROWS, kDequantize, 3, 2, run_dequantize_rows(a))
 #undef ANR_OPERATOR
 #undef ANR_OPERATOR_OF
 
@@ -798,6 +835,12 @@ PyMethodDef g_methods[] = {
     {"rms_norm_q8", as_cfunction(py_rms_norm_q8), METH_FASTCALL | METH_KEYWORDS,
      "rms_norm_q8(x, q, scale, gamma=None, eps=1e-06, residual=None, h=None)\n--\n\n"
      "rms_norm with its result in 8 bits: q int8 [T,C], scale float32 [T], y = q * scale."},
+    {"quantize_rows", as_cfunction(py_quantize_rows), METH_FASTCALL | METH_KEYWORDS,
+     "quantize_rows(x, q, scale, act=0, up=None)\n--\n\n"
+     "q int8 [T,C] and scale float32 [T]: rows of act(x) * up (act(x) without up) in 8 bits, whose values are q * scale.  x and up [T,C]; for weights as\n"
+     "[outputs, inputs] a scale for each output."},
+    {"dequantize_rows", as_cfunction(py_dequantize_rows), METH_FASTCALL | METH_KEYWORDS,
+     "dequantize_rows(q, scale, y)\n--\n\ny = q * scale; q int8 [T,C], scale float32 [T], y [T,C]."},
     {"setup", py_setup, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

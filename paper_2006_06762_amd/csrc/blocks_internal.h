@@ -1,5 +1,5 @@
 // Launch interface between the C-ABI layer and the operators of a transformer block (group norm, rotary positions, gated
-// feed-forward, root-mean-square norm).  As in anr_kernels.h: arguments are validated, launchers neither allocate nor synchronise.
+// feed-forward, root-mean-square norm, rows in 8 bits).  As in anr_kernels.h: arguments are validated, launchers neither allocate nor synchronise.
 #pragma once
 #include "anr.h"
 #include "anr_kernels.h"
@@ -57,6 +57,15 @@ size_t rms_norm_backward_workspace_bytes(const RmsNormArgs& a);
 hipError_t launch_rms_norm(const RmsNormArgs& a, hipStream_t stream);
 hipError_t launch_rms_norm_q8(const RmsNormArgs& a, hipStream_t stream);
 hipError_t launch_rms_norm_backward(const RmsNormArgs& a, hipStream_t stream);
+
+struct RowsQ8Args {
+    const void *x, *up;                 // x: y in the way back; up may be null
+    int8_t* q;
+    float* scale;
+    anr_rows_q8_desc d;                 // leading dimensions filled in
+};
+hipError_t launch_quantize_rows(const RowsQ8Args& a, hipStream_t stream);
+hipError_t launch_dequantize_rows(const RowsQ8Args& a, hipStream_t stream);
 
 // The status of a launch, noted for anr_last_hip_error (api.cpp).
 anr_status launch_result(hipError_t e);

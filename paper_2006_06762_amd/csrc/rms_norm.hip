@@ -3,7 +3,7 @@
 
 #include "blocks_internal.h"
 #include "rms_norm_kernel.h"
-#include "rows_plan.h"
+#include "rows_launch.h"
 
 namespace anr {
 namespace {
@@ -14,26 +14,6 @@ using rows::Plan;
 constexpr int kMostGroups = 1 << 20;             // of a launch: rows beyond them are taken in turn
 // Work-groups of a backward pass, each of which leaves a line of sums.
 constexpr int kLines = 512;
-
-template <typename T>
-constexpr int values_of(int64_t C) { return C >= 16 / (int)sizeof(T) ? 16 / (int)sizeof(T) : 1; }
-
-// f(V, U, WHOLE) as constants for rows of C elements T, by a plan.
-template <typename T, typename F>
-hipError_t with_rows(int64_t C, const Plan& p, F f)
-{
-    constexpr int V = 16 / (int)sizeof(T);
-    if (C < V) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::true_type{});
-    auto of = [&](auto u) { return C % V == 0 ? f(std::integral_constant<int, V>{}, u, std::true_type{}) : f(std::integral_constant<int, V>{}, u, std::false_type{}); };
-    switch (p.units) {
-        case 1: return of(std::integral_constant<int, 1>{});
-        case 2: return of(std::integral_constant<int, 2>{});
-        case 4: return of(std::integral_constant<int, 4>{});
-        default:
-            if constexpr (V == 4) return of(std::integral_constant<int, 8>{});
-            else return of(std::integral_constant<int, 4>{});
-    }
-}
 
 template <typename F>
 hipError_t with_types(const RmsNormArgs& a, F f)
@@ -46,11 +26,7 @@ hipError_t with_types(const RmsNormArgs& a, F f)
 }
 
 template <typename T>
-Plan plan(const anr_rms_norm_desc& d)
-{
-    const int V = values_of<T>(d.C);
-    return rows::plan_of((d.C + V - 1) / V, rows::kHeld / V, d.T);
-}
+Plan plan(const anr_rms_norm_desc& d) { return rows::plan_for<T>(d.C, d.T); }
 
 Args arguments(const RmsNormArgs& g)
 {
@@ -65,8 +41,6 @@ Args arguments(const RmsNormArgs& g)
     a.ldy = g.d.ldy;
     return a;
 }
-
-bool whole_units(const void* p, int64_t ld, int es) { return !p || (is_aligned16(p) && ld * es % 16 == 0); }
 
 template <bool QUANTIZED>
 hipError_t launch_forward(const RmsNormArgs& g, hipStream_t stream)
@@ -84,10 +58,10 @@ hipError_t launch_forward(const RmsNormArgs& g, hipStream_t stream)
         using T = decltype(t);
         using P = decltype(p);
         const Plan of = plan<T>(g.d);
-        return with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
+        return rows::with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
             constexpr int V = decltype(v)::value, U = decltype(u)::value;
             constexpr bool WHOLE = decltype(whole)::value;
-            a.streaming = V > 1 && whole_units(a.h, a.ldh, es) && (QUANTIZED || whole_units(a.y, a.ldy, es)) && g.d.C * es % 16 == 0;
+            a.streaming = V > 1 && rows::whole_units(a.h, a.ldh, es) && (QUANTIZED || rows::whole_units(a.y, a.ldy, es)) && g.d.C * es % 16 == 0;
             const int64_t groups = std::min<int64_t>((a.T + of.rows - 1) / of.rows, kMostGroups);
             return launch_kernel(rmsnorm::forward_kernel<T, P, V, U, WHOLE, QUANTIZED, 1024>, dim3((unsigned)groups), dim3(64 * of.waves, of.rows), 0, stream, a);
         });
@@ -126,10 +100,10 @@ hipError_t launch_rms_norm_backward(const RmsNormArgs& g, hipStream_t stream)
             using T = decltype(t);
             using P = decltype(p);
             const Plan of = plan<T>(g.d);
-            return with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
+            return rows::with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
                 constexpr int V = decltype(v)::value, U = decltype(u)::value;
                 constexpr bool WHOLE = decltype(whole)::value;
-                a.streaming = V > 1 && a.h && whole_units(a.h, a.ldh, es) && g.d.C * es % 16 == 0;
+                a.streaming = V > 1 && a.h && rows::whole_units(a.h, a.ldh, es) && g.d.C * es % 16 == 0;
                 return launch_kernel(rmsnorm::backward_kernel<T, P, V, U, WHOLE, 1024>, dim3((unsigned)n), dim3(64 * of.waves, of.rows), (size_t)(of.rows - 1) * g.d.C * sizeof(float),
                                      stream, a);
             });

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(THREADS) void forward_kernel(const Args a)
             }
             if (!WHOLE || unit.in()) of.sum += sum;
         }
-        of = join_row(of, round);
+        of = join_row<true, QUANTIZED>(of, round);
         const float rstd = 1.f / sqrtf(of.sum / (float)C + a.eps);
         if (!in) continue;
         const Steps steps(of.largest, rstd);
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
             if (!WHOLE || unit.in()) along.sum += sum;
         }
         if (!a.h) continue;
-        along = join_row(along, round);
+        along = join_row<true, false>(along, round);
         if (!in) continue;
         const float part = along.sum / (float)C;
         by_streaming(a.streaming, [&](auto streaming) {

@@ -130,17 +130,18 @@ __device__ __forceinline__ void store_steps(int8_t* p, const float (&v)[V], cons
     }
 }
 
-// A sum and a largest magnitude over the waves of a row (blockDim.x threads; a work-group has blockDim.y rows). `round` alternates from call to call, so that one
-// barrier is enough.
+// A sum and a largest magnitude over the waves of a row (blockDim.x threads; a work-group has blockDim.y rows), those of both that are asked for. `round` alternates
+// from call to call, so that one barrier is enough.
 struct Joined {
     float sum;
     uint32_t largest;
 };
+template <bool SUM, bool LARGEST>
 __device__ __forceinline__ Joined join_row(Joined v, int round)
 {
     __shared__ Joined parts[2][kMostWaves];
-    v.sum = wave_sum(v.sum);
-    v.largest = wave_max(v.largest);
+    if (SUM) v.sum = wave_sum(v.sum);
+    if (LARGEST) v.largest = wave_max(v.largest);
     const int waves = blockDim.x >> 6;
     if (waves == 1) return v;
     const int first = threadIdx.y * waves, wave = threadIdx.x >> 6;
@@ -148,8 +149,8 @@ __device__ __forceinline__ Joined join_row(Joined v, int round)
     __syncthreads();
     v = parts[round][first];
     for (int i = 1; i < waves; ++i) {
-        v.sum += parts[round][first + i].sum;
-        v.largest = max(v.largest, parts[round][first + i].largest);
+        if (SUM) v.sum += parts[round][first + i].sum;
+        if (LARGEST) v.largest = max(v.largest, parts[round][first + i].largest);
     }
     return v;
 }

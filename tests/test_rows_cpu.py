@@ -1,4 +1,4 @@
-"""Root-mean-square norm without a GPU: layout of the descriptor, what is refused, what workspaces are asked for, and that no refused call
+"""Root-mean-square norm and rows in 8 bits without a GPU: layout of the descriptors, what is refused, what workspaces are asked for, and that no refused call
 launches anything."""
 import ctypes
 import os
@@ -30,8 +30,8 @@ def layout_of(tmp_path, fields):
     return [int(v) for v in subprocess.run([str(tmp_path / "l")], check=True, capture_output=True, text=True).stdout.split()], want
 
 
-def test_rms_norm_layout_matches_c(tmp_path):
-    got, want = layout_of(tmp_path, {"anr_rms_norm_desc": B.RmsNormDesc})
+def test_layouts_match_c(tmp_path):
+    got, want = layout_of(tmp_path, {"anr_rms_norm_desc": B.RmsNormDesc, "anr_rows_q8_desc": B.RowsQ8Desc})
     assert got == want
 
 
@@ -105,3 +105,45 @@ def test_rms_norm_binding_refuses():
         B.rms_norm_q8(x, x.char(), g[:4], h=x)
     with pytest.raises(TypeError):
         B.rms_norm_backward(x, x, g, g[:4], x, g.half())
+
+
+def rows_desc(**kw):
+    return B.RowsQ8Desc(**dict(dict(T=9, C=40, act=B.ANR_ACT_NONE, dtype=B.ANR_F16), **kw))
+
+
+def quantize(d, x=P, up=None, q=P2, scale=P3):
+    return B.raw().anr_quantize_rows(ctypes.byref(d) if d else None, x, up, q, scale, None, 0, None)
+
+
+def dequantize(d, q=P2, scale=P3, x=P):
+    return B.raw().anr_dequantize_rows(ctypes.byref(d) if d else None, q, scale, x, None, 0, None)
+
+
+def test_rows_q8_refusals():
+    for call in (quantize, dequantize):
+        assert call(None) == NULL
+        for field, bad in (("T", -1), ("C", 0), ("act", 5), ("act", -1), ("dtype", 3), ("ldx", 39), ("ldq", -1)):
+            assert call(rows_desc(**{field: bad})) == INVALID, (call, field, bad)
+        for field, bad in (("C", (1 << 20) + 1), ("T", 1 << 31), ("ldx", 1 << 40), ("ldq", 1 << 60)):
+            assert call(rows_desc(**{field: bad})) == UNSUPPORTED, (call, field, bad)
+        for name in ("x", "q", "scale"):
+            assert call(rows_desc(), **{name: None}) == NULL
+        assert call(rows_desc(), x=ODD) == INVALID and call(rows_desc(), scale=ctypes.c_void_p(0x10002)) == INVALID and call(rows_desc(), x=P2) == INVALID
+        assert call(rows_desc(T=0), **dict.fromkeys(("x", "q", "scale"))) == OK
+    assert quantize(rows_desc(), up=ODD) == INVALID and quantize(rows_desc(), up=P2) == INVALID and quantize(rows_desc(ld_up=39), up=P) == INVALID
+    assert dequantize(rows_desc(act=B.ANR_ACT_SILU)) == INVALID
+    for op in (B.ANR_OP_QUANTIZE_ROWS, B.ANR_OP_DEQUANTIZE_ROWS):
+        assert B.workspace_size(op, rows_desc()) == 0
+        with pytest.raises(B.AnrError):
+            B.workspace_size(op, rows_desc(ldq=39))
+
+
+def test_rows_q8_binding_refuses():
+    x, s = torch.zeros(4, 8), torch.zeros(4)
+    for args in ((x, x.char(), s), (x.char(), x.char(), s), (x, x, s)):
+        with pytest.raises(TypeError):
+            B.quantize_rows(*args)
+    with pytest.raises(ValueError):
+        B.quantize_rows(x[0], x.char(), s)
+    with pytest.raises(TypeError):
+        B.dequantize_rows(x.char(), s, x.double())
