@@ -81,7 +81,7 @@ typedef enum {
     ANR_OP_GROUP_NORM = 7, ANR_OP_GROUP_NORM_BACKWARD = 8, ANR_OP_ROTARY = 9,
     ANR_OP_GATED_FF = 10, ANR_OP_GATED_FF_BACKWARD = 11,
     ANR_OP_RMS_NORM = 12, ANR_OP_RMS_NORM_BACKWARD = 13, ANR_OP_RMS_NORM_Q8 = 14,
-    ANR_OP_QUANTIZE_ROWS = 15, ANR_OP_DEQUANTIZE_ROWS = 16
+    ANR_OP_QUANTIZE_ROWS = 15, ANR_OP_DEQUANTIZE_ROWS = 16, ANR_OP_GEMM_I8 = 17
 } anr_op;
 
 /* Types of the elements of the operators of a transformer block (from group norm on).  The
@@ -465,6 +465,25 @@ anr_status anr_quantize_rows(const anr_rows_q8_desc *desc, const void *x, const 
 /* y = q scale[t]. */
 anr_status anr_dequantize_rows(const anr_rows_q8_desc *desc, const int8_t *q, const float *scale, void *y,
                                void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Product of 8-bit integers with scales: a [M,K] by weights as [outputs, inputs], w [N,K], d [M,N].
+ * Row-major, leading dimensions in elements, 0 for packed.  16-byte aligned a and w whose K and
+ * leading dimensions are multiples of 16 run the faster kernels.  N <= 2^20, K < 2^17, M and
+ * leading dimensions < 2^22.
+ */
+typedef struct {
+    int64_t M, N, K;
+    int32_t dtype;       /* anr_dtype of d */
+    int32_t bias_dtype;  /* anr_dtype of bias: float32 or `dtype` */
+    int64_t lda, ldw, ldd;
+} anr_gemm_i8_desc;
+
+/* d[m][n] = (sum_k a[m][k] w[n][k]) a_scale[m] w_scale[n] + bias[n].  The sum is exact, what follows
+ * is float32, rounded to `dtype` once.  a_scale: M floats, w_scale: N floats, NULL for ones; bias:
+ * N, or NULL. */
+anr_status anr_gemm_i8(const anr_gemm_i8_desc *desc, const int8_t *a, const int8_t *w, const float *a_scale,
+                       const float *w_scale, const void *bias, void *d, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Bytes of device workspace `op` (an anr_op) needs for `desc` (the matching
  * descriptor type): a function of the descriptor only, enough for any pointer

@@ -32,7 +32,7 @@ ANR_OK, ANR_ERR_NULL, ANR_ERR_INVALID_ARG, ANR_ERR_UNSUPPORTED, ANR_ERR_WORKSPAC
 ANR_LAYOUT_NCHW = 0
 ANR_OP_GEMM, ANR_OP_CONV2D, ANR_OP_CONV_BN_RELU, ANR_OP_DWCONV, ANR_OP_TBG, ANR_OP_TBS, ANR_OP_NRM = range(7)
 ANR_OP_GROUP_NORM, ANR_OP_GROUP_NORM_BACKWARD, ANR_OP_ROTARY, ANR_OP_GATED_FF, ANR_OP_GATED_FF_BACKWARD = range(7, 12)
-ANR_OP_RMS_NORM, ANR_OP_RMS_NORM_BACKWARD, ANR_OP_RMS_NORM_Q8, ANR_OP_QUANTIZE_ROWS, ANR_OP_DEQUANTIZE_ROWS = range(12, 17)
+ANR_OP_RMS_NORM, ANR_OP_RMS_NORM_BACKWARD, ANR_OP_RMS_NORM_Q8, ANR_OP_QUANTIZE_ROWS, ANR_OP_DEQUANTIZE_ROWS, ANR_OP_GEMM_I8 = range(12, 18)
 ANR_F32, ANR_F16, ANR_BF16 = range(3)
 ANR_ACT_NONE, ANR_ACT_RELU, ANR_ACT_SILU, ANR_ACT_GELU, ANR_ACT_GELU_TANH = range(5)
 ANR_ROTARY_HALVES, ANR_ROTARY_ADJACENT, ANR_ROTARY_SECTION_HALVES = range(3)
@@ -42,7 +42,7 @@ EXPORTS = ("anr_gemm", "anr_conv2d", "anr_conv2d_noalloc", "anr_conv2d_packed_si
            "anr_conv2d_packed", "anr_conv_bn_relu_packed", "anr_conv_bn_relu", "anr_dwconv", "anr_tbg", "anr_tbs", "anr_nrm",
            "anr_workspace_size", "anr_conv2d_fast_workspace_size", "anr_conv2d_route", "anr_status_string", "anr_version", "anr_last_hip_error",
            "anr_last_hip_error_string", "anr_group_norm", "anr_group_norm_backward", "anr_rotary", "anr_gated_ff", "anr_gated_ff_backward",
-           "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8", "anr_quantize_rows", "anr_dequantize_rows")
+           "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8", "anr_quantize_rows", "anr_dequantize_rows", "anr_gemm_i8")
 
 
 class GemmDesc(ctypes.Structure):
@@ -115,6 +115,11 @@ class RowsQ8Desc(ctypes.Structure):
                 ("ldx", ctypes.c_int64), ("ld_up", ctypes.c_int64), ("ldq", ctypes.c_int64)]
 
 
+class GemmI8Desc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("dtype", ctypes.c_int32), ("bias_dtype", ctypes.c_int32),
+                ("lda", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldd", ctypes.c_int64)]
+
+
 _vp = ctypes.c_void_p
 _lib.anr_gemm.argtypes = [ctypes.POINTER(GemmDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_conv2d.argtypes = [ctypes.POINTER(ConvDesc), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
@@ -140,6 +145,7 @@ _lib.anr_rms_norm_backward.argtypes = [ctypes.POINTER(RmsNormDesc)] + [_vp] * 8 
 _lib.anr_rms_norm_q8.argtypes = [ctypes.POINTER(RmsNormDesc), _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.anr_quantize_rows.argtypes = [ctypes.POINTER(RowsQ8Desc)] + [_vp] * 5 + [ctypes.c_size_t, _vp]
 _lib.anr_dequantize_rows.argtypes = [ctypes.POINTER(RowsQ8Desc)] + [_vp] * 4 + [ctypes.c_size_t, _vp]
+_lib.anr_gemm_i8.argtypes = [ctypes.POINTER(GemmI8Desc)] + [_vp] * 7 + [ctypes.c_size_t, _vp]
 _lib.anr_workspace_size.argtypes = [ctypes.c_int, _vp, ctypes.POINTER(ctypes.c_size_t)]
 _lib.anr_conv2d_fast_workspace_size.argtypes = [ctypes.POINTER(ConvDesc), ctypes.POINTER(ctypes.c_size_t)]
 _lib.anr_conv2d_route.argtypes = [ctypes.POINTER(ConvDesc), ctypes.POINTER(ConvRoute)]
@@ -147,7 +153,7 @@ for _name in ("anr_gemm", "anr_conv2d", "anr_conv2d_noalloc", "anr_conv2d_packed
               "anr_conv2d_packed", "anr_conv_bn_relu_packed", "anr_conv_bn_relu", "anr_dwconv", "anr_tbg", "anr_tbs",
               "anr_workspace_size", "anr_conv2d_fast_workspace_size", "anr_group_norm", "anr_group_norm_backward", "anr_rotary",
               "anr_gated_ff", "anr_gated_ff_backward", "anr_rms_norm", "anr_rms_norm_backward", "anr_rms_norm_q8",
-              "anr_quantize_rows", "anr_dequantize_rows"):
+              "anr_quantize_rows", "anr_dequantize_rows", "anr_gemm_i8"):
     getattr(_lib, _name).restype = ctypes.c_int
 _lib.anr_status_string.argtypes = [ctypes.c_int]
 _lib.anr_status_string.restype = ctypes.c_char_p
@@ -213,6 +219,7 @@ _fast.anr_rms_norm_backward.argtypes = [_vp] * 9 + [_sz, _vp]
 _fast.anr_rms_norm_q8.argtypes = [_vp] * 4 + [_fl] + [_vp] * 4 + [_sz, _vp]
 _fast.anr_quantize_rows.argtypes = [_vp] * 6 + [_sz, _vp]
 _fast.anr_dequantize_rows.argtypes = [_vp] * 5 + [_sz, _vp]
+_fast.anr_gemm_i8.argtypes = [_vp] * 8 + [_sz, _vp]
 
 _pack_gemm = struct.Struct("@10q").pack
 _pack_conv = struct.Struct("@14i8q2i").pack
@@ -223,8 +230,9 @@ _pack_rotary = struct.Struct("@15i15q").pack
 _pack_gated_ff = struct.Struct("@3q2i8q").pack
 _pack_rms_norm = struct.Struct("@2q2i4q").pack
 _pack_rows_q8 = struct.Struct("@2q2i3q").pack
-assert [struct.calcsize(f) for f in ("@10q", "@14i8q2i", "@4i12q", "@5q", "@8i9q", "@15i15q", "@3q2i8q", "@2q2i4q", "@2q2i3q")] == \
-    [ctypes.sizeof(t) for t in (GemmDesc, ConvDesc, TbgDesc, NrmDesc, GroupNormDesc, RotaryDesc, GatedFfDesc, RmsNormDesc, RowsQ8Desc)]
+_pack_gemm_i8 = struct.Struct("@3q2i3q").pack
+assert [struct.calcsize(f) for f in ("@10q", "@14i8q2i", "@4i12q", "@5q", "@8i9q", "@15i15q", "@3q2i8q", "@2q2i4q", "@2q2i3q", "@3q2i3q")] == \
+    [ctypes.sizeof(t) for t in (GemmDesc, ConvDesc, TbgDesc, NrmDesc, GroupNormDesc, RotaryDesc, GatedFfDesc, RmsNormDesc, RowsQ8Desc, GemmI8Desc)]
 _NO_STRIDES = (0, 0, 0, 0)
 _f32 = torch.float32
 
@@ -771,10 +779,24 @@ def _dequantize_rows(q, scale, y):
     return y
 
 
+def _gemm_i8(a, w, a_scale, w_scale, d, bias=None, ws=None):
+    """d = (a.w^T) * a_scale[:, None] * w_scale + bias; a int8 [M,K], w int8 [N,K], d [M,N] float32, float16 or bfloat16; a_scale float32 [M] and
+    w_scale float32 [N], or None for ones; bias [N] of float32 or d's type."""
+    dtype, (M, K), N = _dtype(d), _matrix("a", a), _matrix("w", w)[0]
+    if bias is not None and (not isinstance(bias, torch.Tensor) or bias.dtype not in (torch.float32, d.dtype)):
+        raise TypeError("bias must be of float32 or of d's type")
+    kind = torch.float32 if bias is None else bias.dtype
+    xs, wt, ds = _rows("a", a, (M, K), torch.int8), _rows("w", w, (N, K), torch.int8), _rows("d", d, (M, N), d.dtype)
+    desc = _pack_gemm_i8(M, N, K, dtype, _DTYPES[kind], xs[1], wt[1], ds[1])
+    args = (xs[0], wt[0], _vector("a_scale", a_scale, (M,), _f32), _vector("w_scale", w_scale, (N,), _f32), _vector("bias", bias, (N,), kind), ds[0])
+    _with_workspace(_fast.anr_gemm_i8, "anr_gemm_i8", ANR_OP_GEMM_I8, desc, args, ws, GemmI8Desc)
+    return d
+
+
 # The operators as programs call them: the functions above without Python's part in the usual case.
 _OPERATORS = ("gemm", "conv2d", "conv_bn_relu", "conv2d_packed", "conv_bn_relu_packed", "dwconv", "tbg", "tbs", "nrm", "group_norm",
               "group_norm_backward", "rotary", "gated_ff", "gated_ff_backward", "rms_norm", "rms_norm_backward", "rms_norm_q8",
-              "quantize_rows", "dequantize_rows")
+              "quantize_rows", "dequantize_rows", "gemm_i8")
 for _name in _OPERATORS:
     globals()["_" + _name].__name__ = globals()["_" + _name].__qualname__ = _name      # (what their errors say)
 _native.setup(tuple(globals()["_" + n] for n in _OPERATORS),
@@ -782,6 +804,6 @@ _native.setup(tuple(globals()["_" + n] for n in _OPERATORS),
               ctypes.cast(_fast.anr_conv2d_fast_workspace_size, _vp).value, ctypes.cast(_fast.anr_workspace_size, _vp).value)
 from paper_2006_06762_amd._native import (gemm, conv2d, conv_bn_relu, conv2d_packed, conv_bn_relu_packed, dwconv, tbg, tbs,  # noqa: E402
                                           nrm, group_norm, group_norm_backward, rotary, gated_ff, gated_ff_backward, rms_norm, rms_norm_backward,
-                                          rms_norm_q8, quantize_rows, dequantize_rows)
+                                          rms_norm_q8, quantize_rows, dequantize_rows, gemm_i8)
 for _name in _OPERATORS:
     globals()[_name].__module__ = __name__          # (where a pickle of one finds it again, in a process that has not imported torch)

@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libanr.so")
 NATIVE = os.path.join(HERE, "_native.so")       # the binding's extension module (csrc/binding_native.cpp)
 
 SOURCES = ["api.cpp", "gemm.hip", "tbg.hip", "conv_direct.hip", "conv_igemm.hip", "conv_gather.hip", "conv_pieces.hip", "conv_pointwise.hip", "conv_stem.hip", "dwconv.hip", "nrm.hip", "static_scratch.hip",
-           "api_blocks.cpp", "group_norm.hip", "rotary.hip", "gated_ff.hip", "mm16_f16.hip", "mm16_bf16.hip", "rms_norm.hip", "rows_q8.hip"]
+           "api_blocks.cpp", "group_norm.hip", "rotary.hip", "gated_ff.hip", "mm16_f16.hip", "mm16_bf16.hip", "rms_norm.hip", "rows_q8.hip", "gemm_i8.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",

@@ -223,6 +223,25 @@ anr_status check_rows_q8(const anr_rows_q8_desc* d, bool back, anr_rows_q8_desc*
     return fill_leading(d->T, back ? 2 : 3, ld, least);
 }
 
+// ---- products of 8-bit integers
+
+anr_status check_gemm_i8(const anr_gemm_i8_desc* d, anr_gemm_i8_desc* out)
+{
+    if (!d) return ANR_ERR_NULL;
+    if (d->M < 0 || d->N < 1 || d->K < 1 || !valid_type(d->dtype) || (d->bias_dtype != ANR_F32 && d->bias_dtype != d->dtype)) return ANR_ERR_INVALID_ARG;
+    // sums in 32 bits, and the kernels' 32-bit offsets inside a tile
+    if (d->K >= 1 << 17 || d->N > 1 << 20 || d->M >= 1 << 22) return ANR_ERR_UNSUPPORTED;
+    *out = *d;
+    const int64_t rows[3] = {d->M, d->N, d->M}, least[3] = {d->K, d->K, d->N};
+    int64_t* const ld[3] = {&out->lda, &out->ldw, &out->ldd};
+    for (int i = 0; i < 3; ++i) {
+        const anr_status st = fill_leading(rows[i], 1, &ld[i], &least[i]);
+        if (st != ANR_OK) return st;
+        if (*ld[i] >= 1 << 22) return ANR_ERR_UNSUPPORTED;
+    }
+    return ANR_OK;
+}
+
 }  // namespace
 
 namespace anr {
@@ -234,6 +253,7 @@ anr_status blocks_workspace_size(int op, const void* desc, size_t* bytes)
     GatedFfArgs ff{};
     RmsNormArgs rn{};
     RowsQ8Args rq{};
+    GemmI8Args gi{};
     anr_status st = ANR_ERR_INVALID_ARG;
     switch (op) {
         case ANR_OP_GROUP_NORM:
@@ -260,6 +280,10 @@ anr_status blocks_workspace_size(int op, const void* desc, size_t* bytes)
         case ANR_OP_DEQUANTIZE_ROWS:
             st = check_rows_q8(static_cast<const anr_rows_q8_desc*>(desc), op == ANR_OP_DEQUANTIZE_ROWS, &rq.d);
             if (st == ANR_OK) *bytes = 0;
+            break;
+        case ANR_OP_GEMM_I8:
+            st = check_gemm_i8(static_cast<const anr_gemm_i8_desc*>(desc), &gi.d);
+            if (st == ANR_OK) *bytes = gemm_i8_workspace_bytes(gi);
             break;
         default: break;
     }
@@ -475,6 +499,28 @@ anr_status anr_dequantize_rows(const anr_rows_q8_desc* d, const int8_t* q, const
     a.q = const_cast<int8_t*>(q);
     a.scale = const_cast<float*>(scale);
     return anr::launch_result(anr::launch_dequantize_rows(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+anr_status anr_gemm_i8(const anr_gemm_i8_desc* d, const int8_t* a, const int8_t* w, const float* a_scale, const float* w_scale, const void* bias, void* out, void* ws,
+                       size_t ws_bytes, void* hip_stream)
+{
+    anr::GemmI8Args g{};
+    anr_status st = check_gemm_i8(d, &g.d);
+    if (st != ANR_OK) return st;
+    if (d->M > 0 && (!a || !w || !out)) return ANR_ERR_NULL;
+    if (!element_aligned(out, d->dtype) || !element_aligned(a_scale, ANR_F32) || !element_aligned(w_scale, ANR_F32) || !element_aligned(bias, d->bias_dtype) ||
+        (out && (out == a || out == w || out == a_scale || out == w_scale || out == bias)))
+        return ANR_ERR_INVALID_ARG;
+    st = check_workspace(ws, ws_bytes, anr::gemm_i8_workspace_bytes(g));
+    if (st != ANR_OK) return st;
+    g.a = a;
+    g.w = w;
+    g.a_scale = a_scale;
+    g.w_scale = w_scale;
+    g.bias = bias;
+    g.out = out;
+    g.ws = ws;
+    return anr::launch_result(anr::launch_gemm_i8(g, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

@@ -24,7 +24,7 @@ namespace {
 
 // ---- what binding.py hands over (setup): its functions, the library's entry points
 enum Op { GEMM, CONV2D, CONV_BN_RELU, CONV2D_PACKED, CONV_BN_RELU_PACKED, DWCONV, TBG, TBS, NRM, GROUP_NORM, GROUP_NORM_BACKWARD, ROTARY, GATED_FF, GATED_FF_BACKWARD, RMS_NORM, RMS_NORM_BACKWARD, RMS_NORM_Q8,
-          QUANTIZE_ROWS, DEQUANTIZE_ROWS, OPS };
+          QUANTIZE_ROWS, DEQUANTIZE_ROWS, GEMM_I8, OPS };
 PyObject* g_python[OPS];
 using Call3 = anr_status (*)(const void*, const void*, const void*, void*, void*, size_t, void*);
 using CallBn = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, float, void*, void*, size_t, void*);
@@ -38,6 +38,7 @@ using CallFfBackward = anr_status (*)(const void*, const void*, const void*, con
 using CallRmsNorm = anr_status (*)(const void*, const void*, const void*, const void*, float, void*, void*, void*, void*, size_t, void*);
 using CallRmsNormBackward = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, size_t, void*);
 using CallQuantize = anr_status (*)(const void*, const void*, const void*, void*, void*, void*, size_t, void*);
+using CallGemmI8 = anr_status (*)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, size_t, void*);
 using CallFastSize = anr_status (*)(const void*, size_t*);
 using CallSize = anr_status (*)(int, const void*, size_t*);
 void* g_entry[OPS];
@@ -684,6 +685,31 @@ bool run_dequantize_rows(PyObject* const* a)
     return t.fine && scale && accepted<Call3>(DEQUANTIZE_ROWS, &d, data(q), data(scale), data(y), nullptr, 0, t.s.stream);
 }
 
+bool run_gemm_i8(PyObject* const* a)
+{
+    Tensors t;
+    const at::Tensor *x = plain_memory(a[0]), *w = plain_memory(a[1]), *out = plain_memory(a[4]), *bias = absent(a[5]) ? nullptr : plain_memory(a[5]);
+    anr_gemm_i8_desc d{};
+    if (!x || !w || !out || x->dim() != 2 || w->dim() != 2 || (a[6] && a[6] != Py_None) || (!absent(a[5]) && !bias)) return false;
+    const at::ScalarType type = out->scalar_type(), kind = bias ? bias->scalar_type() : at::kFloat;
+    d.dtype = type_code(type);
+    d.bias_dtype = type_code(kind);
+    if (d.dtype < 0 || (kind != at::kFloat && kind != type)) return false;
+    d.M = x->size(0);
+    d.K = x->size(1);
+    d.N = w->size(0);
+    t.matrix(a[0], at::kChar, d.M, d.K, &d.lda);
+    t.matrix(a[1], at::kChar, d.N, d.K, &d.ldw);
+    t.matrix(a[4], type, d.M, d.N, &d.ldd);
+    const at::Tensor *xs = t.packed(a[2], at::kFloat, {d.M}), *ws_ = t.packed(a[3], at::kFloat, {d.N});
+    if (bias) t.packed(a[5], kind, {d.N});
+    if (!t.fine) return false;
+    size_t need = 0;
+    if (g_size(ANR_OP_GEMM_I8, &d, &need) != ANR_OK) return false;
+    const Workspace ws(need, t.s);
+    return ws.here && accepted<CallGemmI8>(GEMM_I8, &d, data(x), data(w), data_or_null(xs), data_or_null(ws_), data_or_null(bias), data(out), ws.ptr, ws.bytes, t.s.stream);
+}
+
 // Parameters of each operator, the required ones first, and which of them it returns.
 const char* const kGemm[] = {"A", "B", "C"};
 const char* const kConv[] = {"x", "w", "y", "stride", "pad", "ws", "dil", "groups", "route"};
@@ -702,6 +728,7 @@ const char* const kRmsNormBackward[] = {"dy", "x", "gamma", "rstd", "dx", "dgamm
 const char* const kRmsNormQ8[] = {"x", "q", "scale", "gamma", "eps", "residual", "h"};
 const char* const kQuantize[] = {"x", "q", "scale", "act", "up"};
 const char* const kDequantize[] = {"q", "scale", "y"};
+const char* const kGemmI8[] = {"a", "w", "a_scale", "w_scale", "d", "bias", "ws"};
 
 // The parameters `result` to `last`: one of them itself, more as a tuple.
 PyObject* returned(PyObject* const* a, int result, int last)
@@ -754,6 +781,7 @@ ANR_OPERATOR_OF(py_rms_norm_backward, RMS_NORM_BACKWARD, kRmsNormBackward, 4, 4,
 ANR_OPERATOR_OF(py_rms_norm_q8, RMS_NORM_Q8, kRmsNormQ8, 3, 1, 2, run_rms_norm_q8(a))
 ANR_OPERATOR_OF(py_quantize_rows, QUANTIZE_ROWS, kQuantize, 3, 1, 2, run_quantize_rows(a))
 ANR_OPERATOR(py_dequantize_rows, DEQUANTIZE_ROWS, kDequantize, 3, 2, run_dequantize_rows(a))
+ANR_OPERATOR(py_gemm_i8, GEMM_I8, kGemmI8, 5, 4, run_gemm_i8(a))
 #undef ANR_OPERATOR
 #undef ANR_OPERATOR_OF
 
@@ -841,6 +869,10 @@ PyMethodDef g_methods[] = {
      "[outputs, inputs] a scale for each output."},
     {"dequantize_rows", as_cfunction(py_dequantize_rows), METH_FASTCALL | METH_KEYWORDS,
      "dequantize_rows(q, scale, y)\n--\n\ny = q * scale; q int8 [T,C], scale float32 [T], y [T,C]."},
+    {"gemm_i8", as_cfunction(py_gemm_i8), METH_FASTCALL | METH_KEYWORDS,
+     "gemm_i8(a, w, a_scale, w_scale, d, bias=None, ws=None)\n--\n\n"
+     "d = (a.w^T) * a_scale[:, None] * w_scale + bias; a int8 [M,K], w int8 [N,K], d [M,N] float32, float16 or bfloat16; a_scale float32 [M] and\n"
+     "w_scale float32 [N], or None for ones; bias [N] of float32 or d's type."},
     {"setup", py_setup, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

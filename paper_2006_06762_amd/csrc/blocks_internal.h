@@ -1,5 +1,5 @@
 // Launch interface between the C-ABI layer and the operators of a transformer block (group norm, rotary positions, gated
-// feed-forward, root-mean-square norm, rows in 8 bits).  As in anr_kernels.h: arguments are validated, launchers neither allocate nor synchronise.
+// feed-forward, root-mean-square norm, rows in 8 bits and their products).  As in anr_kernels.h: arguments are validated, launchers neither allocate nor synchronise.
 #pragma once
 #include "anr.h"
 #include "anr_kernels.h"
@@ -66,6 +66,17 @@ struct RowsQ8Args {
 };
 hipError_t launch_quantize_rows(const RowsQ8Args& a, hipStream_t stream);
 hipError_t launch_dequantize_rows(const RowsQ8Args& a, hipStream_t stream);
+
+struct GemmI8Args {
+    const int8_t *a, *w;
+    const float *a_scale, *w_scale;     // null: ones
+    const void* bias;                   // may be null
+    void* out;
+    anr_gemm_i8_desc d;                 // leading dimensions filled in
+    void* ws;
+};
+size_t gemm_i8_workspace_bytes(const GemmI8Args& a);
+hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t stream);
 
 // The status of a launch, noted for anr_last_hip_error (api.cpp).
 anr_status launch_result(hipError_t e);

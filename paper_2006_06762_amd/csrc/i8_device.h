@@ -1,0 +1,64 @@
+// What the kernels of products of 8-bit integers share: D[m][n] = (sum_k X[m][k] W[n][k]) x_scale[m] w_scale[n] + bias[n], both operands rows of k.
+// The sums are exact (32 bits hold k < 2^17 products of magnitudes up to 128); a result takes the rounding of the sum to 24 bits, two of the scales, one of
+// the bias and that to its type.
+#pragma once
+#include "anr_kernels.h"
+#include "element_types.h"
+
+namespace anr {
+namespace i8 {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int BK = 128;                         // k of a chunk: a line of a row
+constexpr int kUnit = 16;                       // k of a lane's operand
+constexpr uint32_t kNowhere = 0x80000000u;      // byte offset past every descriptor's extent: loads zeros
+constexpr int kExtent = 0x7fffffff;
+
+// Scales and bias, each of which may be absent.
+struct Finish {
+    const float *x_scale, *w_scale;
+    const void* bias;
+    int bias_dtype;
+    __device__ __forceinline__ float of_row(int64_t m) const { return x_scale ? x_scale[m] : 1.f; }
+    __device__ __forceinline__ float of_column(int64_t n) const { return w_scale ? w_scale[n] : 1.f; }
+    __device__ __forceinline__ float added(int64_t n) const { return bias ? load_any(bias, n, bias_dtype) : 0.f; }
+    // (a sum with zero leaves everything but the sign of zero as it is)
+    static __device__ __forceinline__ float value(int sum, float row, float column, float added) { return (float)sum * row * column + added; }
+};
+
+struct Args {
+    const int8_t *x, *w;
+    void* d;
+    int64_t ldx, ldw, ldd;
+    int M, N, K;
+    Finish finish;
+    int tiles_m, tiles_n;
+    int band;                       // tiles are walked in bands of so many rows of tiles
+    int splits;                     // work-groups that share a tile's k: their sums go to `parts`, [split][M][N] packed
+    int* parts;
+};
+
+// Sixteen values of k of a row, from k on; those past K are cleared by `clear` where they were read.  Not WHOLE (pointers, leading dimensions and K are any): the
+// row's last unit starts so far ahead that it ends with the row (K >= 16), and the values that it shares with the unit before are cleared in one of the operands,
+// X: other values of k in their place, in both operands alike.
+__device__ __forceinline__ int loose_start(int k, int K) { return min(k, K - kUnit); }
+__device__ __forceinline__ u32x4 load_loose(const int8_t* p)
+{
+    struct __attribute__((packed, aligned(1))) Loose { u32x4 v; };
+    return reinterpret_cast<const Loose*>(p)->v;
+}
+__device__ __forceinline__ void clear_counted(u32x4& v, int k, int K)
+{
+    const int counted = min(k - loose_start(k, K), kUnit);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int bytes = min(max(counted - 4 * i, 0), 4);
+        v[i] &= bytes == 4 ? 0u : 0xffffffffu << (8 * bytes);
+    }
+}
+
+}  // namespace i8
+}  // namespace anr

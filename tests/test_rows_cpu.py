@@ -1,4 +1,4 @@
-"""Root-mean-square norm and rows in 8 bits without a GPU: layout of the descriptors, what is refused, what workspaces are asked for, and that no refused call
+"""Root-mean-square norm, rows in 8 bits and their products without a GPU: layout of the descriptors, what is refused, what workspaces are asked for, and that no refused call
 launches anything."""
 import ctypes
 import os
@@ -31,7 +31,7 @@ def layout_of(tmp_path, fields):
 
 
 def test_layouts_match_c(tmp_path):
-    got, want = layout_of(tmp_path, {"anr_rms_norm_desc": B.RmsNormDesc, "anr_rows_q8_desc": B.RowsQ8Desc})
+    got, want = layout_of(tmp_path, {"anr_rms_norm_desc": B.RmsNormDesc, "anr_rows_q8_desc": B.RowsQ8Desc, "anr_gemm_i8_desc": B.GemmI8Desc})
     assert got == want
 
 
@@ -147,3 +147,44 @@ def test_rows_q8_binding_refuses():
         B.quantize_rows(x[0], x.char(), s)
     with pytest.raises(TypeError):
         B.dequantize_rows(x.char(), s, x.double())
+
+
+def product_desc(**kw):
+    return B.GemmI8Desc(**dict(dict(M=9, N=50, K=64, dtype=B.ANR_BF16, bias_dtype=B.ANR_F32), **kw))
+
+
+def product(d, a=P, w=P2, a_scale=None, w_scale=None, bias=None, out=P3, ws=None, size=0):
+    return B.raw().anr_gemm_i8(ctypes.byref(d) if d else None, a, w, a_scale, w_scale, bias, out, ws, size, None)
+
+
+def test_gemm_i8_refusals():
+    assert product(None) == NULL
+    for field, bad in (("M", -1), ("N", 0), ("K", 0), ("dtype", 3), ("bias_dtype", B.ANR_F16), ("lda", 63), ("ldw", 63), ("ldd", 49), ("lda", -64)):
+        assert product(product_desc(**{field: bad})) == INVALID, (field, bad)
+    for field, bad in (("M", 1 << 22), ("N", (1 << 20) + 1), ("K", 1 << 17), ("lda", 1 << 22), ("ldw", 1 << 22), ("ldd", 1 << 22)):
+        assert product(product_desc(**{field: bad})) == UNSUPPORTED, (field, bad)
+    for name in ("a", "w", "out"):
+        assert product(product_desc(), **{name: None}) == NULL
+    off = ctypes.c_void_p(0x40002)
+    for name in ("a_scale", "w_scale", "bias"):
+        assert product(product_desc(), **{name: off}) == INVALID
+    assert product(product_desc(), out=ODD) == INVALID
+    for name in ("a", "w", "a_scale", "w_scale", "bias"):
+        assert product(product_desc(), **{name: P3}) == INVALID              # the result over an input
+    assert product(product_desc(M=0), None, None, out=None) == OK
+    assert B.workspace_size(B.ANR_OP_GEMM_I8, product_desc(M=0)) == 0 and B.workspace_size(B.ANR_OP_GEMM_I8, product_desc()) == 0
+    d = product_desc(M=200, N=300, K=20000)
+    need = B.workspace_size(B.ANR_OP_GEMM_I8, d)
+    assert need > 0 and need % 4 == 0
+    assert product(d) == WORKSPACE and product(d, ws=P, size=need - 1) == WORKSPACE and product(d, ws=ctypes.c_void_p(0x10008), size=need) == INVALID
+    # the leading dimensions of a single row say nothing
+    assert B.workspace_size(B.ANR_OP_GEMM_I8, product_desc(M=1, lda=1, ldd=1 << 40)) == 0
+
+
+def test_gemm_i8_binding_refuses():
+    a, d, s = torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4, 4), torch.zeros(4)
+    for args in ((a, a, s, s, d), (a.float(), a, s, s, d), (a, a, s, s, d.double()), (a, a, s, s, d, s.half()), (a, a, s, s, a)):
+        with pytest.raises(TypeError):
+            B.gemm_i8(*args)
+    with pytest.raises(ValueError):
+        B.gemm_i8(a[0], a, s, s, d)
