@@ -73,7 +73,7 @@ hipError_t launch_rows_as(const Args& a, hipStream_t stream)
 {
     static LdsLimit limit;
     // waves of a work-group: eight for each CU over all work-groups, as far as there are chunks for them
-    const int groups = (a.N + 15) / 16, chunks = (a.K + i8::BK - 1) / i8::BK;
+    const int groups = (a.N + 15) / 16, chunks = (a.K + i8::kRowsChunk - 1) / i8::kRowsChunk;
     int waves = 2;
     while (waves < 16 && groups * waves < 2048 && 2 * waves <= chunks) waves *= 2;
     const size_t lds = (size_t)waves * TB * 256 * sizeof(int);
@@ -90,75 +90,88 @@ hipError_t launch_rows(const Args& a, bool whole, hipStream_t stream)
 
 // ---- tiles
 
-enum Shape { SHAPE_256, SHAPE_128, SHAPE_128_TWICE };
-int64_t tiles_of(int64_t M, int64_t N, int edge) { return ((M + edge - 1) / edge) * ((N + edge - 1) / edge); }
-int64_t chunks_of(int64_t K) { return (K + i8::BK - 1) / i8::BK; }
+constexpr int64_t kChunk = 128;                  // k of a chunk
+constexpr int kCus = 256;
 
-// The tile with the shortest estimated time: rounds of work-groups over the CUs, each with its chunks and ends (us). A tile of 256 takes a CU
-// for itself, of those of 128 it takes two; one alone is split over two groups of waves.
-struct Choice {
-    Shape shape;
-    double us;
+// A tile, how many of its work-groups a CU takes at a time, and its estimated time in us: a chunk's where a work-group is alone on its CU and where that is full, and that
+// of both ends.
+struct Shape {
+    int m, n, on_cu;
+    double alone, full, ends;
 };
-Choice choose_shape(int64_t tiles256, int64_t tiles128, int64_t chunks)
+enum { TILE_256, TILE_128, TILE_64_128, TILE_64, TILES };
+constexpr Shape kShapes[TILES] = {{256, 256, 1, 1.5, 1.5, 7.0}, {128, 128, 2, 0.42, 1.1, 4.0}, {64, 128, 2, 0.25, 0.66, 4.0}, {64, 64, 4, 0.19, 0.75, 3.4}};
+
+int64_t tiles_of(int64_t M, int64_t N, const Shape& s) { return ((M + s.m - 1) / s.m) * ((N + s.n - 1) / s.n); }
+
+double estimate(const Shape& s, int64_t tiles, int64_t chunks)
 {
-    const double large = (double)((tiles256 + 255) / 256) * (1.7 * (double)chunks + 4.0);
-    const int64_t full = tiles128 / 512, rest = tiles128 % 512;
-    const double pair = 1.14 * (double)chunks + 4.0, alone = 0.60 * (double)chunks + 4.0;
-    const bool twice = tiles128 <= 256;
-    const double small = twice ? alone : (double)full * pair + (rest > 256 ? pair : rest > 0 ? 0.75 * (double)chunks + 4.0 : 0.0);
-    if (large < small) return {SHAPE_256, large};
-    return {twice ? SHAPE_128_TWICE : SHAPE_128, small};
+    const int64_t at_once = (int64_t)s.on_cu * kCus, rounds = tiles / at_once, rest = tiles % at_once, beside = (rest + kCus - 1) / kCus;
+    double us = (double)rounds * (s.full * (double)chunks + s.ends);
+    if (rest > 0) us += (s.on_cu > 1 ? s.alone + (s.full - s.alone) * (double)(beside - 1) / (double)(s.on_cu - 1) : s.full) * (double)chunks + s.ends;
+    return us;
 }
 
-// Work-groups that share a tile's k, for products with few tiles: the number with the shortest estimated time, that of the launch that joins their
-// sums among it. A function of the extents alone.
-int splits_of(int64_t M, int64_t N, int64_t chunks)
+// The tile, and the work-groups that share a tile's k where there are few, with the shortest estimated time, that of the launch that joins their sums among it.  A function of the
+// extents alone.
+struct Choice {
+    int tile, splits;
+};
+Choice choose(int64_t M, int64_t N, int64_t K)
 {
-    int best = 1;
-    double least = choose_shape(tiles_of(M, N, 256), tiles_of(M, N, 128), chunks).us;
-    for (int s = 2; s <= 16 && chunks / s >= 4; ++s) {
-        const double us = choose_shape(s * tiles_of(M, N, 256), s * tiles_of(M, N, 128), (chunks + s - 1) / s).us + 4.0 + 2.0 * s * (double)M * (double)N * 4.0 / 8e6;
-        if (us < least) {
-            least = us;
-            best = s;
+    const int64_t chunks = (K + kChunk - 1) / kChunk;
+    Choice best{TILE_256, 1};
+    double least = 1e30;
+    for (int t = 0; t < TILES; ++t)
+        for (int s = 1; s <= 16 && (s == 1 || chunks / s >= 4); ++s) {
+            const double us = estimate(kShapes[t], s * tiles_of(M, N, kShapes[t]), (chunks + s - 1) / s) + (s > 1 ? 3.0 + 2.0 * s * (double)M * (double)N * 4.0 / 8e6 : 0.0);
+            if (us < least) {
+                least = us;
+                best = {t, s};
+            }
         }
-    }
     return best;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, int G, bool WHOLE>
-hipError_t launch_tile(Args a, hipStream_t stream)
+template <typename T, bool WHOLE, int M, int N, int WM, int WN, int STAGES>
+hipError_t launch_as(Args a, hipStream_t stream)
 {
     static LdsLimit limit;
-    auto* const kernel = i8::tile_kernel<T, BM, BN, WM, WN, G, WHOLE>;
-    constexpr size_t lds = G * i8::lds_bytes<BM, BN>();
+    void (*kernel)(Args);
+    if constexpr (WHOLE) kernel = i8::tile_kernel<T, M, N, WM, WN, kChunk, STAGES>;
+    else kernel = i8::loose_kernel<T, M, N, WM, WN>;
+    constexpr size_t lds = (size_t)(WHOLE ? STAGES : 2) * (M + N) * kChunk;
     const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit);
     if (e != hipSuccess) return e;
-    a.tiles_m = (a.M + BM - 1) / BM;
-    a.tiles_n = (a.N + BN - 1) / BN;
+    a.tiles_m = (a.M + M - 1) / M;
+    a.tiles_n = (a.N + N - 1) / N;
     a.band = 8;
-    return launch_kernel(kernel, dim3((unsigned)(a.tiles_m * a.tiles_n * a.splits)), dim3(64 * WM * WN * G), lds, stream, a);
+    constexpr int LINE = 128 / (int)sizeof(T);
+    a.streaming = N / WN % LINE == 0 && a.ldd % LINE == 0 && reinterpret_cast<uintptr_t>(a.d) % 128 == 0;
+    return launch_kernel(kernel, dim3((unsigned)(a.tiles_m * a.tiles_n * a.splits)), dim3(64 * WM * WN), lds, stream, a);
 }
-template <typename T>
-hipError_t launch_shape(Shape shape, bool whole, const Args& a, hipStream_t stream)
+template <typename T, bool WHOLE>
+hipError_t launch_tile(int tile, const Args& a, hipStream_t stream)
 {
-    if (shape == SHAPE_256) return whole ? launch_tile<T, 256, 256, 2, 2, 1, true>(a, stream) : launch_tile<T, 256, 256, 2, 2, 1, false>(a, stream);
-    if (shape == SHAPE_128) return whole ? launch_tile<T, 128, 128, 2, 2, 1, true>(a, stream) : launch_tile<T, 128, 128, 2, 2, 1, false>(a, stream);
-    return whole ? launch_tile<T, 128, 128, 2, 2, 2, true>(a, stream) : launch_tile<T, 128, 128, 2, 2, 2, false>(a, stream);
+    switch (tile) {
+        case TILE_256: return launch_as<T, WHOLE, 256, 256, 2, 4, 2>(a, stream);
+        case TILE_128: return launch_as<T, WHOLE, 128, 128, 2, 2, 2>(a, stream);
+        case TILE_64_128: return launch_as<T, WHOLE, 64, 128, 2, 2, 3>(a, stream);
+        default: return launch_as<T, WHOLE, 64, 64, 2, 2, 2>(a, stream);
+    }
 }
 
-int splits(const anr_gemm_i8_desc& d)
+Choice choice_of(const anr_gemm_i8_desc& d)
 {
-    if (d.M == 0 || d.K < i8::kUnit || few_rows(d.M)) return 1;
-    return splits_of(d.M, d.N, chunks_of(d.K));
+    if (d.M == 0 || d.K < i8::kUnit || few_rows(d.M)) return {TILE_64, 1};
+    return choose(d.M, d.N, d.K);
 }
 
 }  // namespace
 
 size_t gemm_i8_workspace_bytes(const GemmI8Args& g)
 {
-    const int s = splits(g.d);
+    const int s = choice_of(g.d).splits;
     return s > 1 ? (size_t)s * g.d.M * g.d.N * sizeof(int) : 0;
 }
 
@@ -177,10 +190,10 @@ hipError_t launch_gemm_i8(const GemmI8Args& g, hipStream_t stream)
     a.N = (int)d.N;
     a.K = (int)d.K;
     a.finish = {g.a_scale, g.w_scale, g.bias, d.bias_dtype};
-    a.splits = splits(d);
+    const Choice choice = choice_of(d);
+    a.splits = choice.splits;
     a.parts = static_cast<int*>(g.ws);
     const bool whole = is_aligned16(g.a) && is_aligned16(g.w) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.K % 16 == 0;
-    const int64_t chunks = chunks_of(d.K);
     return with_type(d.dtype, [&](auto t) {
         using T = decltype(t);
         if (d.K < i8::kUnit) {
@@ -188,9 +201,8 @@ hipError_t launch_gemm_i8(const GemmI8Args& g, hipStream_t stream)
             return launch_kernel(short_kernel<T>, dim3((unsigned)columns, (unsigned)std::min<int64_t>({d.M, 65535, (1 << 23) / columns})), dim3(kThreads), 0, stream, a);
         }
         if (few_rows(d.M)) return launch_rows<T>(a, whole, stream);
-        const Shape shape = choose_shape(a.splits * tiles_of(d.M, d.N, 256), a.splits * tiles_of(d.M, d.N, 128), chunks / a.splits).shape;
-        if (a.splits == 1) return launch_shape<T>(shape, whole, a, stream);
-        const hipError_t e = launch_shape<int>(shape, whole, a, stream);
+        if (a.splits == 1) return whole ? launch_tile<T, true>(choice.tile, a, stream) : launch_tile<T, false>(choice.tile, a, stream);
+        const hipError_t e = whole ? launch_tile<int, true>(choice.tile, a, stream) : launch_tile<int, false>(choice.tile, a, stream);
         return e != hipSuccess ? e : launch_join<T>(a, stream);
     });
 }

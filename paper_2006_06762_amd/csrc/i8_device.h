@@ -12,7 +12,6 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int BK = 128;                         // k of a chunk: a line of a row
 constexpr int kUnit = 16;                       // k of a lane's operand
 constexpr uint32_t kNowhere = 0x80000000u;      // byte offset past every descriptor's extent: loads zeros
 constexpr int kExtent = 0x7fffffff;
@@ -39,6 +38,7 @@ struct Args {
     int band;                       // tiles are walked in bands of so many rows of tiles
     int splits;                     // work-groups that share a tile's k: their sums go to `parts`, [split][M][N] packed
     int* parts;
+    bool streaming;                 // D's stores go past L2: a wave's part of a row is whole lines of 128 bytes
 };
 
 // Sixteen values of k of a row, from k on; those past K are cleared by `clear` where they were read.  Not WHOLE (pointers, leading dimensions and K are any): the

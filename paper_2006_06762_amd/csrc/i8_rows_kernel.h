@@ -9,6 +9,8 @@
 namespace anr {
 namespace i8 {
 
+constexpr int kRowsChunk = 128;                 // k of a wave at a time: a line of a row
+
 // Sixteen values of k of a row that starts `row` bytes behind the base.
 template <bool WHOLE, bool CLEAR>
 __device__ __forceinline__ i32x4 load_unit(const int8_t* base, uint32_t row, int k, int K)
@@ -39,14 +41,14 @@ __global__ __launch_bounds__(1024) void rows_kernel(const Args a)
     i32x4 acc[TB];
 #pragma unroll
     for (int t = 0; t < TB; ++t) acc[t] = i32x4{0, 0, 0, 0};
-    const int chunks = (a.K + BK - 1) / BK;
+    const int chunks = (a.K + kRowsChunk - 1) / kRowsChunk;
     for (int c = wave; c < chunks; c += waves * U) {
         i32x4 w[U][2], x[U][TB][2];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int k = (c + u * waves) * BK + (4 * i + g) * kUnit;
+                const int k = (c + u * waves) * kRowsChunk + (4 * i + g) * kUnit;
                 w[u][i] = load_unit<WHOLE, false>(w0, wrow, k, a.K);
 #pragma unroll
                 for (int t = 0; t < TB; ++t) x[u][t][i] = load_unit<WHOLE, true>(a.x, xrow[t], k, a.K);
