@@ -68,24 +68,30 @@ hipError_t launch_join(const Args& a, hipStream_t stream)
 
 constexpr bool few_rows(int64_t M) { return M <= 32; }
 
-template <typename T, int TB, bool WHOLE>
-hipError_t launch_rows_as(const Args& a, hipStream_t stream)
+// Waves of a work-group: as far as there are chunks for them, eight for each CU over all work-groups, or long rows. us, 4 / 8 / 16 waves: 1 token 2048 -> 11264
+// 6.2 / 7.1 / 9.6, 5632 -> 2048 4.9 / 4.1 / 4.6, 1024 -> 1024 2.85 / 2.91 / 3.4, 16384 -> 16384 56.4 / 52.1 / 53.3, 16 tokens 4096 -> 4096 6.1 / 6.2 / 5.4.
+int waves_of(const Args& a, int most)
 {
+    const int64_t groups = (a.N + 15) / 16, chunks = (a.K + i8::kRowsChunk - 1) / i8::kRowsChunk;
+    int waves = 4;
+    while (waves < most && chunks >= 4 * waves && (groups * waves <= 2048 || chunks >= 16 * waves)) waves *= 2;
+    return waves;
+}
+template <typename T, int TB>
+hipError_t launch_rows_as(const Args& a, bool whole, hipStream_t stream)
+{
+    constexpr int STAGES = 2;
     static LdsLimit limit;
-    // waves of a work-group: eight for each CU over all work-groups, as far as there are chunks for them
-    const int groups = (a.N + 15) / 16, chunks = (a.K + i8::kRowsChunk - 1) / i8::kRowsChunk;
-    int waves = 2;
-    while (waves < 16 && groups * waves < 2048 && 2 * waves <= chunks) waves *= 2;
-    const size_t lds = (size_t)waves * TB * 256 * sizeof(int);
-    auto* const kernel = i8::rows_kernel<T, TB, WHOLE>;
+    const int waves = waves_of(a, 16 / TB);
+    void (*const kernel)(Args) = whole ? i8::stream_kernel<T, TB, STAGES> : i8::rows_kernel<T, TB, 4 / TB>;
+    const size_t sums = (size_t)waves * TB * 256 * sizeof(int), lds = whole ? std::max(sums, (size_t)waves * STAGES * 16 * (1 + TB) * i8::kRowsChunk) : sums;
     const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit) : hipSuccess;
-    return e != hipSuccess ? e : launch_kernel(kernel, dim3(groups), dim3(64 * waves), lds, stream, a);
+    return e != hipSuccess ? e : launch_kernel(kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * waves), lds, stream, a);
 }
 template <typename T>
 hipError_t launch_rows(const Args& a, bool whole, hipStream_t stream)
 {
-    if (a.M <= 16) return whole ? launch_rows_as<T, 1, true>(a, stream) : launch_rows_as<T, 1, false>(a, stream);
-    return whole ? launch_rows_as<T, 2, true>(a, stream) : launch_rows_as<T, 2, false>(a, stream);
+    return a.M <= 16 ? launch_rows_as<T, 1>(a, whole, stream) : launch_rows_as<T, 2>(a, whole, stream);
 }
 
 // ---- tiles

@@ -60,5 +60,35 @@ __device__ __forceinline__ void clear_counted(u32x4& v, int k, int K)
     }
 }
 
+// The unit of a row in LDS that holds the row's unit u.
+template <int BK>
+__device__ __forceinline__ int place_of(int row, int u) { return BK == 128 ? u ^ ((row >> 1) & 7) : u ^ ((row >> 2) & 3); }
+
+// Sixteen bytes a lane from memory to LDS, in the order of the lanes from `lds` on: lane l's from byte offset + step of the descriptor's extent.  The lanes'
+// registers are read when the instruction is issued and none is written; s_waitcnt vmcnt and a barrier come before LDS is read.  In asm, because the
+// compiler has every LDS read that follows such a load wait for all of them.
+__device__ __forceinline__ void load_to_lds(i32x4 descriptor, uint32_t offset, int step, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor), "s"(step) : "m0");
+}
+// A scalar register that the vector unit wrote is read by a memory instruction five cycles later at the earliest, which the compiler sees to for its own instructions only: what
+// load_to_lds takes comes from here, and what is made of it stays in the scalar unit.
+template <typename V>
+__device__ __forceinline__ V settled(V v)
+{
+    asm volatile("s_nop 4" : "+s"(v));
+    return v;
+}
+template <int OUTSTANDING>
+__device__ __forceinline__ void wait_for_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(OUTSTANDING) : "memory");
+}
+__device__ __forceinline__ i32x4 descriptor_of(const void* p)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    return settled(i32x4{__builtin_amdgcn_readfirstlane((int)at), __builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xffff), kExtent, 0x00020000});
+}
+
 }  // namespace i8
 }  // namespace anr

@@ -15,10 +15,6 @@
 namespace anr {
 namespace i8 {
 
-// The unit of a row in LDS that holds the row's unit u.
-template <int BK>
-__device__ __forceinline__ int place_of(int row, int u) { return BK == 128 ? u ^ ((row >> 1) & 7) : u ^ ((row >> 2) & 3); }
-
 // The units of a chunk in three parts.
 constexpr int part_of(int units, int part) { return (units * part + 2) / 3; }
 
@@ -324,32 +320,6 @@ __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void loose_kernel
         __builtin_amdgcn_sched_barrier(0);
     }
     finish_tile<T, WM, WN, 2 * (size_t)BUF>(args, at, w, lds, tid);
-}
-
-// Sixteen bytes a lane from memory to LDS, in the order of the lanes from `lds` on: lane l's from byte offset + step of the descriptor's extent.  The lanes'
-// registers are read when the instruction is issued and none is written; s_waitcnt vmcnt and a barrier come before LDS is read.  In asm, because the
-// compiler has every LDS read that follows such a load wait for all of them.
-__device__ __forceinline__ void load_to_lds(i32x4 descriptor, uint32_t offset, int step, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor), "s"(step) : "m0");
-}
-// A scalar register that the vector unit wrote is read by a memory instruction five cycles later at the earliest, which the compiler sees to for its own instructions only: what
-// load_to_lds takes comes from here, and what is made of it stays in the scalar unit.
-template <typename V>
-__device__ __forceinline__ V settled(V v)
-{
-    asm volatile("s_nop 4" : "+s"(v));
-    return v;
-}
-template <int OUTSTANDING>
-__device__ __forceinline__ void wait_for_loads()
-{
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(OUTSTANDING) : "memory");
-}
-__device__ __forceinline__ i32x4 descriptor_of(const void* p)
-{
-    const uint64_t at = reinterpret_cast<uint64_t>(p);
-    return settled(i32x4{__builtin_amdgcn_readfirstlane((int)at), __builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xffff), kExtent, 0x00020000});
 }
 
 // Rows R of one operand as the WAVES waves of a group load them to LDS: a load is 1 KB, whole rows of BK bytes.
