@@ -66,8 +66,6 @@ hipError_t launch_join(const Args& a, hipStream_t stream)
 
 // ---- few rows
 
-constexpr bool few_rows(int64_t M) { return M <= 32; }
-
 // Waves of a work-group: as far as there are chunks for them, eight for each CU over all work-groups, or long rows. us, 4 / 8 / 16 waves: 1 token 2048 -> 11264
 // 6.2 / 7.1 / 9.6, 5632 -> 2048 4.9 / 4.1 / 4.6, 1024 -> 1024 2.85 / 2.91 / 3.4, 16384 -> 16384 56.4 / 52.1 / 53.3, 16 tokens 4096 -> 4096 6.1 / 6.2 / 5.4.
 int waves_of(const Args& a, int most)
@@ -82,8 +80,10 @@ hipError_t launch_rows_as(const Args& a, bool whole, hipStream_t stream)
 {
     constexpr int STAGES = 2;
     static LdsLimit limit;
-    const int waves = waves_of(a, 16 / TB);
-    void (*const kernel)(Args) = whole ? i8::stream_kernel<T, TB, STAGES> : i8::rows_kernel<T, TB, 4 / TB>;
+    const int waves = waves_of(a, TB == 1 ? 16 : TB == 2 ? 8 : 4);
+    void (*kernel)(Args) = i8::stream_kernel<T, TB, STAGES>;
+    if constexpr (TB <= 2)
+        if (!whole) kernel = i8::rows_kernel<T, TB, 4 / TB>;
     const size_t sums = (size_t)waves * TB * 256 * sizeof(int), lds = whole ? std::max(sums, (size_t)waves * STAGES * 16 * (1 + TB) * i8::kRowsChunk) : sums;
     const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit) : hipSuccess;
     return e != hipSuccess ? e : launch_kernel(kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * waves), lds, stream, a);
@@ -91,7 +91,9 @@ hipError_t launch_rows_as(const Args& a, bool whole, hipStream_t stream)
 template <typename T>
 hipError_t launch_rows(const Args& a, bool whole, hipStream_t stream)
 {
-    return a.M <= 16 ? launch_rows_as<T, 1>(a, whole, stream) : launch_rows_as<T, 2>(a, whole, stream);
+    if (a.M <= 16) return launch_rows_as<T, 1>(a, whole, stream);
+    if (a.M <= 32) return launch_rows_as<T, 2>(a, whole, stream);
+    return a.M <= 48 ? launch_rows_as<T, 3>(a, true, stream) : launch_rows_as<T, 4>(a, true, stream);
 }
 
 // ---- tiles
@@ -105,8 +107,8 @@ struct Shape {
     int m, n, on_cu;
     double alone, full, ends;
 };
-enum { TILE_256, TILE_128, TILE_64_128, TILE_64, TILES };
-constexpr Shape kShapes[TILES] = {{256, 256, 1, 1.5, 1.5, 7.0}, {128, 128, 2, 0.42, 1.1, 4.0}, {64, 128, 2, 0.25, 0.66, 4.0}, {64, 64, 4, 0.19, 0.75, 3.4}};
+enum { TILE_256, TILE_128, TILE_64_128, TILE_64, TILES, ROWS = TILES };
+constexpr Shape kShapes[TILES] = {{256, 256, 1, 1.02, 1.02, 6.2}, {128, 128, 2, 0.58, 0.78, 2.8}, {64, 128, 2, 0.22, 0.52, 3.8}, {64, 64, 4, 0.30, 0.67, 2.5}};
 
 int64_t tiles_of(int64_t M, int64_t N, const Shape& s) { return ((M + s.m - 1) / s.m) * ((N + s.n - 1) / s.n); }
 
@@ -118,24 +120,32 @@ double estimate(const Shape& s, int64_t tiles, int64_t chunks)
     return us;
 }
 
-// The tile, and the work-groups that share a tile's k where there are few, with the shortest estimated time, that of the launch that joins their sums among it.  A function of the
-// extents alone.
+// The tile, or the kernels for few rows, and the work-groups that share a tile's k where there are few, with the shortest estimated time, that of the launch that joins their
+// sums among it.  Up to 32 rows go to the kernels for few, up to 64 where these are estimated to be faster.  A function of the extents alone.  The estimates' numbers
+// are fitted to 110 products of 33 to 2048 rows, 512 -> 512 to 11264 -> 4096, each by every tile and 1 to 8 parts of k: what is chosen took 2 % longer than the fastest on
+// average.
 struct Choice {
     int tile, splits;
 };
-Choice choose(int64_t M, int64_t N, int64_t K)
+constexpr int64_t kFewRows = 32, kMostRows = 64;
+Choice choose(int64_t M, int64_t N, int64_t K, bool rows = true, int most_splits = 16)
 {
+    if (rows && M <= kFewRows) return {ROWS, 1};
     const int64_t chunks = (K + kChunk - 1) / kChunk;
     Choice best{TILE_256, 1};
     double least = 1e30;
     for (int t = 0; t < TILES; ++t)
-        for (int s = 1; s <= 16 && (s == 1 || chunks / s >= 4); ++s) {
-            const double us = estimate(kShapes[t], s * tiles_of(M, N, kShapes[t]), (chunks + s - 1) / s) + (s > 1 ? 3.0 + 2.0 * s * (double)M * (double)N * 4.0 / 8e6 : 0.0);
+        for (int s = 1; s <= most_splits && (s == 1 || chunks / s >= 4); ++s) {
+            const double us = estimate(kShapes[t], s * tiles_of(M, N, kShapes[t]), (chunks + s - 1) / s) + (s > 1 ? 2.9 + 2.0 * s * (double)M * (double)N * 4.0 / 4.3e6 : 0.0);
             if (us < least) {
                 least = us;
                 best = {t, s};
             }
         }
+    if (rows && M <= kMostRows) {                // reading W, and X for every sixteen of W's rows
+        const double x_bytes = (double)((N + 15) / 16) * (double)((M + 15) / 16 * 16) * (double)K;
+        if (4.0 + (double)N * (double)K / 5.3e6 + x_bytes / 36e6 < least) return {ROWS, 1};
+    }
     return best;
 }
 
@@ -169,7 +179,7 @@ hipError_t launch_tile(int tile, const Args& a, hipStream_t stream)
 
 Choice choice_of(const anr_gemm_i8_desc& d)
 {
-    if (d.M == 0 || d.K < i8::kUnit || few_rows(d.M)) return {TILE_64, 1};
+    if (d.M == 0 || d.K < i8::kUnit) return {ROWS, 1};
     return choose(d.M, d.N, d.K);
 }
 
@@ -196,7 +206,7 @@ hipError_t launch_gemm_i8(const GemmI8Args& g, hipStream_t stream)
     a.N = (int)d.N;
     a.K = (int)d.K;
     a.finish = {g.a_scale, g.w_scale, g.bias, d.bias_dtype};
-    const Choice choice = choice_of(d);
+    Choice choice = choice_of(d);
     a.splits = choice.splits;
     a.parts = static_cast<int*>(g.ws);
     const bool whole = is_aligned16(g.a) && is_aligned16(g.w) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.K % 16 == 0;
@@ -206,7 +216,8 @@ hipError_t launch_gemm_i8(const GemmI8Args& g, hipStream_t stream)
             const int64_t columns = (d.N + kThreads - 1) / kThreads;     // (a grid has fewer than 2^32 threads)
             return launch_kernel(short_kernel<T>, dim3((unsigned)columns, (unsigned)std::min<int64_t>({d.M, 65535, (1 << 23) / columns})), dim3(kThreads), 0, stream, a);
         }
-        if (few_rows(d.M)) return launch_rows<T>(a, whole, stream);
+        if (choice.tile == ROWS && !whole && d.M > kFewRows) choice = choose(d.M, d.N, d.K, false, 1);
+        if (choice.tile == ROWS) return launch_rows<T>(a, whole, stream);
         if (a.splits == 1) return whole ? launch_tile<T, true>(choice.tile, a, stream) : launch_tile<T, false>(choice.tile, a, stream);
         const hipError_t e = whole ? launch_tile<int, true>(choice.tile, a, stream) : launch_tile<int, false>(choice.tile, a, stream);
         return e != hipSuccess ? e : launch_join<T>(a, stream);
