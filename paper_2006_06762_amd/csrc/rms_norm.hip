@@ -12,8 +12,6 @@ using rmsnorm::Args;
 using rows::Plan;
 
 constexpr int kMostGroups = 1 << 20;             // of a launch: rows beyond them are taken in turn
-// Work-groups of a backward pass, each of which leaves a line of sums.
-constexpr int kLines = 512;
 
 template <typename F>
 hipError_t with_types(const RmsNormArgs& a, F f)
@@ -63,20 +61,14 @@ hipError_t launch_forward(const RmsNormArgs& g, hipStream_t stream)
             constexpr bool WHOLE = decltype(whole)::value;
             a.streaming = V > 1 && rows::whole_units(a.h, a.ldh, es) && (QUANTIZED || rows::whole_units(a.y, a.ldy, es)) && g.d.C * es % 16 == 0;
             const int64_t groups = std::min<int64_t>((a.T + of.rows - 1) / of.rows, kMostGroups);
-            return launch_kernel(rmsnorm::forward_kernel<T, P, V, U, WHOLE, QUANTIZED, 1024>, dim3((unsigned)groups), dim3(64 * of.waves, of.rows), 0, stream, a);
+            return launch_kernel(rmsnorm::forward_kernel<T, P, V, U, WHOLE, QUANTIZED, 1024>, dim3((unsigned)groups), dim3(of.threads, of.rows), 0, stream, a);
         });
     });
 }
 
-template <typename T>
-int lines_of(const anr_rms_norm_desc& d)
+int64_t lines(const anr_rms_norm_desc& d)
 {
-    const Plan of = plan<T>(d);
-    return (int)std::min<int64_t>((d.T + of.rows - 1) / of.rows, kLines);
-}
-int lines(const anr_rms_norm_desc& d)
-{
-    return with_type(d.dtype, [&](auto t) { return lines_of<decltype(t)>(d); });
+    return with_type(d.dtype, [&](auto t) { return rows::backward_plan_for<decltype(t)>(d.C, d.T).lines; });
 }
 
 }  // namespace
@@ -94,17 +86,17 @@ hipError_t launch_rms_norm_backward(const RmsNormArgs& g, hipStream_t stream)
     a.h = g.h;
     a.rstd_in = g.rstd;
     a.sums = g.dgamma ? static_cast<float*>(g.ws) : nullptr;
-    const int es = element_bytes(g.d.dtype), n = g.d.T == 0 ? 0 : lines(g.d);
+    const int es = element_bytes(g.d.dtype), n = g.d.T == 0 ? 0 : (int)lines(g.d);
     if (n > 0) {
         const hipError_t e = with_types(g, [&](auto t, auto p) {
             using T = decltype(t);
             using P = decltype(p);
-            const Plan of = plan<T>(g.d);
+            const Plan of = rows::backward_plan_for<T>(g.d.C, g.d.T).rows;
             return rows::with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
                 constexpr int V = decltype(v)::value, U = decltype(u)::value;
                 constexpr bool WHOLE = decltype(whole)::value;
                 a.streaming = V > 1 && a.h && rows::whole_units(a.h, a.ldh, es) && g.d.C * es % 16 == 0;
-                return launch_kernel(rmsnorm::backward_kernel<T, P, V, U, WHOLE, 1024>, dim3((unsigned)n), dim3(64 * of.waves, of.rows), (size_t)(of.rows - 1) * g.d.C * sizeof(float),
+                return launch_kernel(rmsnorm::backward_kernel<T, P, V, U, WHOLE, 1024>, dim3((unsigned)n), dim3(of.threads, of.rows), of.rows > 1 ? (size_t)of.rows * g.d.C * sizeof(float) : 0,
                                      stream, a);
             });
         });

@@ -13,7 +13,7 @@
 namespace anr {
 namespace rows {
 
-constexpr int kMostWaves = 16;                   // of a row
+constexpr int kMostWaves = 16;                   // of a work-group
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -43,6 +43,12 @@ struct Raw {
         for (int i = 0; i < V; ++i) a[i] = v;
         w[0] = 0;
         __builtin_memcpy(w, a, sizeof a);
+    }
+    // What is converted before and after this is converted twice: between, only the values as they lie in memory take registers.
+    __device__ __forceinline__ void keep_packed()
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) asm("" : "+v"(w[i]));
     }
     __device__ __forceinline__ void floats(float (&out)[V]) const
     {
@@ -130,8 +136,8 @@ __device__ __forceinline__ void store_steps(int8_t* p, const float (&v)[V], cons
     }
 }
 
-// A sum and a largest magnitude over the waves of a row (blockDim.x threads; a work-group has blockDim.y rows), those of both that are asked for. `round` alternates
-// from call to call, so that one barrier is enough.
+// A sum and a largest magnitude over the threads of a row (blockDim.x: whole waves, or 8, 16 or 32 lanes of one; a work-group has blockDim.y rows), those of both that are
+// asked for. `round` alternates from call to call, so that one barrier is enough.
 struct Joined {
     float sum;
     uint32_t largest;
@@ -140,6 +146,11 @@ template <bool SUM, bool LARGEST>
 __device__ __forceinline__ Joined join_row(Joined v, int round)
 {
     __shared__ Joined parts[2][kMostWaves];
+    if (blockDim.x < 64) {
+        if (SUM) v.sum = lanes_join(v.sum, blockDim.x, [](float a, float b) { return a + b; });
+        if (LARGEST) v.largest = lanes_join(v.largest, blockDim.x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+        return v;
+    }
     if (SUM) v.sum = wave_sum(v.sum);
     if (LARGEST) v.largest = wave_max(v.largest);
     const int waves = blockDim.x >> 6;

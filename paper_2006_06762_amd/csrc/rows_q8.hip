@@ -154,7 +154,7 @@ hipError_t launch_quantize_rows(const RowsQ8Args& g, hipStream_t stream)
         const Plan of = plan_for<T>(a.C, a.T);
         return with_rows<T>(a.C, of, [&](auto v, auto u, auto whole) {
             const int64_t groups = std::min<int64_t>((a.T + of.rows - 1) / of.rows, kMostGroups);
-            return launch_kernel(quantize_kernel<T, decltype(v)::value, decltype(u)::value, decltype(whole)::value>, dim3((unsigned)groups), dim3(64 * of.waves, of.rows), 0, stream,
+            return launch_kernel(quantize_kernel<T, decltype(v)::value, decltype(u)::value, decltype(whole)::value>, dim3((unsigned)groups), dim3(of.threads, of.rows), 0, stream,
                                  a);
         });
     });

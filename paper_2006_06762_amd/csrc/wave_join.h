@@ -32,6 +32,18 @@ __device__ __forceinline__ T wave_join(T v, Join join)
     return __builtin_bit_cast(T, all);
 }
 
+// The same over each run of 8, 16 or 32 lanes.
+template <typename T, typename Join>
+__device__ __forceinline__ T lanes_join(T v, int lanes, Join join)
+{
+    v = join(v, of_lane<0xb1, 0xf>(v));
+    v = join(v, of_lane<0x4e, 0xf>(v));
+    v = join(v, of_lane<0x141, 0xf>(v));
+    if (lanes > 8) v = join(v, of_lane<0x140, 0xf>(v));
+    if (lanes > 16) v = join(v, __shfl_xor(v, 16));
+    return v;
+}
+
 template <typename T>
 __device__ __forceinline__ T wave_sum(T v)
 {
