@@ -49,7 +49,7 @@ __global__ __launch_bounds__(THREADS) void forward_kernel(const Args a)
     }
     int round = 0;
     for (int64_t first = (int64_t)blockIdx.x * blockDim.y; first < a.T; first += (int64_t)gridDim.x * blockDim.y, round ^= 1) {
-        const int64_t row = first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1;      // (rows past the end repeat the last one and store nothing)
+        const int64_t row = row_of<(U > 2)>(first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1);      // (rows past the end repeat the last one and store nothing)
         const bool in = first + threadIdx.y < a.T;
         Raw<T, V> x[U], r[U];
 #pragma unroll
@@ -115,7 +115,11 @@ template <typename T, int V, int U, bool WHOLE>
 struct Row {
     rows::Raw<T, V> x[U], dy[U], dh[U];
     float rstd;
-    __device__ __forceinline__ void load(const Args& a, int64_t row)
+    __device__ __forceinline__ void load_dh(const Args& a, int64_t row, int u)
+    {
+        dh[u].load(static_cast<const T*>(a.dh) + row * a.ld_residual + rows::Unit<V, WHOLE>((int)(threadIdx.x + u * blockDim.x), a.C).start);
+    }
+    __device__ __forceinline__ void load(const Args& a, int64_t row, bool with_dh)
     {
         const int threads = blockDim.x, t = threadIdx.x, C = a.C;
 #pragma unroll
@@ -124,9 +128,9 @@ struct Row {
             dy[u].load(static_cast<const T*>(a.dy) + row * a.ldy + start);
             x[u].load(static_cast<const T*>(a.x) + row * a.ldx + start);
         }
-        if (a.dh) {
+        if (with_dh && a.dh) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) dh[u].load(static_cast<const T*>(a.dh) + row * a.ld_residual + rows::Unit<V, WHOLE>(t + u * threads, C).start);
+            for (int u = 0; u < U; ++u) load_dh(a, row, u);
         }
         rstd = a.rstd_in[row];
     }
@@ -140,29 +144,32 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
     using namespace rows;
     extern __shared__ float shared[];            // sums of the rows of a work-group that has several, [rows][C]
     const int threads = blockDim.x, t = threadIdx.x, C = a.C;
+    constexpr bool FEW = U * V <= 8;             // values of a thread: more, and gamma and dh are read where they are used
     Raw<P, V> g[U];
     float sums[U][V];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
+    auto load_gamma = [&](int u) {
         if (a.gamma) g[u].load(static_cast<const P*>(a.gamma) + Unit<V, WHOLE>(t + u * threads, C).start);
         else g[u].fill(from_float<P>(1.f));
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (FEW) load_gamma(u);
 #pragma unroll
         for (int j = 0; j < V; ++j) sums[u][j] = 0.f;
     }
     int round = 0;
     const int64_t step = (int64_t)gridDim.x * blockDim.y, begin = (int64_t)blockIdx.x * blockDim.y;
     auto at = [&](int64_t first) { return first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1; };      // (rows past the end repeat the last one and store nothing)
-    constexpr bool AHEAD = U * V <= 8;
     Row<T, V, U, WHOLE> r, next;
-    if (AHEAD && begin < a.T) next.load(a, at(begin));
+    if (FEW && begin < a.T) next.load(a, rows::row_of<(U > 1)>(at(begin)), true);
     for (int64_t first = begin; first < a.T; first += step, round ^= 1) {
-        const int64_t row = at(first);
+        const int64_t row = rows::row_of<(U > 1)>(at(first));
         const bool in = first + threadIdx.y < a.T;
-        if (AHEAD) {
+        if (FEW) {
             r = next;
-            if (first + step < a.T) next.load(a, at(first + step));
+            if (first + step < a.T) next.load(a, rows::row_of<(U > 1)>(at(first + step)), true);
         } else {
-            r.load(a, row);
+            r.load(a, row, false);
         }
         const float rstd = r.rstd;
         Joined along{0.f, 0u};                   // sum of dhat x
@@ -172,6 +179,7 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
             float xv[V], dv[V], gamma[V], sum = 0.f;
             r.x[u].floats(xv);
             r.dy[u].floats(dv);
+            if (!FEW) load_gamma(u);
             g[u].floats(gamma);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -180,7 +188,7 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
                 if (in) sums[u][j] = fmaf(dv[j], hat, sums[u][j]);
             }
             if (!WHOLE || unit.in()) along.sum += sum;
-            unit_done<U * V>();
+            unit_done<2 * U * V>();
         }
         if (!a.h) continue;
         along = join_row<true, false>(along, round);
@@ -190,7 +198,7 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
         for (int u = 0; u < U; ++u) {
             r.x[u].keep_packed();
             r.dy[u].keep_packed();
-            g[u].keep_packed();
+            if (FEW) g[u].keep_packed();
         }
         by_streaming(a.streaming, [&](auto streaming) {
             constexpr bool S = decltype(streaming)::value;
@@ -201,15 +209,24 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
                 float xv[V], dv[V], gamma[V], extra[V];
                 r.x[u].floats(xv);
                 r.dy[u].floats(dv);
+                if (!FEW) load_gamma(u);
                 g[u].floats(gamma);
+                if (!FEW && a.dh) r.load_dh(a, row, u);
                 if (a.dh) r.dh[u].floats(extra);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     dv[j] = rstd * fmaf(-xv[j] * rstd, part, dv[j] * gamma[j]);
                     if (a.dh) dv[j] += extra[j];
                 }
-                store<S>(static_cast<T*>(a.h) + row * a.ldh + unit.start, dv);
-                unit_done<U * V>();
+                T* const to = static_cast<T*>(a.h) + row * a.ldh + unit.start;
+                if (FEW || WHOLE) {
+                    store<S>(to, dv);
+                } else {                                             // (what another unit has too may be that one's result already, where dx is dh)
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (unit.counts(j)) to[j] = from_float<T>(dv[j]);
+                }
+                unit_done<2 * U * V>();
             }
         });
     }

@@ -94,6 +94,10 @@ struct Unit {
     __device__ __forceinline__ bool counts(int j) const { return WHOLE ? counted == 0 : j >= counted; }
 };
 
+// A row's number (below 2^31), in a scalar register where whole waves have it, so that its addresses are not in as many vector registers.
+template <bool WAVES>
+__device__ __forceinline__ int64_t row_of(int64_t row) { return WAVES ? (int64_t)__builtin_amdgcn_readfirstlane((int)row) : row; }
+
 // The bits of |v|, whose order as whole numbers is that of the magnitudes, infinity and NaN above all others.
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
 constexpr uint32_t kInfinite = 0x7f800000u;

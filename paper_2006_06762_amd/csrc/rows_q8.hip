@@ -42,7 +42,7 @@ __global__ __launch_bounds__(1024) void quantize_kernel(const Args a)
     const int threads = blockDim.x, t = threadIdx.x, C = a.C;
     int round = 0;
     for (int64_t first = (int64_t)blockIdx.x * blockDim.y; first < a.T; first += (int64_t)gridDim.x * blockDim.y, round ^= 1) {
-        const int64_t row = first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1;      // (rows past the end repeat the last one and store nothing)
+        const int64_t row = row_of<(U > 2)>(first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1);      // (rows past the end repeat the last one and store nothing)
         const bool in = first + threadIdx.y < a.T;
         Raw<T, V> x[U], up[U];
 #pragma unroll
