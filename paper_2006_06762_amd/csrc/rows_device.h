@@ -106,35 +106,38 @@ constexpr uint32_t kInfinite = 0x7f800000u;
 // step NaN and the values zeros, so that whatever is made of the row is NaN.  Rows that lie low in float32's range are raised before they are
 // divided by their step, whose inverse would leave it at the other end.
 struct Steps {
-    float raise, inverse;
+    float inverse;
+    bool raised;
     float step;                     // of rows whose values are multiplied by `factor` afterwards
     __device__ __forceinline__ Steps(uint32_t largest, float factor)
     {
         const float most = __builtin_bit_cast(float, largest);
         const bool fine = largest < kInfinite;
-        raise = most < 0x1p-60f ? 0x1p64f : 1.f;
-        inverse = fine && largest != 0 ? 127.f / (most * raise) : 0.f;
+        raised = most < 0x1p-60f;
+        inverse = fine && largest != 0 ? 127.f / (raised ? most * 0x1p64f : most) : 0.f;
         step = fine ? most * factor / 127.f : __builtin_nanf("");
-    }
-    __device__ __forceinline__ int operator()(float v) const
-    {
-        return inverse == 0.f ? 0 : (int)__builtin_amdgcn_fmed3f(rintf(v * raise * inverse), -127.f, 127.f);
     }
 };
 
-// V of them at any address.
+// V of them at any address.  The product with the inverse is rounded to a whole number, ties to even, by a sum with 1.5 2^23, whose last bits are then that number's: one
+// instruction (at most 127 + 2^-16: the largest value's product is off by two roundings).
 template <int V>
-__device__ __forceinline__ void store_steps(int8_t* p, const float (&v)[V], const Steps& steps)
+__device__ __forceinline__ void store_steps(int8_t* p, float (&v)[V], const Steps& steps)
 {
+    if (steps.raised) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] *= 0x1p64f;
+    }
+    auto bits = [&](int i) { return __builtin_bit_cast(uint32_t, fmaf(v[i], steps.inverse, 12582912.f)); };
     if constexpr (V == 1) {
-        p[0] = (int8_t)steps(v[0]);
+        p[0] = steps.inverse == 0.f ? (int8_t)0 : (int8_t)bits(0);
     } else {
         struct __attribute__((packed, aligned(1))) Loose { uint32_t w[V / 4]; };
         Loose l;
 #pragma unroll
         for (int i = 0; i < V / 4; ++i) {
-            const uint32_t a = steps(v[4 * i]), b = steps(v[4 * i + 1]), c = steps(v[4 * i + 2]), d = steps(v[4 * i + 3]);
-            l.w[i] = (a & 0xff) | (b & 0xff) << 8 | (c & 0xff) << 16 | d << 24;
+            const uint32_t low = __builtin_amdgcn_perm(bits(4 * i + 1), bits(4 * i), 0x0c0c0400u), high = __builtin_amdgcn_perm(bits(4 * i + 3), bits(4 * i + 2), 0x04000c0cu);
+            l.w[i] = steps.inverse == 0.f ? 0u : low | high;
         }
         *reinterpret_cast<Loose*>(p) = l;
     }
