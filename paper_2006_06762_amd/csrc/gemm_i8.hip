@@ -80,11 +80,9 @@ hipError_t launch_rows_as(const Args& a, bool whole, hipStream_t stream)
 {
     constexpr int STAGES = 2;
     static LdsLimit limit;
-    const int waves = waves_of(a, TB == 1 ? 16 : TB == 2 ? 8 : 4);
-    void (*kernel)(Args) = i8::stream_kernel<T, TB, STAGES>;
-    if constexpr (TB <= 2)
-        if (!whole) kernel = i8::rows_kernel<T, TB, 4 / TB>;
-    const size_t sums = (size_t)waves * TB * 256 * sizeof(int), lds = whole ? std::max(sums, (size_t)waves * STAGES * 16 * (1 + TB) * i8::kRowsChunk) : sums;
+    const int waves = waves_of(a, i8::most_waves(TB));
+    void (*const kernel)(Args) = whole ? i8::stream_kernel<T, TB, STAGES, true> : i8::stream_kernel<T, TB, STAGES, false>;
+    const size_t lds = std::max((size_t)waves * TB * 256 * sizeof(int), (size_t)waves * STAGES * 16 * (1 + TB) * i8::kRowsChunk);
     const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit) : hipSuccess;
     return e != hipSuccess ? e : launch_kernel(kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * waves), lds, stream, a);
 }
@@ -93,7 +91,7 @@ hipError_t launch_rows(const Args& a, bool whole, hipStream_t stream)
 {
     if (a.M <= 16) return launch_rows_as<T, 1>(a, whole, stream);
     if (a.M <= 32) return launch_rows_as<T, 2>(a, whole, stream);
-    return a.M <= 48 ? launch_rows_as<T, 3>(a, true, stream) : launch_rows_as<T, 4>(a, true, stream);
+    return a.M <= 48 ? launch_rows_as<T, 3>(a, whole, stream) : launch_rows_as<T, 4>(a, whole, stream);
 }
 
 // ---- tiles
@@ -128,21 +126,21 @@ struct Choice {
     int tile, splits;
 };
 constexpr int64_t kFewRows = 32, kMostRows = 64;
-Choice choose(int64_t M, int64_t N, int64_t K, bool rows = true, int most_splits = 16)
+Choice choose(int64_t M, int64_t N, int64_t K)
 {
-    if (rows && M <= kFewRows) return {ROWS, 1};
+    if (M <= kFewRows) return {ROWS, 1};
     const int64_t chunks = (K + kChunk - 1) / kChunk;
     Choice best{TILE_256, 1};
     double least = 1e30;
     for (int t = 0; t < TILES; ++t)
-        for (int s = 1; s <= most_splits && (s == 1 || chunks / s >= 4); ++s) {
+        for (int s = 1; s <= 16 && (s == 1 || chunks / s >= 4); ++s) {
             const double us = estimate(kShapes[t], s * tiles_of(M, N, kShapes[t]), (chunks + s - 1) / s) + (s > 1 ? 2.9 + 2.0 * s * (double)M * (double)N * 4.0 / 4.3e6 : 0.0);
             if (us < least) {
                 least = us;
                 best = {t, s};
             }
         }
-    if (rows && M <= kMostRows) {                // reading W, and X for every sixteen of W's rows
+    if (M <= kMostRows) {                // reading W, and X for every sixteen of W's rows
         const double x_bytes = (double)((N + 15) / 16) * (double)((M + 15) / 16 * 16) * (double)K;
         if (4.0 + (double)N * (double)K / 5.3e6 + x_bytes / 36e6 < least) return {ROWS, 1};
     }
@@ -206,7 +204,7 @@ hipError_t launch_gemm_i8(const GemmI8Args& g, hipStream_t stream)
     a.N = (int)d.N;
     a.K = (int)d.K;
     a.finish = {g.a_scale, g.w_scale, g.bias, d.bias_dtype};
-    Choice choice = choice_of(d);
+    const Choice choice = choice_of(d);
     a.splits = choice.splits;
     a.parts = static_cast<int*>(g.ws);
     const bool whole = is_aligned16(g.a) && is_aligned16(g.w) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.K % 16 == 0;
@@ -216,7 +214,6 @@ hipError_t launch_gemm_i8(const GemmI8Args& g, hipStream_t stream)
             const int64_t columns = (d.N + kThreads - 1) / kThreads;     // (a grid has fewer than 2^32 threads)
             return launch_kernel(short_kernel<T>, dim3((unsigned)columns, (unsigned)std::min<int64_t>({d.M, 65535, (1 << 23) / columns})), dim3(kThreads), 0, stream, a);
         }
-        if (choice.tile == ROWS && !whole && d.M > kFewRows) choice = choose(d.M, d.N, d.K, false, 1);
         if (choice.tile == ROWS) return launch_rows<T>(a, whole, stream);
         if (a.splits == 1) return whole ? launch_tile<T, true>(choice.tile, a, stream) : launch_tile<T, false>(choice.tile, a, stream);
         const hipError_t e = whole ? launch_tile<int, true>(choice.tile, a, stream) : launch_tile<int, false>(choice.tile, a, stream);

@@ -9,15 +9,7 @@ namespace anr {
 namespace i8 {
 
 constexpr int kRowsChunk = 128;                 // k of a wave at a time: a line of a row
-
-// Sixteen values of k of a row that starts `row` bytes behind the base.
-template <bool CLEAR>
-__device__ __forceinline__ i32x4 load_unit(const int8_t* base, uint32_t row, int k, int K)
-{
-    u32x4 v = load_loose(base + row + loose_start(k, K));
-    if (CLEAR) clear_counted(v, k, K);
-    return __builtin_bit_cast(i32x4, v);
-}
+constexpr int most_waves(int TB) { return TB == 1 ? 16 : TB == 2 ? 8 : 4; }      // of a work-group: their buffers fit LDS
 
 // The results of a thread: what they are multiplied with is read before the products, whose sums [wave][TB][4][64] join at the end.  At least four waves.
 template <typename T, int TB>
@@ -51,55 +43,11 @@ struct Results {
     }
 };
 
-// Rows at any address and of any length from 16 on: from memory straight into the operands.  U: chunks of a wave whose loads are on their way together.
-template <typename T, int TB, int U>
-__global__ __launch_bounds__(1024) void rows_kernel(const Args a)
-{
-    extern __shared__ __attribute__((aligned(16))) int sums[];         // [wave][TB][4][64]
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-    const int n0 = blockIdx.x * 16, r = lane & 15, g = lane >> 4;
-    Results<T, TB> results;
-    results.init(a, n0);
-    const int8_t* const w0 = a.w + n0 * a.ldw;
-    const uint32_t wrow = (uint32_t)(min(r, a.N - 1 - n0) * a.ldw);
-    uint32_t xrow[TB];
-#pragma unroll
-    for (int t = 0; t < TB; ++t) xrow[t] = (uint32_t)(min(t * 16 + r, a.M - 1) * a.ldx);
-    i32x4 acc[TB];
-#pragma unroll
-    for (int t = 0; t < TB; ++t) acc[t] = i32x4{0, 0, 0, 0};
-    const int chunks = (a.K + kRowsChunk - 1) / kRowsChunk;
-    for (int c = wave; c < chunks; c += waves * U) {
-        i32x4 w[U][2], x[U][TB][2];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int k = (c + u * waves) * kRowsChunk + (4 * i + g) * kUnit;
-                w[u][i] = load_unit<false>(w0, wrow, k, a.K);
-#pragma unroll
-                for (int t = 0; t < TB; ++t) x[u][t][i] = load_unit<true>(a.x, xrow[t], k, a.K);
-            }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int t = 0; t < TB; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][i], x[u][t][i], acc[t], 0, 0, 0);
-    }
-#pragma unroll
-    for (int t = 0; t < TB; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sums[((wave * TB + t) * 4 + e) * 64 + lane] = acc[t][e];
-    __syncthreads();
-    results.store(a, sums, n0);
-}
-
-// Rows of whole 16-byte units go through LDS: a lane's operand is of one of sixteen rows, and loads whose neighbouring lanes are in different lines take four times as
+// Rows go through LDS: a lane's operand is of one of sixteen rows, and loads whose neighbouring lanes are in different lines take four times as
 // long to issue (32 tokens 4096 -> 11264 19.4 us straight from memory, so 13.6; 1 token 5632 -> 2048 5.4, 4.1).  Each wave has STAGES buffers of its own, of its 16 rows of W and the 16 TB rows of X, and waits for no other one but at the end.
-template <typename T, int TB, int STAGES>
-__global__ __launch_bounds__(1024) void stream_kernel(const Args a)
+// WHOLE: rows of whole 16-byte units (pointers, leading dimensions, K), which go from memory to LDS; others, of any length from 16 on, go through registers, a chunk ahead.
+template <typename T, int TB, int STAGES, bool WHOLE>
+__global__ __launch_bounds__(64 * most_waves(TB)) void stream_kernel(const Args a)
 {
     constexpr int BK = kRowsChunk, STAGE = 16 * (1 + TB) * BK, LOADS = 2 * (1 + TB);
     extern __shared__ __attribute__((aligned(1024))) char lds[];                  // buffers, then sums [wave][TB][4][64]
@@ -128,16 +76,8 @@ __global__ __launch_bounds__(1024) void stream_kernel(const Args a)
     i32x4 acc[TB];
 #pragma unroll
     for (int t = 0; t < TB; ++t) acc[t] = i32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int s = 0; s < STAGES; ++s) load(wave + s * waves, s);
-    Results<T, TB> results;
-    results.init(a, n0);
-    int stage = 0;
-#pragma unroll 1
-    for (int c = wave; c < chunks; c += waves) {
-        wait_for_loads<(STAGES - 1) * LOADS>();
-        const char* const at = lds + (wave * STAGES + stage) * STAGE;
-        i32x4 v[2][1 + TB];
+    i32x4 v[2][1 + TB];
+    auto read = [&](const char* at) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -145,20 +85,65 @@ __global__ __launch_bounds__(1024) void stream_kernel(const Args a)
                 const int r = lane & 15;
                 v[i][j] = *reinterpret_cast<const i32x4*>(at + (j * 16 + r) * BK + place_of<BK>(r, 4 * i + (lane >> 4)) * kUnit);
             }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        load(c + STAGES * waves, stage);
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
-        if ((c + 1) * BK > a.K) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int t = 0; t < TB; ++t)
-                    if (c * BK + (4 * i + (lane >> 4)) * kUnit >= a.K) v[i][1 + t] = i32x4{0, 0, 0, 0};
-        }
+    };
+    auto multiply = [&]() {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int t = 0; t < TB; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[i][0], v[i][1 + t], acc[t], 0, 0, 0);
+    };
+    Results<T, TB> results;
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s) load(wave + s * waves, s);
+        results.init(a, n0);
+        int stage = 0;
+#pragma unroll 1
+        for (int c = wave; c < chunks; c += waves) {
+            wait_for_loads<(STAGES - 1) * LOADS>();
+            read(lds + (wave * STAGES + stage) * STAGE);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            load(c + STAGES * waves, stage);
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
+            if ((c + 1) * BK > a.K) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int t = 0; t < TB; ++t)
+                        if (c * BK + (4 * i + (lane >> 4)) * kUnit >= a.K) v[i][1 + t] = i32x4{0, 0, 0, 0};
+            }
+            multiply();
+        }
+    } else {
+        u32x4 data[STAGES][LOADS];
+        const int8_t* const w0 = a.w + n0 * a.ldw;
+        auto load_loosely = [&](u32x4 (&to)[LOADS], int c) {
+            const int start0 = loose_start(c * BK + unit0, a.K), start1 = loose_start(c * BK + unit1, a.K);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) to[i] = load_loose((i < 2 ? w0 : a.x) + row[i] + (i & 1 ? start1 : start0));
+        };
+        auto use = [&](u32x4 (&from)[LOADS], int c, int stage) {
+            if ((c + 1) * BK > a.K) {
+#pragma unroll
+                for (int i = 2; i < LOADS; ++i) clear_counted(from[i], c * BK + (i & 1 ? unit1 : unit0), a.K);
+            }
+            char* const at = lds + (wave * STAGES + stage) * STAGE;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) *reinterpret_cast<u32x4*>(at + i * 1024 + lane * 16) = from[i];
+            load_loosely(from, c + STAGES * waves);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            read(at);
+            multiply();
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s) load_loosely(data[s], wave + s * waves);
+        results.init(a, n0);
+#pragma unroll 1
+        for (int c = wave; c < chunks; c += STAGES * waves) {        // (chunks past the last one are cleared)
+#pragma unroll
+            for (int s = 0; s < STAGES; ++s) use(data[s], c + s * waves, s);
+        }
     }
     wait_for_loads<0>();
     __syncthreads();

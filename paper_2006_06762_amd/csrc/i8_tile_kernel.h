@@ -68,16 +68,32 @@ __device__ __forceinline__ i32x4 operand(const char* lds, int row0, int step, in
     return *reinterpret_cast<const i32x4*>(lds + r * BK + place_of<BK>(r, u) * 16);
 }
 
-// Eight neighbouring elements of a row, of which `in` exist.
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&v)[8], int in, bool aligned)
+// Eight neighbouring elements of a row at any element's address (STREAMING: past L2, whole aligned units), of which `in` exist (3000 x 512 -> 3001 in bf16 one by one 28.7 us, so 14.7).
+template <bool STREAMING, typename T, typename V>
+__device__ __forceinline__ void store8(T* p, const V (&v)[8], int in)
 {
-    if (aligned && in >= 8) {
-        store_floats<T, 8>(p, v);
+    if (in >= 8) {
+        if constexpr (STREAMING) {
+            T w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = (T)v[i];
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                u32x4 q;
+                __builtin_memcpy(&q, reinterpret_cast<const char*>(w) + 16 * i, 16);
+                __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(p) + i);
+            }
+            return;
+        }
+        struct __attribute__((packed, aligned(sizeof(T)))) Loose { T v[8]; };
+        Loose l;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) l.v[i] = (T)v[i];
+        *reinterpret_cast<Loose*>(p) = l;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < in) p[i] = from_float<T>(v[i]);
+            if (i < in) p[i] = (T)v[i];
     }
 }
 
@@ -169,7 +185,6 @@ __device__ __forceinline__ void finish_tile(const Args& a, const Place& at, Wave
     __syncthreads();
     constexpr int ROW = NB * 128 + 16;                                // bytes; the 16 put eight rows' same column in different banks
     static_assert((size_t)(NT / 64) * 32 * ROW <= ROOM, "fits the chunks' room");
-    char* const own = lds + wave * 32 * ROW;
     constexpr int LANES = NB * 4;                                     // of a row
     const int part = lane % LANES, col = at.n0 + wn * NB * 32 + part * 8;
     float rows[MB], columns[8], added[8];
@@ -184,68 +199,53 @@ __device__ __forceinline__ void finish_tile(const Args& a, const Place& at, Wave
     }
     T* const d = PARTIAL ? reinterpret_cast<T*>(a.parts) + (int64_t)at.split * M * N : static_cast<T*>(a.d);
     const int64_t ldd = PARTIAL ? N : a.ldd;
-    const bool aligned = ((reinterpret_cast<uintptr_t>(d) | (uintptr_t)(ldd * (int64_t)sizeof(T))) & 15) == 0;
+    by_streaming(!PARTIAL && a.streaming, [&](auto streaming) {
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
+        for (int m = 0; m < MB; ++m) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-            {
-                char* const to = own + (lane & 31) * ROW + (n * 32 + 8 * q + 4 * (lane >> 5)) * 4;
-                if constexpr (PARTIAL) {
-                    *reinterpret_cast<i32x4*>(to) = i32x4{acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
-                } else {                                              // (a row's scale is one for a lane here, those of columns are where they are read)
-                    f32x4 v;
+                for (int q = 0; q < 4; ++q) {
+                    char* const to = lds + wave * 32 * ROW + (lane & 31) * ROW + (n * 32 + 8 * q + 4 * (lane >> 5)) * 4;
+                    if constexpr (PARTIAL) {
+                        *reinterpret_cast<i32x4*>(to) = i32x4{acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+                    } else {                                          // (a row's scale is one for a lane here, those of columns are where they are read)
+                        f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = (float)acc[n][m][4 * q + e] * rows[m];
-                    *reinterpret_cast<f32x4*>(to) = v;
-                }
-            }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int i = 0; i < 32 * LANES / 64; ++i) {
-            const int r = i * (64 / LANES) + lane / LANES, row = at.m0 + (wm * MB + m) * 32 + r;
-            if (row >= M) continue;
-            using Four = std::conditional_t<PARTIAL, i32x4, f32x4>;
-            const Four lo = *reinterpret_cast<const Four*>(own + r * ROW + part * 32), hi = *reinterpret_cast<const Four*>(own + r * ROW + part * 32 + 16);
-            T* const to = d + (int64_t)row * ldd + col;
-            if constexpr (PARTIAL) {
-                if (aligned && col + 8 <= N) {
-                    *reinterpret_cast<i32x4*>(to) = lo;
-                    *reinterpret_cast<i32x4*>(to + 4) = hi;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (col + e < N) to[e] = e < 4 ? lo[e & 3] : hi[e & 3];
-                }
-            } else {
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (e < 4 ? lo[e & 3] : hi[e & 3]) * columns[e] + added[e];
-                if (a.streaming && col + 8 <= N) {
-                    const Pack<T, 8> p = pack_floats<T, 8>(v);
-#pragma unroll
-                    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-                        u32x4 q;
-                        __builtin_memcpy(&q, reinterpret_cast<const char*>(&p) + 16 * i, 16);
-                        __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(to) + i);
+                        for (int e = 0; e < 4; ++e) v[e] = (float)acc[n][m][4 * q + e] * rows[m];
+                        *reinterpret_cast<f32x4*>(to) = v;
                     }
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < 32 * LANES / 64; ++i) {
+                const int r = i * (64 / LANES) + lane / LANES, row = at.m0 + (wm * MB + m) * 32 + r;
+                if (row >= M) continue;
+                using Four = std::conditional_t<PARTIAL, i32x4, f32x4>;
+                const char* const from = lds + wave * 32 * ROW + r * ROW + part * 32;
+                const Four lo = *reinterpret_cast<const Four*>(from), hi = *reinterpret_cast<const Four*>(from + 16);
+                T* const to = d + (int64_t)row * ldd + col;
+                if constexpr (PARTIAL) {
+                    const int v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                    store8<false>(to, v, N - col);
                 } else {
-                    store8(to, v, N - col, aligned);
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = (e < 4 ? lo[e & 3] : hi[e & 3]) * columns[e] + added[e];
+                    store8<decltype(streaming)::value>(to, v, N - col);
                 }
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
+    });
 }
 
 // T: D's type; int for sums that go to `parts`.
 //
 // Rows at any address and of any length from 16 on: global -> registers -> LDS -> operands, with two buffers, so that one is multiplied while the other
-// is filled and the loads of the chunk after that are on their way.
+// is filled and the loads of the chunk after that are on their way (two chunks on their way to the registers: 768 x 515 -> 1408 8.1 us, so 9.5).
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void loose_kernel(const Args args)
 {
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void loose_kernel
     sx.init(args.x, args.ldx, at.m0, args.M, K, tid);
     sw.init(args.w, args.ldw, at.n0, args.N, K, tid);
 
-    // Chunks past the last one load what is cleared or not used: no branch in the loop
+    // Chunks past the last one are loaded and cleared: no branch in the loop
     using SX = decltype(sx);
     using SW = decltype(sw);
     auto load = [&](int c, auto part) {
@@ -278,7 +278,6 @@ __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void loose_kernel
     using P0 = std::integral_constant<int, 0>;
     using P1 = std::integral_constant<int, 1>;
     using P2 = std::integral_constant<int, 2>;
-
     // A chunk has four steps of 32 k.  The operands of a step are read from LDS while the one before it is multiplied; the next
     // chunk's units go to the other buffer in the first three steps, each followed by the load of the unit of the chunk after that, and
     // the barrier comes before the fourth, in which the first operands of the next chunk are read.
