@@ -67,7 +67,7 @@ hipError_t launch_join(const Args& a, hipStream_t stream)
 // ---- few rows
 
 // Waves of a work-group: as far as there are chunks for them, eight for each CU over all work-groups, or long rows. us, 4 / 8 / 16 waves: 1 token 2048 -> 11264
-// 6.2 / 7.1 / 9.6, 5632 -> 2048 4.9 / 4.1 / 4.6, 1024 -> 1024 2.85 / 2.91 / 3.4, 16384 -> 16384 56.4 / 52.1 / 53.3, 16 tokens 4096 -> 4096 6.1 / 6.2 / 5.4.
+// 6.0 / 6.9 / 9.7, 5632 -> 2048 4.8 / 4.0 / 4.3, 1024 -> 1024 2.74 / 2.68 / 3.1, 16384 -> 16384 54.1 / 50.6 / 52.2, 8 tokens 4096 -> 4096 5.9 / 5.6 / 5.4.
 int waves_of(const Args& a, int most)
 {
     const int64_t groups = (a.N + 15) / 16, chunks = (a.K + i8::kRowsChunk - 1) / i8::kRowsChunk;

@@ -44,7 +44,7 @@ struct Results {
 };
 
 // Rows go through LDS: a lane's operand is of one of sixteen rows, and loads whose neighbouring lanes are in different lines take four times as
-// long to issue (32 tokens 4096 -> 11264 19.4 us straight from memory, so 13.6; 1 token 5632 -> 2048 5.4, 4.1).  Each wave has STAGES buffers of its own, of its 16 rows of W and the 16 TB rows of X, and waits for no other one but at the end.
+// long to issue (32 tokens 4096 -> 11264 19.4 us straight from memory, so 13.6; 1 token 5632 -> 2048 5.4, 4.0).  Each wave has STAGES buffers of its own, of its 16 rows of W and the 16 TB rows of X, and waits for no other one but at the end.
 // WHOLE: rows of whole 16-byte units (pointers, leading dimensions, K), which go from memory to LDS; others, of any length from 16 on, go through registers, a chunk ahead.
 template <typename T, int TB, int STAGES, bool WHOLE>
 __global__ __launch_bounds__(64 * most_waves(TB)) void stream_kernel(const Args a)
@@ -94,9 +94,10 @@ __global__ __launch_bounds__(64 * most_waves(TB)) void stream_kernel(const Args 
     };
     Results<T, TB> results;
     if constexpr (WHOLE) {
+        load(wave, 0);
+        results.init(a, n0);                                         // (in front of the loads that the first wait leaves on their way)
 #pragma unroll
-        for (int s = 0; s < STAGES; ++s) load(wave + s * waves, s);
-        results.init(a, n0);
+        for (int s = 1; s < STAGES; ++s) load(wave + s * waves, s);
         int stage = 0;
 #pragma unroll 1
         for (int c = wave; c < chunks; c += waves) {
