@@ -79,11 +79,11 @@ template <typename T, int TB>
 hipError_t launch_rows_as(const Args& a, bool whole, hipStream_t stream)
 {
     constexpr int STAGES = 2;
-    static LdsLimit limit;
+    static LdsLimit limits[2];                   // of the two kernels
     const int waves = waves_of(a, i8::most_waves(TB));
     void (*const kernel)(Args) = whole ? i8::stream_kernel<T, TB, STAGES, true> : i8::stream_kernel<T, TB, STAGES, false>;
     const size_t lds = std::max((size_t)waves * TB * 256 * sizeof(int), (size_t)waves * STAGES * 16 * (1 + TB) * i8::kRowsChunk);
-    const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit) : hipSuccess;
+    const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limits[whole]) : hipSuccess;
     return e != hipSuccess ? e : launch_kernel(kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * waves), lds, stream, a);
 }
 template <typename T>
