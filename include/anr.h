@@ -410,9 +410,9 @@ anr_status anr_gated_ff_backward(const anr_gated_ff_desc *desc, const void *dy, 
  * Root-mean-square norm of T tokens of C channels, with the residual's addition.  Row-major,
  * leading dimensions in elements, 0 for packed: x (ldx); residual, or dh in the backward
  * call (ld_residual); h, or dx (ldh); y, dy or q (ldy).  param_dtype is the type of gamma and
- * dgamma: float32 or `dtype`.  C <= 32768, T < 2^31.  Outputs of the forward calls may be x
- * or residual itself, dx may be dy, x or dh itself, with the same leading dimension; two
- * outputs are never the same.
+ * dgamma: float32 or `dtype`.  C <= 32768, T < 2^31.  h and y may be x or residual itself,
+ * dx may be dy, x or dh itself, with the same leading dimension; two outputs are never the
+ * same, and no output overlaps an input in another way.
  */
 typedef struct {
     int64_t T, C;
@@ -425,7 +425,8 @@ typedef struct {
  * rstd = 1/sqrt(m + eps), m the mean of h^2 over a token's channels.  gamma: C, NULL for ones.
  * h: where the sum goes, rounded to `dtype` (y is made from the sum before that), or NULL;
  * NULL where there is no residual.  rstd: T floats for a backward call, or NULL.  eps is
- * finite and not negative.  m is formed in float32: magnitudes up to 2^60. */
+ * finite and not negative.  m is formed in float32: it holds for magnitudes of h up to 2^56,
+ * and squares below 2^-126 may count as zeros. */
 anr_status anr_rms_norm(const anr_rms_norm_desc *desc, const void *x, const void *residual, const void *gamma, float eps,
                         void *h, void *y, float *rstd, void *ws, size_t ws_bytes, void *hip_stream);
 
@@ -447,7 +448,8 @@ anr_status anr_rms_norm_q8(const anr_rms_norm_desc *desc, const void *x, const v
 /*
  * T rows of C values in 8 bits, each with a scale of its own: tokens in front of a product of 8-bit
  * integers, or weights as [outputs, inputs].  Row-major, leading dimensions in elements, 0 for
- * packed: x, or y in the way back (ldx), up (ld_up), q (ldq).  C <= 2^20, T < 2^31.
+ * packed: x, or y in the way back (ldx), up (ld_up), q (ldq).  C <= 2^20, T < 2^31.  No
+ * output overlaps an input.
  */
 typedef struct {
     int64_t T, C;
@@ -470,7 +472,7 @@ anr_status anr_dequantize_rows(const anr_rows_q8_desc *desc, const int8_t *q, co
  * Product of 8-bit integers with scales: a [M,K] by weights as [outputs, inputs], w [N,K], d [M,N].
  * Row-major, leading dimensions in elements, 0 for packed.  16-byte aligned a and w whose K and
  * leading dimensions are multiples of 16 run the faster kernels.  N <= 2^20, K < 2^17, M and
- * leading dimensions < 2^22.
+ * leading dimensions < 2^22.  d overlaps no input.
  */
 typedef struct {
     int64_t M, N, K;

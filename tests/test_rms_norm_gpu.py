@@ -251,3 +251,19 @@ def test_gradients_against_differences(anr):
         e[c] = step
         slope = (f(x, res, gamma + e) - f(x, res, gamma - e)) / (2 * step)
         assert abs(float(dg[c]) - slope) < 1e-5 * (1 + abs(slope))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_largest_magnitudes(anr, t):
+    """Rows of 2^56 all over, whose squares sum to 2^127 at the most: powers of two, exact throughout."""
+    t = TYPES[t]
+    for C in (300, 32768):
+        sign = torch.from_numpy(rng(11).choice([-1.0, 1.0], size=(3, C)))
+        for share in (1.0, 0.5):                 # of the sum that x has
+            x, res = (sign * 2.0 ** 56 * share).to(t).cuda(), (sign * 2.0 ** 56 * (1 - share)).to(t).cuda()
+            y, h, q, scale = torch.empty_like(x), torch.empty_like(x), torch.empty(3, C, dtype=torch.int8, device="cuda"), torch.empty(3, device="cuda")
+            anr.rms_norm(x, y, None, 0.0, res, h)
+            anr.rms_norm_q8(x, q, scale, None, 0.0, res)
+            # (every partial sum is at most 2^15 times a power of two, the mean is 2^112, its root and that one's inverse are powers of two)
+            assert np.array_equal(host(y), sign.numpy()) and np.array_equal(host(h), sign.numpy() * 2.0 ** 56)
+            assert np.array_equal(host(q), 127 * sign.numpy()) and (scale == np.float32(1) / np.float32(127)).all()
