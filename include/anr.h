@@ -470,9 +470,10 @@ anr_status anr_dequantize_rows(const anr_rows_q8_desc *desc, const int8_t *q, co
 
 /*
  * Product of 8-bit integers with scales: a [M,K] by weights as [outputs, inputs], w [N,K], d [M,N].
- * Row-major, leading dimensions in elements, 0 for packed.  16-byte aligned a and w whose K and
- * leading dimensions are multiples of 16 run the faster kernels.  N <= 2^20, K < 2^17, M and
- * leading dimensions < 2^22.  d overlaps no input.
+ * Row-major, leading dimensions in elements, 0 for packed.  4-byte aligned a and w whose
+ * leading dimensions are multiples of 4 run the faster kernels, others are read by the whole
+ * 4-byte words that hold any of their rows.  N <= 2^20, K < 2^17, M and leading dimensions
+ * < 2^22.  d overlaps no input.
  */
 typedef struct {
     int64_t M, N, K;

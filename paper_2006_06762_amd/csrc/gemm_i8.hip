@@ -2,7 +2,6 @@
 //
 //   few rows     i8_rows_kernel.h: reads the weights once
 //   else         i8_tile_kernel.h; products with few tiles share each tile's k among work-groups, whose sums a second launch joins
-//   k below 16   one thread a result
 #include <algorithm>
 
 #include "blocks_internal.h"
@@ -14,21 +13,6 @@ namespace {
 
 using i8::Args;
 constexpr int kThreads = 256;
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void short_kernel(const Args a)
-{
-    const int n = blockIdx.x * kThreads + threadIdx.x;
-    if (n >= a.N) return;
-    int w[i8::kUnit];
-    for (int k = 0; k < a.K; ++k) w[k] = a.w[n * a.ldw + k];
-    const float column = a.finish.of_column(n), added = a.finish.added(n);
-    for (int m = blockIdx.y; m < a.M; m += gridDim.y) {
-        int sum = 0;
-        for (int k = 0; k < a.K; ++k) sum += a.x[m * a.ldx + k] * w[k];
-        static_cast<T*>(a.d)[m * a.ldd + n] = from_float<T>(i8::Finish::value(sum, a.finish.of_row(m), column, added));
-    }
-}
 
 // D from the sums at `parts`, V columns a thread.
 template <typename T, int V>
@@ -76,22 +60,22 @@ int waves_of(const Args& a, int most)
     return waves;
 }
 template <typename T, int TB>
-hipError_t launch_rows_as(const Args& a, bool whole, hipStream_t stream)
+hipError_t launch_rows_as(const Args& a, bool loose, hipStream_t stream)
 {
     constexpr int STAGES = 2;
     static LdsLimit limits[2];                   // of the two kernels
     const int waves = waves_of(a, i8::most_waves(TB));
-    void (*const kernel)(Args) = whole ? i8::stream_kernel<T, TB, STAGES, true> : i8::stream_kernel<T, TB, STAGES, false>;
-    const size_t lds = std::max((size_t)waves * TB * 256 * sizeof(int), (size_t)waves * STAGES * 16 * (1 + TB) * i8::kRowsChunk);
-    const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limits[whole]) : hipSuccess;
+    void (*const kernel)(Args) = loose ? i8::stream_kernel<T, TB, STAGES, true> : i8::stream_kernel<T, TB, STAGES, false>;
+    const size_t lds = std::max((size_t)waves * TB * 256 * sizeof(int), (size_t)waves * STAGES * (loose ? i8::stage_bytes<TB, true>() : i8::stage_bytes<TB, false>()));
+    const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limits[loose]) : hipSuccess;
     return e != hipSuccess ? e : launch_kernel(kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * waves), lds, stream, a);
 }
 template <typename T>
-hipError_t launch_rows(const Args& a, bool whole, hipStream_t stream)
+hipError_t launch_rows(const Args& a, bool loose, hipStream_t stream)
 {
-    if (a.M <= 16) return launch_rows_as<T, 1>(a, whole, stream);
-    if (a.M <= 32) return launch_rows_as<T, 2>(a, whole, stream);
-    return a.M <= 48 ? launch_rows_as<T, 3>(a, whole, stream) : launch_rows_as<T, 4>(a, whole, stream);
+    if (a.M <= 16) return launch_rows_as<T, 1>(a, loose, stream);
+    if (a.M <= 32) return launch_rows_as<T, 2>(a, loose, stream);
+    return a.M <= 48 ? launch_rows_as<T, 3>(a, loose, stream) : launch_rows_as<T, 4>(a, loose, stream);
 }
 
 // ---- tiles
@@ -147,14 +131,12 @@ Choice choose(int64_t M, int64_t N, int64_t K)
     return best;
 }
 
-template <typename T, bool WHOLE, int M, int N, int WM, int WN, int STAGES>
+template <typename T, bool LOOSE, int M, int N, int WM, int WN, int STAGES>
 hipError_t launch_as(Args a, hipStream_t stream)
 {
     static LdsLimit limit;
-    void (*kernel)(Args);
-    if constexpr (WHOLE) kernel = i8::tile_kernel<T, M, N, WM, WN, kChunk, STAGES>;
-    else kernel = i8::loose_kernel<T, M, N, WM, WN>;
-    constexpr size_t lds = (size_t)(WHOLE ? STAGES : 2) * (M + N) * kChunk;
+    void (*const kernel)(Args) = i8::tile_kernel<T, M, N, WM, WN, kChunk, STAGES, LOOSE>;
+    constexpr size_t lds = i8::tile_bytes<M, N, WM * WN, STAGES, LOOSE>();
     const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit);
     if (e != hipSuccess) return e;
     a.tiles_m = (a.M + M - 1) / M;
@@ -164,20 +146,20 @@ hipError_t launch_as(Args a, hipStream_t stream)
     a.streaming = N / WN % LINE == 0 && a.ldd % LINE == 0 && reinterpret_cast<uintptr_t>(a.d) % 128 == 0;
     return launch_kernel(kernel, dim3((unsigned)(a.tiles_m * a.tiles_n * a.splits)), dim3(64 * WM * WN), lds, stream, a);
 }
-template <typename T, bool WHOLE>
+template <typename T, bool LOOSE>
 hipError_t launch_tile(int tile, const Args& a, hipStream_t stream)
 {
     switch (tile) {
-        case TILE_256: return launch_as<T, WHOLE, 256, 256, 2, 4, 2>(a, stream);
-        case TILE_128: return launch_as<T, WHOLE, 128, 128, 2, 2, 2>(a, stream);
-        case TILE_64_128: return launch_as<T, WHOLE, 64, 128, 2, 2, 3>(a, stream);
-        default: return launch_as<T, WHOLE, 64, 64, 2, 2, 2>(a, stream);
+        case TILE_256: return launch_as<T, LOOSE, 256, 256, 2, 4, 2>(a, stream);
+        case TILE_128: return launch_as<T, LOOSE, 128, 128, 2, 2, 2>(a, stream);
+        case TILE_64_128: return launch_as<T, LOOSE, 64, 128, 2, 2, 3>(a, stream);
+        default: return launch_as<T, LOOSE, 64, 64, 2, 2, 2>(a, stream);
     }
 }
 
 Choice choice_of(const anr_gemm_i8_desc& d)
 {
-    if (d.M == 0 || d.K < i8::kUnit) return {ROWS, 1};
+    if (d.M == 0) return {ROWS, 1};
     return choose(d.M, d.N, d.K);
 }
 
@@ -207,16 +189,12 @@ hipError_t launch_gemm_i8(const GemmI8Args& g, hipStream_t stream)
     const Choice choice = choice_of(d);
     a.splits = choice.splits;
     a.parts = static_cast<int*>(g.ws);
-    const bool whole = is_aligned16(g.a) && is_aligned16(g.w) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.K % 16 == 0;
+    const bool loose = reinterpret_cast<uintptr_t>(g.a) % 4 != 0 || reinterpret_cast<uintptr_t>(g.w) % 4 != 0 || d.lda % 4 != 0 || d.ldw % 4 != 0;
     return with_type(d.dtype, [&](auto t) {
         using T = decltype(t);
-        if (d.K < i8::kUnit) {
-            const int64_t columns = (d.N + kThreads - 1) / kThreads;     // (a grid has fewer than 2^32 threads)
-            return launch_kernel(short_kernel<T>, dim3((unsigned)columns, (unsigned)std::min<int64_t>({d.M, 65535, (1 << 23) / columns})), dim3(kThreads), 0, stream, a);
-        }
-        if (choice.tile == ROWS) return launch_rows<T>(a, whole, stream);
-        if (a.splits == 1) return whole ? launch_tile<T, true>(choice.tile, a, stream) : launch_tile<T, false>(choice.tile, a, stream);
-        const hipError_t e = whole ? launch_tile<int, true>(choice.tile, a, stream) : launch_tile<int, false>(choice.tile, a, stream);
+        if (choice.tile == ROWS) return launch_rows<T>(a, loose, stream);
+        if (a.splits == 1) return loose ? launch_tile<T, true>(choice.tile, a, stream) : launch_tile<T, false>(choice.tile, a, stream);
+        const hipError_t e = loose ? launch_tile<int, true>(choice.tile, a, stream) : launch_tile<int, false>(choice.tile, a, stream);
         return e != hipSuccess ? e : launch_join<T>(a, stream);
     });
 }

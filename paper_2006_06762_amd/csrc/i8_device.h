@@ -13,7 +13,6 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kUnit = 16;                       // k of a lane's operand
-constexpr uint32_t kNowhere = 0x80000000u;      // byte offset past every descriptor's extent: loads zeros
 constexpr int kExtent = 0x7fffffff;
 
 // Scales and bias, each of which may be absent.
@@ -41,23 +40,23 @@ struct Args {
     bool streaming;                 // D's stores go past L2: a wave's part of a row is whole lines of 128 bytes
 };
 
-// Sixteen values of k of a row, from k on; those past K are cleared by `clear` where they were read.  Not WHOLE (pointers, leading dimensions and K are any): the
-// row's last unit starts so far ahead that it ends with the row (K >= 16), and the values that it shares with the unit before are cleared in one of the operands,
-// X: other values of k in their place, in both operands alike.
-__device__ __forceinline__ int loose_start(int k, int K) { return min(k, K - kUnit); }
-__device__ __forceinline__ u32x4 load_loose(const int8_t* p)
+// Rows in memory start at whole words, or (loose) anywhere, and end anywhere: they are loaded by whole words from the last one in front of them on, and what is read behind them (a next row, or zeros behind the
+// last one, where the extent of the buffer's descriptor ends) is cleared in one of the operands, X.
+//
+// The first `count` bytes of an operand.
+__device__ __forceinline__ void cut(i32x4& v, int count)
 {
-    struct __attribute__((packed, aligned(1))) Loose { u32x4 v; };
-    return reinterpret_cast<const Loose*>(p)->v;
-}
-__device__ __forceinline__ void clear_counted(u32x4& v, int k, int K)
-{
-    const int counted = min(k - loose_start(k, K), kUnit);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int bytes = min(max(counted - 4 * i, 0), 4);
-        v[i] &= bytes == 4 ? 0u : 0xffffffffu << (8 * bytes);
+    for (int j = 0; j < 4; ++j) {
+        const int bytes = min(max(count - 4 * j, 0), 4);
+        v[j] &= bytes == 4 ? -1 : (int)((1u << (8 * bytes)) - 1u);
     }
+}
+// Sixteen bytes from byte `shift` % 4 on of `before` and v.
+__device__ __forceinline__ i32x4 behind_byte(i32x4 v, int before, uint32_t shift)
+{
+    return i32x4{(int)__builtin_amdgcn_alignbyte(v[0], before, shift), (int)__builtin_amdgcn_alignbyte(v[1], v[0], shift), (int)__builtin_amdgcn_alignbyte(v[2], v[1], shift),
+                 (int)__builtin_amdgcn_alignbyte(v[3], v[2], shift)};
 }
 
 // The unit of a row in LDS that holds the row's unit u.
@@ -70,6 +69,11 @@ __device__ __forceinline__ int place_of(int row, int u) { return BK == 128 ? u ^
 __device__ __forceinline__ void load_to_lds(i32x4 descriptor, uint32_t offset, int step, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor), "s"(step) : "m0");
+}
+// Four bytes a lane, alike.
+__device__ __forceinline__ void load_word_to_lds(i32x4 descriptor, uint32_t offset, int step, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor), "s"(step) : "m0");
 }
 // A scalar register that the vector unit wrote is read by a memory instruction five cycles later at the earliest, which the compiler sees to for its own instructions only: what
 // load_to_lds takes comes from here, and what is made of it stays in the scalar unit.

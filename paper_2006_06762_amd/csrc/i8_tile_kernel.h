@@ -1,8 +1,7 @@
 // Products of 8-bit integers in tiles on the matrix pipes (i8_device.h).
 //
 // A work-group takes a tile of BM x BN, its waves WM x WN parts of it in blocks of 32 x 32 (v_mfma_i32_32x32x32_i8), and walks k in chunks of BK
-// bytes.  Rows that are whole 16-byte units (tile_kernel) go from memory into LDS without a register between, STAGES chunks ahead of their use in as many
-// buffers; others (loose_kernel) through registers, where what lies past their end is cleared.
+// bytes, which go from memory into LDS without a register between, STAGES chunks ahead of their use in as many buffers.
 //
 // LDS: rows of BK bytes, 16-byte units exchanged by as many rows as fill the 64 banks (unit ^ row / 2 % 8 for 128 bytes), so that the sixteen rows' same unit that
 // an operand read takes together lie in different ones.  Loads write LDS in the order of the lanes: the lanes take the units of a row in that order instead.
@@ -15,50 +14,9 @@
 namespace anr {
 namespace i8 {
 
-// The units of a chunk in three parts.
-constexpr int part_of(int units, int part) { return (units * part + 2) / 3; }
-
-// Global -> registers -> LDS of R rows of one operand by NT threads.
-template <int R, int NT, int BK, bool CLEAR>
-struct Stager {
-    static constexpr int PER_ROW = BK / kUnit, UNITS = R * PER_ROW / NT;
-    static_assert(R * PER_ROW % NT == 0 && NT % PER_ROW == 0, "whole units for every thread");
-    const int8_t* base;             // of the tile's first row
-    int K, first, unit;             // this thread's row in the first unit, its unit in the row
-    uint32_t offset[UNITS];         // bytes of a row's start from the base
-    u32x4 data[UNITS];
-
-    __device__ __forceinline__ void init(const int8_t* p, int64_t ld, int row0, int rows, int k, int tid)
-    {
-        base = p + row0 * ld;
-        K = k;
-        first = tid / PER_ROW;
-        unit = tid % PER_ROW;
-#pragma unroll
-        for (int i = 0; i < UNITS; ++i) offset[i] = (uint32_t)(min(first + i * (NT / PER_ROW), rows - row0 - 1) * ld);
-    }
-    // units FIRST to LAST - 1 of the chunk of k from k0 on
-    template <int FIRST, int LAST>
-    __device__ __forceinline__ void load(int k0)
-    {
-        const int start = loose_start(k0 + unit * kUnit, K);
-#pragma unroll
-        for (int i = FIRST; i < LAST; ++i) data[i] = load_loose(base + offset[i] + start);
-    }
-    template <int FIRST, int LAST>
-    __device__ __forceinline__ void store(char* lds, int k0)
-    {
-        if (CLEAR && k0 + BK > K) {
-#pragma unroll
-            for (int i = FIRST; i < LAST; ++i) clear_counted(data[i], k0 + unit * kUnit, K);
-        }
-#pragma unroll
-        for (int i = FIRST; i < LAST; ++i) {
-            const int r = first + i * (NT / PER_ROW);
-            *reinterpret_cast<u32x4*>(lds + r * BK + place_of<BK>(r, unit) * 16) = data[i];
-        }
-    }
-};
+// Bytes of LDS of a work-group: STAGES chunks of 128 k of both operands' rows, and the rows' first words where these are loose.
+template <int BM, int BN, int WAVES, int STAGES, bool LOOSE>
+constexpr size_t tile_bytes() { return (size_t)STAGES * (BM + BN) * 128 + (LOOSE ? 2 * WAVES * 256 : 0); }
 
 // Sixteen k from 32 step + 16 (lane / 32) on of row `row0 + lane % 32`.
 template <int BK>
@@ -138,11 +96,12 @@ struct Wave {
         if (i < NB) wv[set][i] = operand<BK>(w, i * 32, step, lane);
         else xv[set][i - NB] = operand<BK>(x, (i - NB) * 32, step, lane);
     }
-    template <int BK>
-    __device__ __forceinline__ void read_all(int set, const char* x, const char* w, int step, int lane)
+    __device__ __forceinline__ i32x4& of(int set, int i) { return i < NB ? wv[set][i] : xv[set][i - NB]; }
+    // only the first `in` k of a step's 32 count
+    __device__ __forceinline__ void cut_to(int set, int in, int lane)
     {
 #pragma unroll
-        for (int i = 0; i < NB + MB; ++i) read<BK>(set, x, w, step, lane, i);
+        for (int m = 0; m < MB; ++m) cut(xv[set][m], in - (lane >> 5) * kUnit);
     }
     __device__ __forceinline__ void multiply(int set, int i)
     {
@@ -155,21 +114,31 @@ struct Wave {
     }
 };
 
-// What goes between the matrix instructions of a step: `READS` operands, then `UNITS` stores and loads; reads alone as early as one a matrix instruction.
-template <int MULTIPLIES, int READS, int UNITS>
+// Rows that lie in LDS from their second word on, whose first starts up to three bytes ahead of them: an operand is sixteen bytes from the last word of the unit before on. The lanes of the lower half
+// have that of the upper half's unit of the step before, which is kept, those of the upper half that of the lower half's.
+template <int OPERANDS>
+struct Shift {
+    int before[OPERANDS];
+    uint32_t bytes[OPERANDS];
+    __device__ __forceinline__ void put_right(i32x4& v, int i, int lane)
+    {
+        const auto swapped = __builtin_amdgcn_permlane32_swap((uint32_t)before[i], (uint32_t)v[3], false, false);
+        const int word = (int)(lane < 32 ? swapped[1] : swapped[0]);
+        before[i] = v[3];
+        v = behind_byte(v, word, bytes[i]);
+    }
+};
+
+// What goes between the matrix instructions of a step: `READS` reads of operands, as early as one a matrix instruction where there are enough.
+template <int MULTIPLIES, int READS>
 __device__ __forceinline__ void interleave()
 {
-    constexpr int all = READS + 2 * UNITS;
     int done = 0;
 #pragma unroll
     for (int i = 0; i < MULTIPLIES; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
 #pragma unroll
-        for (; done < all && done < (UNITS == 0 && READS < MULTIPLIES ? i + 1 : (i + 1) * all / MULTIPLIES); ++done) {
-            if (done < READS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            else if ((done - READS) % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-            else __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-        }
+        for (; done < READS && done < (READS < MULTIPLIES ? i + 1 : (i + 1) * READS / MULTIPLIES); ++done) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
 }
 
@@ -242,124 +211,62 @@ __device__ __forceinline__ void finish_tile(const Args& a, const Place& at, Wave
     });
 }
 
-// T: D's type; int for sums that go to `parts`.
-//
-// Rows at any address and of any length from 16 on: global -> registers -> LDS -> operands, with two buffers, so that one is multiplied while the other
-// is filled and the loads of the chunk after that are on their way (two chunks on their way to the registers: 768 x 515 -> 1408 8.1 us, so 9.5).
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void loose_kernel(const Args args)
-{
-    constexpr bool PARTIAL = std::is_same_v<T, int>;
-    constexpr int BK = 128, NT = 64 * WM * WN, MB = BM / (32 * WM), NB = BN / (32 * WN);
-    constexpr int XBYTES = BM * BK, BUF = XBYTES + BN * BK;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int K = args.K, chunks = (K + BK - 1) / BK;
-    const Place at(args, BM, BN, chunks, PARTIAL);
-
-    Stager<BM, NT, BK, true> sx;
-    Stager<BN, NT, BK, false> sw;
-    sx.init(args.x, args.ldx, at.m0, args.M, K, tid);
-    sw.init(args.w, args.ldw, at.n0, args.N, K, tid);
-
-    // Chunks past the last one are loaded and cleared: no branch in the loop
-    using SX = decltype(sx);
-    using SW = decltype(sw);
-    auto load = [&](int c, auto part) {
-        constexpr int P = decltype(part)::value;
-        sx.template load<part_of(SX::UNITS, P), part_of(SX::UNITS, P + 1)>(c * BK);
-        sw.template load<part_of(SW::UNITS, P), part_of(SW::UNITS, P + 1)>(c * BK);
-    };
-    auto store = [&](int buf, int c, auto part) {
-        constexpr int P = decltype(part)::value;
-        sx.template store<part_of(SX::UNITS, P), part_of(SX::UNITS, P + 1)>(lds + buf * BUF, c * BK);
-        sw.template store<part_of(SW::UNITS, P), part_of(SW::UNITS, P + 1)>(lds + buf * BUF + XBYTES, c * BK);
-    };
-    using P0 = std::integral_constant<int, 0>;
-    using P1 = std::integral_constant<int, 1>;
-    using P2 = std::integral_constant<int, 2>;
-    // A chunk has four steps of 32 k.  The operands of a step are read from LDS while the one before it is multiplied; the next
-    // chunk's units go to the other buffer in the first three steps, each followed by the load of the unit of the chunk after that, and
-    // the barrier comes before the fourth, in which the first operands of the next chunk are read.
-    Wave<MB, NB> w;
-    w.clear();
-    const char* const x_rows = lds + (wave / WN) * MB * 32 * BK;
-    const char* const w_rows = lds + XBYTES + (wave % WN) * NB * 32 * BK;
-    auto operands = [&](int set, int buf, int s) { w.template read_all<BK>(set, x_rows + buf * BUF, w_rows + buf * BUF, s, lane); };
-    load(at.c0, P0{});
-    load(at.c0, P1{});
-    load(at.c0, P2{});
-    store(0, at.c0, P0{});
-    store(0, at.c0, P1{});
-    store(0, at.c0, P2{});
-    load(at.c0 + 1, P0{});
-    load(at.c0 + 1, P1{});
-    load(at.c0 + 1, P2{});
-    __syncthreads();
-    operands(0, 0, 0);
-#pragma unroll 1
-    for (int c = at.c0; c < at.c1; ++c) {
-        const int buf = (c - at.c0) & 1;
-        auto step = [&](auto part) {
-            constexpr int S = decltype(part)::value;
-            operands((S + 1) & 1, buf, S + 1);
-            w.multiply_all(S & 1);
-            store(buf ^ 1, c + 1, part);
-            load(c + 2, part);
-            interleave<MB * NB, MB + NB, part_of(SX::UNITS, S + 1) - part_of(SX::UNITS, S) + part_of(SW::UNITS, S + 1) - part_of(SW::UNITS, S)>();
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        step(P0{});
-        step(P1{});
-        step(P2{});
-        __syncthreads();
-        operands(0, buf ^ 1, 0);
-        w.multiply_all(1);
-        interleave<MB * NB, MB + NB, 0>();
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    finish_tile<T, WM, WN, 2 * (size_t)BUF>(args, at, w, lds, tid);
-}
-
-// Rows R of one operand as the WAVES waves of a group load them to LDS: a load is 1 KB, whole rows of BK bytes.
-template <int R, int WAVES, int BK>
+// Rows R of one operand as the WAVES waves of a group load them to LDS: a load is 1 KB, whole rows of BK bytes.  They start at whole words; LOOSE: anywhere, and are loaded from the second word that
+// has any of theirs on, the first ones once, R / WAVES a wave.
+template <int R, int WAVES, int BK, bool LOOSE>
 struct Feed {
-    static constexpr int PER_ROW = BK / kUnit, ROWS = 64 / PER_ROW, LOADS = R / ROWS / WAVES;
-    static_assert(R % (ROWS * WAVES) == 0, "whole loads for every wave");
+    static constexpr int PER_ROW = BK / kUnit, ROWS = 64 / PER_ROW, LOADS = R / ROWS / WAVES, STARTS = R / WAVES;
+    static_assert(R % (ROWS * WAVES) == 0 && STARTS <= 64, "whole loads for every wave");
     i32x4 descriptor;
-    uint32_t offset[LOADS];
-    int wave;
-    __device__ __forceinline__ void init(const int8_t* p, int64_t ld, int row0, int rows, int wave_, int lane)
+    int extent, wave, last;
+    uint32_t ahead, pitch, offset[LOADS];        // ahead: bytes of a word in front of the first row
+    // The extent ends with the rows that exist: words past it are zeros.
+    __device__ __forceinline__ void init(const int8_t* p, int64_t ld, int row0, int rows, int K, int wave_, int lane)
     {
-        descriptor = descriptor_of(p + row0 * ld);
+        const int8_t* const base = p + row0 * ld;
+        last = min(R, rows - row0) - 1;
+        ahead = LOOSE ? (uint32_t)reinterpret_cast<uintptr_t>(base) & 3 : 0;
+        pitch = (uint32_t)ld;
+        descriptor = descriptor_of(base - ahead);
+        extent = settled(__builtin_amdgcn_readfirstlane(((int)ahead + last * (int)ld + K + 3) & ~3));
         wave = wave_;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = (i * WAVES + wave) * ROWS + lane / PER_ROW;
-            offset[i] = (uint32_t)(min(r, rows - row0 - 1) * ld) + place_of<BK>(r, lane % PER_ROW) * kUnit;
+            offset[i] = (LOOSE ? (start_of(r) & ~3u) + 4 : start_of(r)) + place_of<BK>(r, lane % PER_ROW) * kUnit;
         }
     }
-    __device__ __forceinline__ void limit(bool any) { descriptor[2] = any ? kExtent : 0; }
+    __device__ __forceinline__ uint32_t start_of(int row) const { return ahead + (uint32_t)min(row, last) * pitch; }
+    __device__ __forceinline__ void limit(bool any) { descriptor[2] = any ? extent : 0; }
     __device__ __forceinline__ void load(int i, int k0, uint32_t lds) const { load_to_lds(descriptor, offset[i], k0, lds + (i * WAVES + wave) * 1024); }
+    __device__ __forceinline__ void load_starts(int k0, uint32_t lds, int lane) const
+    {
+        load_word_to_lds(descriptor, start_of(wave * STARTS + min(lane, STARTS - 1)) & ~3u, k0, lds + wave * 256);
+    }
+    static __device__ __forceinline__ int word_of(int row) { return row / STARTS * 256 + row % STARTS * 4; }
 };
 
-// Rows of whole 16-byte units (pointers, leading dimensions, K).  A buffer is loaded again as soon as all waves have read it, for the chunk STAGES further on.
-template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES>
+// T: D's type; int for sums that go to `parts`.  Memory to LDS without a register between.  A buffer is loaded again as soon as all waves have read it, for the chunk STAGES further on.
+//
+// LOOSE: rows start at any byte.  They are loaded by whole words and put right when they are operands (Shift), by seven instructions of the vector units each
+// (through registers, by 16-byte loads at any address, which issue a lane a clock, 768 x 515 -> 1408 8.5 us, so 6.6; 768 x 8193 -> 1408 39.8, 34.8; 8192 x 8193 -> 4096 284, 285; with the word behind a unit read
+// from LDS beside it 331).
+template <typename T, int BM, int BN, int WM, int WN, int BK, int STAGES, bool LOOSE>
 __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void tile_kernel(const Args args)
 {
     constexpr bool PARTIAL = std::is_same_v<T, int>;
-    constexpr int WAVES = WM * WN, NT = 64 * WAVES, MB = BM / (32 * WM), NB = BN / (32 * WN), STEPS = BK / 32;
-    constexpr int XBYTES = BM * BK, BUF = XBYTES + BN * BK;
+    constexpr int WAVES = WM * WN, MB = BM / (32 * WM), NB = BN / (32 * WN), STEPS = BK / 32;
+    constexpr int XBYTES = BM * BK, BUF = XBYTES + BN * BK, STARTS = STAGES * BUF;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const uint32_t lds_at = settled(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds));
-    const int tid = threadIdx.x, lane = tid & 63, wave = settled(__builtin_amdgcn_readfirstlane(tid >> 6));
+    const int tid = threadIdx.x, lane = tid & 63, wave = settled(__builtin_amdgcn_readfirstlane(tid >> 6)), wm = wave / WN, wn = wave % WN;
     const int K = args.K, chunks = (K + BK - 1) / BK;
     const Place at(args, BM, BN, chunks, PARTIAL);
 
-    Feed<BM, WAVES, BK> fx;
-    Feed<BN, WAVES, BK> fw;
-    fx.init(args.x, args.ldx, at.m0, args.M, wave, lane);
-    fw.init(args.w, args.ldw, at.n0, args.N, wave, lane);
+    Feed<BM, WAVES, BK, LOOSE> fx;
+    Feed<BN, WAVES, BK, LOOSE> fw;
+    fx.init(args.x, args.ldx, at.m0, args.M, K, wave, lane);
+    fw.init(args.w, args.ldw, at.n0, args.N, K, wave, lane);
     constexpr int XLOADS = decltype(fx)::LOADS, LOADS = XLOADS + decltype(fw)::LOADS;
     auto load = [&](int i, int c, int buf) {
         if (i < XLOADS) fx.load(i, c * BK, lds_at + buf * BUF);
@@ -368,89 +275,108 @@ __global__ __launch_bounds__(64 * WM * WN, 64 * WM * WN / 256) void tile_kernel(
 
     Wave<MB, NB> w;
     w.clear();
-    const char* const x_rows = lds + (wave / WN) * MB * 32 * BK;
-    const char* const w_rows = lds + XBYTES + (wave % WN) * NB * 32 * BK;
+    const char* const x_rows = lds + wm * MB * 32 * BK;
+    const char* const w_rows = lds + XBYTES + wn * NB * 32 * BK;
+    Shift<MB + NB> shift;
+    auto read = [&](int set, int buf, int s, int i) { w.template read<BK>(set, x_rows + buf * BUF, w_rows + buf * BUF, s, lane, i); };
+    auto read_all = [&](int set, int buf, int s) {
+#pragma unroll
+        for (int i = 0; i < NB + MB; ++i) read(set, buf, s, i);
+    };
+    auto put_right = [&](int set) {
+        if (!LOOSE) return;
+#pragma unroll
+        for (int i = 0; i < NB + MB; ++i) shift.put_right(w.of(set, i), i, lane);
+    };
 
-    // The whole chunks; one that k ends in comes last.  Loads of chunks past them are of descriptors without an extent, which read nothing: no branch
-    // in the loop, and as many loads on their way in its last rounds as in the others.
-    const int rounds = min(K / BK, at.c1) - at.c0, first = settled(at.c0);
-    if (rounds > 0) {
-        // The loads of a chunk start in the step behind the barrier that frees its buffer; half of them go into the step after that (4096 x 4096 x 4096 by four waves: all in
-        // the first one 73 us, so 67.5; a third or two thirds level).
-        constexpr int LATER = LOADS / 2, MANY = MB * NB > MB + NB ? MB * NB : MB + NB;
+    // Loads of chunks past the last one are of descriptors without an extent, which read nothing: no branch in the loop, and as many loads on their way in its last
+    // rounds as in the others.
+    const int rounds = at.c1 - at.c0, first = settled(at.c0);
+    // The loads of a chunk start in the step behind the barrier that frees its buffer; half of them go into the step after that (4096 x 4096 x 4096 by four waves: all in
+    // the first one 73 us, so 67.5; a third or two thirds level).
+    constexpr int LATER = LOADS / 2, MANY = MB * NB > MB + NB ? MB * NB : MB + NB;
+    // Loose operands are put right in the step that reads them where that has matrix instructions enough (8192 x 8193 -> 4096 291 us, so 285; parts of one block 34.6, so 38).
+    constexpr bool AHEAD = LOOSE && MB * NB >= 8;
+    if (LOOSE) {
+        fx.limit(true);
+        fw.limit(true);
+        fx.load_starts(first * BK, lds_at + STARTS, lane);
+        fw.load_starts(first * BK, lds_at + STARTS + WAVES * 256, lane);
+    }
 #pragma unroll
-        for (int s = 0; s < STAGES; ++s) {
-            fx.limit(s < rounds);
-            fw.limit(s < rounds);
+    for (int s = 0; s < STAGES; ++s) {
+        fx.limit(s < rounds);
+        fw.limit(s < rounds);
 #pragma unroll
-            for (int i = 0; i < LOADS - (s + 1 == STAGES ? LATER : 0); ++i) load(i, first + s, s);
+        for (int i = 0; i < LOADS - (s + 1 == STAGES ? LATER : 0); ++i) load(i, first + s, s);
+    }
+    wait_for_loads<(STAGES - 1) * LOADS - LATER>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_all(0, 0, 0);
+    if (LOOSE) {
+#pragma unroll
+        for (int i = 0; i < MB + NB; ++i) {
+            const int r = (i < NB ? wn * NB + i : wm * MB + i - NB) * 32 + (lane & 31);
+            shift.before[i] = *reinterpret_cast<const int*>(lds + STARTS + (i < NB ? WAVES * 256 + decltype(fw)::word_of(r) : decltype(fx)::word_of(r)));
+            shift.bytes[i] = i < NB ? fw.start_of(r) : fx.start_of(r);
         }
-        wait_for_loads<(STAGES - 1) * LOADS - LATER>();
+        if (AHEAD) put_right(0);
+    }
+    int buf = 0, r = 0;
+    // A step multiplies the operands of one set while those of the next step are read into the other, and COUNT loads, from number `from` on, go to buffer `to`.
+    auto step = [&](int set, int read_from, int read_step, auto count, int from, int c, int to) {
+        constexpr int COUNT = decltype(count)::value;
+        if (!AHEAD) put_right(set);
+        if constexpr (COUNT == 0 && !AHEAD) {
+            read_all(set ^ 1, read_from, read_step);
+            w.multiply_all(set);
+            interleave<MB * NB, MB + NB>();
+            __builtin_amdgcn_sched_barrier(0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MANY; ++i) {
+                if (i < MB * NB) w.multiply(set, i);
+                if (!AHEAD && i < MB + NB) read(set ^ 1, read_from, read_step, i);
+#pragma unroll
+                for (int j = 0; j < MB + NB; ++j) {
+                    if (AHEAD && j / 2 == i) read(set ^ 1, read_from, read_step, j);
+                    if (AHEAD && MANY / 2 + j * (MANY - MANY / 2) / (MB + NB) == i) shift.put_right(w.of(set ^ 1, j), j, lane);
+                }
+#pragma unroll
+                for (int j = 0; j < COUNT; ++j)
+                    if (j * MANY / COUNT == i) load(from + j, c, to);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    constexpr int LAST = (STEPS - 1) & 1;
+    using None = std::integral_constant<int, 0>;
+#pragma unroll 1
+    for (; r + 1 < rounds; ++r) {
+        step(0, buf, 1, std::integral_constant<int, LATER>{}, LOADS - LATER, first + r - 1 + STAGES, buf == 0 ? STAGES - 1 : buf - 1);
+#pragma unroll
+        for (int s = 1; s + 1 < STEPS; ++s) step(s & 1, buf, s + 1, None{}, 0, 0, 0);
+        wait_for_loads<(STAGES - 2) * LOADS>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        w.template read_all<BK>(0, x_rows, w_rows, 0, lane);
-        int buf = 0, r = 0;
-        // A step multiplies the operands of one set while those of the next step are read into the other, and COUNT loads, from number `from` on, go to buffer `to`.
-        auto step = [&](int set, int read_from, int read_step, auto count, int from, int c, int to) {
-            constexpr int COUNT = decltype(count)::value;
-            if constexpr (COUNT == 0) {
-                w.template read_all<BK>(set ^ 1, x_rows + read_from * BUF, w_rows + read_from * BUF, read_step, lane);
-                w.multiply_all(set);
-                interleave<MB * NB, MB + NB, 0>();
-                __builtin_amdgcn_sched_barrier(0);
-            } else {
-#pragma unroll
-                for (int i = 0; i < MANY; ++i) {
-                    if (i < MB * NB) w.multiply(set, i);
-                    if (i < MB + NB) w.template read<BK>(set ^ 1, x_rows + read_from * BUF, w_rows + read_from * BUF, read_step, lane, i);
-#pragma unroll
-                    for (int j = 0; j < COUNT; ++j)
-                        if (j * MANY / COUNT == i) load(from + j, c, to);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        };
-        constexpr int LAST = (STEPS - 1) & 1;
-        using None = std::integral_constant<int, 0>;
-#pragma unroll 1
-        for (; r + 1 < rounds; ++r) {
-            step(0, buf, 1, std::integral_constant<int, LATER>{}, LOADS - LATER, first + r - 1 + STAGES, buf == 0 ? STAGES - 1 : buf - 1);
-#pragma unroll
-            for (int s = 1; s + 1 < STEPS; ++s) step(s & 1, buf, s + 1, None{}, 0, 0, 0);
-            wait_for_loads<(STAGES - 2) * LOADS>();
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            const int next = buf + 1 == STAGES ? 0 : buf + 1;
-            fx.limit(r + STAGES < rounds);
-            fw.limit(r + STAGES < rounds);
-            step(LAST, next, 0, std::integral_constant<int, LOADS - LATER>{}, 0, first + r + STAGES, buf);
-            buf = next;
-        }
-#pragma unroll
-        for (int s = 0; s + 1 < STEPS; ++s) step(s & 1, buf, s + 1, None{}, 0, 0, 0);
-        w.multiply_all(LAST);
-        wait_for_loads<0>();
+        const int next = buf + 1 == STAGES ? 0 : buf + 1;
+        fx.limit(r + STAGES < rounds);
+        fw.limit(r + STAGES < rounds);
+        step(LAST, next, 0, std::integral_constant<int, LOADS - LATER>{}, 0, first + r + STAGES, buf);
+        buf = next;
     }
-    if (K % BK != 0 && at.c1 == chunks) {                             // the chunk that k ends in, through registers
-        __syncthreads();
-        {
-            Stager<BM, NT, BK, true> sx;
-            Stager<BN, NT, BK, false> sw;
-            sx.init(args.x, args.ldx, at.m0, args.M, K, tid);
-            sw.init(args.w, args.ldw, at.n0, args.N, K, tid);
-            const int k0 = (chunks - 1) * BK;
-            sx.template load<0, decltype(sx)::UNITS>(k0);
-            sw.template load<0, decltype(sw)::UNITS>(k0);
-            sx.template store<0, decltype(sx)::UNITS>(lds, k0);
-            sw.template store<0, decltype(sw)::UNITS>(lds + XBYTES, k0);
-        }
-        __syncthreads();
+    // The last chunk, which k may end in: what lies past it counts in neither operand if it is cleared in one.
+    const int in = K - (at.c1 - 1) * BK;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            w.template read_all<BK>(0, x_rows, w_rows, s, lane);
-            w.multiply_all(0);
-        }
+    for (int s = 0; s < STEPS; ++s) {
+        if (s + 1 < STEPS) read_all((s & 1) ^ 1, buf, s + 1);
+        if (!AHEAD) put_right(s & 1);
+        if (in < BK) w.cut_to(s & 1, in - 32 * s, lane);
+        w.multiply_all(s & 1);
+        if (AHEAD && s + 1 < STEPS) put_right((s & 1) ^ 1);
     }
+    wait_for_loads<0>();
     finish_tile<T, WM, WN, STAGES * (size_t)BUF>(args, at, w, lds, tid);
 }
 

@@ -68,6 +68,15 @@ def test_strides(anr, t, spare, shift):
         case(anr, 4, M, N, K, TYPES[t], bias=torch.float32, spare=spare, shift=shift, spare_d=8)
 
 
+@pytest.mark.parametrize("M", [1, 17, 64, 130, 700])
+def test_rows_that_start_at_words(anr, M):
+    """Leading dimensions of whole words and any k: what lies behind a row's end in its last word, and in the lines behind that, counts for nothing."""
+    for N, K, spare in ((70, 515, 1), (70, 513, 3), (33, 1362, 2), (50, 127, 5), (50, 3, 1), (20, 129, 127), (300, 2047, 1), (17, 20001, 3)):
+        for shift in (0, 4, 12):
+            print(M, N, K, spare, shift, flush=True)
+            case(anr, 9, M, N, K, torch.bfloat16, spare=spare, shift=shift + -(spare // 2) % 4, spare_d=0)       # (matrix() starts a row spare // 2 in)
+
+
 @pytest.mark.parametrize("t", TYPES)
 def test_without_scales(anr, t):
     for M, N, K in ((1, 40, 48), (30, 40, 100), (100, 200, 300), (3, 5, 7)):
