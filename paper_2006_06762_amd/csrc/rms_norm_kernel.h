@@ -219,7 +219,7 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
                     if (a.dh) dv[j] += extra[j];
                 }
                 T* const to = static_cast<T*>(a.h) + row * a.ldh + unit.start;
-                if (FEW || WHOLE) {
+                if (FEW || WHOLE || unit.counted == 0) {
                     store<S>(to, dv);
                 } else {                                             // (what another unit has too may be that one's result already, where dx is dh)
 #pragma unroll
