@@ -96,8 +96,15 @@ hipError_t launch_rms_norm_backward(const RmsNormArgs& g, hipStream_t stream)
                 constexpr int V = decltype(v)::value, U = decltype(u)::value;
                 constexpr bool WHOLE = decltype(whole)::value;
                 a.streaming = V > 1 && a.h && rows::whole_units(a.h, a.ldh, es) && g.d.C * es % 16 == 0;
-                return launch_kernel(rmsnorm::backward_kernel<T, P, V, U, WHOLE, 1024>, dim3((unsigned)n), dim3(of.threads, of.rows), of.rows > 1 ? (size_t)of.rows * g.d.C * sizeof(float) : 0,
-                                     stream, a);
+                static LdsLimit limit;
+                void (*const kernel)(Args) = rmsnorm::backward_kernel<T, P, V, U, WHOLE, 1024>;
+                size_t lds = of.rows > 1 ? (size_t)of.rows * g.d.C * sizeof(float) : 0;
+                if (rmsnorm::sums_apart(U * V)) {
+                    lds = (size_t)U * V * rows::kMostThreads * sizeof(float);
+                    const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limit);
+                    if (e != hipSuccess) return e;
+                }
+                return launch_kernel(kernel, dim3((unsigned)n), dim3(of.threads, of.rows), lds, stream, a);
             });
         });
         if (e != hipSuccess) return e;

@@ -9,6 +9,7 @@
 #pragma once
 #include "anr_kernels.h"
 #include "rows_device.h"
+#include "rows_plan.h"
 
 namespace anr {
 namespace rmsnorm {
@@ -115,26 +116,30 @@ template <typename T, int V, int U, bool WHOLE>
 struct Row {
     rows::Raw<T, V> x[U], dy[U], dh[U];
     float rstd;
-    __device__ __forceinline__ void load_dh(const Args& a, int64_t row, int u)
+    __device__ __forceinline__ void load_dh(const Args& a, int64_t row, int t, int u)
     {
-        dh[u].load(static_cast<const T*>(a.dh) + row * a.ld_residual + rows::Unit<V, WHOLE>((int)(threadIdx.x + u * blockDim.x), a.C).start);
+        dh[u].load(rows::at<T>(static_cast<const T*>(a.dh) + row * a.ld_residual, rows::Unit<V, WHOLE>(t + u * (int)blockDim.x, a.C).start));
     }
-    __device__ __forceinline__ void load(const Args& a, int64_t row, bool with_dh)
+    __device__ __forceinline__ void load(const Args& a, int64_t row, int t, bool with_dh)
     {
-        const int threads = blockDim.x, t = threadIdx.x, C = a.C;
+        const int threads = blockDim.x, C = a.C;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int start = rows::Unit<V, WHOLE>(t + u * threads, C).start;
-            dy[u].load(static_cast<const T*>(a.dy) + row * a.ldy + start);
-            x[u].load(static_cast<const T*>(a.x) + row * a.ldx + start);
+            dy[u].load(rows::at<T>(static_cast<const T*>(a.dy) + row * a.ldy, start));
+            x[u].load(rows::at<T>(static_cast<const T*>(a.x) + row * a.ldx, start));
         }
         if (with_dh && a.dh) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) load_dh(a, row, u);
+            for (int u = 0; u < U; ++u) load_dh(a, row, t, u);
         }
         rstd = a.rstd_in[row];
     }
 };
+
+// Whether the sums of a thread with so many values lie in LDS, since its registers do not hold them too (1024 x 32768 bf16 149 us, so 71; with sums of 16 values there and the next row on its way instead 4096 x 8200
+// 62, so 64).
+constexpr bool sums_apart(int values) { return values > 16; }
 
 // A row's values are on their way while those of the row before are used, as far as the registers hold both (bf16 8192 x 4096 with the gradient of the residual 61.5 us, so 57.8;
 // two units of eight 57.1, so 65.6).
@@ -142,34 +147,47 @@ template <typename T, typename P, int V, int U, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
 {
     using namespace rows;
-    extern __shared__ float shared[];            // sums of the rows of a work-group that has several, [rows][C]
+    extern __shared__ __attribute__((aligned(16))) float shared[];   // sums of the rows of a work-group that has several, [rows][C]; or a thread's sums, [unit][V / 4][kMostThreads][4]
     const int threads = blockDim.x, t = threadIdx.x, C = a.C;
     constexpr bool FEW = U * V <= 8;             // values of a thread: more, and gamma and dh are read where they are used
+    constexpr bool APART = sums_apart(U * V), FORMED = U > 2;
     Raw<P, V> g[U];
-    float sums[U][V];
-    auto load_gamma = [&](int u) {
-        if (a.gamma) g[u].load(static_cast<const P*>(a.gamma) + Unit<V, WHOLE>(t + u * threads, C).start);
+    float sums[APART ? 1 : U][V];
+    auto load_gamma = [&](int t, int u) {
+        if (a.gamma) g[u].load(at<P>(a.gamma, Unit<V, WHOLE>(t + u * threads, C).start));
         else g[u].fill(from_float<P>(1.f));
     };
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (FEW) load_gamma(u);
+        if (FEW) load_gamma(t, u);
+        if (APART) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) sums[u][j] = 0.f;
+            for (int j = 0; j < V; j += 4) *reinterpret_cast<f32x4*>(shared + ((u * V + j) * kMostThreads + 4 * t)) = f32x4{0.f, 0.f, 0.f, 0.f};
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sums[u][j] = 0.f;
+        }
     }
+    // (sums that stand apart are a thread's own, and of a work-group that has one row at a time)
+    auto apart = [&](int u, auto f) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) f(*reinterpret_cast<f32x4*>(shared + ((u * V + j) * kMostThreads + 4 * t)), j);
+    };
     int round = 0;
     const int64_t step = (int64_t)gridDim.x * blockDim.y, begin = (int64_t)blockIdx.x * blockDim.y;
-    auto at = [&](int64_t first) { return first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1; };      // (rows past the end repeat the last one and store nothing)
+    auto row_at = [&](int64_t first) { return first + threadIdx.y < a.T ? first + threadIdx.y : a.T - 1; };      // (rows past the end repeat the last one and store nothing)
     Row<T, V, U, WHOLE> r, next;
-    if (FEW && begin < a.T) next.load(a, rows::row_of<(U > 1)>(at(begin)), true);
+    if (FEW && begin < a.T) next.load(a, rows::row_of<(U > 1)>(row_at(begin)), t, true);
     for (int64_t first = begin; first < a.T; first += step, round ^= 1) {
-        const int64_t row = rows::row_of<(U > 1)>(at(first));
+        const int64_t row = rows::row_of<(U > 1)>(row_at(first));
         const bool in = first + threadIdx.y < a.T;
+        int t = threadIdx.x;
+        if (FORMED) asm volatile("" : "+v"(t));  // (another number in each round, as far as the compiler knows: addresses are formed where they are used, kept ones spilled)
         if (FEW) {
             r = next;
-            if (first + step < a.T) next.load(a, rows::row_of<(U > 1)>(at(first + step)), true);
+            if (first + step < a.T) next.load(a, rows::row_of<(U > 1)>(row_at(first + step)), t, true);
         } else {
-            r.load(a, row, false);
+            r.load(a, row, t, false);
         }
         const float rstd = r.rstd;
         Joined along{0.f, 0u};                   // sum of dhat x
@@ -179,13 +197,21 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
             float xv[V], dv[V], gamma[V], sum = 0.f;
             r.x[u].floats(xv);
             r.dy[u].floats(dv);
-            if (!FEW) load_gamma(u);
+            if (!FEW) load_gamma(t, u);
             g[u].floats(gamma);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float hat = xv[j] * rstd;
                 if (WHOLE || unit.counts(j)) sum = fmaf(dv[j] * gamma[j], hat, sum);
-                if (in) sums[u][j] = fmaf(dv[j], hat, sums[u][j]);
+                if (!APART && in) sums[u][j] = fmaf(dv[j], hat, sums[u][j]);
+            }
+            if (APART) {
+                apart(u, [&](f32x4& s, int j) {
+                    f32x4 v = s;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = fmaf(dv[j + e], xv[j + e] * rstd, v[e]);
+                    s = v;
+                });
             }
             if (!WHOLE || unit.in()) along.sum += sum;
             unit_done<2 * U * V>();
@@ -200,6 +226,7 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
             r.dy[u].keep_packed();
             if (FEW) g[u].keep_packed();
         }
+        if (FORMED) asm volatile("" : "+v"(t));
         by_streaming(a.streaming, [&](auto streaming) {
             constexpr bool S = decltype(streaming)::value;
 #pragma unroll
@@ -209,16 +236,16 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
                 float xv[V], dv[V], gamma[V], extra[V];
                 r.x[u].floats(xv);
                 r.dy[u].floats(dv);
-                if (!FEW) load_gamma(u);
+                if (!FEW) load_gamma(t, u);
                 g[u].floats(gamma);
-                if (!FEW && a.dh) r.load_dh(a, row, u);
+                if (!FEW && a.dh) r.load_dh(a, row, t, u);
                 if (a.dh) r.dh[u].floats(extra);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     dv[j] = rstd * fmaf(-xv[j] * rstd, part, dv[j] * gamma[j]);
                     if (a.dh) dv[j] += extra[j];
                 }
-                T* const to = static_cast<T*>(a.h) + row * a.ldh + unit.start;
+                T* const to = at<T>(static_cast<T*>(a.h) + row * a.ldh, unit.start);
                 if (FEW || WHOLE || unit.counted == 0) {
                     store<S>(to, dv);
                 } else {                                             // (what another unit has too may be that one's result already, where dx is dh)
@@ -233,14 +260,24 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
     if (!a.sums) return;
     // the rows of a work-group, then one line of the workspace
     float* const line = a.sums + (int64_t)blockIdx.x * C;
-    if (blockDim.y == 1) {
+    if (APART || blockDim.y == 1) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const Unit<V, WHOLE> unit(t + u * threads, C);
-            if (WHOLE && unit.in()) store<false>(line + unit.start, sums[u]);
+            float v[V];
+            if (APART) {
+                apart(u, [&](const f32x4& s, int j) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[j + e] = s[e];
+                });
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = sums[u][j];
+            }
+            if (WHOLE && unit.in()) store<false>(line + unit.start, v);
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (!WHOLE && unit.counts(j)) line[unit.start + j] = sums[u][j];
+                if (!WHOLE && unit.counts(j)) line[unit.start + j] = v[j];
         }
         return;
     }

@@ -94,6 +94,18 @@ struct Unit {
     __device__ __forceinline__ bool counts(int j) const { return WHOLE ? counted == 0 : j >= counted; }
 };
 
+// Element i of a row: an offset of 32 bits from the row's address, which is a scalar where whole waves have a row.
+template <typename T>
+__device__ __forceinline__ const T* at(const void* row, int i)
+{
+    return reinterpret_cast<const T*>(static_cast<const char*>(row) + (uint32_t)i * (uint32_t)sizeof(T));
+}
+template <typename T>
+__device__ __forceinline__ T* at(void* row, int i)
+{
+    return reinterpret_cast<T*>(static_cast<char*>(row) + (uint32_t)i * (uint32_t)sizeof(T));
+}
+
 // A row's number (below 2^31), in a scalar register where whole waves have it, so that its addresses are not in as many vector registers.
 template <bool WAVES>
 __device__ __forceinline__ int64_t row_of(int64_t row) { return WAVES ? (int64_t)__builtin_amdgcn_readfirstlane((int)row) : row; }

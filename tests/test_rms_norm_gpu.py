@@ -267,3 +267,23 @@ def test_largest_magnitudes(anr, t):
             # (every partial sum is at most 2^15 times a power of two, the mean is 2^112, its root and that one's inverse are powers of two)
             assert np.array_equal(host(y), sign.numpy()) and np.array_equal(host(h), sign.numpy() * 2.0 ** 56)
             assert np.array_equal(host(q), 127 * sign.numpy()) and (scale == np.float32(1) / np.float32(127)).all()
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("C", [9001, 16385, 20001, 32767])
+def test_wide_ragged_rows(anr, t, C):
+    """Rows of more units than a work-group has threads, whose last unit begins inside another one's; more of them than work-groups; in place."""
+    t = TYPES[t]
+    forward_case(anr, 12, 3, C, t, True)
+    for T in (2, 300):
+        print(t, T, C, flush=True)
+        backward_case(anr, 12, T, C, t, True)
+        backward_case(anr, 13, T, C, t, False, torch.float32, spare=3, shift=1)
+    _, x, dh, gamma = make(14, 5, C, t, t)
+    dy, rstd = torch.randn(5, C, device="cuda").to(t), torch.rand(5, device="cuda") + 0.5
+    dx, dgamma = torch.empty_like(x), torch.empty_like(gamma)
+    anr.rms_norm_backward(dy, x, gamma, rstd, dx, dgamma, dh)
+    for which in range(3):
+        ins, dg = [dy.clone(), x.clone(), dh.clone()], torch.empty_like(gamma)
+        anr.rms_norm_backward(ins[0], ins[1], gamma, rstd, ins[which], dg, ins[2])
+        assert torch.equal(ins[which], dx) and torch.equal(dg, dgamma)
