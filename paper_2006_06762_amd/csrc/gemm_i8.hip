@@ -52,9 +52,9 @@ hipError_t launch_join(const Args& a, hipStream_t stream)
 
 // Waves of a work-group: as far as there are chunks for them, eight for each CU over all work-groups, or long rows. us, 4 / 8 / 16 waves: 1 token 2048 -> 11264
 // 6.0 / 6.9 / 9.7, 5632 -> 2048 4.8 / 4.0 / 4.3, 1024 -> 1024 2.74 / 2.68 / 3.1, 16384 -> 16384 54.1 / 50.6 / 52.2, 8 tokens 4096 -> 4096 5.9 / 5.6 / 5.4.
-int waves_of(const Args& a, int most)
+int waves_of(int64_t N, int64_t K, int most)
 {
-    const int64_t groups = (a.N + 15) / 16, chunks = (a.K + i8::kRowsChunk - 1) / i8::kRowsChunk;
+    const int64_t groups = (N + 15) / 16, chunks = (K + i8::kRowsChunk - 1) / i8::kRowsChunk;
     int waves = 4;
     while (waves < most && chunks >= 4 * waves && (groups * waves <= 2048 || chunks >= 16 * waves)) waves *= 2;
     return waves;
@@ -64,7 +64,7 @@ hipError_t launch_rows_as(const Args& a, bool loose, hipStream_t stream)
 {
     constexpr int STAGES = 2;
     static LdsLimit limits[2];                   // of the two kernels
-    const int waves = waves_of(a, i8::most_waves(TB));
+    const int waves = waves_of(a.N, a.K, i8::most_waves(TB));
     void (*const kernel)(Args) = loose ? i8::stream_kernel<T, TB, STAGES, true> : i8::stream_kernel<T, TB, STAGES, false>;
     const size_t lds = std::max((size_t)waves * TB * 256 * sizeof(int), (size_t)waves * STAGES * (loose ? i8::stage_bytes<TB, true>() : i8::stage_bytes<TB, false>()));
     const hipError_t e = lds > 65536 ? raise_lds_limit(reinterpret_cast<const void*>(kernel), lds, limits[loose]) : hipSuccess;
@@ -84,13 +84,15 @@ constexpr int64_t kChunk = 128;                  // k of a chunk
 constexpr int kCus = 256;
 
 // A tile, how many of its work-groups a CU takes at a time, and its estimated time in us: a chunk's where a work-group is alone on its CU and where that is full, and that
-// of both ends.
+// of both ends.  The deep ones have a chunk or two more on their way, for products of few tiles: 64 tokens 4096 -> 11264 in tiles of 64 with two, three and four buffers 17.7 / 11.3 / 10.4 us, 256 tokens in
+// tiles of 128 with two and three 24.1 / 16.9 and 512 tokens 27.9 / 32.1.
 struct Shape {
     int m, n, on_cu;
     double alone, full, ends;
 };
-enum { TILE_256, TILE_128, TILE_64_128, TILE_64, TILES, ROWS = TILES };
-constexpr Shape kShapes[TILES] = {{256, 256, 1, 1.02, 1.02, 6.2}, {128, 128, 2, 0.58, 0.78, 2.8}, {64, 128, 2, 0.22, 0.52, 3.8}, {64, 64, 4, 0.30, 0.67, 2.5}};
+enum { TILE_256, TILE_128, TILE_128_DEEP, TILE_64_128, TILE_64, TILES, ROWS = TILES };
+constexpr Shape kShapes[TILES] = {
+    {256, 256, 1, 1.12, 1.12, 4.0}, {128, 128, 2, 0.57, 0.63, 3.9}, {128, 128, 1, 0.40, 0.40, 4.1}, {64, 128, 2, 0.26, 0.48, 3.8}, {64, 64, 2, 0.21, 0.38, 2.9}};
 
 int64_t tiles_of(int64_t M, int64_t N, const Shape& s) { return ((M + s.m - 1) / s.m) * ((N + s.n - 1) / s.n); }
 
@@ -102,32 +104,33 @@ double estimate(const Shape& s, int64_t tiles, int64_t chunks)
     return us;
 }
 
+// The kernels for few rows: reading W, and X for every sixteen of W's rows, and a round of the waves' chunks.
+double estimate_rows(int64_t M, int64_t N, int64_t K)
+{
+    const int64_t groups = (N + 15) / 16, blocks = (M + 15) / 16, chunks = (K + kChunk - 1) / kChunk, waves = waves_of(N, K, i8::most_waves((int)blocks));
+    return 2.6 + (double)N * (double)K / 9.0e6 + (double)(groups * blocks * 16) * (double)K / 49e6 + 0.051 * (double)((1 + blocks) * ((chunks + waves - 1) / waves));
+}
+
 // The tile, or the kernels for few rows, and the work-groups that share a tile's k where there are few, with the shortest estimated time, that of the launch that joins their
-// sums among it.  Up to 32 rows go to the kernels for few, up to 64 where these are estimated to be faster.  A function of the extents alone.  The estimates' numbers
-// are fitted to 110 products of 33 to 2048 rows, 512 -> 512 to 11264 -> 4096, each by every tile and 1 to 8 parts of k: what is chosen took 2 % longer than the fastest on
-// average.
+// sums among it.  A function of the extents alone.  The estimates' numbers are fitted to 255 products of 1 to 2048 rows, 256 -> 4096 to 4096 -> 16384, each by every tile and 1 to 8
+// parts of k: what is chosen took 1 % longer than the fastest on average.
 struct Choice {
     int tile, splits;
 };
-constexpr int64_t kFewRows = 32, kMostRows = 64;
+constexpr int64_t kMostRows = 64;
 Choice choose(int64_t M, int64_t N, int64_t K)
 {
-    if (M <= kFewRows) return {ROWS, 1};
     const int64_t chunks = (K + kChunk - 1) / kChunk;
-    Choice best{TILE_256, 1};
-    double least = 1e30;
+    Choice best{ROWS, 1};
+    double least = M <= kMostRows ? estimate_rows(M, N, K) : 1e30;
     for (int t = 0; t < TILES; ++t)
         for (int s = 1; s <= 16 && (s == 1 || chunks / s >= 4); ++s) {
-            const double us = estimate(kShapes[t], s * tiles_of(M, N, kShapes[t]), (chunks + s - 1) / s) + (s > 1 ? 2.9 + 2.0 * s * (double)M * (double)N * 4.0 / 4.3e6 : 0.0);
+            const double us = estimate(kShapes[t], s * tiles_of(M, N, kShapes[t]), (chunks + s - 1) / s) + (s > 1 ? 3.6 + 2.0 * s * (double)M * (double)N * 4.0 / 5.0e6 : 0.0);
             if (us < least) {
                 least = us;
                 best = {t, s};
             }
         }
-    if (M <= kMostRows) {                // reading W, and X for every sixteen of W's rows
-        const double x_bytes = (double)((N + 15) / 16) * (double)((M + 15) / 16 * 16) * (double)K;
-        if (4.0 + (double)N * (double)K / 5.3e6 + x_bytes / 36e6 < least) return {ROWS, 1};
-    }
     return best;
 }
 
@@ -152,8 +155,9 @@ hipError_t launch_tile(int tile, const Args& a, hipStream_t stream)
     switch (tile) {
         case TILE_256: return launch_as<T, LOOSE, 256, 256, 2, 4, 2>(a, stream);
         case TILE_128: return launch_as<T, LOOSE, 128, 128, 2, 2, 2>(a, stream);
+        case TILE_128_DEEP: return launch_as<T, LOOSE, 128, 128, 2, 2, 3>(a, stream);
         case TILE_64_128: return launch_as<T, LOOSE, 64, 128, 2, 2, 3>(a, stream);
-        default: return launch_as<T, LOOSE, 64, 64, 2, 2, 2>(a, stream);
+        default: return launch_as<T, LOOSE, 64, 64, 2, 2, 4>(a, stream);
     }
 }
 
