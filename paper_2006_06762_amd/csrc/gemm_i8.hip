@@ -84,15 +84,15 @@ constexpr int64_t kChunk = 128;                  // k of a chunk
 constexpr int kCus = 256;
 
 // A tile, how many of its work-groups a CU takes at a time, and its estimated time in us: a chunk's where a work-group is alone on its CU and where that is full, and that
-// of both ends.  The deep ones have a chunk or two more on their way, for products of few tiles: 64 tokens 4096 -> 11264 in tiles of 64 with two, three and four buffers 17.7 / 11.3 / 10.4 us, 256 tokens in
-// tiles of 128 with two and three 24.1 / 16.9 and 512 tokens 27.9 / 32.1.
+// of both ends.  The deep ones have a chunk more on their way, for products of few tiles: 64 tokens 4096 -> 11264 in tiles of 64 with two, three and four buffers 17.7 / 11.3 / 10.4 us, 777 tokens 640 -> 1363
+// 5.2 / 5.4 / 5.7; 256 tokens 4096 -> 11264 in tiles of 128 with two and three 24.1 / 16.9 and 512 tokens 27.9 / 32.1.
 struct Shape {
     int m, n, on_cu;
     double alone, full, ends;
 };
-enum { TILE_256, TILE_128, TILE_128_DEEP, TILE_64_128, TILE_64, TILES, ROWS = TILES };
+enum { TILE_256, TILE_128, TILE_128_DEEP, TILE_64_128, TILE_64, TILE_64_DEEP, TILES, ROWS = TILES };
 constexpr Shape kShapes[TILES] = {
-    {256, 256, 1, 1.12, 1.12, 4.0}, {128, 128, 2, 0.57, 0.63, 3.9}, {128, 128, 1, 0.40, 0.40, 4.1}, {64, 128, 2, 0.26, 0.48, 3.8}, {64, 64, 2, 0.21, 0.38, 2.9}};
+    {256, 256, 1, 1.18, 1.18, 4.5}, {128, 128, 2, 0.59, 0.69, 3.3}, {128, 128, 1, 0.35, 0.35, 4.6}, {64, 128, 2, 0.30, 0.50, 3.1}, {64, 64, 3, 0.22, 0.69, 2.9}, {64, 64, 2, 0.175, 0.46, 3.4}};
 
 int64_t tiles_of(int64_t M, int64_t N, const Shape& s) { return ((M + s.m - 1) / s.m) * ((N + s.n - 1) / s.n); }
 
@@ -108,11 +108,11 @@ double estimate(const Shape& s, int64_t tiles, int64_t chunks)
 double estimate_rows(int64_t M, int64_t N, int64_t K)
 {
     const int64_t groups = (N + 15) / 16, blocks = (M + 15) / 16, chunks = (K + kChunk - 1) / kChunk, waves = waves_of(N, K, i8::most_waves((int)blocks));
-    return 2.6 + (double)N * (double)K / 9.0e6 + (double)(groups * blocks * 16) * (double)K / 49e6 + 0.051 * (double)((1 + blocks) * ((chunks + waves - 1) / waves));
+    return 3.0 + (double)N * (double)K / 11.1e6 + (double)(groups * blocks * 16) * (double)K / 71e6 + 0.078 * (double)((1 + blocks) * ((chunks + waves - 1) / waves));
 }
 
 // The tile, or the kernels for few rows, and the work-groups that share a tile's k where there are few, with the shortest estimated time, that of the launch that joins their
-// sums among it.  A function of the extents alone.  The estimates' numbers are fitted to 255 products of 1 to 2048 rows, 256 -> 4096 to 4096 -> 16384, each by every tile and 1 to 8
+// sums among it.  A function of the extents alone.  The estimates' numbers are fitted to 272 products of 1 to 2048 rows, 256 -> 4096 to 4096 -> 16384, each by every tile and 1 to 8
 // parts of k: what is chosen took 1 % longer than the fastest on average.
 struct Choice {
     int tile, splits;
@@ -125,7 +125,7 @@ Choice choose(int64_t M, int64_t N, int64_t K)
     double least = M <= kMostRows ? estimate_rows(M, N, K) : 1e30;
     for (int t = 0; t < TILES; ++t)
         for (int s = 1; s <= 16 && (s == 1 || chunks / s >= 4); ++s) {
-            const double us = estimate(kShapes[t], s * tiles_of(M, N, kShapes[t]), (chunks + s - 1) / s) + (s > 1 ? 3.6 + 2.0 * s * (double)M * (double)N * 4.0 / 5.0e6 : 0.0);
+            const double us = estimate(kShapes[t], s * tiles_of(M, N, kShapes[t]), (chunks + s - 1) / s) + (s > 1 ? 3.45 + 2.0 * s * (double)M * (double)N * 4.0 / 4.6e6 : 0.0);
             if (us < least) {
                 least = us;
                 best = {t, s};
@@ -157,6 +157,7 @@ hipError_t launch_tile(int tile, const Args& a, hipStream_t stream)
         case TILE_128: return launch_as<T, LOOSE, 128, 128, 2, 2, 2>(a, stream);
         case TILE_128_DEEP: return launch_as<T, LOOSE, 128, 128, 2, 2, 3>(a, stream);
         case TILE_64_128: return launch_as<T, LOOSE, 64, 128, 2, 2, 3>(a, stream);
+        case TILE_64: return launch_as<T, LOOSE, 64, 64, 2, 2, 3>(a, stream);
         default: return launch_as<T, LOOSE, 64, 64, 2, 2, 4>(a, stream);
     }
 }
