@@ -78,6 +78,21 @@ def test_rows_that_start_at_words(anr, M):
 
 
 @pytest.mark.parametrize("t", TYPES)
+def test_rows_that_start_at_any_byte(anr, t):
+    """Odd lengths, each row at another byte of a word, over tiles of every kind, long k that work-groups share, few rows and the longest row offsets in a tile."""
+    for M, N, K in ((100, 130, 20001), (200, 300, 16383), (65, 64, 9001), (300, 129, 8195), (2100, 1100, 1030), (1025, 770, 2049), (513, 4100, 259), (40, 9000, 1025), (7, 300, 16385), (1, 4097, 4097)):
+        print(t, M, N, K, flush=True)
+        case(anr, 10, M, N, K, TYPES[t], bias=TYPES[t], shift=1)
+    a, w = (torch.randint(-128, 128, (s, 300001), dtype=torch.int8, device="cuda") for s in (260, 140))
+    d = torch.empty(260, 140, dtype=TYPES[t], device="cuda")
+    sa, sw = torch.rand(260, device="cuda"), torch.rand(140, device="cuda")
+    want = (a[:, 3:1004].cpu().double().numpy() @ w[:, 77777:78778].cpu().double().numpy().T) * (host(sa)[:, None] * host(sw))
+    anr.gemm_i8(a[:, 3:1004], w[:, 77777:78778], sa, sw, d)
+    if t != "f16":
+        within("d", d, want, 3.01 * U * np.abs(want), TYPES[t])
+
+
+@pytest.mark.parametrize("t", TYPES)
 def test_without_scales(anr, t):
     for M, N, K in ((1, 40, 48), (30, 40, 100), (100, 200, 300), (3, 5, 7)):
         case(anr, 5, M, N, K, TYPES[t], scales=False)
