@@ -51,7 +51,6 @@ hipError_t launch_forward(const RmsNormArgs& g, hipStream_t stream)
     a.eps = g.eps;
     a.rstd = g.rstd;
     a.scale = g.scale;
-    const int es = element_bytes(g.d.dtype);
     return with_types(g, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
@@ -59,7 +58,7 @@ hipError_t launch_forward(const RmsNormArgs& g, hipStream_t stream)
         return rows::with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
             constexpr int V = decltype(v)::value, U = decltype(u)::value;
             constexpr bool WHOLE = decltype(whole)::value;
-            a.streaming = V > 1 && rows::whole_units(a.h, a.ldh, es) && (QUANTIZED || rows::whole_units(a.y, a.ldy, es)) && g.d.C * es % 16 == 0;
+            a.streaming = V > 1;
             const int64_t groups = std::min<int64_t>((a.T + of.rows - 1) / of.rows, kMostGroups);
             return launch_kernel(rmsnorm::forward_kernel<T, P, V, U, WHOLE, QUANTIZED, 1024>, dim3((unsigned)groups), dim3(of.threads, of.rows), 0, stream, a);
         });
@@ -95,7 +94,8 @@ hipError_t launch_rms_norm_backward(const RmsNormArgs& g, hipStream_t stream)
             return rows::with_rows<T>(g.d.C, of, [&](auto v, auto u, auto whole) {
                 constexpr int V = decltype(v)::value, U = decltype(u)::value;
                 constexpr bool WHOLE = decltype(whole)::value;
-                a.streaming = V > 1 && a.h && rows::whole_units(a.h, a.ldh, es) && g.d.C * es % 16 == 0;
+                // (4096 x 9001 bf16 with the residual's gradient 104 us by ordinary stores, 117 past L2; 4096 x 4003 42.4, 38.7)
+                a.streaming = V > 1 && (U == 1 || (is_aligned16(a.h) && a.ldh * es % 16 == 0));
                 static LdsLimit limit;
                 void (*const kernel)(Args) = rmsnorm::backward_kernel<T, P, V, U, WHOLE, 1024>;
                 size_t lds = of.rows > 1 ? (size_t)of.rows * g.d.C * sizeof(float) : 0;

@@ -41,8 +41,5 @@ BackwardPlan backward_plan_for(int64_t C, int64_t T_)
     return backward_plan_of((C + V - 1) / V, kHeld / V, T_);
 }
 
-// Whether rows are whole aligned units of 16 bytes (an absent matrix has none that are not).
-inline bool whole_units(const void* p, int64_t ld, int es) { return !p || (is_aligned16(p) && ld * es % 16 == 0); }
-
 }  // namespace rows
 }  // namespace anr

@@ -119,7 +119,6 @@ struct BackArgs {
     void* y;
     int64_t T, ldq, ldy;
     int C;
-    bool streaming;
 };
 
 template <typename T, int V>
@@ -129,16 +128,14 @@ __global__ __launch_bounds__(kBackThreads) void dequantize_kernel(const BackArgs
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
     const Unit<V, false> unit(i, a.C);
     if (!unit.in()) return;
-    by_streaming(a.streaming, [&](auto streaming) {
-        for (int64_t row = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; row < a.T; row += (int64_t)gridDim.y * blockDim.y) {
-            const Loose l = *reinterpret_cast<const Loose*>(a.q + row * a.ldq + unit.start);
-            const float scale = a.scale[row];
-            float v[V];
+    for (int64_t row = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; row < a.T; row += (int64_t)gridDim.y * blockDim.y) {
+        const Loose l = *reinterpret_cast<const Loose*>(a.q + row * a.ldq + unit.start);
+        const float scale = a.scale[row];
+        float v[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = (float)l.v[j] * scale;
-            store<decltype(streaming)::value>(static_cast<T*>(a.y) + row * a.ldy + unit.start, v);
-        }
-    });
+        for (int j = 0; j < V; ++j) v[j] = (float)l.v[j] * scale;
+        store<true>(static_cast<T*>(a.y) + row * a.ldy + unit.start, v);
+    }
 }
 
 }  // namespace
@@ -163,11 +160,10 @@ hipError_t launch_quantize_rows(const RowsQ8Args& g, hipStream_t stream)
 hipError_t launch_dequantize_rows(const RowsQ8Args& g, hipStream_t stream)
 {
     if (g.d.T == 0) return hipSuccess;
-    const int es = element_bytes(g.d.dtype);
     return with_type(g.d.dtype, [&](auto t) {
         using T = decltype(t);
         const int V = values_of<T>(g.d.C), units = (int)((g.d.C + V - 1) / V);
-        const BackArgs a{g.q, g.scale, const_cast<void*>(g.x), g.d.T, g.d.ldq, g.d.ldx, (int)g.d.C, V > 1 && whole_units(g.x, g.d.ldx, es) && g.d.C % V == 0};
+        const BackArgs a{g.q, g.scale, const_cast<void*>(g.x), g.d.T, g.d.ldq, g.d.ldx, (int)g.d.C};
         int wide = 1;                            // threads on a row, a power of two
         while (wide < kBackThreads && wide < units) wide *= 2;
         const int64_t rows = kBackThreads / wide;
