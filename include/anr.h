@@ -440,8 +440,10 @@ anr_status anr_rms_norm_backward(const anr_rms_norm_desc *desc, const void *dy, 
                                  void *hip_stream);
 
 /* anr_rms_norm with y in 8 bits: scale[t] = (largest |y| of token t) / 127 and q = y / scale to
- * the nearest whole number, ties to even (y is not rounded before that).  A token of zeros has
- * scale and q zero.  One with an infinity or NaN has a NaN as its scale and q zero. */
+ * the nearest whole number, ties to even (y is not rounded before that).  Formed from h gamma, which
+ * holds for magnitudes from 2^-126 to 2^127.  A token whose h gamma are all zeros has scale and q zero, also with
+ * eps = 0 (y of anr_rms_norm is then 0 times an infinity, NaN).  One with an infinity or NaN among
+ * h gamma or y has a NaN as its scale and q zero.  q is zero too where the scale is below float32's smallest number. */
 anr_status anr_rms_norm_q8(const anr_rms_norm_desc *desc, const void *x, const void *residual, const void *gamma,
                            float eps, void *h, int8_t *q, float *scale, void *ws, size_t ws_bytes, void *hip_stream);
 
@@ -460,7 +462,8 @@ typedef struct {
 
 /* v = act(x) up (act(x) where up is NULL), scale[t] = (largest |v| of row t) / 127 and q = v / scale
  * to the nearest whole number, ties to even.  A row of zeros has scale and q zero; one with an
- * infinity or NaN has a NaN as its scale and q zero. */
+ * infinity or NaN has a NaN as its scale and q zero.  q is zero too where the scale is below float32's
+ * smallest number. */
 anr_status anr_quantize_rows(const anr_rows_q8_desc *desc, const void *x, const void *up, int8_t *q, float *scale,
                              void *ws, size_t ws_bytes, void *hip_stream);
 

@@ -115,8 +115,8 @@ __device__ __forceinline__ int64_t row_of(int64_t row) { return WAVES ? (int64_t
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
 constexpr uint32_t kInfinite = 0x7f800000u;
 
-// A row in 8 bits: whole steps of `step`, the largest magnitude of the row being 127 of them.  Rows of zeros have the step zero; an infinity or NaN makes the
-// step NaN and the values zeros, so that whatever is made of the row is NaN.  Rows that lie low in float32's range are raised before they are
+// A row in 8 bits: whole steps of `step`, the largest magnitude of the row being 127 of them.  Rows of zeros have the step zero, whatever the factor; an infinity or NaN
+// makes the step NaN, so that whatever is made of the row is NaN.  Values are zeros where the step is none that they could be divided by: zero (a 127th of what is below 2^-143 rounds to it) or NaN.  Rows that lie low in float32's range are raised before they are
 // divided by their step, whose inverse would leave it at the other end.
 struct Steps {
     float inverse, rest;            // their sum is the inverse of the step of the (raised) values, to 2^-45 of itself; to 2^-29 at the upper end of the range, where `rest` is denormal
@@ -124,13 +124,13 @@ struct Steps {
     float step;                     // of rows whose values are multiplied by `factor` afterwards
     __device__ __forceinline__ Steps(uint32_t largest, float factor)
     {
-        const float most = __builtin_bit_cast(float, largest);
-        const bool fine = largest < kInfinite;
+        const float most = __builtin_bit_cast(float, largest), result = largest == 0 ? 0.f : most * factor;
+        const bool fine = magnitude(result) < kInfinite;
         raised = most < 0x1p-60f;
         const float unit = (raised ? most * 0x1p64f : most) / 127.f;
-        inverse = fine && largest != 0 ? __builtin_amdgcn_rcpf(unit) : 0.f;
+        inverse = fine && result >= 0x1p-143f ? __builtin_amdgcn_rcpf(unit) : 0.f;
         rest = fmaf(-inverse, unit, 1.f) * inverse;
-        step = fine ? most * factor / 127.f : __builtin_nanf("");
+        step = fine ? result / 127.f : __builtin_nanf("");
     }
 };
 
