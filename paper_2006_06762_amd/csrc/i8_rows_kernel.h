@@ -3,13 +3,11 @@
 // Bound: reading W once.  A work-group takes 16 rows of W, its waves share the k in chunks of 128 and join their sums in LDS; the matrix instructions
 // (v_mfma_i32_16x16x64_i8) are sixteen tokens wide, which cost nothing here.
 #pragma once
+#include "gemm_i8_plan.h"
 #include "i8_device.h"
 
 namespace anr {
 namespace i8 {
-
-constexpr int kRowsChunk = 128;                 // k of a wave at a time: a line of a row
-constexpr int most_waves(int TB) { return TB == 1 ? 16 : TB == 2 ? 8 : 4; }      // of a work-group: their buffers fit LDS
 
 // The results of a thread: what they are multiplied with is read before the products, whose sums [wave][TB][4][64] join at the end.  At least four waves.
 template <typename T, int TB>
