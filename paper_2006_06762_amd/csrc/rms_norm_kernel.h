@@ -247,6 +247,7 @@ __global__ __launch_bounds__(THREADS) void backward_kernel(const Args a)
                     if (a.dh) dv[j] += extra[j];
                 }
                 T* const to = at<T>(static_cast<T*>(a.h) + row * a.ldh, unit.start);
+                // (FEW: what two units have both store, alike; dh was loaded in front of join_row, whose barrier, or a single wave's own order, has those loads ahead of every store here)
                 if (FEW || WHOLE || unit.counted == 0) {
                     store<S>(to, dv);
                 } else {                                             // (what another unit has too may be that one's result already, where dx is dh)
