@@ -55,7 +55,7 @@ inline double estimate_rows(int64_t M, int64_t N, int64_t K)
 
 // The tile, or the kernels for few rows, and the work-groups that share a tile's k where there are few, with the shortest estimated time, that of the launch that joins their
 // sums among it.  A function of the extents alone.  The estimates' numbers are fitted to 272 products of 1 to 2048 rows, 256 -> 4096 to 4096 -> 16384, each by every tile and 1 to 8
-// parts of k: what is chosen took 1 % longer than the fastest on average.
+// parts of k: what is chosen took 1 % longer than the fastest on average, 14 to 34 % for 20 to 48 rows 11264 -> 4096 (13.0 to 13.6 us in parts of k, 9.8 to 11.9 by the kernels for few rows).
 struct Choice {
     int tile, splits;
 };

@@ -135,7 +135,7 @@ struct Steps {
 };
 
 // V of them at any address.  The quotient by the step is off by less than 2^-28 of itself before it is rounded to 24 bits, and so exact where they hold it: half a step stays
-// one (by `inverse` alone one of two halves came out on its wrong side, as 1.5 in steps of 3; 8192 x 11264 bf16 gated 84.6 us, so 85.2, 1024 x 32768 normed 62.4, 65.5).  It is rounded to a
+// one (by `inverse` alone one of two halves came out on its wrong side, as 1.5 in steps of 3; 8192 x 11264 bf16 gated 84.3 us, so 85.7, 8192 x 4096 normed with its residual 42.1, 42.1, 1024 x 32768 62.2, 64.7).  It is rounded to a
 // whole number, ties to even, by a sum with 1.5 2^23, whose last bits are then that number's (at most 127 + 2^-16).
 template <int V>
 __device__ __forceinline__ void store_steps(int8_t* p, float (&v)[V], const Steps& steps)
